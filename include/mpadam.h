@@ -480,6 +480,169 @@ int32_t mpadam_toy_status(mpadam_toy_state* s, int32_t* code);
 /* Frees the scratch (synchronises the device first).  NULL is a no-op. */
 int32_t mpadam_toy_destroy(mpadam_toy_state* s);
 
+/* ------------------------------------------------------------------------
+ * AdamW over a list of tensors, with moments in binary32 or in 8 bits: the
+ * optimizer that the paper compares M+Adam with (its Sec. 3 preliminaries).
+ *
+ * Arithmetic: IEEE binary32, nearest-even, every operation rounded on its own
+ * (no fused multiply-add).  Per element, with g' = g s when the step is given
+ * a multiplier s, else g:
+ *   m' = b1 m + (1-b1) g'           v' = b2 v + (1-b2) (g' g')
+ *   r' = sqrt(v')                   u  = (ka m') / (r' c2 + eps)
+ *   w' = (w - kwd w) - u            (w - u when weight_decay = 0)
+ * with ka = lr / (1 - beta1^t), c2 = 1 / sqrt(1 - beta2^t), 1-b1, 1-b2 and
+ * kwd = lr * weight_decay computed in binary64 and rounded once.
+ *
+ * 8-bit moments (state_dtype MPADAM_E4M3): m and r = sqrt(v) are held as E4M3
+ * codes with one E8M0 scale (a byte; 2^(byte - 127)) per 128 consecutive
+ * elements of the tensor; v = r r when read.  A step re-encodes both with 2^k,
+ * k the smallest integer with A <= 448 * 2^k (A = the block's largest finite
+ * magnitude; k at least -127, and 0 when A is 0).  Nearest-even, or stochastic
+ * with 16 random bits R per value: for y = |x| 2^-k the E4M3 value at or below
+ * y + R 2^-16 steps, a step being the spacing of the E4M3 grid at y (below
+ * 2^-6: y + 2^-6 is rounded to binary32 first).  A root above 0 is stored as
+ * at least the smallest code: an update never divides by an underflowed
+ * moment.  NaN stores 0x7F; infinities saturate.
+ *   Why stochastic: with beta2 = 0.999 a step moves the root by about 2^-11
+ * of itself while E4M3's spacing is 2^-4 to 2^-3, so a nearest-rounded second
+ * moment would stand still.
+ *
+ * Random bits: Philox4x32-10 as above with key = seed.  A BF16 weight takes the
+ * same 16-bit lane as mpadam_step's; element i's moments take word i mod 4 of
+ * block i div 4 with the counter's second word's highest bit set, the low half
+ * for m and the high half for r.  Global element index: off[0] = 0, off[k+1] =
+ * off[k] + numel[k] rounded up to a multiple of 128.
+ * ------------------------------------------------------------------------ */
+
+/* One tensor: w has the config's weight_dtype; m, v are binary32, or E4M3
+ * codes (numel bytes) with m_scale, v_scale (ceil(numel / 128) bytes each; NULL
+ * for binary32).  compute: optional BF16 copy of binary32 weights, rounded like
+ * a BF16 weight is (nearest), overwritten every step; NULL for none.
+ * Pointers must be aligned to their element size; tensors whose pointers are
+ * all 16-byte aligned take the vectorised path. */
+typedef struct {
+  void* w;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  uint16_t* compute;
+  int64_t numel;
+} mpadam_adamw_tensor;
+
+/* Valid ranges (else MPADAM_EINVAL): 0 <= beta1, beta2 < 1; eps > 0 finite;
+ * weight_decay >= 0 finite; state_rounding stochastic only with E4M3 states;
+ * rounding stochastic only with BF16 weights. */
+typedef struct {
+  float beta1, beta2;
+  float eps;
+  float weight_decay;      /* decoupled: w -= lr * weight_decay * w */
+  int32_t weight_dtype;    /* MPADAM_F32 or MPADAM_BF16 */
+  int32_t grad_dtype;      /* MPADAM_F32 or MPADAM_BF16 */
+  int32_t state_dtype;     /* MPADAM_F32 or MPADAM_E4M3 */
+  int32_t rounding;        /* mpadam_rounding of BF16 weights */
+  int32_t state_rounding;  /* mpadam_rounding of E4M3 states */
+  int32_t reserved;        /* must be 0 */
+  uint64_t seed;
+} mpadam_adamw_config;
+
+typedef struct mpadam_adamw_state mpadam_adamw_state;
+
+/* Copies the list, validates, and uploads its tables (synchronously, on the
+ * current device).  Errors: EINVAL, EALLOC, ECUDA.  On error *out is NULL. */
+int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32_t n, const mpadam_adamw_config* cfg,
+                            mpadam_adamw_state** out);
+
+/* Step t (>= 1) with learning rate lr (finite, >= 0) over every tensor,
+ * asynchronously on `stream`, one kernel launch (and one per 448 tensors when
+ * a list of more than 448 tensors comes with other gradient pointers than the
+ * step before).  grads: host array of n device pointers of grad_dtype.
+ * grad_scale: device binary32 that multiplies every gradient (see
+ * mpadam_grad_norm), or NULL; where it is NaN the step changes nothing.
+ * A captured step may be replayed.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* grads, int64_t step, float lr,
+                          const float* grad_scale, struct CUstream_st* stream);
+
+/* Synchronises the device and frees the library's tables; NULL is a no-op. */
+int32_t mpadam_adamw_destroy(mpadam_adamw_state* s);
+
+/* ------------------------------------------------------------------------
+ * Global norm of a list of gradients.
+ * ------------------------------------------------------------------------ */
+typedef struct mpadam_grad_norm_state mpadam_grad_norm_state;
+
+/* For a list of n tensors of numel[k] gradients each.  Errors: EINVAL,
+ * EALLOC, ECUDA.  On error *out is NULL. */
+int32_t mpadam_grad_norm_create(const int64_t* numel, int32_t n, int32_t grad_dtype, mpadam_grad_norm_state** out);
+
+/* out (device, two binary32): the 2-norm over all gradients, and the
+ * multiplier that clips them to max_norm (> 0; +INFINITY: never):
+ * min(1, max_norm / norm), NaN when the norm is not finite.  Squares are
+ * summed in binary32 within a thread and in binary64 across threads, in an
+ * order that depends on the list alone, so the same gradients give the same
+ * bits; a gradient above about 1.8e19 overflows its square and makes the norm
+ * infinite.  Asynchronous on `stream`; one launch (lists of more than 448
+ * tensors as for mpadam_adamw_step).  Errors: EINVAL, ECUDA. */
+int32_t mpadam_grad_norm(mpadam_grad_norm_state* s, const void* const* grads, float max_norm, float* out,
+                         struct CUstream_st* stream);
+
+int32_t mpadam_grad_norm_destroy(mpadam_grad_norm_state* s);
+
+/* ------------------------------------------------------------------------
+ * E4M3 matrices with a power-of-two scale per block of 128, and their product:
+ * a linear layer's arithmetic in 8 bits (the paper's FP8 compute, Sec. 5.2,
+ * names neither block size nor rule).
+ *
+ * A matrix [rows, cols] is stored as row-major E4M3 codes, row stride a
+ * multiple of 16 bytes, base 16-byte aligned, and E8M0 scales (byte b stands
+ * for 2^(b - 127)), one per 128 consecutive values of a row, in tiles of 128
+ * rows x 4 blocks: with groups = ceil(ceil(cols / 128) / 4), row i's block c is
+ * at byte ((i / 128) groups + c / 4) 512 + (i mod 32) 16 + (i mod 128 / 32) 4 +
+ * c mod 4 (integer divisions), ceil(rows / 128) groups 512 bytes in all, base
+ * 16-byte aligned.
+ * ------------------------------------------------------------------------ */
+
+/* Quantises x (device, binary32 or BF16, row stride ld >= cols elements): codes
+ * E4M3(x 2^-k), nearest-even, saturating at +-448 (NaN stores 0x7F), with k the
+ * smallest integer with A <= 448 * 2^k, at least -127 (0 when A is 0), A the
+ * largest finite |x| of the block: 128 values along the row, or (square != 0)
+ * the square of 128 x 128 that the row's block lies in.  q, s, ldq: the matrix as
+ * it lies (q may be NULL: not wanted); qt, st, ldqt: its transpose, [cols,
+ * rows], blocks along the original columns unless square (qt may be NULL).
+ * Padding scales are written as 1; padding codes are left alone.  One launch.
+ * rows, cols < 2^31.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_e4m3_quantize(const void* x, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ld, int32_t square,
+                             uint8_t* q, uint8_t* s, int64_t ldq, uint8_t* qt, uint8_t* st, int64_t ldqt,
+                             struct CUstream_st* stream);
+
+/* d[m, n] = a b^T, or d += a b^T (accumulate != 0; binary32 d only), for a [m, k]
+ * and b [n, k] stored as above: sums over k of the codes' products times both
+ * scales in binary32 on the tensor cores, rounded once into d (d_dtype
+ * MPADAM_F32 or MPADAM_BF16, row stride ldd >= n elements).  k = 0 gives 0.
+ * m, n, k < 2^31.  Asynchronous on `stream`.  Errors: EINVAL, EUNSUPPORTED (no
+ * driver entry for tensor maps), ECUDA. */
+typedef struct {
+  const uint8_t* a;
+  const uint8_t* a_scale;
+  int64_t lda;
+  const uint8_t* b;
+  const uint8_t* b_scale;
+  int64_t ldb;
+  void* d;
+  int64_t ldd;
+  int64_t m, n, k;
+  int32_t d_dtype;
+  int32_t accumulate;
+} mpadam_e4m3_product;
+
+int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, struct CUstream_st* stream);
+
+/* Device-side status of the products on the current device: waits for
+ * `stream`, returns in *code the error bits that their kernels recorded since
+ * the last read (non-zero: a bounded wait gave up, and that product's results
+ * are incomplete), and clears them.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_e4m3_status(struct CUstream_st* stream, int32_t* code);
+
 #ifdef __cplusplus
 }
 #endif

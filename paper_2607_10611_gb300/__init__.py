@@ -7,7 +7,7 @@ PyTorch is used only for device memory and streams.
 """
 from .builder import build  # noqa: F401
 
-__all__ = ["build", "native", "MPAdam"]
+__all__ = ["build", "native", "MPAdam", "AdamW", "GradNorm", "fp8"]
 
 
 def __getattr__(name):
@@ -17,4 +17,10 @@ def __getattr__(name):
     if name == "MPAdam":
         from .optimizer import MPAdam
         return MPAdam
+    if name in ("AdamW", "GradNorm"):
+        from . import adamw
+        return getattr(adamw, name)
+    if name == "fp8":
+        import importlib
+        return importlib.import_module(".fp8", __name__)
     raise AttributeError(name)

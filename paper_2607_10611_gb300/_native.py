@@ -27,7 +27,10 @@ EXPORTED = ["mpadam_create", "mpadam_create_ex", "mpadam_fp8_init", "mpadam_step
             "mpadam_set_tail_pool", "mpadam_launch_info", "mpadam_rng_lanes", "mpadam_step_noalloc", "mpadam_noalloc_status", "mpadam_device_status",
             "mpadam_toy_create", "mpadam_toy_step", "mpadam_toy_run", "mpadam_toy_status", "mpadam_toy_destroy",
             "mpadam_host_buffer_alloc", "mpadam_host_buffer_free", "mpadam_debug_fail_allocation", "mpadam_debug_spoil_pool",
-            "mpadam_debug_tile_schedule", "mpadam_debug_pool_rule", "mpadam_debug_ring_layout"]
+            "mpadam_debug_tile_schedule", "mpadam_debug_pool_rule", "mpadam_debug_ring_layout",
+            "mpadam_adamw_create", "mpadam_adamw_step", "mpadam_adamw_destroy", "mpadam_grad_norm_create",
+            "mpadam_grad_norm", "mpadam_grad_norm_destroy", "mpadam_e4m3_quantize", "mpadam_e4m3_matmul",
+            "mpadam_e4m3_status"]
 
 
 class MPAdamError(RuntimeError):
@@ -67,6 +70,25 @@ class mpadam_toy_config(ctypes.Structure):
                 ("reserved", ctypes.c_int32), ("lr_add", ctypes.c_float), ("lr_mul", ctypes.c_float),
                 ("rmax", ctypes.c_float), ("tau", ctypes.c_float), ("c_lo", ctypes.c_float),
                 ("c_hi", ctypes.c_float), ("seed", ctypes.c_uint64)]
+
+
+class mpadam_adamw_tensor(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("compute", ctypes.c_void_p), ("numel", ctypes.c_int64)]
+
+
+class mpadam_adamw_config(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("weight_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("state_dtype", ctypes.c_int32), ("rounding", ctypes.c_int32), ("state_rounding", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("seed", ctypes.c_uint64)]
+
+
+class mpadam_e4m3_product(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("a_scale", ctypes.c_void_p), ("lda", ctypes.c_int64),
+                ("b", ctypes.c_void_p), ("b_scale", ctypes.c_void_p), ("ldb", ctypes.c_int64),
+                ("d", ctypes.c_void_p), ("ldd", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64),
+                ("k", ctypes.c_int64), ("d_dtype", ctypes.c_int32), ("accumulate", ctypes.c_int32)]
 
 
 TOY_MODES = {"additive": 0, "multiplicative": 1, "combined": 2}
@@ -131,6 +153,15 @@ def lib() -> ctypes.CDLL:
             "mpadam_debug_tile_schedule": [P, i32, i32, i32, i32, P, P, P, i32, P],
             "mpadam_debug_pool_rule": [i64, i32, i32, i32, i32, P],
             "mpadam_debug_ring_layout": [P, i32, i32, P],
+            "mpadam_adamw_create": [P, i32, P, P],
+            "mpadam_adamw_step": [P, P, i64, ctypes.c_float, P, P],
+            "mpadam_adamw_destroy": [P],
+            "mpadam_grad_norm_create": [P, i32, i32, P],
+            "mpadam_grad_norm": [P, P, ctypes.c_float, P, P],
+            "mpadam_grad_norm_destroy": [P],
+            "mpadam_e4m3_quantize": [P, i32, i64, i64, i64, i32, P, P, i64, P, P, i64, P],
+            "mpadam_e4m3_matmul": [P, P],
+            "mpadam_e4m3_status": [P, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -366,3 +397,65 @@ def mpadam_debug_ring_layout(cfg: mpadam_config, misaligned: bool, smem_bytes: i
     out = (ctypes.c_int32 * 8)()
     _check(lib().mpadam_debug_ring_layout(ctypes.byref(cfg), int(misaligned), smem_bytes, out))
     return dict(zip(("stages", "stage_bytes", "off_g", "off_m", "off_v", "off_ve", "off_s", "static_bytes"), out))
+
+
+def mpadam_adamw_create(tensors: Sequence[tuple], cfg: mpadam_adamw_config) -> int:
+    """tensors: (w, m, v, m_scale, v_scale, compute, numel) per tensor, pointers as ints (0 = NULL)."""
+    arr = (mpadam_adamw_tensor * max(1, len(tensors)))()
+    for i, (w, m, v, ms, vs, c, n) in enumerate(tensors):
+        arr[i] = mpadam_adamw_tensor(w or None, m or None, v or None, ms or None, vs or None, c or None, n)
+    out = ctypes.c_void_p()
+    _check(lib().mpadam_adamw_create(arr, len(tensors), ctypes.byref(cfg), ctypes.byref(out)))
+    return out.value
+
+
+def mpadam_adamw_step(state: int, grads: Sequence[int], step: int, lr: float, grad_scale: int = 0,
+                      stream: int = 0) -> None:
+    """grads: one pointer per tensor; an array.array of 64-bit words ("Q" or WORD) is passed as it is."""
+    arr = grads if type(grads) is array.array and grads.typecode in ("Q", WORD) else _ptr_array(grads)
+    status = lib().mpadam_adamw_step(state, arr.buffer_info()[0], step, lr, grad_scale or None, stream or None)
+    if status:
+        _check(status)
+
+
+def mpadam_adamw_destroy(state: int) -> None:
+    _check(lib().mpadam_adamw_destroy(state))
+
+
+def mpadam_grad_norm_create(numel: Sequence[int], grad_dtype: int) -> int:
+    arr = (ctypes.c_int64 * max(1, len(numel)))(*numel)
+    out = ctypes.c_void_p()
+    _check(lib().mpadam_grad_norm_create(arr, len(numel), grad_dtype, ctypes.byref(out)))
+    return out.value
+
+
+def mpadam_grad_norm(state: int, grads: Sequence[int], max_norm: float, out: int, stream: int = 0) -> None:
+    arr = grads if type(grads) is array.array and grads.typecode in ("Q", WORD) else _ptr_array(grads)
+    status = lib().mpadam_grad_norm(state, arr.buffer_info()[0], max_norm, out or None, stream or None)
+    if status:
+        _check(status)
+
+
+def mpadam_grad_norm_destroy(state: int) -> None:
+    _check(lib().mpadam_grad_norm_destroy(state))
+
+
+def mpadam_e4m3_quantize(x: int, x_dtype: int, rows: int, cols: int, ld: int, square: int, q: int, s: int, ldq: int,
+                         qt: int, st: int, ldqt: int, stream: int = 0) -> None:
+    status = lib().mpadam_e4m3_quantize(x or None, x_dtype, rows, cols, ld, square, q or None, s or None, ldq,
+                                        qt or None, st or None, ldqt, stream or None)
+    if status:
+        _check(status)
+
+
+def mpadam_e4m3_matmul(product: mpadam_e4m3_product, stream: int = 0) -> None:
+    status = lib().mpadam_e4m3_matmul(ctypes.byref(product), stream or None)
+    if status:
+        _check(status)
+
+
+def mpadam_e4m3_status(stream: int = 0) -> int:
+    """Waits for `stream`; returns and clears the products' device error bits (0: no bounded wait gave up)."""
+    out = ctypes.c_int32()
+    _check(lib().mpadam_e4m3_status(stream or None, ctypes.byref(out)))
+    return out.value

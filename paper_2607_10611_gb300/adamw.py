@@ -1,0 +1,160 @@
+"""AdamW and the global gradient norm over lists of torch tensors: argument
+marshalling around mpadam_adamw_* and mpadam_grad_norm_* (no arithmetic here).
+"""
+from __future__ import annotations
+
+from typing import Optional, Sequence
+
+import torch
+
+from . import _native as N
+from .optimizer import _pointers, _raw_stream
+
+_FLOAT = {"f32": torch.float32, "bf16": torch.bfloat16}
+_STATE = {"f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+BLOCK = 128  # elements that share a scale of 8-bit moments
+
+
+def _check(tensors, dtype, what):
+    for t in tensors:
+        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{what}: expected contiguous CUDA tensors of {dtype}")
+
+
+def _check_grads(grads, numels, dtype, device):
+    """What a kernel would read past or misread: a gradient of another size, type, layout or device."""
+    if len(grads) != len(numels):
+        raise ValueError(f"{len(grads)} gradients for {len(numels)} tensors")
+    for g, n in zip(grads, numels):
+        if g.dtype != dtype or g.numel() != n or g.device != device or not g.is_contiguous():
+            raise ValueError(f"gradients must be contiguous {dtype} tensors on {device}, as large as their weights")
+
+
+class AdamW:
+    """One fused AdamW step per call over every tensor of a list.
+
+    w: contiguous CUDA tensors of `weight_dtype` ("f32" or "bf16"), updated in
+    place, as are the moments m and v: binary32 tensors (state_dtype "f32"), or
+    (state_dtype "e4m3") float8_e4m3fn tensors of the same sizes with m_scales
+    and v_scales, float8_e8m0fnu tensors of ceil(numel / 128) scales each; v then
+    holds the second moment's square root.  init_state() makes either.
+    compute: with binary32 weights, BF16 tensors that every step overwrites with
+    the rounded weights (entries may be None).  The tensors' memory has to stay
+    where it is; the object keeps references to them.
+    """
+
+    def __init__(self, w: Sequence[torch.Tensor], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor], *,
+                 m_scales: Optional[Sequence[torch.Tensor]] = None,
+                 v_scales: Optional[Sequence[torch.Tensor]] = None,
+                 compute: Optional[Sequence[Optional[torch.Tensor]]] = None, weight_dtype: str = "bf16",
+                 grad_dtype: str = "bf16", state_dtype: str = "f32", rounding: str = "nearest",
+                 state_rounding: Optional[str] = None, seed: int = 0, beta1: float = 0.9, beta2: float = 0.999,
+                 eps: float = 1e-8, weight_decay: float = 0.01):
+        self.w, self.m, self.v = list(w), list(m), list(v)
+        n = len(self.w)
+        low = state_dtype == "e4m3"
+        if low and (m_scales is None or v_scales is None):
+            raise ValueError("8-bit moments need m_scales and v_scales")
+        if not low and (m_scales is not None or v_scales is not None):
+            raise ValueError("binary32 moments have no scales")
+        self.m_scales, self.v_scales = (list(m_scales), list(v_scales)) if low else ([None] * n, [None] * n)
+        self.compute = list(compute) if compute is not None else [None] * n
+        if not (len(self.m) == len(self.v) == len(self.m_scales) == len(self.v_scales) == len(self.compute) == n):
+            raise ValueError("one entry per tensor in every list")
+        _check(self.w, _FLOAT[weight_dtype], "weights")
+        _check(self.m + self.v, _STATE[state_dtype], "moments")
+        copies = [c for c in self.compute if c is not None]
+        _check(copies, torch.bfloat16, "compute copies")
+        scales = self.m_scales + self.v_scales if low else []
+        _check(scales, torch.float8_e8m0fnu, "scales")
+        self.device = self.w[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        if any(t.device != self.device for t in self.w + self.m + self.v + copies + scales):
+            raise ValueError("all tensors of a list must be on one device")
+        self.numels = [t.numel() for t in self.w]
+        for k, size in enumerate(self.numels):
+            if self.m[k].numel() != size or self.v[k].numel() != size:
+                raise ValueError(f"tensor {k}: moments differ in size from the weights")
+            if self.compute[k] is not None and self.compute[k].numel() != size:
+                raise ValueError(f"tensor {k}: the compute copy differs in size from the weights")
+            if low and not self.m_scales[k].numel() == self.v_scales[k].numel() == -(-size // BLOCK):
+                raise ValueError(f"tensor {k}: needs one scale per {BLOCK} elements")
+        self.grad_dtype = _FLOAT[grad_dtype]
+        if state_rounding is None:
+            state_rounding = "stochastic" if low else "nearest"
+        cfg = N.mpadam_adamw_config(beta1, beta2, eps, weight_decay, N.DTYPE[weight_dtype], N.DTYPE[grad_dtype],
+                                    N.DTYPE[state_dtype], N.ROUNDING[rounding], N.ROUNDING[state_rounding], 0, seed)
+        ptr = lambda t: t.data_ptr() if t is not None else 0
+        with torch.cuda.device(self.device):
+            self.state = N.mpadam_adamw_create(
+                [tuple(map(ptr, row)) + (size,) for *row, size in
+                 zip(self.w, self.m, self.v, self.m_scales, self.v_scales, self.compute, self.numels)], cfg)
+
+    @staticmethod
+    def init_state(w: Sequence[torch.Tensor], state_dtype: str = "e4m3") -> dict:
+        """Zero moments for the weights w, as keyword arguments of AdamW: m, v (and m_scales, v_scales)."""
+        new = lambda: [torch.zeros(t.shape, dtype=_STATE[state_dtype], device=t.device) for t in w]
+        got = {"m": new(), "v": new(), "state_dtype": state_dtype}
+        if state_dtype == "e4m3":
+            one = lambda t: torch.full((-(-t.numel() // BLOCK),), 127, dtype=torch.uint8,
+                                       device=t.device).view(torch.float8_e8m0fnu)
+            got.update(m_scales=[one(t) for t in w], v_scales=[one(t) for t in w])
+        return got
+
+    def step(self, grads: Sequence[torch.Tensor], t: int, lr: float, grad_scale: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None):
+        """Step t (from 1) with learning rate lr, asynchronously.  grad_scale: a CUDA float32 tensor whose first
+        element multiplies every gradient (GradNorm's [1:]), NaN: the step changes nothing."""
+        _check_grads(grads, self.numels, self.grad_dtype, self.device)
+        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.device != self.device
+                                       or grad_scale.numel() < 1):
+            raise ValueError(f"grad_scale must be a float32 tensor on {self.device}")
+        s = stream.cuda_stream if stream else _raw_stream(self.device)
+        N.mpadam_adamw_step(self.state, _pointers(grads), t, lr,
+                            grad_scale.data_ptr() if grad_scale is not None else 0, s)
+
+    def close(self):
+        if getattr(self, "state", None):
+            N.mpadam_adamw_destroy(self.state)
+            self.state = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GradNorm:
+    """The global 2-norm of a list of gradients with the given sizes, and the multiplier that clips them."""
+
+    def __init__(self, numels: Sequence[int], grad_dtype: str = "bf16", device: Optional[torch.device] = None):
+        self.numels, self.grad_dtype = [int(n) for n in numels], _FLOAT[grad_dtype]
+        device = torch.device("cuda" if device is None else device)
+        if device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        self.device = device
+        with torch.cuda.device(device):
+            self.state = N.mpadam_grad_norm_create(self.numels, N.DTYPE[grad_dtype])
+
+    def __call__(self, grads: Sequence[torch.Tensor], max_norm: float = float("inf"),
+                 out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """float32 [2], asynchronously: the norm, and min(1, max_norm / norm) (NaN when the norm is not finite)."""
+        _check_grads(grads, self.numels, self.grad_dtype, self.device)
+        if out is None:
+            out = torch.empty(2, dtype=torch.float32, device=self.device)
+        elif out.dtype != torch.float32 or out.device != self.device or out.numel() < 2 or not out.is_contiguous():
+            raise ValueError(f"out must be two contiguous float32 elements on {self.device}")
+        s = stream.cuda_stream if stream else _raw_stream(self.device)
+        N.mpadam_grad_norm(self.state, _pointers(grads), max_norm, out.data_ptr(), s)
+        return out
+
+    def close(self):
+        if getattr(self, "state", None):
+            N.mpadam_grad_norm_destroy(self.state)
+            self.state = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

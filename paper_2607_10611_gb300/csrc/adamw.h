@@ -1,0 +1,75 @@
+// adamw.h -- launch arguments of the AdamW step and of the gradient norm over a
+// list of tensors (internal to the CUDA library; the C ABI is mpadam_adamw_* and
+// mpadam_grad_norm_* in include/mpadam.h).
+#pragma once
+
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "step_args.h"
+
+namespace mpadam {
+
+constexpr int kListTile = 2048;      // elements per tile; a tensor's last tile may be short
+constexpr int kInlineGrads = 448;    // gradient pointers that travel with one launch
+
+// One tensor of the list. Its tiles are tile0, tile0 + 1, ...
+struct ListTensor {
+  void* w;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  uint16_t* compute;
+  int64_t numel;
+  int64_t goff;     // global index of element 0 (a multiple of 128)
+  int64_t tile0;
+  int64_t aligned;  // every pointer of the tensor is a multiple of 16 bytes
+};
+
+// Gradient pointers: in the launch itself, or (grads != nullptr) in device memory.
+struct GradTable {
+  const void* const* grads;
+  const void* inline_grads[kInlineGrads];
+};
+
+struct AdamwScalars {
+  float b1, b2, omb1, omb2, ka, c2, eps, kwd;
+};
+
+struct AdamwArgs {
+  const ListTensor* tensors;
+  const int32_t* tile_tensor;  // [tiles] the tensor each tile belongs to
+  int64_t tiles;
+  AdamwScalars s;
+  const float* grad_scale;     // device multiplier of the gradients, or nullptr
+  uint32_t rk0[kPhiloxRounds], rk1[kPhiloxRounds];
+  uint32_t t_lo, t_hi;
+  GradTable g;
+};
+
+struct AdamwKind {
+  bool w_f32, g_f32, state_e4m3, sr, state_sr;
+};
+
+cudaError_t launch_adamw(const AdamwArgs& a, const AdamwKind& k, cudaStream_t stream);
+
+struct NormArgs {
+  const ListTensor* tensors;
+  const int32_t* tile_tensor;
+  int64_t tiles;
+  double* partial;       // [ctas] of the launch
+  uint32_t* done;        // CTAs that have written theirs; 0 between launches
+  float* out;            // norm, multiplier
+  float max_norm;
+  int32_t g_f32;
+  GradTable g;
+};
+
+constexpr int kNormCtas = 152 * 4;
+cudaError_t launch_grad_norm(const NormArgs& a, cudaStream_t stream);
+
+// Copies count gradient pointers into a device table at `first`.
+cudaError_t fill_grads(const void** table, const void* const* grads, int32_t first, int32_t count, cudaStream_t stream);
+
+}  // namespace mpadam

@@ -1,0 +1,337 @@
+// fp8_matmul.cu -- D[m, n] (+)= A[m, k] B[n, k]^T for E4M3 matrices with a
+// power-of-two scale per block of 128 along k:
+//   D_ij = sum over blocks c of 2^(ea_ic + eb_jc) sum over k in c of A_ik B_jk.
+// The tensor cores apply the scales themselves (block-scaled tcgen05.mma: one
+// E8M0 scale per row and 32 values of k, four such steps sharing a block's
+// scale) and accumulate in binary32.
+//
+// Layout of a tile.  The rows of b lie along the 128 lanes of tensor memory and
+// the rows of a along its columns, so that a warp that reads a column holds 32
+// neighbouring elements of a row of D and stores them straight from registers.
+// It also makes the a side the one whose tile may be small: a single token is a
+// tile of 16 columns and no tensor work is spent on rows that are not there.
+#include <algorithm>
+#include <atomic>
+
+#include "fp8.h"
+#include "step_kernel.cuh"
+
+namespace mpadam {
+
+namespace {
+
+constexpr int kTileN = 128;   // rows of b per tile (lanes of tensor memory)
+constexpr int kTileK = 128;   // values of k per stage (bytes of a row: one 128-byte swizzle atom)
+constexpr int kSms = 152;      // GB300
+constexpr int kEpiWarps = 8;
+constexpr int kMatmulThreads = 32 * (4 + kEpiWarps);  // a producer and an issuing warp (and two idle ones), then the epilogue
+
+enum MatmulError : int32_t { kErrCopy = 1, kErrStage = 2, kErrAcc = 4, kErrAccFree = 8 };
+
+__device__ int32_t g_matmul_error;
+
+template <int TM>
+struct Shape {
+  static constexpr int kScaleTilesA = (TM + 127) / 128;
+  static constexpr int kScaleBytes = kScaleTile * (1 + kScaleTilesA);
+  static constexpr int kStageBytes = (kTileN + TM) * kTileK + 2048;  // codes, then scales; keeps 1024-byte alignment
+  static constexpr int kStages = TM >= 256 ? 4 : TM >= 128 ? 6 : 8;
+  static constexpr int kAccs = TM >= 256 ? 1 : 2;
+  // Tensor memory: accumulators, then two sets of scales (4 columns for b, 4 per 128 rows for a).
+  static constexpr int kScaleCols = 4 + 4 * kScaleTilesA;
+  static constexpr int kUsedCols = kAccs * TM + 2 * kScaleCols;
+  static constexpr int kCols = kUsedCols <= 64 ? 64 : kUsedCols <= 128 ? 128 : kUsedCols <= 256 ? 256 : 512;
+  static constexpr int kDynSmem = kStages * kStageBytes + 1024;
+};
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Descriptor of an operand tile in shared memory: rows of 128 bytes in the
+// 128-byte swizzle, groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)2 << 61;
+}
+// Descriptor of a tile of scales: 32 rows of 16 bytes, no swizzle, groups of 8 rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+// Scales of 128 rows into four columns, the same in each quarter of the lanes.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                           uint32_t add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+
+// 16 columns of this warp's 32 lanes.
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Instruction descriptor: E4M3 operands, E8M0 scales, m = 128 lanes, n = TM columns; the scales' byte of the two
+// operands' 32-bit columns.
+template <int TM>
+__device__ __forceinline__ uint32_t instr_desc(uint32_t byte) {
+  return (uint32_t)(TM >> 3) << 17 | 1u << 23 | (uint32_t)(kTileN >> 4) << 24 | byte << 4 | byte << 29;
+}
+
+template <int TM, bool F32>
+__global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_constant__ MatmulArgs p) {
+  using S = Shape<TM>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ alignas(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int32_t failed;
+  const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t bar0 = smem_addr(bars);
+  auto full = [&](int s) { return bar0 + 8u * s; };
+  auto empty = [&](int s) { return bar0 + 8u * (S::kStages + s); };
+  auto acc_full = [&](int s) { return bar0 + 8u * (2 * S::kStages + s); };
+  auto acc_free = [&](int s) { return bar0 + 8u * (2 * S::kStages + S::kAccs + s); };
+  const uint32_t drained = bar0 + 8u * (2 * S::kStages + 2 * S::kAccs);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 1);
+    }
+    for (int s = 0; s < S::kAccs; ++s) {
+      mbar_init(acc_full(s), 1);
+      mbar_init(acc_free(s), kEpiWarps);
+    }
+    mbar_init(drained, 1);
+    failed = 0;
+    mbar_init_fence();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_s)),
+                 "r"((uint32_t)S::kCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;
+  const uint32_t tmem_scales = tmem + S::kAccs * TM;
+
+  const int tiles_n = (p.n + kTileN - 1) / kTileN, tiles_m = (p.m + TM - 1) / TM;
+  const int tiles = tiles_n * tiles_m;
+  const int steps = (p.k + kTileK - 1) / kTileK;
+  const int groups = (steps + 3) / 4;
+  const int last_scale_a = (p.m - 1) / 128;
+  volatile int32_t* stop = &failed;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int s = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      int issued = 0;
+      for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+        const int tn = t / tiles_m, tm = t % tiles_m;
+        for (int k = 0; k < steps; ++k) {
+          if (*stop || !mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
+          const uint32_t st = smem + s * S::kStageBytes;
+          const bool scales = (k & 3) == 0;
+          mbar_arrive_tx(full(s), (kTileN + TM) * kTileK + (scales ? S::kScaleBytes : 0));
+          tma_load_2d(st, &p.b, k * kTileK, tn * kTileN, full(s));
+          tma_load_2d(st + kTileN * kTileK, &p.a, k * kTileK, tm * TM, full(s));
+          if (scales) {
+            const uint32_t sc = st + (kTileN + TM) * kTileK;
+            bulk_load(sc, p.sb + ((int64_t)tn * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
+            for (int j = 0; j < S::kScaleTilesA; ++j) {
+              const int r = min(tm * TM / 128 + j, last_scale_a);
+              bulk_load(sc + kScaleTile * (1 + j), p.sa + ((int64_t)r * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
+            }
+          }
+          ++issued;
+          if (++s == S::kStages) { s = 0; phase ^= 1; }
+        }
+      }
+      if (!ok) {
+        *stop = 1;
+        atomicOr(p.err, kErrStage);
+        // the copies in flight, those of the last stages, before the block's memory goes
+        for (int i = 0; i < min(issued, S::kStages); ++i) {
+          if (s == 0) { s = S::kStages; phase ^= 1; }
+          --s;
+          mbar_wait(full(s), phase);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int s = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+        if (*stop || !mbar_wait(acc_free(acc), acc_phase ^ 1)) { ok = false; atomicOr(p.err, kErrAccFree); break; }
+        tc_fence_after();
+        const uint32_t d = tmem + acc * TM;
+        for (int k = 0; k < steps; ++k) {
+          if (*stop || !mbar_wait(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
+          tc_fence_after();
+          const uint32_t st = smem + s * S::kStageBytes;
+          const uint32_t sb = tmem_scales + ((k >> 2) & 1) * S::kScaleCols, sa = sb + 4;
+          if ((k & 3) == 0) {
+            const uint32_t sc = st + (kTileN + TM) * kTileK;
+            copy_scales(sb, scale_desc(sc));
+            for (int j = 0; j < S::kScaleTilesA; ++j) copy_scales(sa + 4 * j, scale_desc(sc + kScaleTile * (1 + j)));
+          }
+          // A tile of fewer than 128 rows of a starts inside its scale tile, at a multiple of 16 rows: columns hold 32
+          // rows each, and the first row's lane follows from the tile's place.
+          const uint64_t db = operand_desc(st), da = operand_desc(st + kTileN * kTileK);
+          const uint32_t id = instr_desc<TM>(k & 3);
+          const int tm = t % tiles_m;
+          const uint32_t sa_col = TM < 128 ? sa + (uint32_t)(tm * TM % 128) / 32 : sa;
+#pragma unroll
+          for (int i = 0; i < kTileK / 32; ++i)
+            mma_scaled(d, db + 2 * i, da + 2 * i, id, sb, sa_col, k > 0 || i > 0);
+          mma_commit(empty(s));
+          if (++s == S::kStages) { s = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        mma_commit(acc_full(acc));
+        if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
+      }
+      if (!ok) {  // the products in flight, before their memory goes
+        *stop = 1;
+        mma_commit(drained);
+        mbar_wait(drained, 0);
+      }
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    constexpr int kHalf = TM / 2 >= 16 ? TM / 2 : 16;  // columns of one warp
+    const bool mine = half * kHalf < TM;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+      if (*stop || !mbar_wait(acc_full(acc), acc_phase)) {
+        if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
+        break;
+      }
+      __syncwarp();
+      tc_fence_after();
+      const int tn = t / tiles_m, tm = t % tiles_m;
+      const int n = tn * kTileN + quarter * 32 + lane;
+      if (mine) {
+        for (int c = half * kHalf; c < half * kHalf + kHalf; c += 16) {
+          const int m0 = tm * TM + c;
+          if (m0 >= p.m) break;
+          uint32_t r[16];
+          __syncwarp();
+          tmem_load16(tmem + acc * TM + c + ((uint32_t)(quarter * 32) << 16), r);
+          tmem_wait_load();
+          if (n < p.n) {
+            const int rows = min(16, p.m - m0);
+            const int64_t at = (int64_t)m0 * p.ldd + n;
+            if (F32) {
+              float* d = static_cast<float*>(p.d) + at;
+              if (p.accumulate) {
+                float old[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) old[j] = j < rows ? d[j * p.ldd] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__fadd_rn(old[j], __uint_as_float(r[j])));
+              }
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (j < rows) d[j * p.ldd] = __uint_as_float(r[j]);
+            } else {
+              uint16_t* d = static_cast<uint16_t*>(p.d) + at;
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (j < rows) d[j * p.ldd] = (uint16_t)bf16x2_rn(__uint_as_float(r[j]), 0.0f);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(acc_free(acc));
+      if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::kCols) : "memory");
+}
+
+template <int TM, bool F32>
+cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
+  using S = Shape<TM>;
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use this much shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(matmul_kernel<TM, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kDynSmem);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit);
+  }
+  const int64_t tiles = (int64_t)((a.n + kTileN - 1) / kTileN) * ((a.m + TM - 1) / TM);
+  matmul_kernel<TM, F32><<<(unsigned)std::min<int64_t>(tiles, kSms), kMatmulThreads, S::kDynSmem, stream>>>(a);
+  return cudaGetLastError();
+}
+
+template <int TM>
+cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
+  return a.f32 ? launch<TM, true>(a, stream) : launch<TM, false>(a, stream);
+}
+
+}  // namespace
+
+int matmul_tile(int64_t m, int64_t n, int64_t k) {
+  return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : m <= 128 ? 128 : 256;
+}
+
+cudaError_t launch_matmul(MatmulArgs& a, int tile, cudaStream_t stream) {
+  switch (tile) {
+    case 16: return launch<16>(a, stream);
+    case 32: return launch<32>(a, stream);
+    case 64: return launch<64>(a, stream);
+    case 128: return launch<128>(a, stream);
+    default: return launch<256>(a, stream);
+  }
+}
+
+cudaError_t matmul_error_word(int32_t** p) {
+  return cudaGetSymbolAddress(reinterpret_cast<void**>(p), g_matmul_error);
+}
+
+}  // namespace mpadam

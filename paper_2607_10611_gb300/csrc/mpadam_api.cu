@@ -18,11 +18,17 @@
 #include <string>
 #include <vector>
 
+#include "host.h"
 #include "mpadam.h"
 #include "step_args.h"
 #include "step_kernel.cuh"
 #include "toy.h"
 
+using mpadam::cuda_fail;
+using mpadam::dev_malloc;
+using mpadam::fail;
+using mpadam::is_aligned;
+using mpadam::round_keys;
 using mpadam::StepArgs;
 using mpadam::StepScalars;
 using mpadam::TensorAux;
@@ -44,18 +50,18 @@ bool injected_failure() {
   return false;
 }
 
-// Every device and pinned allocation of the library goes through these.
-cudaError_t dev_malloc(void** p, size_t bytes) {
-  if (injected_failure()) { *p = nullptr; return cudaErrorMemoryAllocation; }
-  return cudaMalloc(p, bytes);
-}
-template <typename T>
-cudaError_t dev_malloc(T** p, size_t bytes) {
-  return dev_malloc(reinterpret_cast<void**>(p), bytes);
-}
 cudaError_t host_malloc(void** p, size_t bytes) {
   if (injected_failure()) { *p = nullptr; return cudaErrorMemoryAllocation; }
   return cudaMallocHost(p, bytes);
+}
+
+}  // namespace
+
+namespace mpadam {
+
+cudaError_t dev_malloc(void** p, size_t bytes) {
+  if (injected_failure()) { *p = nullptr; return cudaErrorMemoryAllocation; }
+  return cudaMalloc(p, bytes);
 }
 
 int32_t fail(int32_t code, const char* fmt, ...) {
@@ -72,15 +78,26 @@ int32_t cuda_fail(cudaError_t e, const char* what) {
   return fail(MPADAM_ECUDA, "%s: %s (%s)", what, cudaGetErrorString(e), cudaGetErrorName(e));
 }
 
+void round_keys(uint64_t seed, uint32_t* rk0, uint32_t* rk1) {
+  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+  for (int r = 0; r < kPhiloxRounds; ++r) {
+    rk0[r] = k0;
+    rk1[r] = k1;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+}
+
+}  // namespace mpadam
+
+namespace {
+
 size_t elem_size(int32_t dt) { return dt == MPADAM_F32 ? 4 : (dt == MPADAM_BF16 ? 2 : 1); }
 
 // Bytes of n stored weights (NVFP4: two per byte).
 size_t weight_bytes(int32_t wd, int64_t n) {
   return wd == MPADAM_NVFP4 ? (size_t)((n + 1) / 2) : (size_t)n * elem_size(wd);
 }
-
-// a: a power of two
-bool is_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // Per-step binary32 scalars of the canonical update, from binary64.
 float toward_zero(double x) {
@@ -141,17 +158,6 @@ void make_pairs(const StepScalars& s, mpadam::StepPairs* p) {
   p->nc2 = twice(s.wd_on ? -0x1.4p-21f : -0x1.4p-22f);  // 1.25 2^-22, twice with decay
   p->nc0 = twice(-0x1p-96f);
   p->m1 = twice(-1.0f);
-}
-
-// Philox4x32-10 round keys: key + r * (0x9E3779B9, 0xBB67AE85), r = 0..9.
-void round_keys(uint64_t seed, uint32_t* rk0, uint32_t* rk1) {
-  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
-  for (int r = 0; r < mpadam::kPhiloxRounds; ++r) {
-    rk0[r] = k0;
-    rk1[r] = k1;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
-  }
 }
 
 // Shared-memory ring of a step kernel instance: one stage holds one tile of
