@@ -30,6 +30,7 @@ struct QuantArgs {
   uint8_t* st;
   int64_t ldq, ldqt;
   int32_t f32, square;
+  int32_t vec;         // rows of x start on 16-byte boundaries (set by the launch)
 };
 
 cudaError_t launch_quantize(const QuantArgs& a, cudaStream_t stream);

@@ -10,16 +10,14 @@ namespace mpadam {
 
 namespace {
 
+// A CTA takes a tile of 128 x 128 and a thread a patch of 8 x 8, in registers
+// from the load to the last store: nothing is staged.  A warp is 4 patches wide
+// and 8 high, so that every access, to either output, is of whole 32-byte
+// sectors: 64 bytes of a row of x in BF16, 32 of a row of codes, 64 of a row of
+// the transpose's.
 constexpr int kQuantThreads = 256;
-constexpr int kQuantWarps = kQuantThreads / 32;
-constexpr int kTile = 128;     // a CTA takes a tile of 128 x 128
-constexpr int kPitch = 129;    // words of a tile's row in shared memory: columns fall on different banks
+constexpr int kTile = 128;
 
-// The bits of |x| where x is finite, else 0.
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-  return b < 0x7F800000u ? b : 0u;
-}
 // The smallest k >= -127 with a <= 448 2^k, a given by its bits; 0 for a = 0.
 // 448 = 1.75 2^8, so k = floor(log2 a) - 8, and one more where a's mantissa is
 // above 1.75: adding 0x1FFFFF carries into the exponent exactly then.
@@ -36,22 +34,110 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   return h;
 }
 
+// A patch: 8 rows of 8 values, BF16 ones packed in pairs.
 template <bool F32>
-__device__ __forceinline__ float load(const void* x, int64_t at) {
-  if (F32) return __ldg(static_cast<const float*>(x) + at);
-  return __uint_as_float((uint32_t)__ldg(static_cast<const uint16_t*>(x) + at) << 16);
-}
+struct Patch;
 
-// Codes of 128 values v[i] at i = 4 lane .. 4 lane + 3, stored where inside.
-__device__ __forceinline__ void store_codes(uint8_t* q, int64_t left, int lane, const float (&v)[4], float inv) {
-  const uint32_t c = e4m3x2(__fmul_rn(v[0], inv), __fmul_rn(v[1], inv)) |
-                     e4m3x2(__fmul_rn(v[2], inv), __fmul_rn(v[3], inv)) << 16;
-  const int i = 4 * lane;
-  if (i + 4 <= left) {
-    *reinterpret_cast<uint32_t*>(q + i) = c;
+template <>
+struct Patch<true> {
+  float x[8][8];
+  static constexpr uint32_t kInf = 0x7F800000u;
+  __device__ __forceinline__ void load_row(const void* p, int64_t at, int64_t left, bool vec, int r) {
+    const float* q = static_cast<const float*>(p) + at;
+    if (vec && left >= 8) {
+      const float4 a = __ldcs(reinterpret_cast<const float4*>(q)), b = __ldcs(reinterpret_cast<const float4*>(q) + 1);
+      x[r][0] = a.x, x[r][1] = a.y, x[r][2] = a.z, x[r][3] = a.w;
+      x[r][4] = b.x, x[r][5] = b.y, x[r][6] = b.z, x[r][7] = b.w;
+    } else {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[r][c] = c < left ? q[c] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void clear_row(int r) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[r][c] = 0.0f;
+  }
+  __device__ __forceinline__ float get(int r, int c) const { return x[r][c]; }
+  // Largest |value| of each row and column over the warp's lanes that share it, as bits; FINITE: of the finite ones.
+  template <bool FINITE>
+  __device__ __forceinline__ void maxima(uint32_t (&rows)[8], uint32_t (&cols)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rows[i] = cols[i] = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        uint32_t a = __float_as_uint(x[r][c]) & 0x7FFFFFFFu;
+        if (FINITE && a >= kInf) a = 0;
+        rows[r] = max(rows[r], a);
+        cols[c] = max(cols[c], a);
+      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) rows[i] = max(rows[i], __shfl_xor_sync(~0u, rows[i], d));
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) cols[i] = max(cols[i], __shfl_xor_sync(~0u, cols[i], d));
+    }
+  }
+  static __device__ __forceinline__ uint32_t wide(uint32_t a) { return a; }
+};
+
+template <>
+struct Patch<false> {
+  uint32_t x[8][4];
+  static constexpr uint32_t kInf = 0x7F80u;
+  __device__ __forceinline__ void load_row(const void* p, int64_t at, int64_t left, bool vec, int r) {
+    const uint16_t* q = static_cast<const uint16_t*>(p) + at;
+    if (vec && left >= 8) {
+      const uint4 a = __ldcs(reinterpret_cast<const uint4*>(q));
+      x[r][0] = a.x, x[r][1] = a.y, x[r][2] = a.z, x[r][3] = a.w;
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        x[r][c] = (2 * c < left ? (uint32_t)q[2 * c] : 0u) | (2 * c + 1 < left ? (uint32_t)q[2 * c + 1] << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ void clear_row(int r) { x[r][0] = x[r][1] = x[r][2] = x[r][3] = 0; }
+  __device__ __forceinline__ float get(int r, int c) const { return c & 1 ? bf16_hi(x[r][c / 2]) : bf16_lo(x[r][c / 2]); }
+  // In 16-bit halves, two rows or columns to a word.
+  template <bool FINITE>
+  __device__ __forceinline__ void maxima(uint32_t (&rows)[8], uint32_t (&cols)[8]) const {
+    uint32_t rp[4], cp[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t a = x[r][c] & 0x7FFF7FFFu;
+        if (FINITE) a &= ~__vcmpgeu2(a, 0x7F807F80u);
+        m = __vmaxu2(m, a);
+        cp[c] = __vmaxu2(cp[c], a);
+      }
+      m = __vmaxu2(m, m >> 16);  // in the low half
+      rp[r / 2] = r & 1 ? __byte_perm(rp[r / 2], m, 0x5410) : m;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) rp[i] = __vmaxu2(rp[i], __shfl_xor_sync(~0u, rp[i], d));
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) cp[i] = __vmaxu2(cp[i], __shfl_xor_sync(~0u, cp[i], d));
+      rows[2 * i] = rp[i] & 0xFFFFu, rows[2 * i + 1] = rp[i] >> 16;
+      cols[2 * i] = cp[i] & 0xFFFFu, cols[2 * i + 1] = cp[i] >> 16;
+    }
+  }
+  static __device__ __forceinline__ uint32_t wide(uint32_t a) { return a << 16; }
+};
+
+// 8 codes (two words), `left` of them inside.
+__device__ __forceinline__ void store_codes(uint8_t* q, int64_t left, uint32_t lo, uint32_t hi) {
+  if (left >= 8) {
+    *reinterpret_cast<uint2*>(q) = make_uint2(lo, hi);
   } else {
-    for (int j = 0; j < 4; ++j)
-      if (i + j < left) q[i + j] = (uint8_t)(c >> (8 * j));
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) q[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
   }
 }
 
@@ -64,75 +150,100 @@ __device__ __forceinline__ void store_scale(uint8_t* s, int64_t row, int64_t blo
 }
 
 template <bool F32>
-__global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const __grid_constant__ QuantArgs p) {
-  extern __shared__ float tile[];  // [kTile][kPitch]
-  __shared__ uint32_t square_max[kQuantWarps];
+__global__ void __launch_bounds__(kQuantThreads, F32 ? 2 : 3) quantize_kernel(const __grid_constant__ QuantArgs p) {
+  __shared__ uint32_t row_max[4][kTile], col_max[2][kTile];
+  __shared__ alignas(16) float row_inv[kTile], col_inv[kTile];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int wc = warp & 3, wr = warp >> 2;
+  const int pc = wc * 32 + (lane & 3) * 8, pr = wr * 64 + (lane >> 2) * 8;  // the patch's place in the tile
   const int64_t blocks_c = (p.cols + kTile - 1) / kTile, blocks_r = (p.rows + kTile - 1) / kTile;
   const int64_t tr = blockIdx.x / blocks_c, tc = blockIdx.x % blocks_c;
-  const int64_t r0 = tr * kTile, c0 = tc * kTile;
+  const int64_t r0 = tr * kTile + pr, c0 = tc * kTile + pc;
   const int64_t left_r = p.rows - r0, left_c = p.cols - c0;
 
-  uint32_t seen = 0;
-  for (int r = warp; r < kTile; r += kQuantWarps) {
+  Patch<F32> x;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = lane + 32 * j;
-      const float v = r < left_r && c < left_c ? load<F32>(p.x, (r0 + r) * p.ld + c0 + c) : 0.0f;
-      tile[r * kPitch + c] = v;
-      seen = max(seen, finite_bits(v));
-    }
+  for (int r = 0; r < 8; ++r) {
+    if (r < left_r && left_c > 0) x.load_row(p.x, (r0 + r) * p.ld + c0, left_c, p.vec, r);
+    else x.clear_row(r);
   }
-  if (p.square) {
-    seen = __reduce_max_sync(~0u, seen);
-    if (lane == 0) square_max[warp] = seen;
+  // Maxima of all |values|; where one is not finite, once more over the finite ones.
+  uint32_t rows[8], cols[8];
+  x.template maxima<false>(rows, cols);
+  auto publish = [&] {
+    if ((lane & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) row_max[wc][pr + i] = rows[i];
+    }
+    if (lane < 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) col_max[wr][pc + i] = cols[i];
+    }
+  };
+  publish();
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = max(most, rows[i]);
+  if (__syncthreads_or(most >= Patch<F32>::kInf)) {
+    x.template maxima<true>(rows, cols);
+    publish();
+    __syncthreads();
+  }
+  // Half of the threads finish a row each, the others a column.
+  {
+    const int i = threadIdx.x & 127;
+    const bool is_row = threadIdx.x < 128;
+    uint32_t a;
+    if (p.square) {
+      a = max(max(row_max[0][i], row_max[1][i]), max(row_max[2][i], row_max[3][i]));
+      a = __reduce_max_sync(~0u, a);
+      __syncthreads();
+      if (lane == 0) row_max[0][warp] = a;
+      __syncthreads();
+      a = max(max(row_max[0][0], row_max[0][1]), max(row_max[0][2], row_max[0][3]));
+    } else {
+      a = is_row ? max(max(row_max[0][i], row_max[1][i]), max(row_max[2][i], row_max[3][i])) : max(col_max[0][i], col_max[1][i]);
+    }
+    const int k = block_exponent(Patch<F32>::wide(a));
+    if (is_row) {
+      row_inv[i] = inverse_scale(k);
+      if (p.q) store_scale(p.s, tr * kTile + i, tc, blocks_c, tr * kTile + i < p.rows ? k : 0);
+    } else {
+      col_inv[i] = inverse_scale(k);
+      if (p.qt) store_scale(p.st, tc * kTile + i, tr, blocks_r, tc * kTile + i < p.cols ? k : 0);
+    }
   }
   __syncthreads();
-  int k = 0;
-  if (p.square) {
-    seen = 0;
-    for (int w = 0; w < kQuantWarps; ++w) seen = max(seen, square_max[w]);
-    k = block_exponent(seen);
-  }
-  if (p.q) {
-    for (int r = warp; r < kTile; r += kQuantWarps) {
-      float v[4];
-      uint32_t a = 0;
+  if (p.q && left_c > 0) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = tile[r * kPitch + 4 * lane + j];
-        a = max(a, finite_bits(v[j]));
-      }
-      if (!p.square) k = block_exponent(__reduce_max_sync(~0u, a));
-      const bool row = r < left_r;
-      if (row) store_codes(p.q + (r0 + r) * p.ldq + c0, left_c, lane, v, inverse_scale(k));
-      if (lane == 0) store_scale(p.s, r0 + r, tc, blocks_c, row ? k : 0);
+    for (int r = 0; r < 8; ++r) {
+      if (r >= left_r) break;
+      const float inv = row_inv[pr + r];
+      uint32_t c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[j] = e4m3x2(__fmul_rn(x.get(r, 2 * j), inv), __fmul_rn(x.get(r, 2 * j + 1), inv));
+      store_codes(p.q + (r0 + r) * p.ldq + c0, left_c, c[0] | c[1] << 16, c[2] | c[3] << 16);
     }
   }
-  if (p.qt) {
-    for (int c = warp; c < kTile; c += kQuantWarps) {
-      float v[4];
-      uint32_t a = 0;
+  if (p.qt && left_r > 0) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = tile[(4 * lane + j) * kPitch + c];
-        a = max(a, finite_bits(v[j]));
-      }
-      if (!p.square) k = block_exponent(__reduce_max_sync(~0u, a));
-      const bool col = c < left_c;
-      if (col) store_codes(p.qt + (c0 + c) * p.ldqt + r0, left_r, lane, v, inverse_scale(k));
-      if (lane == 0) store_scale(p.st, c0 + c, tr, blocks_r, col ? k : 0);
+    for (int c = 0; c < 8; ++c) {
+      if (c >= left_c) break;
+      const float inv = col_inv[pc + c];
+      uint32_t u[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) u[j] = e4m3x2(__fmul_rn(x.get(2 * j, c), inv), __fmul_rn(x.get(2 * j + 1, c), inv));
+      store_codes(p.qt + (c0 + c) * p.ldqt + r0, left_r, u[0] | u[1] << 16, u[2] | u[3] << 16);
     }
   }
 }
 
 template <bool F32>
-cudaError_t launch(const QuantArgs& a, cudaStream_t stream) {
-  constexpr int kSmem = kTile * kPitch * 4;
-  cudaError_t e = cudaFuncSetAttribute(quantize_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-  if (e != cudaSuccess) return e;
+cudaError_t launch(QuantArgs a, cudaStream_t stream) {
+  const int64_t size = F32 ? 4 : 2;
+  a.vec = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.ld * size % 16 == 0 || a.rows == 1);
   const int64_t tiles = ((a.cols + kTile - 1) / kTile) * ((a.rows + kTile - 1) / kTile);
-  quantize_kernel<F32><<<(unsigned)tiles, kQuantThreads, kSmem, stream>>>(a);
+  quantize_kernel<F32><<<(unsigned)tiles, kQuantThreads, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
