@@ -173,6 +173,20 @@ def lib() -> ctypes.CDLL:
     return _LIB
 
 
+_EXT = None
+
+
+def ext():
+    """The C++ module that marshals torch tensors (csrc/torch_ext.cpp), raising MPAdamError as this one does."""
+    global _EXT
+    if _EXT is None:
+        lib()
+        module = _build.load_ext()
+        module.set_error(MPAdamError)
+        _EXT = module
+    return _EXT
+
+
 def mpadam_last_error() -> str:
     return lib().mpadam_last_error().decode(errors="replace")
 

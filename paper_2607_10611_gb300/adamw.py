@@ -1,5 +1,6 @@
 """AdamW and the global gradient norm over lists of torch tensors: argument
 marshalling around mpadam_adamw_* and mpadam_grad_norm_* (no arithmetic here).
+What every call does with its list of gradients is csrc/torch_ext.cpp's.
 """
 from __future__ import annotations
 
@@ -8,7 +9,6 @@ from typing import Optional, Sequence
 import torch
 
 from . import _native as N
-from .optimizer import _pointers, _raw_stream
 
 _FLOAT = {"f32": torch.float32, "bf16": torch.bfloat16}
 _STATE = {"f32": torch.float32, "e4m3": torch.float8_e4m3fn}
@@ -19,15 +19,6 @@ def _check(tensors, dtype, what):
     for t in tensors:
         if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
             raise ValueError(f"{what}: expected contiguous CUDA tensors of {dtype}")
-
-
-def _check_grads(grads, numels, dtype, device):
-    """What a kernel would read past or misread: a gradient of another size, type, layout or device."""
-    if len(grads) != len(numels):
-        raise ValueError(f"{len(grads)} gradients for {len(numels)} tensors")
-    for g, n in zip(grads, numels):
-        if g.dtype != dtype or g.numel() != n or g.device != device or not g.is_contiguous():
-            raise ValueError(f"gradients must be contiguous {dtype} tensors on {device}, as large as their weights")
 
 
 class AdamW:
@@ -78,7 +69,6 @@ class AdamW:
                 raise ValueError(f"tensor {k}: the compute copy differs in size from the weights")
             if low and not self.m_scales[k].numel() == self.v_scales[k].numel() == -(-size // BLOCK):
                 raise ValueError(f"tensor {k}: needs one scale per {BLOCK} elements")
-        self.grad_dtype = _FLOAT[grad_dtype]
         if state_rounding is None:
             state_rounding = "stochastic" if low else "nearest"
         cfg = N.mpadam_adamw_config(beta1, beta2, eps, weight_decay, N.DTYPE[weight_dtype], N.DTYPE[grad_dtype],
@@ -88,6 +78,8 @@ class AdamW:
             self.state = N.mpadam_adamw_create(
                 [tuple(map(ptr, row)) + (size,) for *row, size in
                  zip(self.w, self.m, self.v, self.m_scales, self.v_scales, self.compute, self.numels)], cfg)
+        self._spec = N.ext().list_spec(self.numels, grad_dtype == "f32", self.device.index)
+        self._step = N.ext().adamw_step
 
     @staticmethod
     def init_state(w: Sequence[torch.Tensor], state_dtype: str = "e4m3") -> dict:
@@ -104,13 +96,7 @@ class AdamW:
              stream: Optional[torch.cuda.Stream] = None):
         """Step t (from 1) with learning rate lr, asynchronously.  grad_scale: a CUDA float32 tensor whose first
         element multiplies every gradient (GradNorm's [1:]), NaN: the step changes nothing."""
-        _check_grads(grads, self.numels, self.grad_dtype, self.device)
-        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.device != self.device
-                                       or grad_scale.numel() < 1):
-            raise ValueError(f"grad_scale must be a float32 tensor on {self.device}")
-        s = stream.cuda_stream if stream else _raw_stream(self.device)
-        N.mpadam_adamw_step(self.state, _pointers(grads), t, lr,
-                            grad_scale.data_ptr() if grad_scale is not None else 0, s)
+        self._step(self.state, self._spec, grads, t, lr, grad_scale, stream.cuda_stream if stream else None)
 
     def close(self):
         if getattr(self, "state", None):
@@ -128,25 +114,23 @@ class GradNorm:
     """The global 2-norm of a list of gradients with the given sizes, and the multiplier that clips them."""
 
     def __init__(self, numels: Sequence[int], grad_dtype: str = "bf16", device: Optional[torch.device] = None):
-        self.numels, self.grad_dtype = [int(n) for n in numels], _FLOAT[grad_dtype]
+        self.numels = [int(n) for n in numels]
         device = torch.device("cuda" if device is None else device)
         if device.index is None:
             device = torch.device("cuda", torch.cuda.current_device())
         self.device = device
         with torch.cuda.device(device):
             self.state = N.mpadam_grad_norm_create(self.numels, N.DTYPE[grad_dtype])
+        self._spec = N.ext().list_spec(self.numels, grad_dtype == "f32", device.index)
+        self._norm = N.ext().grad_norm
 
     def __call__(self, grads: Sequence[torch.Tensor], max_norm: float = float("inf"),
                  out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """float32 [2], asynchronously: the norm, and min(1, max_norm / norm) (NaN when the norm is not finite)."""
-        _check_grads(grads, self.numels, self.grad_dtype, self.device)
-        if out is None:
-            out = torch.empty(2, dtype=torch.float32, device=self.device)
-        elif out.dtype != torch.float32 or out.device != self.device or out.numel() < 2 or not out.is_contiguous():
-            raise ValueError(f"out must be two contiguous float32 elements on {self.device}")
-        s = stream.cuda_stream if stream else _raw_stream(self.device)
-        N.mpadam_grad_norm(self.state, _pointers(grads), max_norm, out.data_ptr(), s)
-        return out
+        if stream is None:
+            return self._norm(self.state, self._spec, grads, max_norm, out, None)
+        with torch.cuda.stream(stream):  # so that a new out belongs to it
+            return self._norm(self.state, self._spec, grads, max_norm, out, None)
 
     def close(self):
         if getattr(self, "state", None):

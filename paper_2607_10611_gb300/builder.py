@@ -1,13 +1,19 @@
-"""Build the CUDA library libmpadam.so for sm_103a (GB300), in tree.
+"""Build the CUDA library libmpadam.so for sm_103a (GB300), in tree, and the
+Python module _mpadam_torch beside it (tensor marshalling in C++, for the
+installed torch).
 
-Each translation unit compiles in its own nvcc process (in parallel), then
-one nvcc call links the shared library.  Output: paper_2607_10611_gb300/_build/.
+Each translation unit compiles in its own compiler process (in parallel), then
+one call links each of the two.  Output: paper_2607_10611_gb300/_build/.
 """
 from __future__ import annotations
 
+import importlib.machinery
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
@@ -17,6 +23,9 @@ CSRC = PKG / "csrc"
 INCLUDE = ROOT / "include"
 OUT_DIR = PKG / "_build"
 LIB = OUT_DIR / "libmpadam.so"
+EXT = OUT_DIR / "_mpadam_torch.so"
+EXT_SOURCE = "torch_ext.cpp"
+EXT_TORCH = OUT_DIR / "torch_version"  # the torch that EXT was built for
 
 SOURCES = ["mpadam_api.cu", "step_bf16.cu", "step_e4m3.cu", "step_e4m3b.cu", "step_nvfp4.cu", "toy.cu",
            "train_api.cu", "adamw.cu", "fp8_quant.cu", "fp8_matmul.cu"]
@@ -40,14 +49,27 @@ def nvcc() -> str:
 
 
 def _inputs():
-    return [CSRC / s for s in SOURCES] + [CSRC / h for h in HEADERS] + [INCLUDE / "mpadam.h", Path(__file__)]
+    return [CSRC / s for s in SOURCES + [EXT_SOURCE]] + [CSRC / h for h in HEADERS] + [INCLUDE / "mpadam.h", Path(__file__)]
 
 
 def needs_build() -> bool:
-    if not LIB.exists():
+    if not LIB.exists() or not EXT.exists() or not EXT_TORCH.exists():
+        return True
+    if EXT_TORCH.read_text() != importlib.metadata.version("torch"):
         return True
     t = LIB.stat().st_mtime
     return any(p.stat().st_mtime > t for p in _inputs())
+
+
+def _torch_dir() -> Path:
+    return Path(importlib.util.find_spec("torch").origin).parent
+
+
+def _ext_flags():
+    inc = _torch_dir() / "include"
+    cuda = Path(nvcc()).resolve().parent.parent / "include"
+    return ["-O2", "-std=c++17", "-fPIC", "-DNDEBUG", f"-I{INCLUDE}", f"-I{inc}",
+            f"-I{inc / 'torch' / 'csrc' / 'api' / 'include'}", f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}"]
 
 
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) -> Path:
@@ -65,8 +87,18 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             raise RuntimeError(f"nvcc failed for {src}:\n{r.stdout}\n{r.stderr}")
         return obj, r.stdout + r.stderr
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    def compile_ext():
+        obj = OUT_DIR / (Path(EXT_SOURCE).stem + ".o")
+        cmd = [os.environ.get("CXX", "g++"), *_ext_flags(), "-c", str(CSRC / EXT_SOURCE), "-o", str(obj)]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"compilation failed for {EXT_SOURCE}:\n{r.stdout}\n{r.stderr}")
+        return obj
+
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        ext = ex.submit(compile_ext)
         results = list(ex.map(compile_one, SOURCES))
+        ext_obj = ext.result()
     if verbose or ptxas_info:
         for _, log in results:
             if log.strip():
@@ -77,7 +109,27 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    tmp = OUT_DIR / f".mpadam_torch.{os.getpid()}.so"
+    cmd = [os.environ.get("CXX", "g++"), "-shared", "-o", str(tmp), str(ext_obj), f"-L{_torch_dir() / 'lib'}",
+           "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", f"-L{OUT_DIR}", "-l:libmpadam.so",
+           "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link of {EXT.name} failed:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, EXT)
+    EXT_TORCH.write_text(importlib.metadata.version("torch"))
     return LIB
+
+
+def load_ext():
+    """The module _mpadam_torch; there is no fallback."""
+    import torch  # noqa: F401  (its libraries have to be loaded first)
+    if not EXT.exists():
+        raise RuntimeError(f"{EXT} is missing: build the CUDA library first (paper_2607_10611_gb300.build())")
+    spec = importlib.util.spec_from_loader("_mpadam_torch", importlib.machinery.ExtensionFileLoader("_mpadam_torch", str(EXT)))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
 
 
 if __name__ == "__main__":

@@ -1,0 +1,398 @@
+// torch_ext.cpp -- the Python module _mpadam_torch: what the list operators and
+// the 8-bit layer do on torch's side of the C ABI (include/mpadam.h), in C++
+// because a short call's time is its host's.  It looks at tensors, allocates
+// outputs with torch and calls the library; it holds no arithmetic.
+//
+// From Python, a step over 98 small tensors took 36 us against 5 on the GPU, the
+// norm of 4000 ragged ones 1195 against 91, a linear layer of 1023 x 768 x 2304
+// forward and backward 434 against 48.
+#include <Python.h>
+
+#include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <memory>
+#include <vector>
+
+#include "mpadam.h"
+
+namespace {
+
+using at::Tensor;
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+constexpr auto kCodes = at::kFloat8_e4m3fn;
+constexpr auto kScales = at::kFloat8_e8m0fnu;
+
+PyObject* g_error = nullptr;  // _native.MPAdamError
+
+// Raises the library's last error as MPAdamError; returns nullptr.
+PyObject* raise(int32_t status) {
+  PyObject* e = g_error ? PyObject_CallFunction(g_error, "is", (int)status, mpadam_last_error()) : nullptr;
+  if (e) {
+    PyErr_SetObject(g_error, e);
+    Py_DECREF(e);
+  } else if (!PyErr_Occurred()) {
+    PyErr_SetString(PyExc_RuntimeError, mpadam_last_error());
+  }
+  return nullptr;
+}
+// The same from inside C++ calls; the backward pass runs without the interpreter's lock.
+void check(int32_t status) {
+  if (!status) return;
+  TORCH_CHECK(PyGILState_Check(), mpadam_last_error());
+  raise(status);
+  throw python_error();
+}
+
+const Tensor& tensor_of(PyObject* o, const char* what) {
+  TORCH_CHECK_VALUE(THPVariable_Check(o), what, " must be a torch tensor");
+  return THPVariable_Unpack(o);
+}
+cudaStream_t current_stream(const Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
+
+int32_t type_of(const Tensor& t) { return t.scalar_type() == at::kFloat ? MPADAM_F32 : MPADAM_BF16; }
+bool is_real(const Tensor& t) { return t.is_cuda() && (t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16); }
+// A matrix whose rows are contiguous and do not overlap.
+bool has_rows(const Tensor& t) {
+  const int64_t r = t.size(0), c = t.size(1);
+  return r == 0 || c == 0 || ((c == 1 || t.stride(1) == 1) && (r == 1 || t.stride(0) >= c));
+}
+
+// ---------------------------------------------------------------------------
+// Lists of gradients
+// ---------------------------------------------------------------------------
+// What the gradients of a list have to be.
+struct Spec {
+  std::vector<int64_t> numel;
+  at::ScalarType type;
+  int device;
+};
+constexpr const char* kSpecName = "mpadam_list_spec";
+
+// list_spec(numels, binary32?, device index) -> capsule
+PyObject* list_spec(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 3 && PyList_Check(a[0]), "list_spec(list of sizes, binary32, device)");
+  auto s = std::make_unique<Spec>();
+  for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[0]); ++i) s->numel.push_back(PyLong_AsLongLong(PyList_GET_ITEM(a[0], i)));
+  s->type = PyObject_IsTrue(a[1]) ? at::kFloat : at::kBFloat16;
+  s->device = (int)PyLong_AsLong(a[2]);
+  if (PyErr_Occurred()) return nullptr;
+  return PyCapsule_New(s.release(), kSpecName,
+                       [](PyObject* c) { delete static_cast<Spec*>(PyCapsule_GetPointer(c, kSpecName)); });
+  END_HANDLE_TH_ERRORS
+}
+
+// Pointers of a list of gradients that meet the spec.
+struct Pointers {
+  std::vector<const void*> p;
+  Pointers(PyObject* grads, const Spec& s) {
+    PyObject* seq = PySequence_Fast(grads, "gradients must be a sequence of tensors");
+    if (!seq) throw python_error();
+    const std::unique_ptr<PyObject, void (*)(PyObject*)> hold(seq, [](PyObject* o) { Py_DECREF(o); });
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+    TORCH_CHECK_VALUE((size_t)n == s.numel.size(), n, " gradients for ", s.numel.size(), " tensors");
+    p.resize(n ? n : 1);
+    PyObject** items = PySequence_Fast_ITEMS(seq);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const Tensor& t = tensor_of(items[i], "a gradient");
+      TORCH_CHECK_VALUE(t.scalar_type() == s.type && t.numel() == s.numel[i] && t.is_cuda() && t.get_device() == s.device &&
+                            t.is_contiguous(),
+                        "gradients must be contiguous ", s.type, " tensors on cuda:", s.device, ", as large as their weights");
+      p[i] = t.const_data_ptr();
+    }
+  }
+};
+
+cudaStream_t stream_of(PyObject* o, int device) {
+  return o == Py_None ? c10::cuda::getCurrentCUDAStream(device).stream() : reinterpret_cast<cudaStream_t>(PyLong_AsSize_t(o));
+}
+
+// adamw_step(state, spec, grads, t, lr, grad_scale or None, stream or None)
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 7, "adamw_step takes 7 arguments");
+  auto* state = static_cast<mpadam_adamw_state*>(PyLong_AsVoidPtr(a[0]));
+  auto* spec = static_cast<Spec*>(PyCapsule_GetPointer(a[1], kSpecName));
+  const int64_t t = PyLong_AsLongLong(a[3]);
+  const double lr = PyFloat_AsDouble(a[4]);
+  if (PyErr_Occurred()) return nullptr;
+  const cudaStream_t stream = stream_of(a[6], spec->device);
+  if (PyErr_Occurred()) return nullptr;
+  const Pointers g(a[2], *spec);
+  const float* scale = nullptr;
+  if (a[5] != Py_None) {
+    const Tensor& x = tensor_of(a[5], "grad_scale");
+    TORCH_CHECK_VALUE(x.scalar_type() == at::kFloat && x.is_cuda() && x.get_device() == spec->device && x.numel() >= 1,
+                      "grad_scale must be a float32 tensor on cuda:", spec->device);
+    scale = x.const_data_ptr<float>();
+  }
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)spec->device);
+  if (const int32_t rc = mpadam_adamw_step(state, g.p.data(), t, (float)lr, scale, stream)) return raise(rc);
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// grad_norm(state, spec, grads, max_norm, out or None, stream or None) -> out
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 6, "grad_norm takes 6 arguments");
+  auto* state = static_cast<mpadam_grad_norm_state*>(PyLong_AsVoidPtr(a[0]));
+  auto* spec = static_cast<Spec*>(PyCapsule_GetPointer(a[1], kSpecName));
+  const double max_norm = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred()) return nullptr;
+  const cudaStream_t stream = stream_of(a[5], spec->device);
+  if (PyErr_Occurred()) return nullptr;
+  const Pointers g(a[2], *spec);
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)spec->device);
+  Tensor out;
+  if (a[4] != Py_None) {
+    out = tensor_of(a[4], "out");
+    TORCH_CHECK_VALUE(out.scalar_type() == at::kFloat && out.is_cuda() && out.get_device() == spec->device && out.numel() >= 2 &&
+                          out.is_contiguous(),
+                      "out must be two contiguous float32 elements on cuda:", spec->device);
+  } else {
+    out = at::empty({2}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, (c10::DeviceIndex)spec->device));
+  }
+  if (const int32_t rc = mpadam_grad_norm(state, g.p.data(), (float)max_norm, out.data_ptr<float>(), stream)) return raise(rc);
+  return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// ---------------------------------------------------------------------------
+// E4M3 matrices
+// ---------------------------------------------------------------------------
+struct Matrix {
+  Tensor codes, scales;
+  int64_t rows() const { return codes.size(0); }
+  int64_t cols() const { return codes.size(1); }
+  uint8_t* q() const { return static_cast<uint8_t*>(codes.data_ptr()); }
+  uint8_t* s() const { return static_cast<uint8_t*>(scales.data_ptr()); }
+  // A single row's stride is of no matter, so its codes may have any.
+  int64_t ld() const { return rows() > 1 ? codes.stride(0) : (cols() + 15) / 16 * 16; }
+
+  static Matrix empty(int64_t rows, int64_t cols, const at::Device& device) {
+    const auto o = at::TensorOptions().device(device);
+    const int64_t ld = (cols + 15) / 16 * 16;
+    Tensor codes = at::empty({rows, ld}, o.dtype(kCodes));
+    if (ld != cols) codes = codes.narrow(1, 0, cols);
+    return {codes, at::empty({(rows + 127) / 128, (cols + 511) / 512, 32, 4, 4}, o.dtype(kScales))};
+  }
+  static Matrix checked(PyObject* c, PyObject* s) {
+    Matrix m{tensor_of(c, "codes"), tensor_of(s, "scales")};
+    TORCH_CHECK_VALUE(m.codes.scalar_type() == kCodes && m.codes.dim() == 2 && m.codes.is_cuda(),
+                      "codes must be a CUDA float8_e4m3fn matrix");
+    TORCH_CHECK_VALUE(has_rows(m.codes), "codes must have contiguous rows");
+    const int64_t want[5] = {(m.rows() + 127) / 128, (m.cols() + 511) / 512, 32, 4, 4};
+    TORCH_CHECK_VALUE(m.scales.scalar_type() == kScales && m.scales.sizes() == at::IntArrayRef(want, 5) &&
+                          m.scales.is_contiguous() && m.scales.device() == m.codes.device(),
+                      "scales must be a contiguous float8_e8m0fnu tensor of ", at::IntArrayRef(want, 5), " beside the codes");
+    return m;
+  }
+};
+
+// x as it lies and its transpose, where asked for.
+void quantize(const Tensor& x, bool square, Matrix* q, Matrix* qt) {
+  const int64_t rows = x.size(0), cols = x.size(1);
+  if (q) *q = Matrix::empty(rows, cols, x.device());
+  if (qt) *qt = Matrix::empty(cols, rows, x.device());
+  check(mpadam_e4m3_quantize(x.const_data_ptr(), type_of(x), rows, cols, rows > 1 ? std::max(x.stride(0), cols) : cols, square,
+                             q ? q->q() : nullptr, q ? q->s() : nullptr, q ? q->ld() : 0, qt ? qt->q() : nullptr,
+                             qt ? qt->s() : nullptr, qt ? qt->ld() : 0, current_stream(x)));
+}
+
+void multiply(const Matrix& a, const Matrix& b, const Tensor& out, bool accumulate) {
+  mpadam_e4m3_product p{};
+  p.a = a.q(), p.a_scale = a.s(), p.lda = a.ld();
+  p.b = b.q(), p.b_scale = b.s(), p.ldb = b.ld();
+  p.d = out.data_ptr();
+  p.m = a.rows(), p.n = b.rows(), p.k = a.cols();
+  p.ldd = p.m > 1 ? std::max(out.stride(0), p.n) : p.n;
+  p.d_dtype = type_of(out);
+  p.accumulate = accumulate;
+  check(mpadam_e4m3_matmul(&p, current_stream(out)));
+}
+
+Tensor product(const Matrix& a, const Matrix& b, at::ScalarType type) {
+  Tensor out = at::empty({a.rows(), b.rows()}, a.codes.options().dtype(type));
+  multiply(a, b, out, false);
+  return out;
+}
+
+// check_matrix(codes, scales)
+PyObject* check_matrix(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 2, "check_matrix takes 2 arguments");
+  Matrix::checked(a[0], a[1]);
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// quantize(x, square, as it lies?, transposed?) -> (codes, scales or None twice, ...) of both
+PyObject* py_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 4, "quantize takes 4 arguments");
+  const Tensor& x = tensor_of(a[0], "x");
+  TORCH_CHECK_VALUE(x.dim() == 2 && is_real(x), "x must be a CUDA float32 or bfloat16 matrix");
+  TORCH_CHECK_VALUE(has_rows(x), "x must have contiguous rows");
+  const bool square = PyObject_IsTrue(a[1]), as_is = PyObject_IsTrue(a[2]), turned = PyObject_IsTrue(a[3]);
+  const c10::cuda::CUDAGuard guard(x.device());
+  Matrix q, qt;
+  quantize(x, square, as_is ? &q : nullptr, turned ? &qt : nullptr);
+  return Py_BuildValue("(NNNN)", THPVariable_Wrap(q.codes), THPVariable_Wrap(q.scales), THPVariable_Wrap(qt.codes),
+                       THPVariable_Wrap(qt.scales));
+  END_HANDLE_TH_ERRORS
+}
+
+// matmul(a codes, a scales, b codes, b scales, out or None, binary32 result?, accumulate) -> out
+PyObject* py_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 7, "matmul takes 7 arguments");
+  const Matrix x = Matrix::checked(a[0], a[1]), y = Matrix::checked(a[2], a[3]);
+  const bool accumulate = PyObject_IsTrue(a[6]);
+  TORCH_CHECK_VALUE(x.cols() == y.cols(), "inner sizes differ: ", x.cols(), " and ", y.cols());
+  TORCH_CHECK_VALUE(x.codes.device() == y.codes.device(), "the operands are on different devices");
+  const c10::cuda::CUDAGuard guard(x.codes.device());
+  Tensor out;
+  if (a[4] != Py_None) {
+    out = tensor_of(a[4], "out");
+    TORCH_CHECK_VALUE(is_real(out) && out.dim() == 2 && out.size(0) == x.rows() && out.size(1) == y.rows() && has_rows(out) &&
+                          out.device() == x.codes.device(),
+                      "out must be a float32 or bfloat16 [", x.rows(), ", ", y.rows(), "] with contiguous rows beside the operands");
+    multiply(x, y, out, accumulate);
+  } else {
+    TORCH_CHECK_VALUE(!accumulate, "accumulate needs out");
+    out = product(x, y, PyObject_IsTrue(a[5]) ? at::kFloat : at::kBFloat16);
+  }
+  return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// ---------------------------------------------------------------------------
+// The linear layer
+// ---------------------------------------------------------------------------
+// x as a matrix of its last dimension, with contiguous rows.
+Tensor rows_of(const Tensor& x) {
+  const Tensor m = x.dim() == 2 ? x : x.reshape({-1, x.size(-1)});
+  return has_rows(m) ? m : m.contiguous();
+}
+Tensor with_shape(const Tensor& y, const Tensor& x) {
+  if (x.dim() == 2) return y;
+  auto shape = x.sizes().vec();
+  shape.back() = y.size(1);
+  return y.view(shape);
+}
+
+struct Linear : torch::autograd::Function<Linear> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, bool need_x, bool need_w,
+                        const c10::optional<Tensor>& grad_w) {
+    const c10::cuda::CUDAGuard guard(x.device());
+    const Tensor m = rows_of(x);
+    Matrix q, qt, qw, qwt;
+    quantize(m, false, &q, need_w ? &qt : nullptr);
+    quantize(rows_of(w), true, &qw, need_x ? &qwt : nullptr);
+    ctx->save_for_backward({qt.codes, qt.scales, qwt.codes, qwt.scales});
+    ctx->saved_data["need_x"] = need_x;
+    ctx->saved_data["need_w"] = need_w;
+    ctx->saved_data["x_type"] = (int64_t)x.scalar_type();
+    ctx->saved_data["w_type"] = (int64_t)w.scalar_type();
+    ctx->saved_data["shape"] = x.sizes();
+    if (grad_w) ctx->saved_data["grad_w"] = *grad_w;
+    return with_shape(product(q, qw, x.scalar_type()), x);
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    TORCH_CHECK(!at::GradMode::is_enabled(), "the 8-bit linear layer is differentiable once: no create_graph");
+    const Tensor& dy = grads[0];
+    const bool need_x = ctx->saved_data["need_x"].toBool(), need_w = ctx->saved_data["need_w"].toBool();
+    const auto saved = ctx->get_saved_variables();
+    const Matrix qt{saved[0], saved[1]}, qwt{saved[2], saved[3]};
+    const c10::cuda::CUDAGuard guard(dy.device());
+    Matrix q, qdt;
+    quantize(rows_of(dy), false, need_x ? &q : nullptr, need_w ? &qdt : nullptr);
+    Tensor dx, dw;
+    if (need_x) dx = product(q, qwt, (at::ScalarType)ctx->saved_data["x_type"].toInt()).view(ctx->saved_data["shape"].toIntVector());
+    if (need_w) {
+      const auto held = ctx->saved_data.find("grad_w");
+      if (held != ctx->saved_data.end()) multiply(qdt, qt, held->second.toTensor(), true);
+      else dw = product(qdt, qt, (at::ScalarType)ctx->saved_data["w_type"].toInt());
+    }
+    return {dx, dw, Tensor(), Tensor(), Tensor()};
+  }
+};
+
+void check_activations(const Tensor& x) {
+  TORCH_CHECK_VALUE(x.dim() >= 1 && is_real(x), "x must be a CUDA float32 or bfloat16 tensor");
+}
+
+// linear(x, w, grad_w or None) -> y
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 3, "linear takes 3 arguments");
+  const Tensor &x = tensor_of(a[0], "x"), &w = tensor_of(a[1], "w");
+  check_activations(x);
+  TORCH_CHECK_VALUE(w.dim() == 2 && is_real(w) && w.device() == x.device(), "w must be a float32 or bfloat16 matrix beside x");
+  TORCH_CHECK_VALUE(w.size(1) == x.size(-1), "inner sizes differ: ", x.size(-1), " and ", w.size(1));
+  c10::optional<Tensor> grad_w;
+  if (a[2] != Py_None) {
+    grad_w = tensor_of(a[2], "grad_w");
+    TORCH_CHECK_VALUE(grad_w->scalar_type() == at::kFloat && grad_w->sizes() == w.sizes() && grad_w->device() == x.device() &&
+                          has_rows(*grad_w),
+                      "grad_w must be a float32 tensor of w's shape beside it");
+  }
+  const bool on = at::GradMode::is_enabled(), need_x = on && x.requires_grad(), need_w = on && w.requires_grad();
+  if (need_x || need_w) return THPVariable_Wrap(Linear::apply(x, w, need_x, need_w, grad_w));
+  const c10::cuda::CUDAGuard guard(x.device());
+  Matrix q, qw;
+  quantize(rows_of(x), false, &q, nullptr);
+  quantize(rows_of(w), true, &qw, nullptr);
+  return THPVariable_Wrap(with_shape(product(q, qw, x.scalar_type()), x));
+  END_HANDLE_TH_ERRORS
+}
+
+// linear_held(x, codes, scales) -> y
+PyObject* linear_held(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 3, "linear_held takes 3 arguments");
+  const Tensor& x = tensor_of(a[0], "x");
+  check_activations(x);
+  const Matrix w = Matrix::checked(a[1], a[2]);
+  TORCH_CHECK_VALUE(w.codes.device() == x.device(), "the weight is on another device than x");
+  TORCH_CHECK_VALUE(w.cols() == x.size(-1), "inner sizes differ: ", x.size(-1), " and ", w.cols());
+  TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && x.requires_grad()),
+                    "a quantised weight passes no gradient: give linear() the weight itself");
+  const c10::cuda::CUDAGuard guard(x.device());
+  Matrix q;
+  quantize(rows_of(x), false, &q, nullptr);
+  return THPVariable_Wrap(with_shape(product(q, w, x.scalar_type()), x));
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* set_error(PyObject*, PyObject* cls) {
+  Py_INCREF(cls);
+  Py_XSETREF(g_error, cls);
+  Py_RETURN_NONE;
+}
+
+#define MPADAM_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
+PyMethodDef kMethods[] = {{"list_spec", MPADAM_FAST(list_spec)},
+                          {"adamw_step", MPADAM_FAST(adamw_step)},
+                          {"grad_norm", MPADAM_FAST(grad_norm)},
+                          {"check_matrix", MPADAM_FAST(check_matrix)},
+                          {"quantize", MPADAM_FAST(py_quantize)},
+                          {"matmul", MPADAM_FAST(py_matmul)},
+                          {"linear", MPADAM_FAST(linear)},
+                          {"linear_held", MPADAM_FAST(linear_held)},
+                          {"set_error", set_error, METH_O, nullptr},
+                          {nullptr, nullptr, 0, nullptr}};
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_mpadam_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__mpadam_torch() { return PyModule_Create(&kModule); }
