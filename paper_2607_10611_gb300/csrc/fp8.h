@@ -37,6 +37,7 @@ cudaError_t launch_quantize(const QuantArgs& a, cudaStream_t stream);
 
 struct MatmulArgs {
   CUtensorMap a, b;            // codes [m, k] and [n, k]
+  CUtensorMap sa_map, sb_map;  // their scales, [row tiles, groups of 4 blocks, 128 words] (CTA pairs only)
   const uint8_t* sa;           // scales of a and b
   const uint8_t* sb;
   void* d;                     // [m, n], row stride ldd
@@ -46,10 +47,14 @@ struct MatmulArgs {
   int32_t* err;                // device error word
 };
 
-// Rows of a that a tile takes (the box height of a's tensor map) in a product
-// of this shape, and the launch.
-int matmul_tile(int64_t m, int64_t n, int64_t k);
-cudaError_t launch_matmul(MatmulArgs& a, int tile, cudaStream_t stream);
+// How a product of this shape is cut up, and its launch.
+struct MatmulPlan {
+  int tile;    // rows of a per tile
+  bool pair;   // tiles of 256 x 256 by pairs of CTAs, which need the scales' maps
+  int box() const { return pair ? tile / 2 : tile; }  // rows of a's boxes
+};
+MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k);
+cudaError_t launch_matmul(MatmulArgs& a, const MatmulPlan& plan, cudaStream_t stream);
 // Address of the device error word that matmul kernels set.
 cudaError_t matmul_error_word(int32_t** p);
 

@@ -291,19 +291,306 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::kCols) : "memory");
 }
 
-template <int TM, bool F32>
-cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
-  using S = Shape<TM>;
-  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use this much shared memory
+// ---------------------------------------------------------------------------
+// Tiles of 256 x 256 by pairs of CTAs: the two SMs' tensor cores work on one
+// product of 256 lanes (128 in each SM's tensor memory) by 256 columns, each SM
+// holding half of either operand.  A stage is then 32 KB for 2 x 128 x 128 x 256
+// multiply-adds an SM, against 48 KB where one CTA makes a tile of 128 x 256.
+// ---------------------------------------------------------------------------
+constexpr int kPairTile = 256;
+constexpr int kPairStageBytes = 2 * 128 * kTileK + 2048;  // b's rows, a's rows, scales of 128 rows of b and 256 of a
+constexpr int kPairStages = 6;
+constexpr int kPairDynSmem = kPairStages * kPairStageBytes + 1024;
+constexpr uint32_t kPairTx = 2 * 2 * 128 * kTileK, kPairScaleTx = 2 * 3 * kScaleTile;  // of both CTAs
+constexpr int kGroupRows = 8;  // row tiles of a that neighbouring clusters share out, so that they meet in L2
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// The address of `addr` in the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void pair_copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void pair_mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                                uint32_t add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(add)
+      : "memory");
+}
+// Arrives at `bar` in both CTAs when all that was issued before is done.
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+// 32 columns of this warp's 32 lanes.
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+      "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+}
+
+// Tile t's place: kGroupRows row tiles of a at a time, all of b's before the next ones.
+__device__ __forceinline__ void pair_place(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int group = t / (kGroupRows * tiles_n), first = group * kGroupRows;
+  const int rows = min(kGroupRows, tiles_m - first), in = t - group * kGroupRows * tiles_n;
+  tm = first + in % rows;
+  tn = in / rows;
+}
+
+template <bool F32>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
+    matmul_pair_kernel(const __grid_constant__ MatmulArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ alignas(8) uint64_t bars[2 * kPairStages + 3];
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int32_t failed;
+  const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const uint32_t bar0 = smem_addr(bars);
+  auto full = [&](int s) { return bar0 + 8u * s; };                   // the leader's alone
+  auto empty = [&](int s) { return bar0 + 8u * (kPairStages + s); };  // each CTA's own
+  const uint32_t acc_full = bar0 + 8u * (2 * kPairStages), acc_free = acc_full + 8u, drained = acc_full + 16u;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kPairStages; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 1);
+    }
+    mbar_init(acc_full, 1);
+    mbar_init(acc_free, 2 * kEpiWarps);
+    mbar_init(drained, 1);
+    failed = 0;
+    mbar_init_fence();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_s)), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;
+
+  const int tiles_n = (p.n + kPairTile - 1) / kPairTile, tiles_m = (p.m + kPairTile - 1) / kPairTile;
+  const int tiles = tiles_n * tiles_m, pairs = gridDim.x / 2;
+  const int steps = (p.k + kTileK - 1) / kTileK;
+  volatile int32_t* stop = &failed;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int s = 0, issued = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x / 2; t < tiles && ok; t += pairs) {
+        int tm, tn;
+        pair_place(t, tiles_m, tiles_n, tm, tn);
+        for (int k = 0; k < steps; ++k) {
+          if (*stop || !mbar_wait_cluster(empty(s), phase ^ 1)) { ok = false; break; }
+          const uint32_t st = smem + s * kPairStageBytes, bar = peer_addr(full(s), 0);
+          const bool scales = (k & 3) == 0;
+          if (rank == 0) mbar_arrive_tx(full(s), kPairTx + (scales ? kPairScaleTx : 0));
+          pair_load_2d(st, &p.b, k * kTileK, tn * kPairTile + (int)rank * 128, bar);
+          pair_load_2d(st + 128 * kTileK, &p.a, k * kTileK, tm * kPairTile + (int)rank * 128, bar);
+          if (scales) {
+            const uint32_t sc = st + 2 * 128 * kTileK;
+            pair_load_3d(sc, &p.sb_map, 0, k >> 2, tn * 2 + (int)rank, bar);
+            pair_load_3d(sc + kScaleTile, &p.sa_map, 0, k >> 2, tm * 2, bar);
+          }
+          ++issued;
+          if (++s == kPairStages) { s = 0; phase ^= 1; }
+        }
+      }
+      if (!ok) {
+        *stop = 1;
+        atomicOr(p.err, kErrStage);
+        // the copies in flight: the leader sees both CTAs' last stages arrive, the other one waits about as long
+        for (int i = 0; i < min(issued, kPairStages); ++i) {
+          if (s == 0) { s = kPairStages; phase ^= 1; }
+          --s;
+          if (rank == 0) mbar_wait_cluster(full(s), phase);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      int s = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int t = blockIdx.x / 2; t < tiles && ok; t += pairs) {
+        if (*stop || !mbar_wait_cluster(acc_free, acc_phase ^ 1)) { ok = false; atomicOr(p.err, kErrAccFree); break; }
+        tc_fence_after();
+        for (int k = 0; k < steps; ++k) {
+          if (*stop || !mbar_wait_cluster(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
+          tc_fence_after();
+          const uint32_t st = smem + s * kPairStageBytes;
+          const uint32_t sb = tmem + kPairTile + ((k >> 2) & 1) * 12, sa = sb + 4;
+          if ((k & 3) == 0) {
+            const uint32_t sc = st + 2 * 128 * kTileK;
+            pair_copy_scales(sb, scale_desc(sc));
+            pair_copy_scales(sa, scale_desc(sc + kScaleTile));
+            pair_copy_scales(sa + 4, scale_desc(sc + 2 * kScaleTile));
+          }
+          const uint64_t db = operand_desc(st), da = operand_desc(st + 128 * kTileK);
+          const uint32_t byte = k & 3;
+          const uint32_t id = (uint32_t)(kPairTile >> 3) << 17 | 1u << 23 | (uint32_t)(kPairTile >> 4) << 24 | byte << 4 | byte << 29;
+#pragma unroll
+          for (int i = 0; i < kTileK / 32; ++i) pair_mma_scaled(tmem, db + 2 * i, da + 2 * i, id, sb, sa, k > 0 || i > 0);
+          pair_commit(empty(s));
+          if (++s == kPairStages) { s = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        pair_commit(acc_full);
+        acc_phase ^= 1;
+      }
+      if (!ok) {  // the products in flight, before their memory goes
+        *stop = 1;
+        pair_commit(drained);
+        mbar_wait_cluster(drained, 0);
+      }
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t free_bar = peer_addr(acc_free, 0);
+    uint32_t acc_phase = 0;
+    for (int t = blockIdx.x / 2; t < tiles; t += pairs) {
+      if (*stop || !mbar_wait_cluster(acc_full, acc_phase)) {
+        if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
+        break;
+      }
+      acc_phase ^= 1;
+      __syncwarp();
+      tc_fence_after();
+      int tm, tn;
+      pair_place(t, tiles_m, tiles_n, tm, tn);
+      const int n = tn * kPairTile + (int)rank * 128 + quarter * 32 + lane, m0 = tm * kPairTile + half * 128;
+      // All of this warp's values first, so that the next tile's products can begin.
+      uint32_t r[128];
+      const uint32_t from = tmem + half * 128 + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_load32(from + 32 * c, r + 32 * c);
+      tmem_wait_load();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(free_bar);
+      const int rows = min(128, p.m - m0);
+      if (n < p.n && rows > 0) {
+        const int64_t at = (int64_t)m0 * p.ldd + n;
+        if (F32) {
+          float* d = static_cast<float*>(p.d) + at;
+          if (p.accumulate) {
+#pragma unroll
+            for (int c = 0; c < 128; c += 16) {
+              float old[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) old[j] = c + j < rows ? d[(c + j) * p.ldd] : 0.0f;
+#pragma unroll
+              for (int j = 0; j < 16; ++j) r[c + j] = __float_as_uint(__fadd_rn(old[j], __uint_as_float(r[c + j])));
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (c + j < rows) d[(c + j) * p.ldd] = __uint_as_float(r[c + j]);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 128; ++j)
+              if (j < rows) d[j * p.ldd] = __uint_as_float(r[j]);
+          }
+        } else {
+          uint16_t* d = static_cast<uint16_t*>(p.d) + at;
+#pragma unroll
+          for (int j = 0; j < 128; ++j)
+            if (j < rows) d[j * p.ldd] = (uint16_t)bf16x2_rn(__uint_as_float(r[j]), 0.0f);
+        }
+      }
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// Lets a kernel use `bytes` of shared memory on the current device, once.
+template <typename K>
+cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>& ready) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
-  if (!(ready.load(std::memory_order_relaxed) & bit)) {
-    e = cudaFuncSetAttribute(matmul_kernel<TM, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kDynSmem);
-    if (e != cudaSuccess) return e;
-    ready.fetch_or(bit);
-  }
+  if (ready.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) ready.fetch_or(bit);
+  return e;
+}
+
+template <bool F32>
+cudaError_t launch_pair(const MatmulArgs& a, cudaStream_t stream) {
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem(matmul_pair_kernel<F32>, kPairDynSmem, ready);
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = (int64_t)((a.n + kPairTile - 1) / kPairTile) * ((a.m + kPairTile - 1) / kPairTile);
+  matmul_pair_kernel<F32><<<2 * (unsigned)std::min<int64_t>(tiles, kSms / 2), kMatmulThreads, kPairDynSmem, stream>>>(a);
+  return cudaGetLastError();
+}
+
+template <int TM, bool F32>
+cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
+  using S = Shape<TM>;
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem(matmul_kernel<TM, F32>, S::kDynSmem, ready);
+  if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)((a.n + kTileN - 1) / kTileN) * ((a.m + TM - 1) / TM);
   matmul_kernel<TM, F32><<<(unsigned)std::min<int64_t>(tiles, kSms), kMatmulThreads, S::kDynSmem, stream>>>(a);
   return cudaGetLastError();
@@ -316,17 +603,23 @@ cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-int matmul_tile(int64_t m, int64_t n, int64_t k) {
-  return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : m <= 128 ? 128 : 256;
+MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k) {
+  if (m <= 16) return {16, false};
+  if (m <= 32) return {32, false};
+  if (m <= 64) return {64, false};
+  // Pairs of CTAs, unless their large tiles leave SMs without one and there are more tiles of 128 x 128 to go round.
+  const int64_t large = ((m + 255) / 256) * ((n + 255) / 256), small = ((m + 127) / 128) * ((n + 127) / 128);
+  if (large >= kSms / 2 || small <= large) return {256, true};
+  return {128, false};
 }
 
-cudaError_t launch_matmul(MatmulArgs& a, int tile, cudaStream_t stream) {
-  switch (tile) {
+cudaError_t launch_matmul(MatmulArgs& a, const MatmulPlan& plan, cudaStream_t stream) {
+  if (plan.pair) return a.f32 ? launch_pair<true>(a, stream) : launch_pair<false>(a, stream);
+  switch (plan.tile) {
     case 16: return launch<16>(a, stream);
     case 32: return launch<32>(a, stream);
     case 64: return launch<64>(a, stream);
-    case 128: return launch<128>(a, stream);
-    default: return launch<256>(a, stream);
+    default: return launch<128>(a, stream);
   }
 }
 

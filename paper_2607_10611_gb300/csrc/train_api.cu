@@ -335,6 +335,16 @@ EncodeTiled encode_tiled() {
   return f;
 }
 
+// Tensor map of scales, [row tiles, groups, 128 words], boxes of `box` row tiles of one group.
+bool scale_map(CUtensorMap* map, const uint8_t* s, int64_t rows, int64_t k, int box) {
+  const cuuint64_t groups = (cuuint64_t)(k + 511) / 512;
+  const cuuint64_t dims[3] = {128, groups, (cuuint64_t)(rows + 127) / 128}, strides[2] = {kScaleTile, kScaleTile * groups};
+  const cuuint32_t boxes[3] = {128, 1, (cuuint32_t)box}, steps[3] = {1, 1, 1};
+  return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<uint8_t*>(s), dims, strides, boxes, steps,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Tensor map of codes [rows, k], row stride ld bytes, boxes of `box` rows x 128 bytes in the 128-byte swizzle.
 bool code_map(CUtensorMap* map, const uint8_t* q, int64_t rows, int64_t k, int64_t ld, int box) {
   const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
@@ -369,9 +379,10 @@ extern "C" int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, cudaStream_t
   if (p->lda < p->k || p->ldb < p->k || p->lda % 16 || p->ldb % 16)
     return fail(MPADAM_EINVAL, "lda and ldb must be multiples of 16, >= k");
   MatmulArgs a;
-  const int tile = matmul_tile(p->m, p->n, p->k);
+  const MatmulPlan plan = matmul_plan(p->m, p->n, p->k);
   if (!encode_tiled()) return fail(MPADAM_EUNSUPPORTED, "the driver offers no cuTensorMapEncodeTiled");
-  if (!code_map(&a.a, p->a, p->m, p->k, p->lda, tile) || !code_map(&a.b, p->b, p->n, p->k, p->ldb, 128))
+  if (!code_map(&a.a, p->a, p->m, p->k, p->lda, plan.box()) || !code_map(&a.b, p->b, p->n, p->k, p->ldb, 128) ||
+      (plan.pair && (!scale_map(&a.sa_map, p->a_scale, p->m, p->k, 2) || !scale_map(&a.sb_map, p->b_scale, p->n, p->k, 1))))
     return fail(MPADAM_EINVAL, "no tensor map for these codes");
   a.sa = p->a_scale;
   a.sb = p->b_scale;
@@ -384,7 +395,7 @@ extern "C" int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, cudaStream_t
   a.accumulate = p->accumulate;
   cudaError_t e = matmul_error_word(&a.err);
   if (e != cudaSuccess) return cuda_fail(e, "the products' error word");
-  e = launch_matmul(a, tile, stream);
+  e = launch_matmul(a, plan, stream);
   if (e != cudaSuccess) return cuda_fail(e, "launch of the product");
   return MPADAM_OK;
 }
