@@ -158,9 +158,10 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
       bool ok = true;
       int issued = 0;
       for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+        if (*stop) { ok = false; break; }
         const int tn = t / tiles_m, tm = t % tiles_m;
         for (int k = 0; k < steps; ++k) {
-          if (*stop || !mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
+          if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
           const uint32_t st = smem + s * S::kStageBytes;
           const bool scales = (k & 3) == 0;
           mbar_arrive_tx(full(s), (kTileN + TM) * kTileK + (scales ? S::kScaleBytes : 0));
@@ -199,7 +200,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
         tc_fence_after();
         const uint32_t d = tmem + acc * TM;
         for (int k = 0; k < steps; ++k) {
-          if (*stop || !mbar_wait(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
+          if (!mbar_wait(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
           tc_fence_after();
           const uint32_t st = smem + s * S::kStageBytes;
           const uint32_t sb = tmem_scales + ((k >> 2) & 1) * S::kScaleCols, sa = sb + 4;
@@ -432,10 +433,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
       uint32_t phase = 0;
       bool ok = true;
       for (int t = blockIdx.x / 2; t < tiles && ok; t += pairs) {
+        if (*stop) { ok = false; break; }
         int tm, tn;
         pair_place(t, tiles_m, tiles_n, tm, tn);
         for (int k = 0; k < steps; ++k) {
-          if (*stop || !mbar_wait_cluster(empty(s), phase ^ 1)) { ok = false; break; }
+          if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
           const uint32_t st = smem + s * kPairStageBytes, bar = peer_addr(full(s), 0);
           const bool scales = (k & 3) == 0;
           if (rank == 0) mbar_arrive_tx(full(s), kPairTx + (scales ? kPairScaleTx : 0));
@@ -457,7 +459,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
         for (int i = 0; i < min(issued, kPairStages); ++i) {
           if (s == 0) { s = kPairStages; phase ^= 1; }
           --s;
-          if (rank == 0) mbar_wait_cluster(full(s), phase);
+          if (rank == 0) mbar_wait(full(s), phase);
         }
       }
     }
@@ -470,7 +472,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
         if (*stop || !mbar_wait_cluster(acc_free, acc_phase ^ 1)) { ok = false; atomicOr(p.err, kErrAccFree); break; }
         tc_fence_after();
         for (int k = 0; k < steps; ++k) {
-          if (*stop || !mbar_wait_cluster(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
+          if (!mbar_wait(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
           tc_fence_after();
           const uint32_t st = smem + s * kPairStageBytes;
           const uint32_t sb = tmem + kPairTile + ((k >> 2) & 1) * 12, sa = sb + 4;
@@ -495,7 +497,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
       if (!ok) {  // the products in flight, before their memory goes
         *stop = 1;
         pair_commit(drained);
-        mbar_wait_cluster(drained, 0);
+        mbar_wait(drained, 0);
       }
     }
   } else if (warp >= 4) {
