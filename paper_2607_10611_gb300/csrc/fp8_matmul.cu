@@ -26,7 +26,7 @@ constexpr int kSms = 152;      // GB300
 constexpr int kEpiWarps = 8;
 constexpr int kMatmulThreads = 32 * (4 + kEpiWarps);  // a producer and an issuing warp (and two idle ones), then the epilogue
 
-enum MatmulError : int32_t { kErrCopy = 1, kErrStage = 2, kErrAcc = 4, kErrAccFree = 8 };
+enum MatmulError : int32_t { kErrCopy = 1, kErrStage = 2, kErrAcc = 4 };
 
 __device__ int32_t g_matmul_error;
 
@@ -59,14 +59,19 @@ __device__ __forceinline__ void mbar_arrive_tx(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.release.cta.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 // Descriptor of an operand tile in shared memory: rows of 128 bytes in the
-// 128-byte swizzle, groups of 8 rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
-         (uint64_t)2 << 61;
-}
+// 128-byte swizzle, groups of 8 rows 1024 bytes apart.  Its low word holds the
+// address (in units of 16 bytes; blocks' shared memory ends below 2^18), its
+// high word is a constant.
+constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
 // Descriptor of a tile of scales: 32 rows of 16 bytes, no swizzle, groups of 8 rows 128 bytes apart.
-__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+constexpr uint32_t kScaleHigh = (128 >> 4) | 1u << 14;
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr) { return addr >> 4 | 1u << 16; }
+__device__ __forceinline__ uint64_t desc(uint32_t low, uint32_t high) { return (uint64_t)high << 32 | low; }
+// One lane of the warp, always the same one; to be called by whole warps.
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
 }
 // Scales of 128 rows into four columns, the same in each quarter of the lanes.
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
@@ -191,45 +196,55 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      int s = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0;
-      bool ok = true;
-      for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-        if (*stop || !mbar_wait(acc_free(acc), acc_phase ^ 1)) { ok = false; atomicOr(p.err, kErrAccFree); break; }
-        tc_fence_after();
-        const uint32_t d = tmem + acc * TM;
-        for (int k = 0; k < steps; ++k) {
-          if (!mbar_wait(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
-          tc_fence_after();
-          const uint32_t st = smem + s * S::kStageBytes;
-          const uint32_t sb = tmem_scales + ((k >> 2) & 1) * S::kScaleCols, sa = sb + 4;
-          if ((k & 3) == 0) {
-            const uint32_t sc = st + (kTileN + TM) * kTileK;
-            copy_scales(sb, scale_desc(sc));
-            for (int j = 0; j < S::kScaleTilesA; ++j) copy_scales(sa + 4 * j, scale_desc(sc + kScaleTile * (1 + j)));
-          }
-          // A tile of fewer than 128 rows of a starts inside its scale tile, at a multiple of 16 rows: columns hold 32
-          // rows each, and the first row's lane follows from the tile's place.
-          const uint64_t db = operand_desc(st), da = operand_desc(st + kTileN * kTileK);
-          const uint32_t id = instr_desc<TM>(k & 3);
-          const int tm = t % tiles_m;
-          const uint32_t sa_col = TM < 128 ? sa + (uint32_t)(tm * TM % 128) / 32 : sa;
+    // The whole warp walks the stages, so that addresses stay in uniform registers, and one lane issues.  After a wait
+    // that gave up it goes on without waiting; what it then computes is not used.
+    const bool issue = elected();
+    const uint32_t low0 = desc_low(smem);
+    int s = 0, acc = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+      if (ok) ok = mbar_wait(acc_free(acc), acc_phase ^ 1);
+      tc_fence_after();
+      const uint32_t d = tmem + acc * TM;
+      // A tile of fewer than 128 rows of a starts inside its scale tile, at a multiple of 32 rows (16 only where it is the
+      // first): a column of scales holds 32 rows.
+      const int col = TM < 128 ? (t % tiles_m * TM % 128) / 32 : 0;
+      for (int g = 0; g < groups; ++g) {
+        const uint32_t sb = tmem_scales + (g & 1) * S::kScaleCols, sa = sb + 4;
 #pragma unroll
-          for (int i = 0; i < kTileK / 32; ++i)
-            mma_scaled(d, db + 2 * i, da + 2 * i, id, sb, sa_col, k > 0 || i > 0);
-          mma_commit(empty(s));
+        for (int j = 0; j < 4; ++j) {
+          const int k = 4 * g + j;
+          if (k >= steps) break;
+          if (ok) ok = mbar_wait(full(s), phase);
+          tc_fence_after();
+          if (issue) {
+            const uint32_t low = low0 + s * (S::kStageBytes >> 4);
+            if (j == 0) {
+              const uint32_t sc = low + ((kTileN + TM) * kTileK >> 4);
+              copy_scales(sb, desc(sc, kScaleHigh));
+#pragma unroll
+              for (int i = 0; i < S::kScaleTilesA; ++i) copy_scales(sa + 4 * i, desc(sc + (i + 1) * (kScaleTile >> 4), kScaleHigh));
+            }
+#pragma unroll
+            for (int i = 0; i < kTileK / 32; ++i)
+              mma_scaled(d, desc(low + 2 * i, kOperandHigh), desc(low + (kTileN * kTileK >> 4) + 2 * i, kOperandHigh),
+                         instr_desc<TM>(j), sb, sa + col, j > 0 || i > 0 || g > 0);
+            mma_commit(empty(s));
+          }
           if (++s == S::kStages) { s = 0; phase ^= 1; }
         }
-        if (!ok) break;
-        mma_commit(acc_full(acc));
-        if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
       }
-      if (!ok) {  // the products in flight, before their memory goes
-        *stop = 1;
+      if (issue) mma_commit(acc_full(acc));
+      if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
+    }
+    if (!ok) {  // the products in flight, before their memory goes
+      *stop = 1;
+      if (issue) {
+        atomicOr(p.err, kErrCopy);
         mma_commit(drained);
-        mbar_wait(drained, 0);
       }
+      mbar_wait(drained, 0);
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -424,7 +439,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
 
   const int tiles_n = (p.n + kPairTile - 1) / kPairTile, tiles_m = (p.m + kPairTile - 1) / kPairTile;
   const int tiles = tiles_n * tiles_m, pairs = gridDim.x / 2;
-  const int steps = (p.k + kTileK - 1) / kTileK;
+  const int steps = (p.k + kTileK - 1) / kTileK, groups = (steps + 3) / 4;
   volatile int32_t* stop = &failed;
 
   if (warp == 0) {
@@ -463,42 +478,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
         }
       }
     }
-  } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      int s = 0;
-      uint32_t phase = 0, acc_phase = 0;
-      bool ok = true;
-      for (int t = blockIdx.x / 2; t < tiles && ok; t += pairs) {
-        if (*stop || !mbar_wait_cluster(acc_free, acc_phase ^ 1)) { ok = false; atomicOr(p.err, kErrAccFree); break; }
-        tc_fence_after();
-        for (int k = 0; k < steps; ++k) {
-          if (!mbar_wait(full(s), phase)) { ok = false; atomicOr(p.err, kErrCopy); break; }
-          tc_fence_after();
-          const uint32_t st = smem + s * kPairStageBytes;
-          const uint32_t sb = tmem + kPairTile + ((k >> 2) & 1) * 12, sa = sb + 4;
-          if ((k & 3) == 0) {
-            const uint32_t sc = st + 2 * 128 * kTileK;
-            pair_copy_scales(sb, scale_desc(sc));
-            pair_copy_scales(sa, scale_desc(sc + kScaleTile));
-            pair_copy_scales(sa + 4, scale_desc(sc + 2 * kScaleTile));
-          }
-          const uint64_t db = operand_desc(st), da = operand_desc(st + 128 * kTileK);
-          const uint32_t byte = k & 3;
-          const uint32_t id = (uint32_t)(kPairTile >> 3) << 17 | 1u << 23 | (uint32_t)(kPairTile >> 4) << 24 | byte << 4 | byte << 29;
+  } else if (warp == 1 && rank == 0) {
+    const bool issue = elected();  // as in matmul_kernel
+    const uint32_t low0 = desc_low(smem);
+    int s = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = blockIdx.x / 2; t < tiles; t += pairs) {
+      if (ok) ok = mbar_wait_cluster(acc_free, acc_phase ^ 1);
+      tc_fence_after();
+      for (int g = 0; g < groups; ++g) {
+        const uint32_t sb = tmem + kPairTile + (g & 1) * 12, sa = sb + 4;
 #pragma unroll
-          for (int i = 0; i < kTileK / 32; ++i) pair_mma_scaled(tmem, db + 2 * i, da + 2 * i, id, sb, sa, k > 0 || i > 0);
-          pair_commit(empty(s));
+        for (int j = 0; j < 4; ++j) {
+          const int k = 4 * g + j;
+          if (k >= steps) break;
+          if (ok) ok = mbar_wait(full(s), phase);
+          tc_fence_after();
+          if (issue) {
+            const uint32_t low = low0 + s * (kPairStageBytes >> 4);
+            if (j == 0) {
+              const uint32_t sc = low + (2 * 128 * kTileK >> 4);
+              pair_copy_scales(sb, desc(sc, kScaleHigh));
+              pair_copy_scales(sa, desc(sc + (kScaleTile >> 4), kScaleHigh));
+              pair_copy_scales(sa + 4, desc(sc + 2 * (kScaleTile >> 4), kScaleHigh));
+            }
+            const uint32_t id = (uint32_t)(kPairTile >> 3) << 17 | 1u << 23 | (uint32_t)(kPairTile >> 4) << 24 |
+                                (uint32_t)j << 4 | (uint32_t)j << 29;
+#pragma unroll
+            for (int i = 0; i < kTileK / 32; ++i)
+              pair_mma_scaled(tmem, desc(low + 2 * i, kOperandHigh), desc(low + (128 * kTileK >> 4) + 2 * i, kOperandHigh), id,
+                              sb, sa, j > 0 || i > 0 || g > 0);
+            pair_commit(empty(s));
+          }
           if (++s == kPairStages) { s = 0; phase ^= 1; }
         }
-        if (!ok) break;
-        pair_commit(acc_full);
-        acc_phase ^= 1;
       }
-      if (!ok) {  // the products in flight, before their memory goes
-        *stop = 1;
+      if (issue) pair_commit(acc_full);
+      acc_phase ^= 1;
+    }
+    if (!ok) {  // the products in flight, before their memory goes
+      *stop = 1;
+      if (issue) {
+        atomicOr(p.err, kErrCopy);
         pair_commit(drained);
-        mbar_wait(drained, 0);
       }
+      mbar_wait(drained, 0);
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2;
