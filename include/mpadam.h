@@ -563,6 +563,12 @@ int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32_t n, const
 int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* grads, int64_t step, float lr,
                           const float* grad_scale, struct CUstream_st* stream);
 
+/* Device-side status of the steps issued so far: synchronises the device,
+ * returns in *code the error bits that they recorded (0 = none; non-zero: a
+ * bounded wait gave up, and that step's results are incomplete) and clears
+ * them.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_adamw_status(mpadam_adamw_state* s, int32_t* code);
+
 /* Synchronises the device and frees the library's tables; NULL is a no-op. */
 int32_t mpadam_adamw_destroy(mpadam_adamw_state* s);
 

@@ -28,7 +28,7 @@ EXPORTED = ["mpadam_create", "mpadam_create_ex", "mpadam_fp8_init", "mpadam_step
             "mpadam_toy_create", "mpadam_toy_step", "mpadam_toy_run", "mpadam_toy_status", "mpadam_toy_destroy",
             "mpadam_host_buffer_alloc", "mpadam_host_buffer_free", "mpadam_debug_fail_allocation", "mpadam_debug_spoil_pool",
             "mpadam_debug_tile_schedule", "mpadam_debug_pool_rule", "mpadam_debug_ring_layout",
-            "mpadam_adamw_create", "mpadam_adamw_step", "mpadam_adamw_destroy", "mpadam_grad_norm_create",
+            "mpadam_adamw_create", "mpadam_adamw_step", "mpadam_adamw_status", "mpadam_adamw_destroy", "mpadam_grad_norm_create",
             "mpadam_grad_norm", "mpadam_grad_norm_destroy", "mpadam_e4m3_quantize", "mpadam_e4m3_matmul",
             "mpadam_e4m3_status"]
 
@@ -155,6 +155,7 @@ def lib() -> ctypes.CDLL:
             "mpadam_debug_ring_layout": [P, i32, i32, P],
             "mpadam_adamw_create": [P, i32, P, P],
             "mpadam_adamw_step": [P, P, i64, ctypes.c_float, P, P],
+            "mpadam_adamw_status": [P, P],
             "mpadam_adamw_destroy": [P],
             "mpadam_grad_norm_create": [P, i32, i32, P],
             "mpadam_grad_norm": [P, P, ctypes.c_float, P, P],
@@ -430,6 +431,13 @@ def mpadam_adamw_step(state: int, grads: Sequence[int], step: int, lr: float, gr
     status = lib().mpadam_adamw_step(state, arr.buffer_info()[0], step, lr, grad_scale or None, stream or None)
     if status:
         _check(status)
+
+
+def mpadam_adamw_status(state: int) -> int:
+    """Synchronises; returns and clears the steps' device error bits (0: no bounded wait gave up)."""
+    out = ctypes.c_int32()
+    _check(lib().mpadam_adamw_status(state or None, ctypes.byref(out)))
+    return out.value
 
 
 def mpadam_adamw_destroy(state: int) -> None:

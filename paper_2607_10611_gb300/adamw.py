@@ -98,6 +98,10 @@ class AdamW:
         element multiplies every gradient (GradNorm's [1:]), NaN: the step changes nothing."""
         self._step(self.state, self._spec, grads, t, lr, grad_scale, stream.cuda_stream if stream else None)
 
+    def device_status(self) -> int:
+        """Device error bits of the steps so far (0 = none); synchronises."""
+        return N.mpadam_adamw_status(self.state)
+
     def close(self):
         if getattr(self, "state", None):
             N.mpadam_adamw_destroy(self.state)

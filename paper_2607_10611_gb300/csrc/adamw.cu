@@ -14,8 +14,6 @@ namespace mpadam {
 
 namespace {
 
-constexpr int kThreads8 = kListTile / 8;  // 8 elements a thread
-
 __device__ __forceinline__ const void* grad_of(const GradTable& g, int k) { return g.grads ? g.grads[k] : g.inline_grads[k]; }
 
 // 8 values at p[at ..], `left` of them inside; whole and aligned ones in vector loads.
@@ -144,49 +142,211 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], int k, const uint3
   return make_uint2(c[0], c[1]);
 }
 
+// ---------------------------------------------------------------------------
+// The step.  One CTA per SM walks a run of tiles.  A producer warp brings each
+// tile's arrays into a ring in shared memory by bulk copies (with the tile's
+// place, its pointers and its blocks' scales beside them, whose addresses need
+// not be aligned); 16 consumer warps update 8 elements a thread and store
+// straight to global memory.  Arrays that are off a 16-byte boundary, and ends
+// that do not fill one, are read by the consumers themselves.
+// ---------------------------------------------------------------------------
+constexpr int kStepConsumers = kAdamwTile / 8;
+constexpr int kStepThreads = kStepConsumers + 32;
+constexpr int kStepSmem = 200 * 1024;  // of the ring, at most
+constexpr int kStepMaxStages = 8;
+constexpr int kTileScales = kAdamwTile / 128;
+
+// What the consumers need to know of a stage's tile.
+struct TileHead {
+  const void* grad;
+  uint8_t *w, *m, *v;
+  uint16_t* compute;
+  uint8_t *m_scale, *v_scale;
+  int64_t at, left, goff;  // the tile's first element, the elements from there to the tensor's end, its global index
+  int32_t staged[4];       // elements of w, g, m, v that are in the stage
+  uint32_t vec;            // bits 0: w, m, v, compute 16-byte aligned; 1: the gradient
+  int32_t pad[3];
+  uint8_t scales[2][kTileScales];
+};
+
+template <bool W32, bool G32, bool LOW>
+struct StepRing {
+  static constexpr int kW = W32 ? 4 : 2, kG = G32 ? 4 : 2, kS = LOW ? 1 : 4;
+  static constexpr int kOffW = (sizeof(TileHead) + 127) / 128 * 128;
+  static constexpr int kOffG = kOffW + kAdamwTile * kW, kOffM = kOffG + kAdamwTile * kG, kOffV = kOffM + kAdamwTile * kS;
+  static constexpr int kBytes = kOffV + kAdamwTile * kS;
+  static constexpr int kFit = kStepSmem / kBytes;
+  static constexpr int kStages = kFit < kStepMaxStages ? kFit : kStepMaxStages;
+  static_assert(kStages >= 3, "a ring of at least three tiles");
+};
+
+// 8 values of an array: from the stage where they are whole in it, else from memory.
+template <bool F32>
+__device__ __forceinline__ void take8(uint32_t stage, int in, int staged, const void* p, int64_t at, int64_t left, bool vec,
+                                      float (&x)[8]) {
+  if (in + 8 <= staged) {
+    uint32_t a[4];
+    if (F32) {
+      uint32_t b[4];
+      lds4(stage + in * 4, a);
+      lds4(stage + in * 4 + 16, b);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(a[j]), x[4 + j] = __uint_as_float(b[j]);
+    } else {
+      lds4(stage + in * 2, a);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[2 * j] = bf16_lo(a[j]), x[2 * j + 1] = bf16_hi(a[j]);
+    }
+  } else {
+    load8<F32>(p, at, left, vec, x);
+  }
+}
+__device__ __forceinline__ uint2 take8_codes(uint32_t stage, int in, int staged, const uint8_t* p, int64_t left, bool vec) {
+  if (in + 8 > staged) return load8_codes(p, left, vec);
+  uint32_t a[2];
+  lds2(stage + in, a);
+  return make_uint2(a[0], a[1]);
+}
+
 template <bool W32, bool G32, bool LOW, bool SR, bool STATE_SR>
-__global__ void __launch_bounds__(kThreads8) adamw_kernel(const __grid_constant__ AdamwArgs p) {
+__global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_constant__ AdamwArgs p) {
+  using R = StepRing<W32, G32, LOW>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ alignas(8) uint64_t bars[2 * R::kStages];
+  const uint32_t smem = (smem_addr(smem_raw) + 127u) & ~127u;
+  uint8_t* ring = smem_raw + (smem - smem_addr(smem_raw));
+  const uint32_t bar0 = smem_addr(bars);
+  auto full = [&](int s) { return bar0 + 8u * s; };
+  auto empty = [&](int s) { return bar0 + 8u * (R::kStages + s); };
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < R::kStages; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), kStepConsumers / 32);
+    }
+    mbar_init_fence();
+  }
+  __syncthreads();
   float mult = 1.0f;
   if (p.grad_scale) {
     mult = *p.grad_scale;
     if (mult != mult) return;  // the norm was not finite: the step is skipped
   }
-  const AdamwScalars& s = p.s;
-  for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-    const int k = p.tile_tensor[t];
-    const ListTensor& d = p.tensors[k];
-    const void* grad = grad_of(p.g, k);
-    const int64_t at = (t - d.tile0) * kListTile + threadIdx.x * 8;
-    const int64_t left = d.numel - at;
-    const bool vec = d.aligned, gvec = (reinterpret_cast<uintptr_t>(grad) & 15) == 0;
+  const int64_t t0 = p.tiles * blockIdx.x / gridDim.x, t1 = p.tiles * (blockIdx.x + 1) / gridDim.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (warp == kStepConsumers / 32) {
+    int k = p.tile_tensor[t0];
+    ListTensor d = p.tensors[k];
+    const uint8_t* grad = static_cast<const uint8_t*>(grad_of(p.g, k));
+    const uint64_t policy = evict_first_policy();
+    int s = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int64_t t = t0; t < t1; ++t) {
+      const int64_t at0 = (t - d.tile0) * kAdamwTile;
+      if (at0 >= d.numel) {  // the next tensor that has elements
+        k = p.tile_tensor[t];
+        d = p.tensors[k];
+        grad = static_cast<const uint8_t*>(grad_of(p.g, k));
+      }
+      const int64_t at = (t - d.tile0) * kAdamwTile, left = d.numel - at;
+      uint32_t ms = 127, vs = 127;
+      if (LOW && lane * 128 < left) {
+        ms = d.m_scale[at / 128 + lane];
+        vs = d.v_scale[at / 128 + lane];
+      }
+      if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
+      TileHead& h = *reinterpret_cast<TileHead*>(ring + s * R::kBytes);
+      if (LOW) {
+        h.scales[0][lane] = (uint8_t)ms;
+        h.scales[1][lane] = (uint8_t)vs;
+      }
+      if (lane == 0) {
+        const int n = (int)min((int64_t)kAdamwTile, left);
+        auto whole = [&](const void* q, int size) { return (reinterpret_cast<uintptr_t>(q) & 15) ? 0 : n * size / 16 * 16; };
+        const uint8_t *w = static_cast<uint8_t*>(d.w) + at * R::kW, *g = grad + at * R::kG,
+                      *m = static_cast<uint8_t*>(d.m) + at * R::kS, *v = static_cast<uint8_t*>(d.v) + at * R::kS;
+        const int bw = whole(w, R::kW), bg = whole(g, R::kG), bm = whole(m, R::kS), bv = whole(v, R::kS);
+        h.grad = grad;
+        h.w = static_cast<uint8_t*>(d.w), h.m = static_cast<uint8_t*>(d.m), h.v = static_cast<uint8_t*>(d.v);
+        h.compute = d.compute;
+        h.m_scale = d.m_scale, h.v_scale = d.v_scale;
+        h.at = at, h.left = left, h.goff = d.goff;
+        h.staged[0] = bw / R::kW, h.staged[1] = bg / R::kG, h.staged[2] = bm / R::kS, h.staged[3] = bv / R::kS;
+        h.vec = (uint32_t)d.aligned | ((reinterpret_cast<uintptr_t>(grad) & 15) == 0 ? 2u : 0u);
+        const uint32_t st = smem + s * R::kBytes;
+        mbar_expect_tx(full(s), bw + bg + bm + bv);
+        if (bw) tma_load(st + R::kOffW, w, bw, full(s), policy);
+        if (bg) tma_load(st + R::kOffG, g, bg, full(s), policy);
+        if (bm) tma_load(st + R::kOffM, m, bm, full(s), policy);
+        if (bv) tma_load(st + R::kOffV, v, bv, full(s), policy);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full(s));
+      if (++s == R::kStages) { s = 0; phase ^= 1; }
+    }
+    if (!ok) {
+      if (lane == 0) atomicOr(p.err, 1);
+      // the copies in flight, before the block's memory goes (a stage that was never filled has nothing in flight)
+      for (int i = 0; i < R::kStages && i < t1 - t0; ++i) {
+        if (s == 0) { s = R::kStages; phase ^= 1; }
+        --s;
+        mbar_wait(full(s), phase);
+      }
+    }
+    return;
+  }
+
+  const AdamwScalars& c = p.s;
+  const int in = threadIdx.x * 8;
+  int s = 0;
+  uint32_t phase = 0;
+  for (int64_t t = t0; t < t1; ++t) {
+    if (!mbar_wait(full(s), phase)) {
+      if (lane == 0) atomicOr(p.err, 2);
+      return;
+    }
+    const TileHead& h = *reinterpret_cast<const TileHead*>(ring + s * R::kBytes);
+    const uint32_t st = smem + s * R::kBytes;
+    const int64_t left = h.left - in;
+    if (warp * 256 >= h.left) {  // nothing of the tile for this warp
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(s));
+      if (++s == R::kStages) { s = 0; phase ^= 1; }
+      continue;
+    }
+    const int64_t at = h.at + in;
+    const bool vec = h.vec & 1, gvec = h.vec & 2;
     float w[8], g[8], m[8], v[8], r[8];
-    load8<G32>(grad, at, left, gvec, g);
-    load8<W32>(d.w, at, left, vec, w);
-    uint8_t *mc = nullptr, *vc = nullptr;
-    int64_t block = at / 128;
+    take8<G32>(st + R::kOffG, in, h.staged[1], h.grad, at, left, gvec, g);
+    take8<W32>(st + R::kOffW, in, h.staged[0], h.w, at, left, vec, w);
     if (LOW) {
-      mc = static_cast<uint8_t*>(d.m) + at;
-      vc = static_cast<uint8_t*>(d.v) + at;
-      const uint32_t ms = left > 0 ? d.m_scale[block] : 127u, vs = left > 0 ? d.v_scale[block] : 127u;
-      decode8(load8_codes(mc, left, vec), ms, m);
-      decode8(load8_codes(vc, left, vec), vs, v);
+      const uint2 mc = take8_codes(st + R::kOffM, in, h.staged[2], h.m + at, left, vec);
+      const uint2 vc = take8_codes(st + R::kOffV, in, h.staged[3], h.v + at, left, vec);
+      decode8(mc, h.scales[0][threadIdx.x >> 4], m);
+      decode8(vc, h.scales[1][threadIdx.x >> 4], v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
     } else {
-      load8<true>(d.m, at, left, vec, m);
-      load8<true>(d.v, at, left, vec, v);
+      take8<true>(st + R::kOffM, in, h.staged[2], h.m, at, left, vec, m);
+      take8<true>(st + R::kOffV, in, h.staged[3], h.v, at, left, vec, v);
     }
+    uint8_t *const hw = h.w, *const hm = h.m, *const hv = h.v, *const ms = h.m_scale, *const vs = h.v_scale;
+    uint16_t* const compute = h.compute;
+    const int64_t gi = h.goff + at;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(empty(s));
+    if (++s == R::kStages) { s = 0; phase ^= 1; }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float gs = p.grad_scale ? __fmul_rn(g[j], mult) : g[j];
-      m[j] = __fadd_rn(__fmul_rn(m[j], s.b1), __fmul_rn(gs, s.omb1));
-      v[j] = __fadd_rn(__fmul_rn(v[j], s.b2), __fmul_rn(__fmul_rn(gs, gs), s.omb2));
+      m[j] = __fadd_rn(__fmul_rn(m[j], c.b1), __fmul_rn(gs, c.omb1));
+      v[j] = __fadd_rn(__fmul_rn(v[j], c.b2), __fmul_rn(__fmul_rn(gs, gs), c.omb2));
       r[j] = __fsqrt_rn(v[j]);
-      const float u = __fdiv_rn(__fmul_rn(m[j], s.ka), __fadd_rn(__fmul_rn(r[j], s.c2), s.eps));
-      const float base = s.kwd != 0.0f ? __fsub_rn(w[j], __fmul_rn(w[j], s.kwd)) : w[j];
+      const float u = __fdiv_rn(__fmul_rn(m[j], c.ka), __fadd_rn(__fmul_rn(r[j], c.c2), c.eps));
+      const float base = c.kwd != 0.0f ? __fsub_rn(w[j], __fmul_rn(w[j], c.kwd)) : w[j];
       w[j] = __fsub_rn(base, u);
     }
-    const int64_t gi = d.goff + at;
     if (LOW) {
       uint32_t lanes[8] = {};
       if (STATE_SR) {
@@ -198,18 +358,18 @@ __global__ void __launch_bounds__(kThreads8) adamw_kernel(const __grid_constant_
         }
       }
       const int km = block_exponent(m), kv = block_exponent(r);
-      store8_codes(mc, left, vec, encode8<STATE_SR, false>(m, km, lanes, 0));
-      store8_codes(vc, left, vec, encode8<STATE_SR, true>(r, kv, lanes, 16));
+      store8_codes(hm + at, left, vec, encode8<STATE_SR, false>(m, km, lanes, 0));
+      store8_codes(hv + at, left, vec, encode8<STATE_SR, true>(r, kv, lanes, 16));
       if ((threadIdx.x & 15) == 0 && left > 0) {
-        d.m_scale[block] = (uint8_t)(km + 127);
-        d.v_scale[block] = (uint8_t)(kv + 127);
+        ms[at / 128] = (uint8_t)(km + 127);
+        vs[at / 128] = (uint8_t)(kv + 127);
       }
     } else {
-      store8_f32(d.m, at, left, vec, m);
-      store8_f32(d.v, at, left, vec, v);
+      store8_f32(hm, at, left, vec, m);
+      store8_f32(hv, at, left, vec, v);
     }
-    if (W32) store8_f32(d.w, at, left, vec, w);
-    if (!W32 || d.compute) {
+    if (W32) store8_f32(hw, at, left, vec, w);
+    if (!W32 || compute) {
       uint32_t u[4];
       if (!W32 && SR) {
         const uint64_t b = (uint64_t)gi >> 3;
@@ -222,38 +382,97 @@ __global__ void __launch_bounds__(kThreads8) adamw_kernel(const __grid_constant_
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[j] = bf16x2_rn(w[2 * j], w[2 * j + 1]);
       }
-      if (!W32) store8_bf16(d.w, at, left, vec, u);
-      else store8_bf16(d.compute, at, left, vec, u);
+      if (!W32) store8_bf16(hw, at, left, vec, u);
+      else store8_bf16(compute, at, left, vec, u);
     }
   }
 }
 
+// ---------------------------------------------------------------------------
+// The norm.  Each warp walks a run of tiles of 2048 elements, all of a tile's
+// loads in flight at once, and adds squares in eight binary32 sums a thread;
+// these meet in binary64, a partial sum per CTA, which the CTA that comes last
+// adds up in order.  The runs depend on the list alone, so the result's bits do.
+// ---------------------------------------------------------------------------
+constexpr int kNormThreads = 256;
+constexpr int kNormWarps = kNormThreads / 32;
+
 template <bool G32>
-__global__ void __launch_bounds__(kThreads8) grad_norm_kernel(const __grid_constant__ NormArgs p) {
-  __shared__ double part[kThreads8 / 32];
+__global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_constant__ NormArgs p) {
+  __shared__ double part[kNormWarps];
   __shared__ bool last;
-  float acc[4] = {};
-  for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-    const int k = p.tile_tensor[t];
-    const ListTensor& d = p.tensors[k];
-    const void* grad = grad_of(p.g, k);
-    const int64_t at = (t - d.tile0) * kListTile + threadIdx.x * 8;
-    float g[8];
-    load8<G32>(grad, at, d.numel - at, (reinterpret_cast<uintptr_t>(grad) & 15) == 0, g);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t walker = (int64_t)blockIdx.x * kNormWarps + warp, walkers = (int64_t)gridDim.x * kNormWarps;
+  const int64_t t0 = p.tiles * walker / walkers, t1 = p.tiles * (walker + 1) / walkers;
+  float acc[8] = {};
+  int64_t tile0 = 0, numel = 0;
+  const void* grad = nullptr;
+  bool vec = false;
+  for (int64_t t = t0; t < t1; ++t) {
+    if ((t - tile0) * kNormTile >= numel) {
+      const int k = p.tile_tensor[t];
+      tile0 = p.tensors[k].tile0;
+      numel = p.tensors[k].numel;
+      grad = grad_of(p.g, k);
+      vec = (reinterpret_cast<uintptr_t>(grad) & 15) == 0;
+    }
+    const int64_t at = (t - tile0) * kNormTile + lane * 8;
+    if (vec && numel - (t - tile0) * kNormTile >= kNormTile) {
+      constexpr int kLoads = G32 ? 16 : 8;
+      uint4 x[kLoads];
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(grad) + (at - lane * 8) * (G32 ? 4 : 2)) + lane;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j & 3] = __fmaf_rn(g[j], g[j], acc[j & 3]);
+      for (int i = 0; i < kLoads; ++i) x[i] = __ldcs(q + 32 * i);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (G32) {
+            const float a = __uint_as_float(u[j]);
+            acc[4 * (i & 1) + j] = __fmaf_rn(a, a, acc[4 * (i & 1) + j]);
+          } else {
+            const float a = bf16_lo(u[j]), b = bf16_hi(u[j]);
+            acc[2 * j] = __fmaf_rn(a, a, acc[2 * j]);
+            acc[2 * j + 1] = __fmaf_rn(b, b, acc[2 * j + 1]);
+          }
+        }
+      }
+    } else {  // the same elements in the same sums, one at a time: an alignment changes no bit of the result
+      constexpr int kRow = G32 ? 128 : 256, kPer = G32 ? 4 : 8;  // elements of a warp's and a lane's vector load
+      const int64_t end = numel - (t - tile0) * kNormTile;
+      const int64_t first = (t - tile0) * kNormTile;
+      for (int i = 0; i < kNormTile / kRow; ++i)
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const int64_t e = i * kRow + lane * kPer + j;
+          if (e < end) {
+            const float a = G32 ? static_cast<const float*>(grad)[first + e]
+                                : __uint_as_float((uint32_t)static_cast<const uint16_t*>(grad)[first + e] << 16);
+            if (G32) {
+              if (i & 1) acc[4 + (j & 3)] = __fmaf_rn(a, a, acc[4 + (j & 3)]);
+              else acc[j & 3] = __fmaf_rn(a, a, acc[j & 3]);
+            } else {
+              acc[j] = __fmaf_rn(a, a, acc[j]);
+            }
+          }
+        }
+    }
   }
   auto block_sum = [&](double x) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+    if (lane == 0) part[warp] = x;
     __syncthreads();
     x = 0.0;
-    for (int w = 0; w < kThreads8 / 32; ++w) x += part[w];
+    for (int w = 0; w < kNormWarps; ++w) x += part[w];
     return x;
   };
-  const double mine = block_sum(((double)acc[0] + acc[1]) + ((double)acc[2] + acc[3]));
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum += (double)acc[j];
+  const double mine = block_sum(sum);
   if (threadIdx.x == 0) {
     p.partial[blockIdx.x] = mine;
     __threadfence();
@@ -263,7 +482,7 @@ __global__ void __launch_bounds__(kThreads8) grad_norm_kernel(const __grid_const
   if (!last) return;
   __threadfence();
   double x = 0.0;
-  for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads8) x += __ldcg(p.partial + i);
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += kNormThreads) x += __ldcg(p.partial + i);
   x = block_sum(x);
   if (threadIdx.x == 0) {
     const double norm = sqrt(x);
@@ -283,32 +502,50 @@ __global__ void fill_kernel(const __grid_constant__ FillArgs a) {
   for (int i = threadIdx.x; i < a.count; i += blockDim.x) a.table[a.first + i] = a.grads[i];
 }
 
+struct StepKernel {
+  const void* f;
+  int smem;
+};
 template <bool W32, bool G32, bool LOW>
-void* pick(bool sr, bool state_sr) {
+StepKernel pick(bool sr, bool state_sr) {
   if (W32) sr = false;
   if (!LOW) state_sr = false;
-  if (sr) return state_sr ? (void*)adamw_kernel<W32, G32, LOW, !W32, LOW> : (void*)adamw_kernel<W32, G32, LOW, !W32, false>;
-  return state_sr ? (void*)adamw_kernel<W32, G32, LOW, false, LOW> : (void*)adamw_kernel<W32, G32, LOW, false, false>;
+  using R = StepRing<W32, G32, LOW>;
+  const void* f = sr ? (state_sr ? (const void*)adamw_kernel<W32, G32, LOW, !W32, LOW> : (const void*)adamw_kernel<W32, G32, LOW, !W32, false>)
+                     : (state_sr ? (const void*)adamw_kernel<W32, G32, LOW, false, LOW> : (const void*)adamw_kernel<W32, G32, LOW, false, false>);
+  return {f, R::kStages * R::kBytes + 128};
 }
 template <bool W32, bool G32>
-void* pick(const AdamwKind& k) {
+StepKernel pick(const AdamwKind& k) {
   return k.state_e4m3 ? pick<W32, G32, true>(k.sr, k.state_sr) : pick<W32, G32, false>(k.sr, k.state_sr);
+}
+StepKernel pick(const AdamwKind& k) {
+  return k.w_f32 ? (k.g_f32 ? pick<true, true>(k) : pick<true, false>(k)) : (k.g_f32 ? pick<false, true>(k) : pick<false, false>(k));
 }
 
 }  // namespace
 
-cudaError_t launch_adamw(const AdamwArgs& a, const AdamwKind& k, cudaStream_t stream) {
-  void* kernel = k.w_f32 ? (k.g_f32 ? pick<true, true>(k) : pick<true, false>(k))
-                         : (k.g_f32 ? pick<false, true>(k) : pick<false, false>(k));
+cudaError_t prepare_adamw(const AdamwKind& k, int32_t* sms) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+  const StepKernel kernel = pick(k);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel.f, cudaFuncAttributeMaxDynamicSharedMemorySize, kernel.smem);
+  return e;
+}
+
+cudaError_t launch_adamw(const AdamwArgs& a, const AdamwKind& k, int32_t sms, cudaStream_t stream) {
+  const StepKernel kernel = pick(k);
   void* params[] = {const_cast<AdamwArgs*>(&a)};
-  const int64_t grid = a.tiles < 152 * 8 ? a.tiles : 152 * 8;
-  return cudaLaunchKernel(kernel, dim3((unsigned)grid), dim3(kThreads8), params, 0, stream);
+  const unsigned grid = (unsigned)(a.tiles < sms ? a.tiles : sms);
+  return cudaLaunchKernel(kernel.f, dim3(grid), dim3(kStepThreads), params, (size_t)kernel.smem, stream);
 }
 
 cudaError_t launch_grad_norm(const NormArgs& a, cudaStream_t stream) {
-  const unsigned grid = (unsigned)(a.tiles < kNormCtas ? (a.tiles ? a.tiles : 1) : kNormCtas);
-  if (a.g_f32) grad_norm_kernel<true><<<grid, kThreads8, 0, stream>>>(a);
-  else grad_norm_kernel<false><<<grid, kThreads8, 0, stream>>>(a);
+  const int64_t wanted = (a.tiles + kNormWarps - 1) / kNormWarps;
+  const unsigned grid = (unsigned)(wanted < 1 ? 1 : wanted < kNormCtas ? wanted : kNormCtas);
+  if (a.g_f32) grad_norm_kernel<true><<<grid, kNormThreads, 0, stream>>>(a);
+  else grad_norm_kernel<false><<<grid, kNormThreads, 0, stream>>>(a);
   return cudaGetLastError();
 }
 

@@ -10,7 +10,10 @@
 
 namespace mpadam {
 
-constexpr int kListTile = 2048;      // elements per tile; a tensor's last tile may be short
+// Elements per tile; a tensor's last tile may be short.  A CTA takes a tile of a
+// step, a warp one of the norm.
+constexpr int kAdamwTile = 4096;
+constexpr int kNormTile = 2048;
 constexpr int kInlineGrads = 448;    // gradient pointers that travel with one launch
 
 // One tensor of the list. Its tiles are tile0, tile0 + 1, ...
@@ -43,6 +46,7 @@ struct AdamwArgs {
   int64_t tiles;
   AdamwScalars s;
   const float* grad_scale;     // device multiplier of the gradients, or nullptr
+  int32_t* err;                // device error word
   uint32_t rk0[kPhiloxRounds], rk1[kPhiloxRounds];
   uint32_t t_lo, t_hi;
   GradTable g;
@@ -52,7 +56,9 @@ struct AdamwKind {
   bool w_f32, g_f32, state_e4m3, sr, state_sr;
 };
 
-cudaError_t launch_adamw(const AdamwArgs& a, const AdamwKind& k, cudaStream_t stream);
+// Makes the kernel of this kind ready on the current device (and counts its SMs), and launches it.
+cudaError_t prepare_adamw(const AdamwKind& k, int32_t* sms);
+cudaError_t launch_adamw(const AdamwArgs& a, const AdamwKind& k, int32_t sms, cudaStream_t stream);
 
 struct NormArgs {
   const ListTensor* tensors;
@@ -66,7 +72,7 @@ struct NormArgs {
   GradTable g;
 };
 
-constexpr int kNormCtas = 152 * 4;
+constexpr int kNormCtas = 152 * 5;
 cudaError_t launch_grad_norm(const NormArgs& a, cudaStream_t stream);
 
 // Copies count gradient pointers into a device table at `first`.

@@ -45,14 +45,14 @@ struct List {
     cudaFree(d_grads);
   }
 
-  int32_t build(std::vector<ListTensor>& t) {
+  int32_t build(std::vector<ListTensor>& t, int32_t tile) {
     n = (int32_t)t.size();
     int64_t goff = 0;
     for (auto& x : t) {
       x.goff = goff;
       x.tile0 = tiles;
       goff += (x.numel + 127) / 128 * 128;
-      tiles += (x.numel + kListTile - 1) / kListTile;
+      tiles += (x.numel + tile - 1) / tile;
       numel.push_back(x.numel);
     }
     if (tiles >= INT32_MAX) return fail(MPADAM_EINVAL, "the list has too many elements");
@@ -61,7 +61,7 @@ struct List {
     if (!tiles) return MPADAM_OK;
     std::vector<int32_t> owner((size_t)tiles);
     for (int32_t k = 0; k < n; ++k)
-      std::fill_n(owner.begin() + t[k].tile0, (t[k].numel + kListTile - 1) / kListTile, k);
+      std::fill_n(owner.begin() + t[k].tile0, (t[k].numel + tile - 1) / tile, k);
     if (dev_malloc(&d_tensors, sizeof(ListTensor) * n) != cudaSuccess ||
         dev_malloc(&d_tile_tensor, sizeof(int32_t) * tiles) != cudaSuccess ||
         (n > kInlineGrads && dev_malloc(&d_grads, sizeof(void*) * n) != cudaSuccess)) {
@@ -115,7 +115,10 @@ struct List {
 struct mpadam_adamw_state {
   List list;
   mpadam_adamw_config cfg;
+  AdamwKind kind;
+  int32_t sms = 0;
   AdamwArgs args{};
+  ~mpadam_adamw_state() { cudaFree(args.err); }
 };
 struct mpadam_grad_norm_state {
   List list;
@@ -167,8 +170,18 @@ extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32
     std::unique_ptr<mpadam_adamw_state> s(new mpadam_adamw_state());
     s->cfg = c;
     s->list.grad_size = c.grad_dtype == MPADAM_F32 ? 4 : 2;
-    const int32_t rc = s->list.build(list);
+    const int32_t rc = s->list.build(list, kAdamwTile);
     if (rc) return rc;
+    s->kind = {c.weight_dtype == MPADAM_F32, c.grad_dtype == MPADAM_F32, c.state_dtype == MPADAM_E4M3,
+               c.rounding == MPADAM_ROUND_STOCHASTIC, c.state_rounding == MPADAM_ROUND_STOCHASTIC};
+    cudaError_t e = prepare_adamw(s->kind, &s->sms);
+    if (e != cudaSuccess) return cuda_fail(e, "preparing the AdamW step");
+    if (dev_malloc(&s->args.err, sizeof(int32_t)) != cudaSuccess) {
+      cudaGetLastError();
+      return fail(MPADAM_EALLOC, "allocation of the error word failed");
+    }
+    e = cudaMemset(s->args.err, 0, sizeof(int32_t));
+    if (e != cudaSuccess) return cuda_fail(e, "cudaMemset");
     s->args.tensors = s->list.d_tensors;
     s->args.tile_tensor = s->list.d_tile_tensor;
     s->args.tiles = s->list.tiles;
@@ -211,11 +224,20 @@ extern "C" int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* g
   s->args.grad_scale = grad_scale;
   s->args.t_lo = (uint32_t)(uint64_t)step;
   s->args.t_hi = (uint32_t)((uint64_t)step >> 32);
-  const AdamwKind kind{c.weight_dtype == MPADAM_F32, c.grad_dtype == MPADAM_F32, c.state_dtype == MPADAM_E4M3,
-                       c.rounding == MPADAM_ROUND_STOCHASTIC, c.state_rounding == MPADAM_ROUND_STOCHASTIC};
-  const cudaError_t e = launch_adamw(s->args, kind, stream);
+  const cudaError_t e = launch_adamw(s->args, s->kind, s->sms, stream);
   if (e != cudaSuccess) return cuda_fail(e, "launch of the AdamW step");
   return MPADAM_OK;
+}
+
+extern "C" int32_t mpadam_adamw_status(mpadam_adamw_state* s, int32_t* code) {
+  if (!s || !code) return fail(MPADAM_EINVAL, "state or code is NULL");
+  *code = 0;
+  const int32_t rc = check_device(s->list.device);
+  if (rc) return rc;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpy(code, s->args.err, sizeof(int32_t), cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && *code) e = cudaMemset(s->args.err, 0, sizeof(int32_t));
+  return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "reading the error word");
 }
 
 extern "C" int32_t mpadam_adamw_destroy(mpadam_adamw_state* s) {
@@ -241,7 +263,7 @@ extern "C" int32_t mpadam_grad_norm_create(const int64_t* numel, int32_t n, int3
     }
     std::unique_ptr<mpadam_grad_norm_state> s(new mpadam_grad_norm_state());
     s->list.grad_size = grad_dtype == MPADAM_F32 ? 4 : 2;
-    int32_t rc = s->list.build(list);
+    int32_t rc = s->list.build(list, kNormTile);
     NormArgs& a = s->args;
     if (!rc) {
       // the partial sums, and the count of CTAs behind them
