@@ -8,7 +8,7 @@
 // power-of-two scale per 128 elements: the root halves the second moment's
 // range, and the update needs it anyway.
 #include "adamw.h"
-#include "step_kernel.cuh"
+#include "adamw_math.cuh"
 
 namespace mpadam {
 
@@ -146,7 +146,7 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], int k, const uint3
 // The step.  One CTA per SM walks a run of tiles.  A producer warp brings each
 // tile's arrays into a ring in shared memory by bulk copies (with the tile's
 // place, its pointers and its blocks' scales beside them, whose addresses need
-// not be aligned); 16 consumer warps update 8 elements a thread and store
+// not be aligned); 15 consumer warps (with the producer, 16 of 128 registers) update 8 elements a thread and store
 // straight to global memory.  Arrays that are off a 16-byte boundary, and ends
 // that do not fill one, are read by the consumers themselves.
 // ---------------------------------------------------------------------------
@@ -154,7 +154,7 @@ constexpr int kStepConsumers = kAdamwTile / 8;
 constexpr int kStepThreads = kStepConsumers + 32;
 constexpr int kStepSmem = 200 * 1024;  // of the ring, at most
 constexpr int kStepMaxStages = 8;
-constexpr int kTileScales = kAdamwTile / 128;
+static_assert(kAdamwTile / 128 <= 32, "a lane of the producer per block");
 
 // What the consumers need to know of a stage's tile.
 struct TileHead {
@@ -166,7 +166,7 @@ struct TileHead {
   int32_t staged[4];       // elements of w, g, m, v that are in the stage
   uint32_t vec;            // bits 0: w, m, v, compute 16-byte aligned; 1: the gradient
   int32_t pad[3];
-  uint8_t scales[2][kTileScales];
+  uint8_t scales[2][32];
 };
 
 template <bool W32, bool G32, bool LOW>
@@ -206,6 +206,169 @@ __device__ __forceinline__ uint2 take8_codes(uint32_t stage, int in, int staged,
   uint32_t a[2];
   lds2(stage + in, a);
   return make_uint2(a[0], a[1]);
+}
+
+// The 16 random bits of 8 weights, two to a word, and the 32 of 8 elements' moments (gi: the first one's global index).
+__device__ __forceinline__ void weight_lanes(const AdamwArgs& p, int64_t gi, uint32_t (&r)[4]) {
+  const uint64_t b = (uint64_t)gi >> 3;
+  const uint4 x = philox4x32_10((uint32_t)b, (uint32_t)(b >> 32), p.t_lo, p.t_hi, p.rk0, p.rk1);
+  r[0] = x.x, r[1] = x.y, r[2] = x.z, r[3] = x.w;
+}
+__device__ __forceinline__ void state_lanes(const AdamwArgs& p, int64_t gi, uint32_t (&r)[8]) {
+  const uint64_t b = (uint64_t)gi >> 2;  // even: both blocks have the same high word
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint4 x = philox4x32_10((uint32_t)b + i, (uint32_t)(b >> 32) | 0x80000000u, p.t_lo, p.t_hi, p.rk0, p.rk1);
+    r[4 * i] = x.x, r[4 * i + 1] = x.y, r[4 * i + 2] = x.z, r[4 * i + 3] = x.w;
+  }
+}
+__device__ __forceinline__ uint32_t bf16x2_stochastic(float lo, float hi, uint32_t rnd) {
+  return __byte_perm(bf16_sr_sum(lo, ~rnd & 0xFFFFu), bf16_sr_sum(hi, ~rnd >> 16), 0x7632);
+}
+
+// The canonical weight from the updated first moment and root.
+__device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, float m, float r) {
+  const float u = __fdiv_rn(__fmul_rn(m, c.ka), __fadd_rn(__fmul_rn(r, c.c2), c.eps));
+  return __fsub_rn(c.kwd != 0.0f ? __fsub_rn(w, __fmul_rn(w, c.kwd)) : w, u);
+}
+
+// Codes and weights of a thread whose fast results were not decided.
+template <bool STATE_SR>
+__device__ __noinline__ void slow_codes(const float (&m)[8], const float (&r)[8], int km, int kr, const uint32_t (&lanes)[8],
+                                        uint2& cm, uint2& cr) {
+  cm = encode8<STATE_SR, false>(m, km, lanes, 0);
+  cr = encode8<STATE_SR, true>(r, kr, lanes, 16);
+}
+template <bool SR>
+__device__ __noinline__ void slow_weights(const AdamwScalars& c, const float (&w)[8], const float (&m)[8], const float (&r)[8],
+                                          const uint32_t (&rnd)[4], uint32_t (&u)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float a = new_weight(c, w[2 * j], m[2 * j], r[2 * j]), b = new_weight(c, w[2 * j + 1], m[2 * j + 1], r[2 * j + 1]);
+    u[j] = SR ? bf16x2_stochastic(a, b, rnd[j]) : bf16x2_rn(a, b);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The update of 8 BF16 weights with 8-bit moments, where an element has 10 bytes
+// and instructions are the bound: the same results, bit for bit, with about half
+// of the instructions.
+//
+// Moments and root are the canonical ones, two elements at a time.  The weight
+// takes its quotient as a product with rcp.approx.ftz (2^-23 relative): with u =
+// 2^-24, the quotient is within 2^-23 + 2u of the canonical one and the sum adds
+// a rounding on either side, so the canonical weight lies within (|q| + |w'|)
+// 1.0625 2^-22 + 2^-96 of w' (the last term for subnormal quotients).  It is stored
+// where both ends of that interval have the same code (Ziv's test: rounding by
+// given random bits is monotone), else computed exactly: about 1 thread in 800.
+//
+// Codes of the moments: on E4M3's normal range, adding 16 random bits below the
+// grid and cutting off is two integer operations.  A thread with a non-zero value
+// below 2^-6 of its block's scale (about 1 in 500; zeros beside others count as
+// such) takes the general encoder.  Values that are not finite, and second moments from 2^32 on,
+// send the whole warp to the general code (false).
+// ---------------------------------------------------------------------------
+template <bool SR, bool STATE_SR>
+__device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t at, int64_t left, bool vec,
+                                            const float (&w)[8], const float (&g)[8], const float (&m0)[8], const float (&r0)[8],
+                                            uint8_t* hw, uint8_t* hm, uint8_t* hv, uint8_t* ms, uint8_t* vs) {
+  const AdamwScalars& c = p.s;
+  float m[8], r[8];
+  f32x2 wn[4], ne[4], fin = 0;
+  const f32x2 nz = p.minus_zero, mult2 = both(mult), nkwd = both(-c.kwd), nka = both(-c.ka);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    f32x2 gg = pk(g[2 * j], g[2 * j + 1]);
+    if (p.grad_scale) gg = mul2_rn(gg, mult2);
+    const f32x2 mm = add2_rn(prod2(pk(m0[2 * j], m0[2 * j + 1]), both(c.b1), nz), prod2(gg, both(c.omb1), nz));
+    const f32x2 ro = pk(r0[2 * j], r0[2 * j + 1]);
+    const f32x2 vv = add2_rn(prod2(mul2_rn(ro, ro), both(c.b2), nz), prod2(mul2_rn(gg, gg), both(c.omb2), nz));
+    const f32x2 rr = root2(vv);
+    unpk(mm, m[2 * j], m[2 * j + 1]);
+    unpk(rr, r[2 * j], r[2 * j + 1]);
+    fin = fma2_rn(mm, 0ull, fma2_rn(rr, 0ull, fin));
+    float d0, d1, q0, q1, w0, w1;
+    unpk(add2_rn(prod2(rr, both(c.c2), nz), both(c.eps)), d0, d1);
+    const f32x2 q = prod2(mul2_rn(mm, nka), pk(rcp_approx_ftz(d0), rcp_approx_ftz(d1)), nz);
+    f32x2 base = pk(w[2 * j], w[2 * j + 1]);
+    if (c.kwd != 0.0f) base = add2_rn(base, prod2(base, nkwd, nz));
+    wn[j] = add2_rn(base, q);
+    fin = fma2_rn(wn[j], 0ull, fin);
+    unpk(q, q0, q1);
+    unpk(wn[j], w0, w1);
+    ne[j] = fma2_rn(pk(__fadd_rn(fabsf(q0), fabsf(w0)), __fadd_rn(fabsf(q1), fabsf(w1))), both(-0x1.1p-22f), both(-0x1p-96f));
+  }
+  if (__any_sync(~0u, cert_not_finite(fin))) return false;
+
+  uint32_t lanes[8] = {};
+  if (STATE_SR) state_lanes(p, gi, lanes);
+  // Both blocks' exponents from the 16 lanes' maxima, as 16-bit halves of a word: 0 where all are 0, else k + 135.
+  float am = 0.0f, ar = 0.0f, lm = __uint_as_float(0x7F800000u), lr = lm;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    am = fmaxf(fmaxf(am, fabsf(m[j])), fabsf(m[j + 1]));
+    ar = fmaxf(fmaxf(ar, r[j]), r[j + 1]);
+    lm = fminf(fminf(lm, fabsf(m[j])), fabsf(m[j + 1]));
+    lr = fminf(fminf(lr, r[j]), r[j + 1]);
+  }
+  auto biased = [](float a) { return a == 0.0f ? 0u : max(8u, (__float_as_uint(a) + 0x1FFFFFu) >> 23); };
+  uint32_t k2 = biased(am) | biased(ar) << 16;
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) k2 = __vmaxu2(k2, __shfl_xor_sync(~0u, k2, d));
+  const int km = (k2 & 0xFFFFu) ? (int)(k2 & 0xFFFFu) - 135 : 0, kr = k2 >> 16 ? (int)(k2 >> 16) - 135 : 0;
+  const float im = __uint_as_float((uint32_t)(127 - km) << 23), ir = __uint_as_float((uint32_t)(127 - kr) << 23);
+  uint2 cm, cr;
+  if (STATE_SR && ((am != 0.0f && __fmul_rn(lm, im) < 0x1p-6f) || (ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-6f))) {
+    slow_codes<STATE_SR>(m, r, km, kr, lanes, cm, cr);
+  } else if (!STATE_SR && ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-9f) {
+    slow_codes<STATE_SR>(m, r, km, kr, lanes, cm, cr);
+  } else {
+    uint32_t a[4], b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float y0, y1, z0, z1;
+      unpk(mul2_rn(pk(m[2 * j], m[2 * j + 1]), both(im)), y0, y1);
+      unpk(mul2_rn(pk(r[2 * j], r[2 * j + 1]), both(ir)), z0, z1);
+      if (STATE_SR) {
+        y0 = __uint_as_float((__float_as_uint(y0) + (lanes[2 * j] & 0xFFFFu) * 16u) & ~0xFFFFFu);
+        y1 = __uint_as_float((__float_as_uint(y1) + (lanes[2 * j + 1] & 0xFFFFu) * 16u) & ~0xFFFFFu);
+        z0 = __uint_as_float((__float_as_uint(z0) + (lanes[2 * j] >> 16) * 16u) & ~0xFFFFFu);
+        z1 = __uint_as_float((__float_as_uint(z1) + (lanes[2 * j + 1] >> 16) * 16u) & ~0xFFFFFu);
+      }
+      a[j] = e4m3x2(y0, y1);
+      b[j] = e4m3x2(z0, z1);
+    }
+    cm = make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410));
+    cr = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
+  }
+  store8_codes(hm + at, left, vec, cm);
+  store8_codes(hv + at, left, vec, cr);
+  if ((threadIdx.x & 15) == 0 && left > 0) {
+    ms[at / 128] = (uint8_t)(km + 127);
+    vs[at / 128] = (uint8_t)(kr + 127);
+  }
+
+  uint32_t rnd[4] = {}, u[4], differ = 0;
+  if (SR) weight_lanes(p, gi, rnd);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float l0, l1, h0, h1;
+    unpk(add2_rd(wn[j], ne[j]), l0, l1);
+    f32x2 hi;
+    asm("fma.rp.f32x2 %0, %1, %2, %3;" : "=l"(hi) : "l"(ne[j]), "l"(both(-1.0f)), "l"(wn[j]));
+    unpk(hi, h0, h1);
+    if (SR) {
+      const uint32_t n0 = ~rnd[j] & 0xFFFFu, n1 = ~rnd[j] >> 16;
+      u[j] = __byte_perm(__float_as_uint(l0) + n0, __float_as_uint(l1) + n1, 0x7632);
+      differ |= u[j] ^ __byte_perm(__float_as_uint(h0) + n0, __float_as_uint(h1) + n1, 0x7632);
+    } else {
+      u[j] = bf16x2_rn(l0, l1);
+      differ |= u[j] ^ bf16x2_rn(h0, h1);
+    }
+  }
+  if (differ) slow_weights<SR>(c, w, m, r, rnd, u);
+  store8_bf16(hw, at, left, vec, u);
+  return true;
 }
 
 template <bool W32, bool G32, bool LOW, bool SR, bool STATE_SR>
@@ -251,7 +414,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
       }
       const int64_t at = (t - d.tile0) * kAdamwTile, left = d.numel - at;
       uint32_t ms = 127, vs = 127;
-      if (LOW && lane * 128 < left) {
+      if (LOW && lane < kAdamwTile / 128 && lane * 128 < left) {
         ms = d.m_scale[at / 128 + lane];
         vs = d.v_scale[at / 128 + lane];
       }
@@ -317,16 +480,14 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
     }
     const int64_t at = h.at + in;
     const bool vec = h.vec & 1, gvec = h.vec & 2;
-    float w[8], g[8], m[8], v[8], r[8];
+    float w[8], g[8], m[8], v[8];
     take8<G32>(st + R::kOffG, in, h.staged[1], h.grad, at, left, gvec, g);
     take8<W32>(st + R::kOffW, in, h.staged[0], h.w, at, left, vec, w);
     if (LOW) {
       const uint2 mc = take8_codes(st + R::kOffM, in, h.staged[2], h.m + at, left, vec);
       const uint2 vc = take8_codes(st + R::kOffV, in, h.staged[3], h.v + at, left, vec);
       decode8(mc, h.scales[0][threadIdx.x >> 4], m);
-      decode8(vc, h.scales[1][threadIdx.x >> 4], v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
+      decode8(vc, h.scales[1][threadIdx.x >> 4], v);  // the root
     } else {
       take8<true>(st + R::kOffM, in, h.staged[2], h.m, at, left, vec, m);
       take8<true>(st + R::kOffV, in, h.staged[3], h.v, at, left, vec, v);
@@ -337,26 +498,22 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
     __syncwarp();
     if (lane == 0) mbar_arrive(empty(s));
     if (++s == R::kStages) { s = 0; phase ^= 1; }
+    if constexpr (LOW && !W32) {
+      if (fast_update<SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, hw, hm, hv, ms, vs)) continue;
+    }
+    float r[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
+      if (LOW) v[j] = __fmul_rn(v[j], v[j]);
       const float gs = p.grad_scale ? __fmul_rn(g[j], mult) : g[j];
       m[j] = __fadd_rn(__fmul_rn(m[j], c.b1), __fmul_rn(gs, c.omb1));
       v[j] = __fadd_rn(__fmul_rn(v[j], c.b2), __fmul_rn(__fmul_rn(gs, gs), c.omb2));
       r[j] = __fsqrt_rn(v[j]);
-      const float u = __fdiv_rn(__fmul_rn(m[j], c.ka), __fadd_rn(__fmul_rn(r[j], c.c2), c.eps));
-      const float base = c.kwd != 0.0f ? __fsub_rn(w[j], __fmul_rn(w[j], c.kwd)) : w[j];
-      w[j] = __fsub_rn(base, u);
+      w[j] = new_weight(c, w[j], m[j], r[j]);
     }
     if (LOW) {
       uint32_t lanes[8] = {};
-      if (STATE_SR) {
-        const uint64_t b = (uint64_t)gi >> 2;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint4 x = philox4x32_10((uint32_t)(b + i), (uint32_t)((b + i) >> 32) | 0x80000000u, p.t_lo, p.t_hi, p.rk0, p.rk1);
-          lanes[4 * i] = x.x, lanes[4 * i + 1] = x.y, lanes[4 * i + 2] = x.z, lanes[4 * i + 3] = x.w;
-        }
-      }
+      if (STATE_SR) state_lanes(p, gi, lanes);
       const int km = block_exponent(m), kv = block_exponent(r);
       store8_codes(hm + at, left, vec, encode8<STATE_SR, false>(m, km, lanes, 0));
       store8_codes(hv + at, left, vec, encode8<STATE_SR, true>(r, kv, lanes, 16));
@@ -372,12 +529,10 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
     if (!W32 || compute) {
       uint32_t u[4];
       if (!W32 && SR) {
-        const uint64_t b = (uint64_t)gi >> 3;
-        const uint4 x = philox4x32_10((uint32_t)b, (uint32_t)(b >> 32), p.t_lo, p.t_hi, p.rk0, p.rk1);
-        const uint32_t rnd[4] = {x.x, x.y, x.z, x.w};
+        uint32_t rnd[4];
+        weight_lanes(p, gi, rnd);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          u[j] = __byte_perm(bf16_sr_sum(w[2 * j], ~rnd[j] & 0xFFFFu), bf16_sr_sum(w[2 * j + 1], ~rnd[j] >> 16), 0x7632);
+        for (int j = 0; j < 4; ++j) u[j] = bf16x2_stochastic(w[2 * j], w[2 * j + 1], rnd[j]);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[j] = bf16x2_rn(w[2 * j], w[2 * j + 1]);

@@ -12,7 +12,7 @@ namespace mpadam {
 
 // Elements per tile; a tensor's last tile may be short.  A CTA takes a tile of a
 // step, a warp one of the norm.
-constexpr int kAdamwTile = 4096;
+constexpr int kAdamwTile = 3840;
 constexpr int kNormTile = 2048;
 constexpr int kInlineGrads = 448;    // gradient pointers that travel with one launch
 
@@ -45,6 +45,7 @@ struct AdamwArgs {
   const int32_t* tile_tensor;  // [tiles] the tensor each tile belongs to
   int64_t tiles;
   AdamwScalars s;
+  uint64_t minus_zero;         // two binary32 -0 (see prod2)
   const float* grad_scale;     // device multiplier of the gradients, or nullptr
   int32_t* err;                // device error word
   uint32_t rk0[kPhiloxRounds], rk1[kPhiloxRounds];

@@ -185,6 +185,7 @@ extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32
     s->args.tensors = s->list.d_tensors;
     s->args.tile_tensor = s->list.d_tile_tensor;
     s->args.tiles = s->list.tiles;
+    s->args.minus_zero = 0x8000000080000000ull;
     round_keys(c.seed, s->args.rk0, s->args.rk1);
     *out = s.release();
   } catch (const std::bad_alloc&) {

@@ -1,6 +1,9 @@
 """The AdamW step and the gradient norm against plain references: the canonical binary32 sequence bit for bit, and
 binary64 within what its roundings allow."""
+import ctypes
 import math
+import subprocess
+from pathlib import Path
 
 import numpy as np
 import pytest
@@ -353,3 +356,26 @@ def test_refusals():
         norm([g], 0.0)
     with pytest.raises(ValueError):
         norm([g], out=torch.zeros(1, device="cuda"))
+
+
+@pytest.fixture(scope="module")
+def probe(tmp_path_factory):
+    from paper_2607_10611_gb300 import builder as B
+    out = tmp_path_factory.mktemp("root") / "libroot_probe.so"
+    subprocess.run([B.nvcc(), *B.NVCC_FLAGS, "-shared", str(Path(__file__).parent / "cuda" / "root_probe.cu"), "-o", str(out)],
+                   check=True)
+    lib = ctypes.CDLL(str(out))
+    lib.root_probe.argtypes = [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p]
+    return lib
+
+
+def test_square_root_is_the_correctly_rounded_one_everywhere(probe):
+    """Every binary32 value from 0 up to 2^32, where the step turns to the library's square root; and the reciprocal over
+    all normal values within the 2^-23 that the update's bound takes."""
+    wrong = torch.zeros(1, dtype=torch.int64, device="cuda")
+    worst = torch.zeros(1, device="cuda")
+    end = 0x4F800000  # 2^32
+    assert probe.root_probe(0, end, wrong.data_ptr(), worst.data_ptr()) == 0
+    assert int(wrong) == 0, int(wrong)
+    assert probe.root_probe(end, 0x7F000000 - end, wrong.data_ptr(), worst.data_ptr()) == 0
+    assert float(worst) <= 2.0 ** -23
