@@ -82,14 +82,12 @@ __device__ __forceinline__ void store8_codes(uint8_t* q, int64_t left, bool vec,
   }
 }
 
-// 8 E4M3 codes times 2^(scale - 127).
-__device__ __forceinline__ void decode8(uint2 c, uint32_t scale, float (&x)[8]) {
-  const float s = __uint_as_float(scale == 0 ? 0x00400000u : scale << 23);
+// The values of 8 E4M3 codes, and of an E8M0 scale.
+__device__ __forceinline__ void decode8(uint2 c, float (&x)[8]) {
   const uint32_t u[2] = {c.x, c.y};
   e4m3x8_to_f32(u, x);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = __fmul_rn(x[j], s);
 }
+__device__ __forceinline__ float scale_value(uint32_t scale) { return __uint_as_float(scale == 0 ? 0x00400000u : scale << 23); }
 
 // The largest finite |x| (as bits) of the 16 lanes that own a block of 128, and the block's exponent from it: the
 // smallest k >= -127 with A <= 448 2^k (448 = 1.75 2^8: the addition carries into the exponent where the mantissa is
@@ -232,21 +230,20 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
   return __fsub_rn(c.kwd != 0.0f ? __fsub_rn(w, __fmul_rn(w, c.kwd)) : w, u);
 }
 
-// Codes and weights of a thread whose fast results were not decided.
-template <bool STATE_SR>
-__device__ __noinline__ void slow_codes(const float (&m)[8], const float (&r)[8], int km, int kr, const uint32_t (&lanes)[8],
-                                        uint2& cm, uint2& cr) {
-  cm = encode8<STATE_SR, false>(m, km, lanes, 0);
-  cr = encode8<STATE_SR, true>(r, kr, lanes, 16);
+// A moment's code and a weight where the fast result was not decided.  They take and give values, so that nothing of
+// the fast path has to live in memory.
+template <bool SR, bool KEEP>
+__device__ __noinline__ uint32_t slow_code(float x, float inv, uint32_t r) {
+  float y = __fmul_rn(x, inv);
+  if (SR) y = e4m3_stochastic(y, r);
+  if (KEEP && x > 0.0f) y = fmaxf(y, 0x1p-9f);
+  return e4m3x2(y, 0.0f) & 0xFFu;
 }
 template <bool SR>
-__device__ __noinline__ void slow_weights(const AdamwScalars& c, const float (&w)[8], const float (&m)[8], const float (&r)[8],
-                                          const uint32_t (&rnd)[4], uint32_t (&u)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float a = new_weight(c, w[2 * j], m[2 * j], r[2 * j]), b = new_weight(c, w[2 * j + 1], m[2 * j + 1], r[2 * j + 1]);
-    u[j] = SR ? bf16x2_stochastic(a, b, rnd[j]) : bf16x2_rn(a, b);
-  }
+__device__ __noinline__ uint32_t slow_weight(float w, float m, float r, uint32_t rnd16, float ka, float c2, float eps, float kwd) {
+  const AdamwScalars c{0.0f, 0.0f, 0.0f, 0.0f, ka, c2, eps, kwd};
+  const float x = new_weight(c, w, m, r);
+  return SR ? bf16_sr_sum(x, rnd16 ^ 0xFFFFu) >> 16 : bf16x2_rn(x, 0.0f) & 0xFFFFu;
 }
 
 // ---------------------------------------------------------------------------
@@ -254,7 +251,10 @@ __device__ __noinline__ void slow_weights(const AdamwScalars& c, const float (&w
 // and instructions are the bound: the same results, bit for bit, with about half
 // of the instructions.
 //
-// Moments and root are the canonical ones, two elements at a time.  The weight
+// Moments and root are the canonical ones, two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
+// powers of two and a code's square has 8 bits, so b1 (code s) = (b1 s) code and b2 (code s)^2 = (b2 s^2) code^2 bit for
+// bit, for scales from 2^-47 to 2^23, where nothing is subnormal or overflows (others, and moments and weights that
+// are not finite, and second moments from 2^32 on, send the warp to the general code: false).  The weight
 // takes its quotient as a product with rcp.approx.ftz (2^-23 relative): with u =
 // 2^-24, the quotient is within 2^-23 + 2u of the canonical one and the sum adds
 // a rounding on either side, so the canonical weight lies within (|q| + |w'|)
@@ -265,28 +265,28 @@ __device__ __noinline__ void slow_weights(const AdamwScalars& c, const float (&w
 // Codes of the moments: on E4M3's normal range, adding 16 random bits below the
 // grid and cutting off is two integer operations.  A thread with a non-zero value
 // below 2^-6 of its block's scale (about 1 in 500; zeros beside others count as
-// such) takes the general encoder.  Values that are not finite, and second moments from 2^32 on,
-// send the whole warp to the general code (false).
+// such) takes the general encoder.
 // ---------------------------------------------------------------------------
 template <bool SR, bool STATE_SR>
 __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t at, int64_t left, bool vec,
-                                            const float (&w)[8], const float (&g)[8], const float (&m0)[8], const float (&r0)[8],
+                                            const float (&w)[8], const float (&g)[8], const float (&m0)[8], const float (&r0)[8], uint32_t km0, uint32_t kr0,
                                             uint8_t* hw, uint8_t* hm, uint8_t* hv, uint8_t* ms, uint8_t* vs) {
   const AdamwScalars& c = p.s;
   float m[8], r[8];
   f32x2 wn[4], ne[4], fin = 0;
+  const float sm = scale_value(km0), sr = scale_value(kr0);
+  const f32x2 b1 = both(__fmul_rn(c.b1, sm)), b2 = both(__fmul_rn(c.b2, __fmul_rn(sr, sr)));
   const f32x2 nz = p.minus_zero, mult2 = both(mult), nkwd = both(-c.kwd), nka = both(-c.ka);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     f32x2 gg = pk(g[2 * j], g[2 * j + 1]);
     if (p.grad_scale) gg = mul2_rn(gg, mult2);
-    const f32x2 mm = add2_rn(prod2(pk(m0[2 * j], m0[2 * j + 1]), both(c.b1), nz), prod2(gg, both(c.omb1), nz));
+    const f32x2 mm = add2_rn(prod2(pk(m0[2 * j], m0[2 * j + 1]), b1, nz), prod2(gg, both(c.omb1), nz));
     const f32x2 ro = pk(r0[2 * j], r0[2 * j + 1]);
-    const f32x2 vv = add2_rn(prod2(mul2_rn(ro, ro), both(c.b2), nz), prod2(mul2_rn(gg, gg), both(c.omb2), nz));
+    const f32x2 vv = add2_rn(prod2(mul2_rn(ro, ro), b2, nz), prod2(mul2_rn(gg, gg), both(c.omb2), nz));
     const f32x2 rr = root2(vv);
     unpk(mm, m[2 * j], m[2 * j + 1]);
     unpk(rr, r[2 * j], r[2 * j + 1]);
-    fin = fma2_rn(mm, 0ull, fma2_rn(rr, 0ull, fin));
     float d0, d1, q0, q1, w0, w1;
     unpk(add2_rn(prod2(rr, both(c.c2), nz), both(c.eps)), d0, d1);
     const f32x2 q = prod2(mul2_rn(mm, nka), pk(rcp_approx_ftz(d0), rcp_approx_ftz(d1)), nz);
@@ -298,7 +298,7 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     unpk(wn[j], w0, w1);
     ne[j] = fma2_rn(pk(__fadd_rn(fabsf(q0), fabsf(w0)), __fadd_rn(fabsf(q1), fabsf(w1))), both(-0x1.1p-22f), both(-0x1p-96f));
   }
-  if (__any_sync(~0u, cert_not_finite(fin))) return false;
+  if (__any_sync(~0u, cert_not_finite(fin) || min(km0, kr0) < 80u || max(km0, kr0) > 150u)) return false;
 
   uint32_t lanes[8] = {};
   if (STATE_SR) state_lanes(p, gi, lanes);
@@ -317,13 +317,17 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
   for (int d = 1; d < 16; d <<= 1) k2 = __vmaxu2(k2, __shfl_xor_sync(~0u, k2, d));
   const int km = (k2 & 0xFFFFu) ? (int)(k2 & 0xFFFFu) - 135 : 0, kr = k2 >> 16 ? (int)(k2 >> 16) - 135 : 0;
   const float im = __uint_as_float((uint32_t)(127 - km) << 23), ir = __uint_as_float((uint32_t)(127 - kr) << 23);
-  uint2 cm, cr;
-  if (STATE_SR && ((am != 0.0f && __fmul_rn(lm, im) < 0x1p-6f) || (ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-6f))) {
-    slow_codes<STATE_SR>(m, r, km, kr, lanes, cm, cr);
-  } else if (!STATE_SR && ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-9f) {
-    slow_codes<STATE_SR>(m, r, km, kr, lanes, cm, cr);
+  uint32_t a[4], b[4];
+  if (STATE_SR ? (am != 0.0f && __fmul_rn(lm, im) < 0x1p-6f) || (ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-6f)
+               : ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-9f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      a[j] = slow_code<STATE_SR, false>(m[2 * j], im, lanes[2 * j] & 0xFFFFu) |
+             slow_code<STATE_SR, false>(m[2 * j + 1], im, lanes[2 * j + 1] & 0xFFFFu) << 8;
+      b[j] = slow_code<STATE_SR, true>(r[2 * j], ir, lanes[2 * j] >> 16) |
+             slow_code<STATE_SR, true>(r[2 * j + 1], ir, lanes[2 * j + 1] >> 16) << 8;
+    }
   } else {
-    uint32_t a[4], b[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float y0, y1, z0, z1;
@@ -338,17 +342,15 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
       a[j] = e4m3x2(y0, y1);
       b[j] = e4m3x2(z0, z1);
     }
-    cm = make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410));
-    cr = make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
   }
-  store8_codes(hm + at, left, vec, cm);
-  store8_codes(hv + at, left, vec, cr);
+  store8_codes(hm + at, left, vec, make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)));
+  store8_codes(hv + at, left, vec, make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410)));
   if ((threadIdx.x & 15) == 0 && left > 0) {
     ms[at / 128] = (uint8_t)(km + 127);
     vs[at / 128] = (uint8_t)(kr + 127);
   }
 
-  uint32_t rnd[4] = {}, u[4], differ = 0;
+  uint32_t rnd[4] = {}, u[4], differ[4], any = 0;
   if (SR) weight_lanes(p, gi, rnd);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -360,13 +362,22 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     if (SR) {
       const uint32_t n0 = ~rnd[j] & 0xFFFFu, n1 = ~rnd[j] >> 16;
       u[j] = __byte_perm(__float_as_uint(l0) + n0, __float_as_uint(l1) + n1, 0x7632);
-      differ |= u[j] ^ __byte_perm(__float_as_uint(h0) + n0, __float_as_uint(h1) + n1, 0x7632);
+      differ[j] = u[j] ^ __byte_perm(__float_as_uint(h0) + n0, __float_as_uint(h1) + n1, 0x7632);
     } else {
       u[j] = bf16x2_rn(l0, l1);
-      differ |= u[j] ^ bf16x2_rn(h0, h1);
+      differ[j] = u[j] ^ bf16x2_rn(h0, h1);
+    }
+    any |= differ[j];
+  }
+  if (any) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (differ[j] & 0xFFFFu)
+        u[j] = __byte_perm(u[j], slow_weight<SR>(w[2 * j], m[2 * j], r[2 * j], rnd[j] & 0xFFFFu, c.ka, c.c2, c.eps, c.kwd), 0x3254);
+      if (differ[j] >> 16)
+        u[j] = __byte_perm(u[j], slow_weight<SR>(w[2 * j + 1], m[2 * j + 1], r[2 * j + 1], rnd[j] >> 16, c.ka, c.c2, c.eps, c.kwd), 0x5410);
     }
   }
-  if (differ) slow_weights<SR>(c, w, m, r, rnd, u);
   store8_bf16(hw, at, left, vec, u);
   return true;
 }
@@ -480,14 +491,17 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
     }
     const int64_t at = h.at + in;
     const bool vec = h.vec & 1, gvec = h.vec & 2;
+    uint32_t km0 = 127, kr0 = 127;
     float w[8], g[8], m[8], v[8];
     take8<G32>(st + R::kOffG, in, h.staged[1], h.grad, at, left, gvec, g);
     take8<W32>(st + R::kOffW, in, h.staged[0], h.w, at, left, vec, w);
     if (LOW) {
       const uint2 mc = take8_codes(st + R::kOffM, in, h.staged[2], h.m + at, left, vec);
       const uint2 vc = take8_codes(st + R::kOffV, in, h.staged[3], h.v + at, left, vec);
-      decode8(mc, h.scales[0][threadIdx.x >> 4], m);
-      decode8(vc, h.scales[1][threadIdx.x >> 4], v);  // the root
+      decode8(mc, m);
+      decode8(vc, v);
+      km0 = h.scales[0][threadIdx.x >> 4];
+      kr0 = h.scales[1][threadIdx.x >> 4];
     } else {
       take8<true>(st + R::kOffM, in, h.staged[2], h.m, at, left, vec, m);
       take8<true>(st + R::kOffV, in, h.staged[3], h.v, at, left, vec, v);
@@ -499,12 +513,16 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
     if (lane == 0) mbar_arrive(empty(s));
     if (++s == R::kStages) { s = 0; phase ^= 1; }
     if constexpr (LOW && !W32) {
-      if (fast_update<SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, hw, hm, hv, ms, vs)) continue;
+      if (fast_update<SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, km0, kr0, hw, hm, hv, ms, vs)) continue;
     }
     float r[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if (LOW) v[j] = __fmul_rn(v[j], v[j]);
+      if (LOW) {
+        m[j] = __fmul_rn(m[j], scale_value(km0));
+        v[j] = __fmul_rn(v[j], scale_value(kr0));
+        v[j] = __fmul_rn(v[j], v[j]);
+      }
       const float gs = p.grad_scale ? __fmul_rn(g[j], mult) : g[j];
       m[j] = __fadd_rn(__fmul_rn(m[j], c.b1), __fmul_rn(gs, c.omb1));
       v[j] = __fadd_rn(__fmul_rn(v[j], c.b2), __fmul_rn(__fmul_rn(gs, gs), c.omb2));
