@@ -144,15 +144,20 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], int k, const uint3
 // The step.  One CTA per SM walks a run of tiles.  A producer warp brings each
 // tile's arrays into a ring in shared memory by bulk copies (with the tile's
 // place, its pointers and its blocks' scales beside them, whose addresses need
-// not be aligned); 15 consumer warps (with the producer, 16 of 128 registers) update 8 elements a thread and store
+// not be aligned); the consumer warps update 8 elements a thread and store
 // straight to global memory.  Arrays that are off a 16-byte boundary, and ends
 // that do not fill one, are read by the consumers themselves.
 // ---------------------------------------------------------------------------
-constexpr int kStepConsumers = kAdamwTile / 8;
-constexpr int kStepThreads = kStepConsumers + 32;
-constexpr int kStepSmem = 200 * 1024;  // of the ring, at most
+template <bool LOW>
+struct StepShape {
+  static constexpr int kTile = adamw_tile(LOW);
+  static constexpr int kConsumers = kTile / 8;       // 15 warps; with 8-bit moments 11, and two CTAs per SM
+  static constexpr int kThreads = kConsumers + 32;
+  static constexpr int kCtas = LOW ? 2 : 1;          // per SM
+  static constexpr int kSmem = LOW ? 100 * 1024 : 200 * 1024;  // of the ring, at most
+  static_assert(kTile % 256 == 0 && kTile / 128 <= 32, "whole warps; a lane of the producer per block");
+};
 constexpr int kStepMaxStages = 8;
-static_assert(kAdamwTile / 128 <= 32, "a lane of the producer per block");
 
 // What the consumers need to know of a stage's tile.
 struct TileHead {
@@ -171,9 +176,10 @@ template <bool W32, bool G32, bool LOW>
 struct StepRing {
   static constexpr int kW = W32 ? 4 : 2, kG = G32 ? 4 : 2, kS = LOW ? 1 : 4;
   static constexpr int kOffW = (sizeof(TileHead) + 127) / 128 * 128;
-  static constexpr int kOffG = kOffW + kAdamwTile * kW, kOffM = kOffG + kAdamwTile * kG, kOffV = kOffM + kAdamwTile * kS;
-  static constexpr int kBytes = kOffV + kAdamwTile * kS;
-  static constexpr int kFit = kStepSmem / kBytes;
+  static constexpr int kTile = StepShape<LOW>::kTile;
+  static constexpr int kOffG = kOffW + kTile * kW, kOffM = kOffG + kTile * kG, kOffV = kOffM + kTile * kS;
+  static constexpr int kBytes = kOffV + kTile * kS;
+  static constexpr int kFit = StepShape<LOW>::kSmem / kBytes;
   static constexpr int kStages = kFit < kStepMaxStages ? kFit : kStepMaxStages;
   static_assert(kStages >= 3, "a ring of at least three tiles");
 };
@@ -269,14 +275,17 @@ __device__ __noinline__ uint32_t slow_weight(float w, float m, float r, uint32_t
 // ---------------------------------------------------------------------------
 template <bool SR, bool STATE_SR>
 __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t at, int64_t left, bool vec,
-                                            const float (&w)[8], const float (&g)[8], const float (&m0)[8], const float (&r0)[8], uint32_t km0, uint32_t kr0,
-                                            uint8_t* hw, uint8_t* hm, uint8_t* hv, uint8_t* ms, uint8_t* vs) {
+                                            const float (&w)[8], const float (&g)[8], const float (&m0)[8],
+                                            const float (&r0)[8], uint32_t km0, uint32_t kr0, const TileHead& h,
+                                            uint32_t stage_w, int in) {
   const AdamwScalars& c = p.s;
   float m[8], r[8];
-  f32x2 wn[4], ne[4], fin = 0;
+  f32x2 fin = 0;
   const float sm = scale_value(km0), sr = scale_value(kr0);
   const f32x2 b1 = both(__fmul_rn(c.b1, sm)), b2 = both(__fmul_rn(c.b2, __fmul_rn(sr, sr)));
   const f32x2 nz = p.minus_zero, mult2 = both(mult), nkwd = both(-c.kwd), nka = both(-c.ka);
+  uint32_t rnd[4] = {}, u[4], differ = 0;
+  if (SR) weight_lanes(p, gi, rnd);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     f32x2 gg = pk(g[2 * j], g[2 * j + 1]);
@@ -287,18 +296,41 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     const f32x2 rr = root2(vv);
     unpk(mm, m[2 * j], m[2 * j + 1]);
     unpk(rr, r[2 * j], r[2 * j + 1]);
-    float d0, d1, q0, q1, w0, w1;
+    float d0, d1, q0, q1, w0, w1, l0, l1, h0, h1;
     unpk(add2_rn(prod2(rr, both(c.c2), nz), both(c.eps)), d0, d1);
     const f32x2 q = prod2(mul2_rn(mm, nka), pk(rcp_approx_ftz(d0), rcp_approx_ftz(d1)), nz);
     f32x2 base = pk(w[2 * j], w[2 * j + 1]);
     if (c.kwd != 0.0f) base = add2_rn(base, prod2(base, nkwd, nz));
-    wn[j] = add2_rn(base, q);
-    fin = fma2_rn(wn[j], 0ull, fin);
+    const f32x2 wn = add2_rn(base, q);
+    fin = fma2_rn(wn, 0ull, fin);
     unpk(q, q0, q1);
-    unpk(wn[j], w0, w1);
-    ne[j] = fma2_rn(pk(__fadd_rn(fabsf(q0), fabsf(w0)), __fadd_rn(fabsf(q1), fabsf(w1))), both(-0x1.1p-22f), both(-0x1p-96f));
+    unpk(wn, w0, w1);
+    const f32x2 ne = fma2_rn(pk(__fadd_rn(fabsf(q0), fabsf(w0)), __fadd_rn(fabsf(q1), fabsf(w1))), both(-0x1.1p-22f),
+                             both(-0x1p-96f));
+    unpk(add2_rd(wn, ne), l0, l1);
+    f32x2 up;
+    asm("fma.rp.f32x2 %0, %1, %2, %3;" : "=l"(up) : "l"(ne), "l"(both(-1.0f)), "l"(wn));
+    unpk(up, h0, h1);
+    if (SR) {
+      const uint32_t n0 = ~rnd[j] & 0xFFFFu, n1 = ~rnd[j] >> 16;
+      u[j] = __byte_perm(__float_as_uint(l0) + n0, __float_as_uint(l1) + n1, 0x7632);
+      differ |= u[j] ^ __byte_perm(__float_as_uint(h0) + n0, __float_as_uint(h1) + n1, 0x7632);
+    } else {
+      u[j] = bf16x2_rn(l0, l1);
+      differ |= u[j] ^ bf16x2_rn(h0, h1);
+    }
   }
   if (__any_sync(~0u, cert_not_finite(fin) || min(km0, kr0) < 80u || max(km0, kr0) > 150u)) return false;
+  if (differ) {
+    float x[8];
+    take8<false>(stage_w, in, h.staged[0], h.w, at, left, vec, x);
+    if (SR) weight_lanes(p, gi, rnd);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      u[j] = __byte_perm(slow_weight<SR>(x[2 * j], m[2 * j], r[2 * j], rnd[j] & 0xFFFFu, c.ka, c.c2, c.eps, c.kwd),
+                         slow_weight<SR>(x[2 * j + 1], m[2 * j + 1], r[2 * j + 1], rnd[j] >> 16, c.ka, c.c2, c.eps, c.kwd), 0x5410);
+  }
+  store8_bf16(h.w, at, left, vec, u);
 
   uint32_t lanes[8] = {};
   if (STATE_SR) state_lanes(p, gi, lanes);
@@ -343,48 +375,20 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
       b[j] = e4m3x2(z0, z1);
     }
   }
-  store8_codes(hm + at, left, vec, make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)));
-  store8_codes(hv + at, left, vec, make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410)));
+  store8_codes(h.m + at, left, vec, make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)));
+  store8_codes(h.v + at, left, vec, make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410)));
   if ((threadIdx.x & 15) == 0 && left > 0) {
-    ms[at / 128] = (uint8_t)(km + 127);
-    vs[at / 128] = (uint8_t)(kr + 127);
+    h.m_scale[at / 128] = (uint8_t)(km + 127);
+    h.v_scale[at / 128] = (uint8_t)(kr + 127);
   }
-
-  uint32_t rnd[4] = {}, u[4], differ[4], any = 0;
-  if (SR) weight_lanes(p, gi, rnd);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    float l0, l1, h0, h1;
-    unpk(add2_rd(wn[j], ne[j]), l0, l1);
-    f32x2 hi;
-    asm("fma.rp.f32x2 %0, %1, %2, %3;" : "=l"(hi) : "l"(ne[j]), "l"(both(-1.0f)), "l"(wn[j]));
-    unpk(hi, h0, h1);
-    if (SR) {
-      const uint32_t n0 = ~rnd[j] & 0xFFFFu, n1 = ~rnd[j] >> 16;
-      u[j] = __byte_perm(__float_as_uint(l0) + n0, __float_as_uint(l1) + n1, 0x7632);
-      differ[j] = u[j] ^ __byte_perm(__float_as_uint(h0) + n0, __float_as_uint(h1) + n1, 0x7632);
-    } else {
-      u[j] = bf16x2_rn(l0, l1);
-      differ[j] = u[j] ^ bf16x2_rn(h0, h1);
-    }
-    any |= differ[j];
-  }
-  if (any) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (differ[j] & 0xFFFFu)
-        u[j] = __byte_perm(u[j], slow_weight<SR>(w[2 * j], m[2 * j], r[2 * j], rnd[j] & 0xFFFFu, c.ka, c.c2, c.eps, c.kwd), 0x3254);
-      if (differ[j] >> 16)
-        u[j] = __byte_perm(u[j], slow_weight<SR>(w[2 * j + 1], m[2 * j + 1], r[2 * j + 1], rnd[j] >> 16, c.ka, c.c2, c.eps, c.kwd), 0x5410);
-    }
-  }
-  store8_bf16(hw, at, left, vec, u);
   return true;
 }
 
 template <bool W32, bool G32, bool LOW, bool SR, bool STATE_SR>
-__global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_constant__ AdamwArgs p) {
+__global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCtas)
+    adamw_kernel(const __grid_constant__ AdamwArgs p) {
   using R = StepRing<W32, G32, LOW>;
+  constexpr int kTile = StepShape<LOW>::kTile, kConsumers = StepShape<LOW>::kConsumers;
   extern __shared__ uint8_t smem_raw[];
   __shared__ alignas(8) uint64_t bars[2 * R::kStages];
   const uint32_t smem = (smem_addr(smem_raw) + 127u) & ~127u;
@@ -395,7 +399,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
   if (threadIdx.x == 0) {
     for (int s = 0; s < R::kStages; ++s) {
       mbar_init(full(s), 1);
-      mbar_init(empty(s), kStepConsumers / 32);
+      mbar_init(empty(s), kConsumers / 32);
     }
     mbar_init_fence();
   }
@@ -408,7 +412,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
   const int64_t t0 = p.tiles * blockIdx.x / gridDim.x, t1 = p.tiles * (blockIdx.x + 1) / gridDim.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  if (warp == kStepConsumers / 32) {
+  if (warp == kConsumers / 32) {
     int k = p.tile_tensor[t0];
     ListTensor d = p.tensors[k];
     const uint8_t* grad = static_cast<const uint8_t*>(grad_of(p.g, k));
@@ -417,15 +421,15 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
     uint32_t phase = 0;
     bool ok = true;
     for (int64_t t = t0; t < t1; ++t) {
-      const int64_t at0 = (t - d.tile0) * kAdamwTile;
+      const int64_t at0 = (t - d.tile0) * kTile;
       if (at0 >= d.numel) {  // the next tensor that has elements
         k = p.tile_tensor[t];
         d = p.tensors[k];
         grad = static_cast<const uint8_t*>(grad_of(p.g, k));
       }
-      const int64_t at = (t - d.tile0) * kAdamwTile, left = d.numel - at;
+      const int64_t at = (t - d.tile0) * kTile, left = d.numel - at;
       uint32_t ms = 127, vs = 127;
-      if (LOW && lane < kAdamwTile / 128 && lane * 128 < left) {
+      if (LOW && lane < kTile / 128 && lane * 128 < left) {
         ms = d.m_scale[at / 128 + lane];
         vs = d.v_scale[at / 128 + lane];
       }
@@ -436,7 +440,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
         h.scales[1][lane] = (uint8_t)vs;
       }
       if (lane == 0) {
-        const int n = (int)min((int64_t)kAdamwTile, left);
+        const int n = (int)min((int64_t)kTile, left);
         auto whole = [&](const void* q, int size) { return (reinterpret_cast<uintptr_t>(q) & 15) ? 0 : n * size / 16 * 16; };
         const uint8_t *w = static_cast<uint8_t*>(d.w) + at * R::kW, *g = grad + at * R::kG,
                       *m = static_cast<uint8_t*>(d.m) + at * R::kS, *v = static_cast<uint8_t*>(d.v) + at * R::kS;
@@ -493,28 +497,37 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
     const bool vec = h.vec & 1, gvec = h.vec & 2;
     uint32_t km0 = 127, kr0 = 127;
     float w[8], g[8], m[8], v[8];
-    take8<G32>(st + R::kOffG, in, h.staged[1], h.grad, at, left, gvec, g);
-    take8<W32>(st + R::kOffW, in, h.staged[0], h.w, at, left, vec, w);
-    if (LOW) {
-      const uint2 mc = take8_codes(st + R::kOffM, in, h.staged[2], h.m + at, left, vec);
-      const uint2 vc = take8_codes(st + R::kOffV, in, h.staged[3], h.v + at, left, vec);
-      decode8(mc, m);
-      decode8(vc, v);
-      km0 = h.scales[0][threadIdx.x >> 4];
-      kr0 = h.scales[1][threadIdx.x >> 4];
-    } else {
-      take8<true>(st + R::kOffM, in, h.staged[2], h.m, at, left, vec, m);
-      take8<true>(st + R::kOffV, in, h.staged[3], h.v, at, left, vec, v);
+    auto take_all = [&] {
+      take8<G32>(st + R::kOffG, in, h.staged[1], h.grad, at, left, gvec, g);
+      take8<W32>(st + R::kOffW, in, h.staged[0], h.w, at, left, vec, w);
+      if (LOW) {
+        decode8(take8_codes(st + R::kOffM, in, h.staged[2], h.m + at, left, vec), m);
+        decode8(take8_codes(st + R::kOffV, in, h.staged[3], h.v + at, left, vec), v);
+        km0 = h.scales[0][threadIdx.x >> 4];
+        kr0 = h.scales[1][threadIdx.x >> 4];
+      } else {
+        take8<true>(st + R::kOffM, in, h.staged[2], h.m, at, left, vec, m);
+        take8<true>(st + R::kOffV, in, h.staged[3], h.v, at, left, vec, v);
+      }
+    };
+    take_all();
+    const int64_t gi = h.goff + at;
+    // With 8-bit moments the stage is kept to the end: what is needed again is read from it again, not kept in registers.
+    auto release = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(s));
+      if (++s == R::kStages) { s = 0; phase ^= 1; }
+    };
+    if constexpr (LOW && !W32) {
+      if (fast_update<SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, km0, kr0, h, st + R::kOffW, in)) {
+        release();
+        continue;
+      }
+      take_all();
     }
     uint8_t *const hw = h.w, *const hm = h.m, *const hv = h.v, *const ms = h.m_scale, *const vs = h.v_scale;
     uint16_t* const compute = h.compute;
-    const int64_t gi = h.goff + at;
-    __syncwarp();
-    if (lane == 0) mbar_arrive(empty(s));
-    if (++s == R::kStages) { s = 0; phase ^= 1; }
-    if constexpr (LOW && !W32) {
-      if (fast_update<SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, km0, kr0, hw, hm, hv, ms, vs)) continue;
-    }
+    if constexpr (!LOW) release();
     float r[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -558,6 +571,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) adamw_kernel(const __grid_con
       if (!W32) store8_bf16(hw, at, left, vec, u);
       else store8_bf16(compute, at, left, vec, u);
     }
+    if constexpr (LOW) release();
   }
 }
 
@@ -677,7 +691,7 @@ __global__ void fill_kernel(const __grid_constant__ FillArgs a) {
 
 struct StepKernel {
   const void* f;
-  int smem;
+  int smem, threads, ctas;
 };
 template <bool W32, bool G32, bool LOW>
 StepKernel pick(bool sr, bool state_sr) {
@@ -686,7 +700,7 @@ StepKernel pick(bool sr, bool state_sr) {
   using R = StepRing<W32, G32, LOW>;
   const void* f = sr ? (state_sr ? (const void*)adamw_kernel<W32, G32, LOW, !W32, LOW> : (const void*)adamw_kernel<W32, G32, LOW, !W32, false>)
                      : (state_sr ? (const void*)adamw_kernel<W32, G32, LOW, false, LOW> : (const void*)adamw_kernel<W32, G32, LOW, false, false>);
-  return {f, R::kStages * R::kBytes + 128};
+  return {f, R::kStages * R::kBytes + 128, StepShape<LOW>::kThreads, StepShape<LOW>::kCtas};
 }
 template <bool W32, bool G32>
 StepKernel pick(const AdamwKind& k) {
@@ -710,8 +724,9 @@ cudaError_t prepare_adamw(const AdamwKind& k, int32_t* sms) {
 cudaError_t launch_adamw(const AdamwArgs& a, const AdamwKind& k, int32_t sms, cudaStream_t stream) {
   const StepKernel kernel = pick(k);
   void* params[] = {const_cast<AdamwArgs*>(&a)};
-  const unsigned grid = (unsigned)(a.tiles < sms ? a.tiles : sms);
-  return cudaLaunchKernel(kernel.f, dim3(grid), dim3(kStepThreads), params, (size_t)kernel.smem, stream);
+  const int64_t most = (int64_t)sms * kernel.ctas;
+  const unsigned grid = (unsigned)(a.tiles < most ? a.tiles : most);
+  return cudaLaunchKernel(kernel.f, dim3(grid), dim3(kernel.threads), params, (size_t)kernel.smem, stream);
 }
 
 cudaError_t launch_grad_norm(const NormArgs& a, cudaStream_t stream) {

@@ -11,8 +11,8 @@
 namespace mpadam {
 
 // Elements per tile; a tensor's last tile may be short.  A CTA takes a tile of a
-// step, a warp one of the norm.
-constexpr int kAdamwTile = 3840;
+// step (of this size by the moments' type), a warp one of the norm.
+constexpr int adamw_tile(bool state_e4m3) { return state_e4m3 ? 2816 : 3840; }
 constexpr int kNormTile = 2048;
 constexpr int kInlineGrads = 448;    // gradient pointers that travel with one launch
 

@@ -170,7 +170,7 @@ extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32
     std::unique_ptr<mpadam_adamw_state> s(new mpadam_adamw_state());
     s->cfg = c;
     s->list.grad_size = c.grad_dtype == MPADAM_F32 ? 4 : 2;
-    const int32_t rc = s->list.build(list, kAdamwTile);
+    const int32_t rc = s->list.build(list, adamw_tile(c.state_dtype == MPADAM_E4M3));
     if (rc) return rc;
     s->kind = {c.weight_dtype == MPADAM_F32, c.grad_dtype == MPADAM_F32, c.state_dtype == MPADAM_E4M3,
                c.rounding == MPADAM_ROUND_STOCHASTIC, c.state_rounding == MPADAM_ROUND_STOCHASTIC};
