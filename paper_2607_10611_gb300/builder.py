@@ -29,7 +29,7 @@ EXT_TORCH = OUT_DIR / "torch_version"  # the torch that EXT was built for
 
 SOURCES = ["mpadam_api.cu", "step_bf16.cu", "step_e4m3.cu", "step_e4m3b.cu", "step_nvfp4.cu", "toy.cu",
            "train_api.cu", "adamw.cu", "fp8_quant.cu", "fp8_matmul.cu"]
-HEADERS = ["step_args.h", "step_kernel.cuh", "toy.h", "host.h", "adamw.h", "adamw_math.cuh", "fp8.h"]
+HEADERS = ["step_args.h", "step_kernel.cuh", "toy.h", "host.h", "adamw.h", "adamw_math.cuh", "fp8.h", "launch.h"]
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + [

@@ -9,10 +9,13 @@
 // range, and the update needs it anyway.
 #include "adamw.h"
 #include "adamw_math.cuh"
+#include "launch.h"
 
 namespace mpadam {
 
 namespace {
+
+__device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ const void* grad_of(const GradTable& g, int k) { return g.grads ? g.grads[k] : g.inline_grads[k]; }
 
@@ -404,6 +407,7 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
     mbar_init_fence();
   }
   __syncthreads();
+  wait_for_earlier_kernels();
   float mult = 1.0f;
   if (p.grad_scale) {
     mult = *p.grad_scale;
@@ -588,6 +592,7 @@ template <bool G32>
 __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_constant__ NormArgs p) {
   __shared__ double part[kNormWarps];
   __shared__ bool last;
+  wait_for_earlier_kernels();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t walker = (int64_t)blockIdx.x * kNormWarps + warp, walkers = (int64_t)gridDim.x * kNormWarps;
   const int64_t t0 = p.tiles * walker / walkers, t1 = p.tiles * (walker + 1) / walkers;
@@ -723,18 +728,16 @@ cudaError_t prepare_adamw(const AdamwKind& k, int32_t* sms) {
 
 cudaError_t launch_adamw(const AdamwArgs& a, const AdamwKind& k, int32_t sms, cudaStream_t stream) {
   const StepKernel kernel = pick(k);
-  void* params[] = {const_cast<AdamwArgs*>(&a)};
   const int64_t most = (int64_t)sms * kernel.ctas;
   const unsigned grid = (unsigned)(a.tiles < most ? a.tiles : most);
-  return cudaLaunchKernel(kernel.f, dim3(grid), dim3(kernel.threads), params, (size_t)kernel.smem, stream);
+  return launch_dependent(kernel.f, grid, (unsigned)kernel.threads, 0, kernel.smem, &a, stream);
 }
 
 cudaError_t launch_grad_norm(const NormArgs& a, cudaStream_t stream) {
   const int64_t wanted = (a.tiles + kNormWarps - 1) / kNormWarps;
   const unsigned grid = (unsigned)(wanted < 1 ? 1 : wanted < kNormCtas ? wanted : kNormCtas);
-  if (a.g_f32) grad_norm_kernel<true><<<grid, kNormThreads, 0, stream>>>(a);
-  else grad_norm_kernel<false><<<grid, kNormThreads, 0, stream>>>(a);
-  return cudaGetLastError();
+  return launch_dependent(a.g_f32 ? (const void*)grad_norm_kernel<true> : (const void*)grad_norm_kernel<false>, grid, kNormThreads,
+                          0, 0, &a, stream);
 }
 
 cudaError_t fill_grads(const void** table, const void* const* grads, int32_t first, int32_t count, cudaStream_t stream) {

@@ -44,12 +44,14 @@ struct MatmulArgs {
   int64_t ldd;
   int32_t m, n, k;
   int32_t f32, accumulate;
+  int32_t split;
   int32_t* err;                // device error word
 };
 
 // How a product of this shape is cut up, and its launch.
 struct MatmulPlan {
   int tile;    // rows of a per tile
+  int split;   // CTAs that share a tile's k
   bool pair;   // tiles of 256 x 256 by pairs of CTAs, which need the scales' maps
   int box() const { return pair ? tile / 2 : tile; }  // rows of a's boxes
 };

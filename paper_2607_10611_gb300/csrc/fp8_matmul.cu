@@ -14,6 +14,7 @@
 #include <atomic>
 
 #include "fp8.h"
+#include "launch.h"
 #include "step_kernel.cuh"
 
 namespace mpadam {
@@ -34,14 +35,14 @@ template <int TM>
 struct Shape {
   static constexpr int kScaleTilesA = (TM + 127) / 128;
   static constexpr int kScaleBytes = kScaleTile * (1 + kScaleTilesA);
-  static constexpr int kStageBytes = (kTileN + TM) * kTileK + 2048;  // codes, then scales; keeps 1024-byte alignment
-  static constexpr int kStages = TM >= 256 ? 4 : TM >= 128 ? 6 : 8;
-  static constexpr int kAccs = TM >= 256 ? 1 : 2;
-  // Tensor memory: accumulators, then two sets of scales (4 columns for b, 4 per 128 rows for a).
+  static constexpr int kStageBytes = (kTileN + TM) * kTileK + 1024;  // codes, then scales; keeps 1024-byte alignment
+  static constexpr int kStages = TM >= 128 ? 3 : TM >= 64 ? 4 : 5;   // two CTAs an SM
+  // Tensor memory: the accumulator, then two sets of scales (4 columns for b, 4 for a).
   static constexpr int kScaleCols = 4 + 4 * kScaleTilesA;
-  static constexpr int kUsedCols = kAccs * TM + 2 * kScaleCols;
-  static constexpr int kCols = kUsedCols <= 64 ? 64 : kUsedCols <= 128 ? 128 : kUsedCols <= 256 ? 256 : 512;
+  static constexpr int kUsedCols = TM + 2 * kScaleCols;
+  static constexpr int kCols = kUsedCols <= 32 ? 32 : kUsedCols <= 64 ? 64 : kUsedCols <= 128 ? 128 : 256;
   static constexpr int kDynSmem = kStages * kStageBytes + 1024;
+  static_assert(kScaleBytes <= 1024 && TM * kTileN * 4 <= kStages * kStageBytes, "scales and partial sums fit");
 };
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -101,6 +102,23 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
 }
 __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// The address of `addr` in the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+// What earlier kernels of the stream wrote may be used from here on: launches may begin before those have ended.
+__device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Instruction descriptor: E4M3 operands, E8M0 scales, m = 128 lanes, n = TM columns; the scales' byte of the two
 // operands' 32-bit columns.
 template <int TM>
@@ -108,11 +126,37 @@ __device__ __forceinline__ uint32_t instr_desc(uint32_t byte) {
   return (uint32_t)(TM >> 3) << 17 | 1u << 23 | (uint32_t)(kTileN >> 4) << 24 | byte << 4 | byte << 29;
 }
 
+// ---------------------------------------------------------------------------
+// Tiles of 128 x TM, one CTA each, or, where tiles alone leave SMs idle, the 1,
+// 2, 4 or 8 CTAs of a cluster: each takes a run of k, writes its sums to its
+// shared memory and adds up all CTAs' for its share of the tile's lanes, in the
+// CTAs' order, so that the same product gives the same bits.  Two CTAs fit an
+// SM: one's first copies and last stores run under the other's products.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float4 lds_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+// Sums of all CTAs of a cluster over four neighbouring lanes, in the CTAs' order; all loads in flight at once.
+template <int SPLIT>
+__device__ __forceinline__ float4 cluster_sum(uint32_t addr) {
+  float4 v[SPLIT];
+#pragma unroll
+  for (int s = 0; s < SPLIT; ++s) v[s] = lds_cluster(peer_addr(addr, s));
+#pragma unroll
+  for (int s = 1; s < SPLIT; ++s) {
+    v[0].x = __fadd_rn(v[0].x, v[s].x), v[0].y = __fadd_rn(v[0].y, v[s].y);
+    v[0].z = __fadd_rn(v[0].z, v[s].z), v[0].w = __fadd_rn(v[0].w, v[s].w);
+  }
+  return v[0];
+}
+
 template <int TM, bool F32>
-__global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_constant__ MatmulArgs p) {
+__global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_constant__ MatmulArgs p) {
   using S = Shape<TM>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ alignas(8) uint64_t bars[2 * S::kStages + 2 * S::kAccs + 1];
+  __shared__ alignas(8) uint64_t bars[2 * S::kStages + 1];
   __shared__ uint32_t tmem_base_s;
   __shared__ int32_t failed;
   const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -120,20 +164,14 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   const uint32_t bar0 = smem_addr(bars);
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (S::kStages + s); };
-  auto acc_full = [&](int s) { return bar0 + 8u * (2 * S::kStages + s); };
-  auto acc_free = [&](int s) { return bar0 + 8u * (2 * S::kStages + S::kAccs + s); };
-  const uint32_t drained = bar0 + 8u * (2 * S::kStages + 2 * S::kAccs);
+  const uint32_t acc_full = bar0 + 8u * (2 * S::kStages);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    for (int s = 0; s < S::kAccs; ++s) {
-      mbar_init(acc_full(s), 1);
-      mbar_init(acc_free(s), kEpiWarps);
-    }
-    mbar_init(drained, 1);
+    mbar_init(acc_full, 1);
     failed = 0;
     mbar_init_fence();
   }
@@ -147,48 +185,40 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
-  const uint32_t tmem_scales = tmem + S::kAccs * TM;
+  const uint32_t tmem_scales = tmem + TM;
+  wait_for_earlier_kernels();
 
-  const int tiles_n = (p.n + kTileN - 1) / kTileN, tiles_m = (p.m + TM - 1) / TM;
-  const int tiles = tiles_n * tiles_m;
-  const int steps = (p.k + kTileK - 1) / kTileK;
-  const int groups = (steps + 3) / 4;
-  const int last_scale_a = (p.m - 1) / 128;
+  const int tiles_m = (p.m + TM - 1) / TM;
+  const int tile = blockIdx.x / p.split, rank = blockIdx.x % p.split;
+  const int tn = tile / tiles_m, tm = tile % tiles_m;
+  const int steps_all = (p.k + kTileK - 1) / kTileK, groups = (steps_all + 3) / 4;
+  const int k0 = 4 * (int)((int64_t)groups * rank / p.split), k1 = min(steps_all, 4 * (int)((int64_t)groups * (rank + 1) / p.split));
   volatile int32_t* stop = &failed;
 
   if (warp == 0) {
     if (lane == 0) {
       int s = 0;
       uint32_t phase = 0;
-      bool ok = true;
-      int issued = 0;
-      for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-        if (*stop) { ok = false; break; }
-        const int tn = t / tiles_m, tm = t % tiles_m;
-        for (int k = 0; k < steps; ++k) {
-          if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
-          const uint32_t st = smem + s * S::kStageBytes;
-          const bool scales = (k & 3) == 0;
-          mbar_arrive_tx(full(s), (kTileN + TM) * kTileK + (scales ? S::kScaleBytes : 0));
-          tma_load_2d(st, &p.b, k * kTileK, tn * kTileN, full(s));
-          tma_load_2d(st + kTileN * kTileK, &p.a, k * kTileK, tm * TM, full(s));
-          if (scales) {
-            const uint32_t sc = st + (kTileN + TM) * kTileK;
-            bulk_load(sc, p.sb + ((int64_t)tn * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
-            for (int j = 0; j < S::kScaleTilesA; ++j) {
-              const int r = min(tm * TM / 128 + j, last_scale_a);
-              bulk_load(sc + kScaleTile * (1 + j), p.sa + ((int64_t)r * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
-            }
-          }
-          ++issued;
-          if (++s == S::kStages) { s = 0; phase ^= 1; }
+      int k = k0;
+      for (; k < k1; ++k) {
+        if (!mbar_wait(empty(s), phase ^ 1)) break;
+        const uint32_t st = smem + s * S::kStageBytes;
+        const bool scales = (k & 3) == 0;
+        mbar_arrive_tx(full(s), (kTileN + TM) * kTileK + (scales ? S::kScaleBytes : 0));
+        tma_load_2d(st, &p.b, k * kTileK, tn * kTileN, full(s));
+        tma_load_2d(st + kTileN * kTileK, &p.a, k * kTileK, tm * TM, full(s));
+        if (scales) {
+          const uint32_t sc = st + (kTileN + TM) * kTileK;
+          bulk_load(sc, p.sb + ((int64_t)tn * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
+          bulk_load(sc + kScaleTile, p.sa + ((int64_t)(tm * TM / 128) * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
         }
+        if (++s == S::kStages) { s = 0; phase ^= 1; }
       }
-      if (!ok) {
+      if (k < k1) {
         *stop = 1;
         atomicOr(p.err, kErrStage);
         // the copies in flight, those of the last stages, before the block's memory goes
-        for (int i = 0; i < min(issued, S::kStages); ++i) {
+        for (int i = 0; i < min(k - k0, S::kStages); ++i) {
           if (s == 0) { s = S::kStages; phase ^= 1; }
           --s;
           mbar_wait(full(s), phase);
@@ -200,103 +230,85 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
     // that gave up it goes on without waiting; what it then computes is not used.
     const bool issue = elected();
     const uint32_t low0 = desc_low(smem);
-    int s = 0, acc = 0;
-    uint32_t phase = 0, acc_phase = 0;
+    // A tile of fewer than 128 rows of a starts inside its scale tile, at a multiple of 32 rows (16 only where it is the
+    // first): a column of scales holds 32 rows.
+    const int col = TM < 128 ? (tm * TM % 128) / 32 : 0;
+    int s = 0;
+    uint32_t phase = 0;
     bool ok = true;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-      if (ok) ok = mbar_wait(acc_free(acc), acc_phase ^ 1);
-      tc_fence_after();
-      const uint32_t d = tmem + acc * TM;
-      // A tile of fewer than 128 rows of a starts inside its scale tile, at a multiple of 32 rows (16 only where it is the
-      // first): a column of scales holds 32 rows.
-      const int col = TM < 128 ? (t % tiles_m * TM % 128) / 32 : 0;
-      for (int g = 0; g < groups; ++g) {
-        const uint32_t sb = tmem_scales + (g & 1) * S::kScaleCols, sa = sb + 4;
+    for (int kg = k0; kg < k1; kg += 4) {
+      const uint32_t sb = tmem_scales + ((kg >> 2) & 1) * S::kScaleCols, sa = sb + 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int k = 4 * g + j;
-          if (k >= steps) break;
-          if (ok) ok = mbar_wait(full(s), phase);
-          tc_fence_after();
-          if (issue) {
-            const uint32_t low = low0 + s * (S::kStageBytes >> 4);
-            if (j == 0) {
-              const uint32_t sc = low + ((kTileN + TM) * kTileK >> 4);
-              copy_scales(sb, desc(sc, kScaleHigh));
-#pragma unroll
-              for (int i = 0; i < S::kScaleTilesA; ++i) copy_scales(sa + 4 * i, desc(sc + (i + 1) * (kScaleTile >> 4), kScaleHigh));
-            }
-#pragma unroll
-            for (int i = 0; i < kTileK / 32; ++i)
-              mma_scaled(d, desc(low + 2 * i, kOperandHigh), desc(low + (kTileN * kTileK >> 4) + 2 * i, kOperandHigh),
-                         instr_desc<TM>(j), sb, sa + col, j > 0 || i > 0 || g > 0);
-            mma_commit(empty(s));
+      for (int j = 0; j < 4; ++j) {
+        if (kg + j >= k1) break;
+        if (ok) ok = mbar_wait(full(s), phase);
+        tc_fence_after();
+        if (issue) {
+          const uint32_t low = low0 + s * (S::kStageBytes >> 4);
+          if (j == 0) {
+            const uint32_t sc = low + ((kTileN + TM) * kTileK >> 4);
+            copy_scales(sb, desc(sc, kScaleHigh));
+            copy_scales(sa, desc(sc + (kScaleTile >> 4), kScaleHigh));
           }
-          if (++s == S::kStages) { s = 0; phase ^= 1; }
+#pragma unroll
+          for (int i = 0; i < kTileK / 32; ++i)
+            mma_scaled(tmem, desc(low + 2 * i, kOperandHigh), desc(low + (kTileN * kTileK >> 4) + 2 * i, kOperandHigh),
+                       instr_desc<TM>(j), sb, sa + col, j > 0 || i > 0 || kg > k0);
+          mma_commit(empty(s));
         }
+        if (++s == S::kStages) { s = 0; phase ^= 1; }
       }
-      if (issue) mma_commit(acc_full(acc));
-      if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
     }
-    if (!ok) {  // the products in flight, before their memory goes
+    if (issue) {
+      mma_commit(acc_full);
+      if (!ok) atomicOr(p.err, kErrCopy);
+    }
+    if (!ok) {
       *stop = 1;
-      if (issue) {
-        atomicOr(p.err, kErrCopy);
-        mma_commit(drained);
-      }
-      mbar_wait(drained, 0);
+      mbar_wait(acc_full, 0);  // the products in flight, before their memory goes
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2;
     constexpr int kHalf = TM / 2 >= 16 ? TM / 2 : 16;  // columns of one warp
-    const bool mine = half * kHalf < TM;
-    int acc = 0;
-    uint32_t acc_phase = 0;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-      if (*stop || !mbar_wait(acc_full(acc), acc_phase)) {
-        if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
-        break;
-      }
+    if (!mbar_wait(acc_full, 0)) {
+      if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
+    } else if (half * kHalf < TM) {
       __syncwarp();
       tc_fence_after();
-      const int tn = t / tiles_m, tm = t % tiles_m;
       const int n = tn * kTileN + quarter * 32 + lane;
-      if (mine) {
-        for (int c = half * kHalf; c < half * kHalf + kHalf; c += 16) {
-          const int m0 = tm * TM + c;
-          if (m0 >= p.m) break;
-          uint32_t r[16];
-          __syncwarp();
-          tmem_load16(tmem + acc * TM + c + ((uint32_t)(quarter * 32) << 16), r);
-          tmem_wait_load();
-          if (n < p.n) {
-            const int rows = min(16, p.m - m0);
-            const int64_t at = (int64_t)m0 * p.ldd + n;
-            if (F32) {
-              float* d = static_cast<float*>(p.d) + at;
-              if (p.accumulate) {
-                float old[16];
+      for (int c = half * kHalf; c < half * kHalf + kHalf; c += 16) {
+        const int m0 = tm * TM + c;
+        if (m0 >= p.m) break;
+        uint32_t r[16];
+        __syncwarp();
+        tmem_load16(tmem + c + ((uint32_t)(quarter * 32) << 16), r);
+        tmem_wait_load();
+        const int rows = min(16, p.m - m0);
+        if (p.split > 1) {  // the stages' memory is free: every copy has been used
 #pragma unroll
-                for (int j = 0; j < 16; ++j) old[j] = j < rows ? d[j * p.ldd] : 0.0f;
+          for (int j = 0; j < 16; ++j) sts_u32(smem + ((c + j) * kTileN + quarter * 32 + lane) * 4, r[j]);
+        } else if (n < p.n) {
+          const int64_t at = (int64_t)m0 * p.ldd + n;
+          if (F32) {
+            float* d = static_cast<float*>(p.d) + at;
+            if (p.accumulate) {
+              float old[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__fadd_rn(old[j], __uint_as_float(r[j])));
-              }
+              for (int j = 0; j < 16; ++j) old[j] = j < rows ? d[j * p.ldd] : 0.0f;
 #pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (j < rows) d[j * p.ldd] = __uint_as_float(r[j]);
-            } else {
-              uint16_t* d = static_cast<uint16_t*>(p.d) + at;
-#pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (j < rows) d[j * p.ldd] = (uint16_t)bf16x2_rn(__uint_as_float(r[j]), 0.0f);
+              for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__fadd_rn(old[j], __uint_as_float(r[j])));
             }
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (j < rows) d[j * p.ldd] = __uint_as_float(r[j]);
+          } else {
+            uint16_t* d = static_cast<uint16_t*>(p.d) + at;
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (j < rows) d[j * p.ldd] = (uint16_t)bf16x2_rn(__uint_as_float(r[j]), 0.0f);
           }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(acc_free(acc));
-      if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
     }
   }
   __syncwarp();
@@ -305,6 +317,29 @@ __global__ void __launch_bounds__(kMatmulThreads, 1) matmul_kernel(const __grid_
   tc_fence_after();
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::kCols) : "memory");
+  if (p.split > 1) {
+    cluster_sync();
+    const int width = kTileN / p.split, rows = min(TM, p.m - tm * TM);
+#pragma unroll 2
+    for (int e = threadIdx.x; e < rows * width / 4; e += kMatmulThreads) {
+      const int j = 4 * e / width, l = rank * width + 4 * e % width, n = tn * kTileN + l;
+      const uint32_t at = smem + (j * kTileN + l) * 4;
+      const float4 v = p.split == 2 ? cluster_sum<2>(at) : p.split == 4 ? cluster_sum<4>(at) : cluster_sum<8>(at);
+      const float x[4] = {v.x, v.y, v.z, v.w};
+      const int64_t to = (int64_t)(tm * TM + j) * p.ldd + n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (n + i >= p.n) break;
+        if (F32) {
+          float* d = static_cast<float*>(p.d) + to + i;
+          *d = p.accumulate ? __fadd_rn(*d, x[i]) : x[i];
+        } else {
+          static_cast<uint16_t*>(p.d)[to + i] = (uint16_t)bf16x2_rn(x[i], 0.0f);
+        }
+      }
+    }
+    cluster_sync();  // nobody leaves while its sums are read
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -320,20 +355,6 @@ constexpr int kPairDynSmem = kPairStages * kPairStageBytes + 1024;
 constexpr uint32_t kPairTx = 2 * 2 * 128 * kTileK, kPairScaleTx = 2 * 3 * kScaleTile;  // of both CTAs
 constexpr int kGroupRows = 8;  // row tiles of a that neighbouring clusters share out, so that they meet in L2
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-}
-// The address of `addr` in the cluster's CTA `rank`.
-__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
 __device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
@@ -436,6 +457,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
+  wait_for_earlier_kernels();
 
   const int tiles_n = (p.n + kPairTile - 1) / kPairTile, tiles_m = (p.m + kPairTile - 1) / kPairTile;
   const int tiles = tiles_n * tiles_m, pairs = gridDim.x / 2;
@@ -608,8 +630,8 @@ cudaError_t launch_pair(const MatmulArgs& a, cudaStream_t stream) {
   const cudaError_t e = allow_smem(matmul_pair_kernel<F32>, kPairDynSmem, ready);
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)((a.n + kPairTile - 1) / kPairTile) * ((a.m + kPairTile - 1) / kPairTile);
-  matmul_pair_kernel<F32><<<2 * (unsigned)std::min<int64_t>(tiles, kSms / 2), kMatmulThreads, kPairDynSmem, stream>>>(a);
-  return cudaGetLastError();
+  return launch_dependent((const void*)matmul_pair_kernel<F32>, 2 * (unsigned)std::min<int64_t>(tiles, kSms / 2), kMatmulThreads, 0,
+                          kPairDynSmem, &a, stream);
 }
 
 template <int TM, bool F32>
@@ -619,8 +641,8 @@ cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
   const cudaError_t e = allow_smem(matmul_kernel<TM, F32>, S::kDynSmem, ready);
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)((a.n + kTileN - 1) / kTileN) * ((a.m + TM - 1) / TM);
-  matmul_kernel<TM, F32><<<(unsigned)std::min<int64_t>(tiles, kSms), kMatmulThreads, S::kDynSmem, stream>>>(a);
-  return cudaGetLastError();
+  return launch_dependent((const void*)matmul_kernel<TM, F32>, (unsigned)(tiles * a.split), kMatmulThreads, a.split, S::kDynSmem, &a,
+                          stream);
 }
 
 template <int TM>
@@ -631,17 +653,23 @@ cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
 }  // namespace
 
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k) {
-  if (m <= 16) return {16, false};
-  if (m <= 32) return {32, false};
-  if (m <= 64) return {64, false};
-  // Pairs of CTAs, unless their large tiles leave SMs without one and there are more tiles of 128 x 128 to go round.
-  const int64_t large = ((m + 255) / 256) * ((n + 255) / 256), small = ((m + 127) / 128) * ((n + 127) / 128);
-  if (large >= kSms / 2 || small <= large) return {256, true};
-  return {128, false};
+  // Pairs of CTAs from 40 tiles of 256 x 256 on, about half of what runs at once (36 tiles, 1023 x 2304 x 768: 8.2 us
+  // by pairs, 6.8 by single CTAs; 40, 1280 x 2048 x 4096: 15.0 and 15.9; 43, 256 x 11008 x 4096: 17.3 and 19.2).  Else
+  // tiles of 128 x up to 128, a tile's k shared out among CTAs while all of them run at once with one an SM: an SM takes
+  // in about 60 GB/s, so idle ones cost (1 x 4096 x 4096 10.3 us by 32 CTAs, 6.2 by 128), but with a second CTA on some
+  // SMs the others wait (1024 x 2048 x 2048 8.9 us by 128, 12.3 by 256).
+  const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
+  if (m > 128 && large >= 40) return {kPairTile, 1, true};
+  const int tile = m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
+  const int64_t tiles = ((m + tile - 1) / tile) * ((n + kTileN - 1) / kTileN), groups = (k + 511) / 512;
+  int split = 1;
+  while (split < 8 && 2 * split <= groups && 2 * split * tiles <= kSms + 8) split *= 2;
+  return {tile, split, false};
 }
 
 cudaError_t launch_matmul(MatmulArgs& a, const MatmulPlan& plan, cudaStream_t stream) {
   if (plan.pair) return a.f32 ? launch_pair<true>(a, stream) : launch_pair<false>(a, stream);
+  a.split = plan.split;
   switch (plan.tile) {
     case 16: return launch<16>(a, stream);
     case 32: return launch<32>(a, stream);

@@ -4,6 +4,7 @@
 // of 128 x 128, whose codes and scales are the same seen from the transpose.
 // One pass gives the codes as they lie, the transpose's, or both.
 #include "fp8.h"
+#include "launch.h"
 #include "step_kernel.cuh"
 
 namespace mpadam {
@@ -153,6 +154,8 @@ template <bool F32>
 __global__ void __launch_bounds__(kQuantThreads, F32 ? 2 : 3) quantize_kernel(const __grid_constant__ QuantArgs p) {
   __shared__ uint32_t row_max[4][kTile], col_max[2][kTile];
   __shared__ alignas(16) float row_inv[kTile], col_inv[kTile];
+  // A product that follows may set itself up from here on; it waits for this kernel's end before it reads.
+  asm volatile("griddepcontrol.wait;\ngriddepcontrol.launch_dependents;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int wc = warp & 3, wr = warp >> 2;
   const int pc = wc * 32 + (lane & 3) * 8, pr = wr * 64 + (lane >> 2) * 8;  // the patch's place in the tile
@@ -243,8 +246,7 @@ cudaError_t launch(QuantArgs a, cudaStream_t stream) {
   const int64_t size = F32 ? 4 : 2;
   a.vec = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.ld * size % 16 == 0 || a.rows == 1);
   const int64_t tiles = ((a.cols + kTile - 1) / kTile) * ((a.rows + kTile - 1) / kTile);
-  quantize_kernel<F32><<<(unsigned)tiles, kQuantThreads, 0, stream>>>(a);
-  return cudaGetLastError();
+  return launch_dependent((const void*)quantize_kernel<F32>, (unsigned)tiles, kQuantThreads, 0, 0, &a, stream);
 }
 
 }  // namespace
