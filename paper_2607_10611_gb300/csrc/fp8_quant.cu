@@ -46,7 +46,7 @@ struct Patch<true> {
   __device__ __forceinline__ void load_row(const void* p, int64_t at, int64_t left, bool vec, int r) {
     const float* q = static_cast<const float*>(p) + at;
     if (vec && left >= 8) {
-      const float4 a = __ldcs(reinterpret_cast<const float4*>(q)), b = __ldcs(reinterpret_cast<const float4*>(q) + 1);
+      const float4 a = __ldg(reinterpret_cast<const float4*>(q)), b = __ldg(reinterpret_cast<const float4*>(q) + 1);
       x[r][0] = a.x, x[r][1] = a.y, x[r][2] = a.z, x[r][3] = a.w;
       x[r][4] = b.x, x[r][5] = b.y, x[r][6] = b.z, x[r][7] = b.w;
     } else {
@@ -91,7 +91,7 @@ struct Patch<false> {
   __device__ __forceinline__ void load_row(const void* p, int64_t at, int64_t left, bool vec, int r) {
     const uint16_t* q = static_cast<const uint16_t*>(p) + at;
     if (vec && left >= 8) {
-      const uint4 a = __ldcs(reinterpret_cast<const uint4*>(q));
+      const uint4 a = __ldg(reinterpret_cast<const uint4*>(q));
       x[r][0] = a.x, x[r][1] = a.y, x[r][2] = a.z, x[r][3] = a.w;
     } else {
 #pragma unroll
@@ -151,7 +151,7 @@ __device__ __forceinline__ void store_scale(uint8_t* s, int64_t row, int64_t blo
 }
 
 template <bool F32>
-__global__ void __launch_bounds__(kQuantThreads, F32 ? 2 : 3) quantize_kernel(const __grid_constant__ QuantArgs p) {
+__global__ void __launch_bounds__(kQuantThreads, F32 ? 2 : 4) quantize_kernel(const __grid_constant__ QuantArgs p) {
   __shared__ uint32_t row_max[4][kTile], col_max[2][kTile];
   __shared__ alignas(16) float row_inv[kTile], col_inv[kTile];
   // A product that follows may set itself up from here on; it waits for this kernel's end before it reads.
