@@ -45,11 +45,15 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, int64_t left, b
   }
 }
 
-__device__ __forceinline__ void store8_f32(void* p, int64_t at, int64_t left, bool vec, const float (&x)[8]) {
+// vec32: the array is on a 32-byte boundary, so that a thread's 8 values go in one access and fill a sector (two of 16
+// bytes: GPT-2's step 561 us, so 557).
+__device__ __forceinline__ void store8_f32(void* p, int64_t at, int64_t left, bool vec32, const float (&x)[8]) {
   float* q = static_cast<float*>(p) + at;
-  if (vec && left >= 8) {
-    __stcs(reinterpret_cast<float4*>(q), make_float4(x[0], x[1], x[2], x[3]));
-    __stcs(reinterpret_cast<float4*>(q) + 1, make_float4(x[4], x[5], x[6], x[7]));
+  if (vec32 && left >= 8) {
+    uint32_t u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(x[j]);
+    st8(q, u);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -144,7 +148,7 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], int k, const uint3
 }
 
 // ---------------------------------------------------------------------------
-// The step.  One CTA per SM walks a run of tiles.  A producer warp brings each
+// The step.  Every CTA walks its share of the tiles.  A producer warp brings each
 // tile's arrays into a ring in shared memory by bulk copies (with the tile's
 // place, its pointers and its blocks' scales beside them, whose addresses need
 // not be aligned); the consumer warps update 8 elements a thread and store
@@ -170,7 +174,7 @@ struct TileHead {
   uint8_t *m_scale, *v_scale;
   int64_t at, left, goff;  // the tile's first element, the elements from there to the tensor's end, its global index
   int32_t staged[4];       // elements of w, g, m, v that are in the stage
-  uint32_t vec;            // bits 0: w, m, v, compute 16-byte aligned; 1: the gradient
+  uint32_t vec;            // 1: w, m, v, compute on 16-byte boundaries; 2: the gradient; 4: w, m, v on 32-byte ones
   int32_t pad[3];
   uint8_t scales[2][32];
 };
@@ -413,29 +417,52 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
     mult = *p.grad_scale;
     if (mult != mult) return;  // the norm was not finite: the step is skipped
   }
-  const int64_t t0 = p.tiles * blockIdx.x / gridDim.x, t1 = p.tiles * (blockIdx.x + 1) / gridDim.x;
+  // Every gridDim.x-th tile: the CTAs walk the list side by side.
+  const int64_t count = (p.tiles - blockIdx.x + gridDim.x - 1) / gridDim.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (warp == kConsumers / 32) {
-    int k = p.tile_tensor[t0];
-    ListTensor d = p.tensors[k];
-    const uint8_t* grad = static_cast<const uint8_t*>(grad_of(p.g, k));
+    // Each lane looks up one of the next 32 tiles, so that the chain of loads (the tile's tensor, its pointers, its
+    // gradient) is waited for once in 32 tiles, and half of those early.
+    struct Place {
+      const uint8_t* grad;
+      uint8_t *w, *m, *v, *ms, *vs;
+      uint16_t* compute;
+      int64_t at, left, goff;
+      uint32_t vec;
+    };
+    auto look_up = [&](int64_t i) {
+      Place x{};
+      if (i < count) {
+        const int64_t t = blockIdx.x + i * gridDim.x;
+        const int k = p.tile_tensor[t];
+        const ListTensor d = p.tensors[k];
+        x.grad = static_cast<const uint8_t*>(grad_of(p.g, k));
+        x.w = static_cast<uint8_t*>(d.w), x.m = static_cast<uint8_t*>(d.m), x.v = static_cast<uint8_t*>(d.v);
+        x.ms = d.m_scale, x.vs = d.v_scale, x.compute = d.compute;
+        x.at = (t - d.tile0) * kTile, x.left = d.numel - x.at, x.goff = d.goff;
+        x.vec = d.aligned | ((reinterpret_cast<uintptr_t>(x.grad) & 15) == 0 ? 2u : 0u);
+      }
+      return x;
+    };
     const uint64_t policy = evict_first_policy();
+    Place mine = look_up(lane), next{};
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int64_t t = t0; t < t1; ++t) {
-      const int64_t at0 = (t - d.tile0) * kTile;
-      if (at0 >= d.numel) {  // the next tensor that has elements
-        k = p.tile_tensor[t];
-        d = p.tensors[k];
-        grad = static_cast<const uint8_t*>(grad_of(p.g, k));
-      }
-      const int64_t at = (t - d.tile0) * kTile, left = d.numel - at;
+    for (int64_t i = 0; i < count; ++i) {
+      const int owner = (int)(i & 31);
+      if (owner == 16) next = look_up(i + 16 + lane);
+      if (owner == 0 && i > 0) mine = next;
       uint32_t ms = 127, vs = 127;
-      if (LOW && lane < kTile / 128 && lane * 128 < left) {
-        ms = d.m_scale[at / 128 + lane];
-        vs = d.v_scale[at / 128 + lane];
+      if (LOW) {
+        const int blocks = __shfl_sync(~0u, (int)((min(mine.left, (int64_t)kTile) + 127) / 128), owner);
+        const uint64_t mp = __shfl_sync(~0u, reinterpret_cast<uint64_t>(mine.ms + mine.at / 128), owner);
+        const uint64_t vp = __shfl_sync(~0u, reinterpret_cast<uint64_t>(mine.vs + mine.at / 128), owner);
+        if (lane < blocks) {
+          ms = reinterpret_cast<const uint8_t*>(mp)[lane];
+          vs = reinterpret_cast<const uint8_t*>(vp)[lane];
+        }
       }
       if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
       TileHead& h = *reinterpret_cast<TileHead*>(ring + s * R::kBytes);
@@ -443,34 +470,35 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
         h.scales[0][lane] = (uint8_t)ms;
         h.scales[1][lane] = (uint8_t)vs;
       }
-      if (lane == 0) {
-        const int n = (int)min((int64_t)kTile, left);
+      __syncwarp();
+      if (lane == owner) {
+        const Place& d = mine;
+        const int n = (int)min((int64_t)kTile, d.left);
         auto whole = [&](const void* q, int size) { return (reinterpret_cast<uintptr_t>(q) & 15) ? 0 : n * size / 16 * 16; };
-        const uint8_t *w = static_cast<uint8_t*>(d.w) + at * R::kW, *g = grad + at * R::kG,
-                      *m = static_cast<uint8_t*>(d.m) + at * R::kS, *v = static_cast<uint8_t*>(d.v) + at * R::kS;
+        const uint8_t *w = d.w + d.at * R::kW, *g = d.grad + d.at * R::kG, *m = d.m + d.at * R::kS, *v = d.v + d.at * R::kS;
         const int bw = whole(w, R::kW), bg = whole(g, R::kG), bm = whole(m, R::kS), bv = whole(v, R::kS);
-        h.grad = grad;
-        h.w = static_cast<uint8_t*>(d.w), h.m = static_cast<uint8_t*>(d.m), h.v = static_cast<uint8_t*>(d.v);
+        h.grad = d.grad;
+        h.w = d.w, h.m = d.m, h.v = d.v;
         h.compute = d.compute;
-        h.m_scale = d.m_scale, h.v_scale = d.v_scale;
-        h.at = at, h.left = left, h.goff = d.goff;
+        h.m_scale = d.ms, h.v_scale = d.vs;
+        h.at = d.at, h.left = d.left, h.goff = d.goff;
         h.staged[0] = bw / R::kW, h.staged[1] = bg / R::kG, h.staged[2] = bm / R::kS, h.staged[3] = bv / R::kS;
-        h.vec = (uint32_t)d.aligned | ((reinterpret_cast<uintptr_t>(grad) & 15) == 0 ? 2u : 0u);
+        h.vec = d.vec;
         const uint32_t st = smem + s * R::kBytes;
         mbar_expect_tx(full(s), bw + bg + bm + bv);
         if (bw) tma_load(st + R::kOffW, w, bw, full(s), policy);
         if (bg) tma_load(st + R::kOffG, g, bg, full(s), policy);
         if (bm) tma_load(st + R::kOffM, m, bm, full(s), policy);
         if (bv) tma_load(st + R::kOffV, v, bv, full(s), policy);
+        mbar_arrive(full(s));
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(full(s));
       if (++s == R::kStages) { s = 0; phase ^= 1; }
     }
     if (!ok) {
       if (lane == 0) atomicOr(p.err, 1);
       // the copies in flight, before the block's memory goes (a stage that was never filled has nothing in flight)
-      for (int i = 0; i < R::kStages && i < t1 - t0; ++i) {
+      for (int i = 0; i < R::kStages && i < count; ++i) {
         if (s == 0) { s = R::kStages; phase ^= 1; }
         --s;
         mbar_wait(full(s), phase);
@@ -483,7 +511,7 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
   const int in = threadIdx.x * 8;
   int s = 0;
   uint32_t phase = 0;
-  for (int64_t t = t0; t < t1; ++t) {
+  for (int64_t i = 0; i < count; ++i) {
     if (!mbar_wait(full(s), phase)) {
       if (lane == 0) atomicOr(p.err, 2);
       return;
@@ -498,7 +526,7 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
       continue;
     }
     const int64_t at = h.at + in;
-    const bool vec = h.vec & 1, gvec = h.vec & 2;
+    const bool vec = h.vec & 1, gvec = h.vec & 2, vec32 = h.vec & 4;
     uint32_t km0 = 127, kr0 = 127;
     float w[8], g[8], m[8], v[8];
     auto take_all = [&] {
@@ -557,10 +585,10 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
         vs[at / 128] = (uint8_t)(kv + 127);
       }
     } else {
-      store8_f32(hm, at, left, vec, m);
-      store8_f32(hv, at, left, vec, v);
+      store8_f32(hm, at, left, vec32, m);
+      store8_f32(hv, at, left, vec32, v);
     }
-    if (W32) store8_f32(hw, at, left, vec, w);
+    if (W32) store8_f32(hw, at, left, vec32, w);
     if (!W32 || compute) {
       uint32_t u[4];
       if (!W32 && SR) {

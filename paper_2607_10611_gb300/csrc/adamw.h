@@ -27,7 +27,8 @@ struct ListTensor {
   int64_t numel;
   int64_t goff;     // global index of element 0 (a multiple of 128)
   int64_t tile0;
-  int64_t aligned;  // every pointer of the tensor is a multiple of 16 bytes
+  uint32_t aligned; // 1: every pointer is a multiple of 16 bytes; 4: w, m, v of 32
+  uint32_t pad;
 };
 
 // Gradient pointers: in the launch itself, or (grads != nullptr) in device memory.

@@ -157,7 +157,7 @@ extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32
       const mpadam_adamw_tensor& t = tensors[k];
       ListTensor& x = list[k];
       if (t.numel < 0) return fail(MPADAM_EINVAL, "tensor %d has a negative size", k);
-      x = {t.w, t.m, t.v, t.m_scale, t.v_scale, t.compute, t.numel, 0, 0, 0};
+      x = {t.w, t.m, t.v, t.m_scale, t.v_scale, t.compute, t.numel, 0, 0, 0, 0};
       if (c.state_dtype == MPADAM_F32 && (t.m_scale || t.v_scale)) return fail(MPADAM_EINVAL, "tensor %d: binary32 moments have no scales", k);
       if (t.compute && c.weight_dtype != MPADAM_F32) return fail(MPADAM_EINVAL, "tensor %d: a compute copy is for binary32 weights", k);
       if (t.numel == 0) continue;
@@ -165,7 +165,8 @@ extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32
       if (c.state_dtype == MPADAM_E4M3 && (!t.m_scale || !t.v_scale)) return fail(MPADAM_EINVAL, "tensor %d: 8-bit moments need their scales", k);
       if (!is_aligned(t.w, wsz) || !is_aligned(t.m, ssz) || !is_aligned(t.v, ssz) || !is_aligned(t.compute, 2))
         return fail(MPADAM_EINVAL, "tensor %d: a pointer is not aligned to its element size", k);
-      x.aligned = is_aligned(t.w, 16) && is_aligned(t.m, 16) && is_aligned(t.v, 16) && is_aligned(t.compute, 16);
+      x.aligned = (is_aligned(t.w, 16) && is_aligned(t.m, 16) && is_aligned(t.v, 16) && is_aligned(t.compute, 16) ? 1u : 0u) |
+                  (is_aligned(t.w, 32) && is_aligned(t.m, 32) && is_aligned(t.v, 32) ? 4u : 0u);
     }
     std::unique_ptr<mpadam_adamw_state> s(new mpadam_adamw_state());
     s->cfg = c;
