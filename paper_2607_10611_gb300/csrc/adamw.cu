@@ -243,8 +243,8 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
   return __fsub_rn(c.kwd != 0.0f ? __fsub_rn(w, __fmul_rn(w, c.kwd)) : w, u);
 }
 
-// A moment's code and a weight where the fast result was not decided.  They take and give values, so that nothing of
-// the fast path has to live in memory.
+// A moment's code and a weight off the fast path.  They take and give values, so that nothing of the fast path has to
+// live in memory.
 template <bool SR, bool KEEP>
 __device__ __noinline__ uint32_t slow_code(float x, float inv, uint32_t r) {
   float y = __fmul_rn(x, inv);
@@ -252,47 +252,41 @@ __device__ __noinline__ uint32_t slow_code(float x, float inv, uint32_t r) {
   if (KEEP && x > 0.0f) y = fmaxf(y, 0x1p-9f);
   return e4m3x2(y, 0.0f) & 0xFFu;
 }
-template <bool SR>
-__device__ __noinline__ uint32_t slow_weight(float w, float m, float r, uint32_t rnd16, float ka, float c2, float eps, float kwd) {
+__device__ __noinline__ float slow_weight(float w, float m, float r, float ka, float c2, float eps, float kwd) {
   const AdamwScalars c{0.0f, 0.0f, 0.0f, 0.0f, ka, c2, eps, kwd};
-  const float x = new_weight(c, w, m, r);
-  return SR ? bf16_sr_sum(x, rnd16 ^ 0xFFFFu) >> 16 : bf16x2_rn(x, 0.0f) & 0xFFFFu;
+  return new_weight(c, w, m, r);
 }
 
 // ---------------------------------------------------------------------------
-// The update of 8 BF16 weights with 8-bit moments, where an element has 10 bytes
-// and instructions are the bound: the same results, bit for bit, with about half
-// of the instructions.
+// The update of 8 weights with 8-bit moments, where an element has 10 bytes (with
+// BF16 weights) and instructions are the bound: the same results, bit for bit,
+// with two thirds of the instructions.
 //
-// Moments and root are the canonical ones, two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
-// powers of two and a code's square has 8 bits, so b1 (code s) = (b1 s) code and b2 (code s)^2 = (b2 s^2) code^2 bit for
-// bit, for scales from 2^-47 to 2^23, where nothing is subnormal or overflows (others, and moments and weights that
-// are not finite, and second moments from 2^32 on, send the warp to the general code: false).  The weight
-// takes its quotient as a product with rcp.approx.ftz (2^-23 relative): with u =
-// 2^-24, the quotient is within 2^-23 + 2u of the canonical one and the sum adds
-// a rounding on either side, so the canonical weight lies within (|q| + |w'|)
-// 1.0625 2^-22 + 2^-96 of w' (the last term for subnormal quotients).  It is stored
-// where both ends of that interval have the same code (Ziv's test: rounding by
-// given random bits is monotone), else computed exactly: about 1 thread in 800.
+// Two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
+// powers of two and a code's square has 8 bits, so b1 (code s) = (b1 s) code and
+// b2 (code s)^2 = (b2 s^2) code^2 bit for bit, for scales from 2^-47 to 2^23,
+// where nothing is subnormal or overflows.  Other scales, weights that are not
+// finite (as where a moment is not) and second moments from 2^32 on send the warp
+// to the general code (false).  Quotients are correctly rounded where the first
+// moment times the rate is at least 2^-100; a thread that has a smaller one beside
+// others takes the general division.
 //
 // Codes of the moments: on E4M3's normal range, adding 16 random bits below the
 // grid and cutting off is two integer operations.  A thread with a non-zero value
 // below 2^-6 of its block's scale (about 1 in 500; zeros beside others count as
 // such) takes the general encoder.
 // ---------------------------------------------------------------------------
-template <bool SR, bool STATE_SR>
+template <bool W32, bool SR, bool STATE_SR>
 __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t at, int64_t left, bool vec,
                                             const float (&w)[8], const float (&g)[8], const float (&m0)[8],
                                             const float (&r0)[8], uint32_t km0, uint32_t kr0, const TileHead& h,
                                             uint32_t stage_w, int in) {
   const AdamwScalars& c = p.s;
-  float m[8], r[8];
+  float m[8], r[8], x[8];
   f32x2 fin = 0;
   const float sm = scale_value(km0), sr = scale_value(kr0);
   const f32x2 b1 = both(__fmul_rn(c.b1, sm)), b2 = both(__fmul_rn(c.b2, __fmul_rn(sr, sr)));
   const f32x2 nz = p.minus_zero, mult2 = both(mult), nkwd = both(-c.kwd), nka = both(-c.ka);
-  uint32_t rnd[4] = {}, u[4], differ = 0;
-  if (SR) weight_lanes(p, gi, rnd);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     f32x2 gg = pk(g[2 * j], g[2 * j + 1]);
@@ -303,44 +297,14 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     const f32x2 rr = root2(vv);
     unpk(mm, m[2 * j], m[2 * j + 1]);
     unpk(rr, r[2 * j], r[2 * j + 1]);
-    float d0, d1, q0, q1, w0, w1, l0, l1, h0, h1;
-    unpk(add2_rn(prod2(rr, both(c.c2), nz), both(c.eps)), d0, d1);
-    const f32x2 q = prod2(mul2_rn(mm, nka), pk(rcp_approx_ftz(d0), rcp_approx_ftz(d1)), nz);
+    const f32x2 nd = add2_rn(prod2(rr, both(-c.c2), nz), both(-c.eps));
     f32x2 base = pk(w[2 * j], w[2 * j + 1]);
     if (c.kwd != 0.0f) base = add2_rn(base, prod2(base, nkwd, nz));
-    const f32x2 wn = add2_rn(base, q);
+    const f32x2 wn = add2_rn(base, quotient2(mul2_rn(mm, nka), nd));
     fin = fma2_rn(wn, 0ull, fin);
-    unpk(q, q0, q1);
-    unpk(wn, w0, w1);
-    const f32x2 ne = fma2_rn(pk(__fadd_rn(fabsf(q0), fabsf(w0)), __fadd_rn(fabsf(q1), fabsf(w1))), both(-0x1.1p-22f),
-                             both(-0x1p-96f));
-    unpk(add2_rd(wn, ne), l0, l1);
-    f32x2 up;
-    asm("fma.rp.f32x2 %0, %1, %2, %3;" : "=l"(up) : "l"(ne), "l"(both(-1.0f)), "l"(wn));
-    unpk(up, h0, h1);
-    if (SR) {
-      const uint32_t n0 = ~rnd[j] & 0xFFFFu, n1 = ~rnd[j] >> 16;
-      u[j] = __byte_perm(__float_as_uint(l0) + n0, __float_as_uint(l1) + n1, 0x7632);
-      differ |= u[j] ^ __byte_perm(__float_as_uint(h0) + n0, __float_as_uint(h1) + n1, 0x7632);
-    } else {
-      u[j] = bf16x2_rn(l0, l1);
-      differ |= u[j] ^ bf16x2_rn(h0, h1);
-    }
+    unpk(wn, x[2 * j], x[2 * j + 1]);
   }
   if (__any_sync(~0u, cert_not_finite(fin) || min(km0, kr0) < 80u || max(km0, kr0) > 150u)) return false;
-  if (differ) {
-    float x[8];
-    take8<false>(stage_w, in, h.staged[0], h.w, at, left, vec, x);
-    if (SR) weight_lanes(p, gi, rnd);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      u[j] = __byte_perm(slow_weight<SR>(x[2 * j], m[2 * j], r[2 * j], rnd[j] & 0xFFFFu, c.ka, c.c2, c.eps, c.kwd),
-                         slow_weight<SR>(x[2 * j + 1], m[2 * j + 1], r[2 * j + 1], rnd[j] >> 16, c.ka, c.c2, c.eps, c.kwd), 0x5410);
-  }
-  store8_bf16(h.w, at, left, vec, u);
-
-  uint32_t lanes[8] = {};
-  if (STATE_SR) state_lanes(p, gi, lanes);
   // Both blocks' exponents from the 16 lanes' maxima, as 16-bit halves of a word: 0 where all are 0, else k + 135.
   float am = 0.0f, ar = 0.0f, lm = __uint_as_float(0x7F800000u), lr = lm;
 #pragma unroll
@@ -350,6 +314,33 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     lm = fminf(fminf(lm, fabsf(m[j])), fabsf(m[j + 1]));
     lr = fminf(fminf(lr, r[j]), r[j + 1]);
   }
+  if (am != 0.0f && __fmul_rn(lm, c.ka) < 0x1p-100f && c.ka != 0.0f) {
+    float y[8];
+    take8<W32>(stage_w, in, h.staged[0], h.w, at, left, vec, y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = slow_weight(y[j], m[j], r[j], c.ka, c.c2, c.eps, c.kwd);
+  }
+  uint32_t u[4];
+  if (!W32 && SR) {
+    uint32_t rnd[4];
+    weight_lanes(p, gi, rnd);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)  // (finite: no look for NaN)
+      u[j] = __byte_perm(__float_as_uint(x[2 * j]) + (~rnd[j] & 0xFFFFu), __float_as_uint(x[2 * j + 1]) + 0xFFFFu - (rnd[j] >> 16),
+                         0x7632);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = bf16x2_rn(x[2 * j], x[2 * j + 1]);
+  }
+  if (W32) {
+    store8_f32(h.w, at, left, h.vec & 4, x);
+    if (h.compute) store8_bf16(h.compute, at, left, vec, u);
+  } else {
+    store8_bf16(h.w, at, left, vec, u);
+  }
+
+  uint32_t lanes[8] = {};
+  if (STATE_SR) state_lanes(p, gi, lanes);
   auto biased = [](float a) { return a == 0.0f ? 0u : max(8u, (__float_as_uint(a) + 0x1FFFFFu) >> 23); };
   uint32_t k2 = biased(am) | biased(ar) << 16;
 #pragma unroll
@@ -550,8 +541,8 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
       if (lane == 0) mbar_arrive(empty(s));
       if (++s == R::kStages) { s = 0; phase ^= 1; }
     };
-    if constexpr (LOW && !W32) {
-      if (fast_update<SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, km0, kr0, h, st + R::kOffW, in)) {
+    if constexpr (LOW) {
+      if (p.plain && fast_update<W32, SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, km0, kr0, h, st + R::kOffW, in)) {
         release();
         continue;
       }

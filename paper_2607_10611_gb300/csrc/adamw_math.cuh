@@ -37,4 +37,22 @@ __device__ __forceinline__ f32x2 root2(f32x2 v) {
   return fma2_rn(fma2_rn(e, mul2_rn(y, both(0.5f)), s), both(-0x1p-48f), 0ull);  // (the sum makes the root of 0 positive)
 }
 
+// a / d rounded correctly, for nd = -d with d in [2^-100, 2^100], and a = 0 or
+// |a| >= 2^-100, in the same paper's way: y, the reciprocal after one Newton
+// step, is the correctly rounded one (tested for every mantissa,
+// tests/test_gpu_adamw.py); a quotient within one unit that is corrected with its
+// exact remainder and such a reciprocal then is too.  Six instructions for two
+// values, and the hardware's reciprocals.
+__device__ __forceinline__ f32x2 reciprocal2(f32x2 nd) {
+  float d0, d1;
+  unpk(nd, d0, d1);
+  const f32x2 y = pk(rcp_approx_ftz(-d0), rcp_approx_ftz(-d1));
+  return fma2_rn(fma2_rn(nd, y, both(1.0f)), y, y);
+}
+__device__ __forceinline__ f32x2 quotient2(f32x2 a, f32x2 nd) {
+  const f32x2 y = reciprocal2(nd);
+  const f32x2 q = mul2_rn(a, y);
+  return fma2_rn(fma2_rn(nd, q, a), y, q);
+}
+
 }  // namespace mpadam

@@ -223,6 +223,8 @@ extern "C" int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* g
   q.c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(b2, t)));
   q.eps = c.eps;
   q.kwd = (float)((double)lr * (double)c.weight_decay);
+  // r' < 2^16 on the fast path, so r' c2 + eps stays within [2^-100, 2^100]
+  s->args.plain = c.eps >= 0x1p-100f && c.eps <= 0x1p90f && q.c2 <= 0x1p80f;
   s->args.grad_scale = grad_scale;
   s->args.t_lo = (uint32_t)(uint64_t)step;
   s->args.t_hi = (uint32_t)((uint64_t)step >> 32);

@@ -365,17 +365,40 @@ def probe(tmp_path_factory):
     subprocess.run([B.nvcc(), *B.NVCC_FLAGS, "-shared", str(Path(__file__).parent / "cuda" / "root_probe.cu"), "-o", str(out)],
                    check=True)
     lib = ctypes.CDLL(str(out))
-    lib.root_probe.argtypes = [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p]
+    U, P = ctypes.c_uint32, ctypes.c_void_p
+    lib.root_probe.argtypes = lib.reciprocal_probe.argtypes = [U, U, P]
+    lib.quotient_probe.argtypes = [P, P, ctypes.c_int64, P]
     return lib
 
 
+def _bits(x):
+    return int(np.float32(x).view(np.uint32))
+
+
 def test_square_root_is_the_correctly_rounded_one_everywhere(probe):
-    """Every binary32 value from 0 up to 2^32, where the step turns to the library's square root; and the reciprocal over
-    all normal values within the 2^-23 that the update's bound takes."""
+    """Every binary32 value from 0 up to 2^32, where the step turns to the library's square root."""
     wrong = torch.zeros(1, dtype=torch.int64, device="cuda")
-    worst = torch.zeros(1, device="cuda")
-    end = 0x4F800000  # 2^32
-    assert probe.root_probe(0, end, wrong.data_ptr(), worst.data_ptr()) == 0
+    assert probe.root_probe(0, _bits(2.0 ** 32), wrong.data_ptr()) == 0
     assert int(wrong) == 0, int(wrong)
-    assert probe.root_probe(end, 0x7F000000 - end, wrong.data_ptr(), worst.data_ptr()) == 0
-    assert float(worst) <= 2.0 ** -23
+
+
+def test_reciprocal_is_the_correctly_rounded_one_everywhere(probe):
+    """Every binary32 value in [2^-100, 2^100]."""
+    wrong = torch.zeros(1, dtype=torch.int64, device="cuda")
+    assert probe.reciprocal_probe(_bits(2.0 ** -100), _bits(2.0 ** 100) - _bits(2.0 ** -100) + 1, wrong.data_ptr()) == 0
+    assert int(wrong) == 0, int(wrong)
+
+
+def test_quotient_is_the_correctly_rounded_one(probe):
+    """Random operands over the range, and mantissas at either end, where quotients come closest to ties."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    n = 1 << 26
+    for near in (False, True):
+        ints = lambda lo, hi: torch.randint(lo, hi, (n,), device="cuda", generator=g, dtype=torch.int32)
+        mantissa = (lambda: torch.where(ints(0, 2) == 1, ints(0, 64), (1 << 23) - 1 - ints(0, 64))) if near else \
+            (lambda: ints(0, 1 << 23))
+        d = ((ints(-60, 60) + 127) << 23 | mantissa()).view(torch.float32)
+        a = ((ints(-60, 60) + 127) << 23 | mantissa()).view(torch.float32)
+        wrong = torch.zeros(1, dtype=torch.int64, device="cuda")
+        assert probe.quotient_probe(a.data_ptr(), d.data_ptr(), n, wrong.data_ptr()) == 0
+        assert int(wrong) == 0, int(wrong)
