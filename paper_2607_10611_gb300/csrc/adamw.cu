@@ -608,7 +608,7 @@ constexpr int kNormThreads = 256;
 constexpr int kNormWarps = kNormThreads / 32;
 
 template <bool G32>
-__global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_constant__ NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, 5) grad_norm_kernel(const __grid_constant__ NormArgs p) {
   __shared__ double part[kNormWarps];
   __shared__ bool last;
   wait_for_earlier_kernels();
@@ -616,58 +616,69 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
   const int64_t walker = (int64_t)blockIdx.x * kNormWarps + warp, walkers = (int64_t)gridDim.x * kNormWarps;
   const int64_t t0 = p.tiles * walker / walkers, t1 = p.tiles * (walker + 1) / walkers;
   float acc[8] = {};
-  int64_t tile0 = 0, numel = 0;
-  const void* grad = nullptr;
-  bool vec = false;
-  for (int64_t t = t0; t < t1; ++t) {
-    if ((t - tile0) * kNormTile >= numel) {
-      const int k = p.tile_tensor[t];
-      tile0 = p.tensors[k].tile0;
-      numel = p.tensors[k].numel;
-      grad = grad_of(p.g, k);
-      vec = (reinterpret_cast<uintptr_t>(grad) & 15) == 0;
+  constexpr int kSize = G32 ? 4 : 2, kPer = 16 / kSize, kRow = 32 * kPer, kLoads = kNormTile / kRow;
+  for (int64_t base = t0; base < t1; base += 32) {
+    // Each lane looks up one of the next 32 tiles: where it starts, and how many elements it has.
+    const uint8_t* at = nullptr;
+    int elements = 0;
+    if (base + lane < t1) {
+      const int k = p.tile_tensor[base + lane];
+      const int64_t first = (base + lane - p.tensors[k].tile0) * kNormTile;
+      at = static_cast<const uint8_t*>(grad_of(p.g, k)) + first * kSize;
+      elements = (int)min((int64_t)kNormTile, p.tensors[k].numel - first);
     }
-    const int64_t at = (t - tile0) * kNormTile + lane * 8;
-    if (vec && numel - (t - tile0) * kNormTile >= kNormTile) {
-      constexpr int kLoads = G32 ? 16 : 8;
-      uint4 x[kLoads];
-      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(grad) + (at - lane * 8) * (G32 ? 4 : 2)) + lane;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) x[i] = __ldcs(q + 32 * i);
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    const int here = (int)min((int64_t)32, t1 - base);
+    for (int i = 0; i < here; ++i) {
+      const uint8_t* q = reinterpret_cast<const uint8_t*>(__shfl_sync(~0u, reinterpret_cast<uint64_t>(at), i));
+      const int n = __shfl_sync(~0u, elements, i);
+      const bool vec = (reinterpret_cast<uintptr_t>(q) & 15) == 0;
+      // The squares of a lane's vector r.
+      auto add = [&](const uint4& x, int r) {
+        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if (G32) {
             const float a = __uint_as_float(u[j]);
-            acc[4 * (i & 1) + j] = __fmaf_rn(a, a, acc[4 * (i & 1) + j]);
+            acc[4 * (r & 1) + j] = __fmaf_rn(a, a, acc[4 * (r & 1) + j]);
           } else {
             const float a = bf16_lo(u[j]), b = bf16_hi(u[j]);
             acc[2 * j] = __fmaf_rn(a, a, acc[2 * j]);
             acc[2 * j + 1] = __fmaf_rn(b, b, acc[2 * j + 1]);
           }
         }
-      }
-    } else {  // the same elements in the same sums, one at a time: an alignment changes no bit of the result
-      constexpr int kRow = G32 ? 128 : 256, kPer = G32 ? 4 : 8;  // elements of a warp's and a lane's vector load
-      const int64_t end = numel - (t - tile0) * kNormTile;
-      const int64_t first = (t - tile0) * kNormTile;
-      for (int i = 0; i < kNormTile / kRow; ++i)
+      };
+      if (vec && n == kNormTile) {
+        uint4 x[kLoads];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          const int64_t e = i * kRow + lane * kPer + j;
-          if (e < end) {
-            const float a = G32 ? static_cast<const float*>(grad)[first + e]
-                                : __uint_as_float((uint32_t)static_cast<const uint16_t*>(grad)[first + e] << 16);
-            if (G32) {
-              if (i & 1) acc[4 + (j & 3)] = __fmaf_rn(a, a, acc[4 + (j & 3)]);
-              else acc[j & 3] = __fmaf_rn(a, a, acc[j & 3]);
-            } else {
-              acc[j] = __fmaf_rn(a, a, acc[j]);
+        for (int r = 0; r < kLoads; ++r) x[r] = __ldcs(reinterpret_cast<const uint4*>(q) + r * 32 + lane);
+#pragma unroll
+        for (int r = 0; r < kLoads; ++r) add(x[r], r);
+      } else {
+        // The same elements in the same sums, whether they can be read in vectors or not: no alignment changes a bit.
+#pragma unroll 1
+        for (int r0 = 0; r0 * kRow < n; r0 += 4) {
+          uint4 x[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int e = (r0 + r) * kRow + lane * kPer;
+            uint32_t u[4] = {0, 0, 0, 0};
+            if (vec && e + kPer <= n) {
+              const uint4 y = __ldcs(reinterpret_cast<const uint4*>(q + e * kSize));
+              u[0] = y.x, u[1] = y.y, u[2] = y.z, u[3] = y.w;
+            } else if (e < n) {
+#pragma unroll
+              for (int j = 0; j < kPer; ++j)
+                if (e + j < n) {
+                  if (G32) u[j] = reinterpret_cast<const uint32_t*>(q)[e + j];
+                  else u[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(q)[e + j] << (16 * (j & 1));
+                }
             }
+            x[r] = make_uint4(u[0], u[1], u[2], u[3]);
           }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) add(x[r], r);
         }
+      }
     }
   }
   auto block_sum = [&](double x) {
