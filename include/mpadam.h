@@ -643,6 +643,12 @@ typedef struct {
 
 int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, struct CUstream_st* stream);
 
+/* Host only, no GPU: how a product of this shape is cut up: plan[0] = rows of a
+ * per tile (columns of d^T), plan[1] = CTAs that share a tile's k, plan[2] = 1
+ * when pairs of CTAs make tiles of 256 rows of b, 0 when single ones make tiles
+ * of 128.  Errors: EINVAL. */
+int32_t mpadam_debug_e4m3_plan(int64_t m, int64_t n, int64_t k, int32_t* plan);
+
 /* Device-side status of the products on the current device: waits for
  * `stream`, returns in *code the error bits that their kernels recorded since
  * the last read (non-zero: a bounded wait gave up, and that product's results

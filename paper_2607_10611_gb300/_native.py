@@ -30,7 +30,7 @@ EXPORTED = ["mpadam_create", "mpadam_create_ex", "mpadam_fp8_init", "mpadam_step
             "mpadam_debug_tile_schedule", "mpadam_debug_pool_rule", "mpadam_debug_ring_layout",
             "mpadam_adamw_create", "mpadam_adamw_step", "mpadam_adamw_status", "mpadam_adamw_destroy", "mpadam_grad_norm_create",
             "mpadam_grad_norm", "mpadam_grad_norm_destroy", "mpadam_e4m3_quantize", "mpadam_e4m3_matmul",
-            "mpadam_e4m3_status"]
+            "mpadam_e4m3_status", "mpadam_debug_e4m3_plan"]
 
 
 class MPAdamError(RuntimeError):
@@ -163,6 +163,7 @@ def lib() -> ctypes.CDLL:
             "mpadam_e4m3_quantize": [P, i32, i64, i64, i64, i32, P, P, i64, P, P, i64, P],
             "mpadam_e4m3_matmul": [P, P],
             "mpadam_e4m3_status": [P, P],
+            "mpadam_debug_e4m3_plan": [i64, i64, i64, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -481,3 +482,10 @@ def mpadam_e4m3_status(stream: int = 0) -> int:
     out = ctypes.c_int32()
     _check(lib().mpadam_e4m3_status(stream or None, ctypes.byref(out)))
     return out.value
+
+
+def mpadam_debug_e4m3_plan(m: int, n: int, k: int) -> tuple:
+    """How a product of this shape is cut up: (rows of a per tile, CTAs that share a tile's k, whether by pairs of CTAs)."""
+    out = (ctypes.c_int32 * 3)()
+    _check(lib().mpadam_debug_e4m3_plan(m, n, k, out))
+    return out[0], out[1], bool(out[2])

@@ -52,7 +52,7 @@ struct MatmulArgs {
 struct MatmulPlan {
   int tile;    // rows of a per tile
   int split;   // CTAs that share a tile's k
-  bool pair;   // tiles of 256 x 256 by pairs of CTAs, which need the scales' maps
+  bool pair;   // tiles of 256 x `tile` by pairs of CTAs, which need the scales' maps
   int box() const { return pair ? tile / 2 : tile; }  // rows of a's boxes
 };
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k);

@@ -131,7 +131,9 @@ __device__ __forceinline__ uint32_t instr_desc(uint32_t byte) {
 // 2, 4 or 8 CTAs of a cluster: each takes a run of k, writes its sums to its
 // shared memory and adds up all CTAs' for its share of the tile's lanes, in the
 // CTAs' order, so that the same product gives the same bits.  Two CTAs fit an
-// SM: one's first copies and last stores run under the other's products.
+// SM: one's first copies and last stores run under the other's products.  Tiles
+// of fewer than 128 rows of a are for an a that has no more (matmul_plan), so
+// that every tile starts with its scale tile.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float4 lds_cluster(uint32_t addr) {
   float4 v;
@@ -210,7 +212,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
         if (scales) {
           const uint32_t sc = st + (kTileN + TM) * kTileK;
           bulk_load(sc, p.sb + ((int64_t)tn * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
-          bulk_load(sc + kScaleTile, p.sa + ((int64_t)(tm * TM / 128) * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
+          bulk_load(sc + kScaleTile, p.sa + ((int64_t)tm * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
         }
         if (++s == S::kStages) { s = 0; phase ^= 1; }
       }
@@ -230,9 +232,6 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
     // that gave up it goes on without waiting; what it then computes is not used.
     const bool issue = elected();
     const uint32_t low0 = desc_low(smem);
-    // A tile of fewer than 128 rows of a starts inside its scale tile, at a multiple of 32 rows (16 only where it is the
-    // first): a column of scales holds 32 rows.
-    const int col = TM < 128 ? (tm * TM % 128) / 32 : 0;
     int s = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -253,7 +252,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
 #pragma unroll
           for (int i = 0; i < kTileK / 32; ++i)
             mma_scaled(tmem, desc(low + 2 * i, kOperandHigh), desc(low + (kTileN * kTileK >> 4) + 2 * i, kOperandHigh),
-                       instr_desc<TM>(j), sb, sa + col, j > 0 || i > 0 || kg > k0);
+                       instr_desc<TM>(j), sb, sa, j > 0 || i > 0 || kg > k0);
           mma_commit(empty(s));
         }
         if (++s == S::kStages) { s = 0; phase ^= 1; }
@@ -343,17 +342,32 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of 256 x 256 by pairs of CTAs: the two SMs' tensor cores work on one
-// product of 256 lanes (128 in each SM's tensor memory) by 256 columns, each SM
+// Tiles of 256 x TM by pairs of CTAs: the two SMs' tensor cores work on one
+// product of 256 lanes (128 in each SM's tensor memory) by TM columns, each SM
 // holding half of either operand.  A stage is then 32 KB for 2 x 128 x 128 x 256
 // multiply-adds an SM, against 48 KB where one CTA makes a tile of 128 x 256.
 // ---------------------------------------------------------------------------
-constexpr int kPairTile = 256;
-constexpr int kPairStageBytes = 2 * 128 * kTileK + 2048;  // b's rows, a's rows, scales of 128 rows of b and 256 of a
+constexpr int kPairTileN = 256;
 constexpr int kPairStages = 6;
-constexpr int kPairDynSmem = kPairStages * kPairStageBytes + 1024;
-constexpr uint32_t kPairTx = 2 * 2 * 128 * kTileK, kPairScaleTx = 2 * 3 * kScaleTile;  // of both CTAs
 constexpr int kGroupRows = 8;  // row tiles of a that neighbouring clusters share out, so that they meet in L2
+
+template <int TM>
+struct PairShape {
+  // Two accumulators where tensor memory has room for them beside the scales: the next tile's products then need not
+  // wait until this one's have been read out (about 3000 cycles a tile).
+  static constexpr int kAccs = TM > 192 ? 1 : 2;
+  static constexpr int kScaleTilesA = 2;  // 128-row tiles that TM rows from a multiple of TM may touch
+  static constexpr int kScaleCols = 4 + 4 * kScaleTilesA;
+  static constexpr int kBytesB = 128 * kTileK, kBytesA = TM / 2 * kTileK, kBytesScales = kScaleTile * (1 + kScaleTilesA);
+  static constexpr int kStageBytes = kBytesB + kBytesA + 2048;  // b's rows, a's rows, scales of 128 rows of b and of a's
+  static constexpr int kDynSmem = kPairStages * kStageBytes + 1024;
+  static constexpr uint32_t kTx = 2 * (kBytesB + kBytesA), kScaleTx = 2 * kBytesScales;  // of both CTAs
+  static_assert(kStageBytes % 1024 == 0 && kBytesScales <= 2048, "layout of a stage");
+  // A column of scales holds 32 rows, and a product's scales have to start at an even column (an odd one is a misaligned
+  // address), so tiles start at multiples of 64 rows.
+  static_assert(TM == 256 || TM == 192, "tiles start at multiples of 64 rows, in at most two scale tiles");
+  static_assert(kAccs * TM + 2 * kScaleCols <= 512, "tensor memory");
+};
 
 __device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
@@ -421,11 +435,12 @@ __device__ __forceinline__ void pair_place(int t, int tiles_m, int tiles_n, int&
   tn = in / rows;
 }
 
-template <bool F32>
+template <int TM, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
     matmul_pair_kernel(const __grid_constant__ MatmulArgs p) {
+  using S = PairShape<TM>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ alignas(8) uint64_t bars[2 * kPairStages + 3];
+  __shared__ alignas(8) uint64_t bars[2 * kPairStages + 2 * S::kAccs + 1];
   __shared__ uint32_t tmem_base_s;
   __shared__ int32_t failed;
   const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -434,15 +449,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
   const uint32_t bar0 = smem_addr(bars);
   auto full = [&](int s) { return bar0 + 8u * s; };                   // the leader's alone
   auto empty = [&](int s) { return bar0 + 8u * (kPairStages + s); };  // each CTA's own
-  const uint32_t acc_full = bar0 + 8u * (2 * kPairStages), acc_free = acc_full + 8u, drained = acc_full + 16u;
+  auto acc_full = [&](int a) { return bar0 + 8u * (2 * kPairStages + a); };
+  auto acc_free = [&](int a) { return bar0 + 8u * (2 * kPairStages + S::kAccs + a); };
+  const uint32_t drained = bar0 + 8u * (2 * kPairStages + 2 * S::kAccs);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kPairStages; ++s) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    mbar_init(acc_full, 1);
-    mbar_init(acc_free, 2 * kEpiWarps);
+    for (int a = 0; a < S::kAccs; ++a) {
+      mbar_init(acc_full(a), 1);
+      mbar_init(acc_free(a), 2 * kEpiWarps);
+    }
     mbar_init(drained, 1);
     failed = 0;
     mbar_init_fence();
@@ -459,7 +478,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
   const uint32_t tmem = tmem_base_s;
   wait_for_earlier_kernels();
 
-  const int tiles_n = (p.n + kPairTile - 1) / kPairTile, tiles_m = (p.m + kPairTile - 1) / kPairTile;
+  const int tiles_n = (p.n + kPairTileN - 1) / kPairTileN, tiles_m = (p.m + TM - 1) / TM;
   const int tiles = tiles_n * tiles_m, pairs = gridDim.x / 2;
   const int steps = (p.k + kTileK - 1) / kTileK, groups = (steps + 3) / 4;
   volatile int32_t* stop = &failed;
@@ -475,15 +494,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
         pair_place(t, tiles_m, tiles_n, tm, tn);
         for (int k = 0; k < steps; ++k) {
           if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
-          const uint32_t st = smem + s * kPairStageBytes, bar = peer_addr(full(s), 0);
+          const uint32_t st = smem + s * S::kStageBytes, bar = peer_addr(full(s), 0);
           const bool scales = (k & 3) == 0;
-          if (rank == 0) mbar_arrive_tx(full(s), kPairTx + (scales ? kPairScaleTx : 0));
-          pair_load_2d(st, &p.b, k * kTileK, tn * kPairTile + (int)rank * 128, bar);
-          pair_load_2d(st + 128 * kTileK, &p.a, k * kTileK, tm * kPairTile + (int)rank * 128, bar);
+          if (rank == 0) mbar_arrive_tx(full(s), S::kTx + (scales ? S::kScaleTx : 0));
+          pair_load_2d(st, &p.b, k * kTileK, tn * kPairTileN + (int)rank * 128, bar);
+          pair_load_2d(st + S::kBytesB, &p.a, k * kTileK, tm * TM + (int)rank * (TM / 2), bar);
           if (scales) {
-            const uint32_t sc = st + 2 * 128 * kTileK;
+            const uint32_t sc = st + S::kBytesB + S::kBytesA;
             pair_load_3d(sc, &p.sb_map, 0, k >> 2, tn * 2 + (int)rank, bar);
-            pair_load_3d(sc + kScaleTile, &p.sa_map, 0, k >> 2, tm * 2, bar);
+            pair_load_3d(sc + kScaleTile, &p.sa_map, 0, k >> 2, tm * TM / 128, bar);
           }
           ++issued;
           if (++s == kPairStages) { s = 0; phase ^= 1; }
@@ -492,7 +511,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
       if (!ok) {
         *stop = 1;
         atomicOr(p.err, kErrStage);
-        // the copies in flight: the leader sees both CTAs' last stages arrive, the other one waits about as long
+        // the copies in flight: the leader sees both CTAs' last stages arrive, the other one waits for it in the end
         for (int i = 0; i < min(issued, kPairStages); ++i) {
           if (s == 0) { s = kPairStages; phase ^= 1; }
           --s;
@@ -503,14 +522,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
   } else if (warp == 1 && rank == 0) {
     const bool issue = elected();  // as in matmul_kernel
     const uint32_t low0 = desc_low(smem);
-    int s = 0;
+    int s = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
     for (int t = blockIdx.x / 2; t < tiles; t += pairs) {
-      if (ok) ok = mbar_wait_cluster(acc_free, acc_phase ^ 1);
+      if (ok) ok = mbar_wait_cluster(acc_free(acc), acc_phase ^ 1);
       tc_fence_after();
+      const uint32_t d = tmem + acc * TM;
+      int tm, tn;
+      pair_place(t, tiles_m, tiles_n, tm, tn);
+      const uint32_t col = (uint32_t)(tm * TM % 128) / 32;  // 0 or 2
       for (int g = 0; g < groups; ++g) {
-        const uint32_t sb = tmem + kPairTile + (g & 1) * 12, sa = sb + 4;
+        const uint32_t sb = tmem + S::kAccs * TM + (g & 1) * S::kScaleCols, sa = sb + 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int k = 4 * g + j;
@@ -518,26 +541,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
           if (ok) ok = mbar_wait(full(s), phase);
           tc_fence_after();
           if (issue) {
-            const uint32_t low = low0 + s * (kPairStageBytes >> 4);
+            const uint32_t low = low0 + s * (S::kStageBytes >> 4);
             if (j == 0) {
-              const uint32_t sc = low + (2 * 128 * kTileK >> 4);
+              const uint32_t sc = low + ((S::kBytesB + S::kBytesA) >> 4);
               pair_copy_scales(sb, desc(sc, kScaleHigh));
-              pair_copy_scales(sa, desc(sc + (kScaleTile >> 4), kScaleHigh));
-              pair_copy_scales(sa + 4, desc(sc + 2 * (kScaleTile >> 4), kScaleHigh));
+#pragma unroll
+              for (int i = 0; i < S::kScaleTilesA; ++i)
+                pair_copy_scales(sa + 4 * i, desc(sc + (i + 1) * (kScaleTile >> 4), kScaleHigh));
             }
-            const uint32_t id = (uint32_t)(kPairTile >> 3) << 17 | 1u << 23 | (uint32_t)(kPairTile >> 4) << 24 |
-                                (uint32_t)j << 4 | (uint32_t)j << 29;
+            const uint32_t id = (uint32_t)(TM >> 3) << 17 | 1u << 23 | (uint32_t)(kPairTileN >> 4) << 24 | (uint32_t)j << 4 |
+                                (uint32_t)j << 29;
 #pragma unroll
             for (int i = 0; i < kTileK / 32; ++i)
-              pair_mma_scaled(tmem, desc(low + 2 * i, kOperandHigh), desc(low + (128 * kTileK >> 4) + 2 * i, kOperandHigh), id,
-                              sb, sa, j > 0 || i > 0 || g > 0);
+              pair_mma_scaled(d, desc(low + 2 * i, kOperandHigh), desc(low + (S::kBytesB >> 4) + 2 * i, kOperandHigh), id, sb,
+                              sa + col, j > 0 || i > 0 || g > 0);
             pair_commit(empty(s));
           }
           if (++s == kPairStages) { s = 0; phase ^= 1; }
         }
       }
-      if (issue) pair_commit(acc_full);
-      acc_phase ^= 1;
+      if (issue) pair_commit(acc_full(acc));
+      if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
     }
     if (!ok) {  // the products in flight, before their memory goes
       *stop = 1;
@@ -549,36 +573,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t free_bar = peer_addr(acc_free, 0);
+    constexpr int kHalf = TM / 2;  // columns of one warp
+    int acc = 0;
     uint32_t acc_phase = 0;
     for (int t = blockIdx.x / 2; t < tiles; t += pairs) {
-      if (*stop || !mbar_wait_cluster(acc_full, acc_phase)) {
+      if (*stop || !mbar_wait_cluster(acc_full(acc), acc_phase)) {
         if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
         break;
       }
-      acc_phase ^= 1;
       __syncwarp();
       tc_fence_after();
       int tm, tn;
       pair_place(t, tiles_m, tiles_n, tm, tn);
-      const int n = tn * kPairTile + (int)rank * 128 + quarter * 32 + lane, m0 = tm * kPairTile + half * 128;
-      // All of this warp's values first, so that the next tile's products can begin.
-      uint32_t r[128];
-      const uint32_t from = tmem + half * 128 + ((uint32_t)(quarter * 32) << 16);
+      const int n = tn * kPairTileN + (int)rank * 128 + quarter * 32 + lane, m0 = tm * TM + half * kHalf;
+      // All of this warp's values first, so that the accumulator is free again.
+      uint32_t r[kHalf];
+      const uint32_t from = tmem + acc * TM + half * kHalf + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_load32(from + 32 * c, r + 32 * c);
+      for (int c = 0; c < kHalf / 32; ++c) tmem_load32(from + 32 * c, r + 32 * c);
       tmem_wait_load();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(free_bar);
-      const int rows = min(128, p.m - m0);
+      if (lane == 0) mbar_arrive_cluster(peer_addr(acc_free(acc), 0));
+      if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
+      const int rows = min(kHalf, p.m - m0);
       if (n < p.n && rows > 0) {
         const int64_t at = (int64_t)m0 * p.ldd + n;
         if (F32) {
           float* d = static_cast<float*>(p.d) + at;
           if (p.accumulate) {
 #pragma unroll
-            for (int c = 0; c < 128; c += 16) {
+            for (int c = 0; c < kHalf; c += 16) {
               float old[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) old[j] = c + j < rows ? d[(c + j) * p.ldd] : 0.0f;
@@ -590,13 +615,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
             }
           } else {
 #pragma unroll
-            for (int j = 0; j < 128; ++j)
+            for (int j = 0; j < kHalf; ++j)
               if (j < rows) d[j * p.ldd] = __uint_as_float(r[j]);
           }
         } else {
           uint16_t* d = static_cast<uint16_t*>(p.d) + at;
 #pragma unroll
-          for (int j = 0; j < 128; ++j)
+          for (int j = 0; j < kHalf; ++j)
             if (j < rows) d[j * p.ldd] = (uint16_t)bf16x2_rn(__uint_as_float(r[j]), 0.0f);
         }
       }
@@ -624,14 +649,20 @@ cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>& ready) {
   return e;
 }
 
-template <bool F32>
+template <int TM, bool F32>
 cudaError_t launch_pair(const MatmulArgs& a, cudaStream_t stream) {
+  using S = PairShape<TM>;
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem(matmul_pair_kernel<F32>, kPairDynSmem, ready);
+  const cudaError_t e = allow_smem(matmul_pair_kernel<TM, F32>, S::kDynSmem, ready);
   if (e != cudaSuccess) return e;
-  const int64_t tiles = (int64_t)((a.n + kPairTile - 1) / kPairTile) * ((a.m + kPairTile - 1) / kPairTile);
-  return launch_dependent((const void*)matmul_pair_kernel<F32>, 2 * (unsigned)std::min<int64_t>(tiles, kSms / 2), kMatmulThreads, 0,
-                          kPairDynSmem, &a, stream);
+  const int64_t tiles = (int64_t)((a.n + kPairTileN - 1) / kPairTileN) * ((a.m + TM - 1) / TM);
+  return launch_dependent((const void*)matmul_pair_kernel<TM, F32>, 2 * (unsigned)std::min<int64_t>(tiles, kSms / 2), kMatmulThreads,
+                          0, S::kDynSmem, &a, stream);
+}
+
+template <int TM>
+cudaError_t launch_pair(const MatmulArgs& a, cudaStream_t stream) {
+  return a.f32 ? launch_pair<TM, true>(a, stream) : launch_pair<TM, false>(a, stream);
 }
 
 template <int TM, bool F32>
@@ -650,6 +681,18 @@ cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
   return a.f32 ? launch<TM, true>(a, stream) : launch<TM, false>(a, stream);
 }
 
+// Columns of a pair's tile: those with which all of a product's waves take less, by the time of one wave of each size
+// (fitted to 16 to 64 steps of k on shapes from 2048 to 11008: 7.4, 12.1, 17.1 and 23.0 us with 256 columns and 16, 32, 44
+// and 64 steps, 5.8, 9.5, 12.2 and 17.5 with 192).  4096 cubed takes 53.6 us with 256 and 47.5 with 192, 8192 x 2048 x
+// 5632 68.3 and 61.0, 8192 cubed 322.6 and 333.1, 2048 x 5632 x 8192 70.3 and 75.8.
+int pair_tile(int64_t m, int64_t n, int64_t k) {
+  auto time = [&](int tm, double step, double tile) {
+    const int64_t tiles = ((m + tm - 1) / tm) * ((n + kPairTileN - 1) / kPairTileN);
+    return (double)((tiles + kSms / 2 - 1) / (kSms / 2)) * ((double)((k + kTileK - 1) / kTileK) * step + tile);
+  };
+  return time(192, 0.245, 1.86) < time(256, 0.326, 2.2) ? 192 : 256;
+}
+
 }  // namespace
 
 MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k) {
@@ -659,7 +702,7 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k) {
   // in about 60 GB/s, so idle ones cost (1 x 4096 x 4096 10.3 us by 32 CTAs, 6.2 by 128), but with a second CTA on some
   // SMs the others wait (1024 x 2048 x 2048 8.9 us by 128, 12.3 by 256).
   const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
-  if (m > 128 && large >= 40) return {kPairTile, 1, true};
+  if (m > 128 && large >= 40) return {pair_tile(m, n, k), 1, true};
   const int tile = m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
   const int64_t tiles = ((m + tile - 1) / tile) * ((n + kTileN - 1) / kTileN), groups = (k + 511) / 512;
   int split = 1;
@@ -668,7 +711,7 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k) {
 }
 
 cudaError_t launch_matmul(MatmulArgs& a, const MatmulPlan& plan, cudaStream_t stream) {
-  if (plan.pair) return a.f32 ? launch_pair<true>(a, stream) : launch_pair<false>(a, stream);
+  if (plan.pair) return plan.tile == 256 ? launch_pair<256>(a, stream) : launch_pair<192>(a, stream);
   a.split = plan.split;
   switch (plan.tile) {
     case 16: return launch<16>(a, stream);

@@ -440,3 +440,12 @@ extern "C" int32_t mpadam_e4m3_status(cudaStream_t stream, int32_t* code) {
   if (e != cudaSuccess) return cuda_fail(e, "cudaStreamSynchronize");
   return MPADAM_OK;
 }
+
+extern "C" int32_t mpadam_debug_e4m3_plan(int64_t m, int64_t n, int64_t k, int32_t* plan) {
+  if (!plan) return fail(MPADAM_EINVAL, "plan is NULL");
+  if (m < 1 || n < 1 || k < 1 || m > INT32_MAX || n > INT32_MAX || k > INT32_MAX)
+    return fail(MPADAM_EINVAL, "m, n and k must be in [1, 2^31)");
+  const MatmulPlan p = matmul_plan(m, n, k);
+  plan[0] = p.tile, plan[1] = p.split, plan[2] = p.pair;
+  return MPADAM_OK;
+}

@@ -104,6 +104,11 @@ SHAPES = [(1, 1, 1), (1, 128, 128), (2, 300, 16), (3, 5, 7), (8, 4096, 640), (16
           (2049, 130, 260), (520, 5000, 300)]
 
 
+# Pairs of CTAs with tiles of 256 and of 192 rows of a: several tiles a pair, tiles that start inside a scale tile, edges.
+SHAPES += [(1920, 2560, 512), (1925, 2550, 900), (2816, 2560, 130), (5000, 1100, 1537), (1023, 5632, 300),
+           (4864, 4096, 260), (2048, 2050, 700), (4100, 4100, 140)]
+
+
 @pytest.mark.parametrize("m,n,k", SHAPES)
 def test_product_of_whole_numbers_is_exact(m, n, k):
     (va, ea), (vb, eb) = _exact_operands(m, n, k, m + 7 * n + 13 * k)

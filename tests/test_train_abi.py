@@ -1,6 +1,7 @@
 """Refusals of the AdamW, gradient-norm and 8-bit matrix entry points that are decided on the host, before any CUDA call
 (no GPU needed)."""
 import math
+import random
 
 import pytest
 
@@ -87,3 +88,20 @@ def test_matmul_refuses(N, bad):
 def test_sizes_of_zero_need_no_pointers(N):
     N.mpadam_e4m3_quantize(**{**QUANT, "rows": 0, "x": 0, "q": 0, "qt": 0})
     N.mpadam_e4m3_matmul(N.mpadam_e4m3_product(**{**PRODUCT, "m": 0, "a": None, "d": None}))
+
+
+def test_products_are_cut_up_so_that_scales_start_where_they_can(N):
+    """Tiles of fewer than 128 rows only for an a that has no more (their scales then start with their scale tile), pairs'
+    tiles at multiples of 64 rows; a tile's k shared out only among as many CTAs as there are groups of 512."""
+    g = random.Random(0)
+    seen = set()
+    for _ in range(3000):
+        m, n, k = (int(math.exp(g.uniform(0, math.log(20000)))) for _ in range(3))
+        tile, split, pair = N.mpadam_debug_e4m3_plan(m, n, k)
+        seen.add((tile, pair))
+        if pair:
+            assert tile in (192, 256) and split == 1
+        else:
+            assert tile == 128 or m <= tile
+            assert split in (1, 2, 4, 8) and split <= max(1, -(-k // 512))
+    assert seen == {(16, False), (32, False), (64, False), (128, False), (192, True), (256, True)}
