@@ -625,7 +625,7 @@ int32_t mpadam_e4m3_quantize(const void* x, int32_t x_dtype, int64_t rows, int64
  * and b [n, k] stored as above: sums over k of the codes' products times both
  * scales in binary32 on the tensor cores, rounded once into d (d_dtype
  * MPADAM_F32 or MPADAM_BF16, row stride ldd >= n elements).  k = 0 gives 0.
- * m, n, k < 2^31.  Asynchronous on `stream`.  Errors: EINVAL, EUNSUPPORTED (no
+ * m, n, k <= 2^31 - 1024.  Asynchronous on `stream`.  Errors: EINVAL, EUNSUPPORTED (no
  * driver entry for tensor maps), ECUDA. */
 typedef struct {
   const uint8_t* a;

@@ -223,8 +223,8 @@ extern "C" int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* g
   q.c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(b2, t)));
   q.eps = c.eps;
   q.kwd = (float)((double)lr * (double)c.weight_decay);
-  // r' < 2^16 on the fast path, so r' c2 + eps stays within [2^-100, 2^100]
-  s->args.plain = c.eps >= 0x1p-100f && c.eps <= 0x1p90f && q.c2 <= 0x1p80f;
+  // r' < 2^16 on the fast path: denominators lie in [2^-100, 2^25], and quotients of 2^-100 and more are not subnormal
+  s->args.plain = c.eps >= 0x1p-100f && c.eps <= 0x1p20f && q.c2 <= 0x1p8f;
   s->args.grad_scale = grad_scale;
   s->args.t_lo = (uint32_t)(uint64_t)step;
   s->args.t_hi = (uint32_t)((uint64_t)step >> 32);
@@ -347,6 +347,8 @@ extern "C" int32_t mpadam_e4m3_quantize(const void* x, int32_t x_dtype, int64_t 
 
 namespace {
 
+constexpr int64_t kMatmulMax = INT32_MAX - 1023;  // the kernels round sizes up to tiles in 32 bits
+
 using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
 
 EncodeTiled encode_tiled() {
@@ -384,8 +386,8 @@ bool code_map(CUtensorMap* map, const uint8_t* q, int64_t rows, int64_t k, int64
 
 extern "C" int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, cudaStream_t stream) {
   if (!p) return fail(MPADAM_EINVAL, "product is NULL");
-  if (p->m < 0 || p->n < 0 || p->k < 0 || p->m > INT32_MAX || p->n > INT32_MAX || p->k > INT32_MAX)
-    return fail(MPADAM_EINVAL, "m, n and k must be in [0, 2^31)");
+  if (p->m < 0 || p->n < 0 || p->k < 0 || p->m > kMatmulMax || p->n > kMatmulMax || p->k > kMatmulMax)
+    return fail(MPADAM_EINVAL, "m, n and k must be in [0, 2^31 - 1024]");
   if (p->d_dtype != MPADAM_F32 && p->d_dtype != MPADAM_BF16)
     return fail(MPADAM_EINVAL, "d_dtype must be MPADAM_F32 or MPADAM_BF16 (got %d)", p->d_dtype);
   if (p->accumulate != 0 && p->accumulate != 1) return fail(MPADAM_EINVAL, "accumulate must be 0 or 1");
@@ -443,8 +445,8 @@ extern "C" int32_t mpadam_e4m3_status(cudaStream_t stream, int32_t* code) {
 
 extern "C" int32_t mpadam_debug_e4m3_plan(int64_t m, int64_t n, int64_t k, int32_t* plan) {
   if (!plan) return fail(MPADAM_EINVAL, "plan is NULL");
-  if (m < 1 || n < 1 || k < 1 || m > INT32_MAX || n > INT32_MAX || k > INT32_MAX)
-    return fail(MPADAM_EINVAL, "m, n and k must be in [1, 2^31)");
+  if (m < 1 || n < 1 || k < 1 || m > kMatmulMax || n > kMatmulMax || k > kMatmulMax)
+    return fail(MPADAM_EINVAL, "m, n and k must be in [1, 2^31 - 1024]");
   const MatmulPlan p = matmul_plan(m, n, k);
   plan[0] = p.tile, plan[1] = p.split, plan[2] = p.pair;
   return MPADAM_OK;

@@ -73,8 +73,9 @@ class Problem:
     def optimizer(self, **kw):
         hp = {k: v for k, v in HP.items() if k != "lr"}
         low = dict(m_scales=self.gms, v_scales=self.gvs) if self.state == "e4m3" else {}
-        return AdamW(self.gw, self.gm, self.gv, weight_dtype=self.weights, grad_dtype=self.gdtype,
-                     state_dtype=self.state, compute=self.gc, **low, **{**hp, **kw})
+        self.opt = AdamW(self.gw, self.gm, self.gv, weight_dtype=self.weights, grad_dtype=self.gdtype,
+                         state_dtype=self.state, compute=self.gc, **low, **{**hp, **kw})
+        return self.opt
 
     def reference_step(self, grads, t, seed, rounding, state_rounding, mult=None, hp=HP):
         goff = 0
@@ -102,6 +103,8 @@ class Problem:
             goff += -(-n // 128) * 128
 
     def check(self):
+        if hasattr(self, "opt"):
+            assert self.opt.device_status() == 0
         for i, n in enumerate(self.sizes):
             def same(t, want):
                 got = t.cpu()
@@ -145,6 +148,29 @@ def test_many_tiles_and_steps_beyond_32_bits():
     opt.step(dev, t, HP["lr"])
     p.reference_step(host, t, 5, "stochastic", "stochastic")
     p.check()
+
+
+@pytest.mark.parametrize("weights", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(), dict(eps=1e-30), dict(eps=1e-33), dict(eps=1e7), dict(beta1=0.0), dict(beta2=0.0),
+                                dict(beta2=0.9999999), dict(weight_decay=0.0), dict(lr=0.0)])
+def test_every_range_bit_for_bit(kw, weights):
+    """Gradients and moments from subnormal to beyond where squares overflow, by blocks and within them: the step's common
+    path, what it leaves to the general code, and every border between the two."""
+    hp = {**HP, **kw}
+    p = Problem([128 * 40, 3000], weights, "f32", "e4m3", seed=11)
+    opt = p.optimizer(rounding="stochastic" if weights == "bf16" else "nearest", seed=9, **{k: v for k, v in hp.items() if k != "lr"})
+    for t in (1, 2, 3, 500):
+        host, dev = p.grads()
+        for i, n in enumerate(p.sizes):
+            scale = np.exp2(p.rng.uniform(-45, 30, -(-n // 128))).repeat(128)[:n]
+            scale[::131] *= np.exp2(p.rng.uniform(-90, 50, scale[::131].size))
+            with np.errstate(over="ignore", under="ignore"):
+                host[i] = (host[i] * scale).astype(np.float32)
+            host[i][5::17] = 0.0
+            dev[i].copy_(torch.from_numpy(host[i]))
+        opt.step(dev, t, hp["lr"])
+        p.reference_step(host, t, 9, "stochastic" if weights == "bf16" else "nearest", "stochastic", hp=hp)
+        p.check()
 
 
 @pytest.mark.parametrize("decay", [0.0, 0.3])

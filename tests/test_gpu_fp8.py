@@ -241,6 +241,15 @@ def test_linear_adds_to_the_weight_gradient_it_is_given():
     assert bool(((total.cpu().double() - 0.5 - 2 * want).abs() <= 1e-5 * (1 + want.abs().max())).all())
 
 
+def test_linear_of_no_tokens():
+    x, w, dy = _layer(0, 96, 40, 1)
+    for shape in ((0, 96), (2, 0, 96)):
+        y = fp8.linear(x.view(shape), w)
+        assert y.shape == (*shape[:-1], 40)
+        dx, dw = torch.autograd.grad(y, (x, w), torch.zeros_like(y))
+        assert dx.shape == (0, 96) and torch.equal(dw, torch.zeros_like(dw))
+
+
 @pytest.mark.parametrize("tokens", [1, 5, 40])
 def test_serving_with_a_held_weight_gives_the_same(tokens):
     x, w, _ = _layer(tokens, 512, 700, 3)

@@ -78,7 +78,7 @@ PRODUCT = dict(a=0x1000, a_scale=0x2000, lda=48, b=0x3000, b_scale=0x4000, ldb=4
 
 
 @pytest.mark.parametrize("bad", [
-    dict(m=-1), dict(n=1 << 31), dict(k=-1), dict(d_dtype=2), dict(accumulate=2), dict(accumulate=1, d_dtype=1),
+    dict(m=-1), dict(n=1 << 31), dict(k=-1), dict(n=(1 << 31) - 1023, ldd=1 << 31), dict(d_dtype=2), dict(accumulate=2), dict(accumulate=1, d_dtype=1),
     dict(d=None), dict(d=0x5002), dict(ldd=8), dict(a=None), dict(a=0x1008), dict(b_scale=None), dict(a_scale=0x2001),
     dict(lda=32), dict(ldb=40)])
 def test_matmul_refuses(N, bad):
