@@ -9,13 +9,16 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <memory>
+#include <string>
 #include <vector>
 
 #include "mpadam.h"
@@ -23,7 +26,6 @@
 namespace {
 
 using at::Tensor;
-using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
 
 constexpr auto kCodes = at::kFloat8_e4m3fn;
@@ -177,12 +179,22 @@ struct Matrix {
   // A single row's stride is of no matter, so its codes may have any.
   int64_t ld() const { return rows() > 1 ? codes.stride(0) : (cols() + 15) / 16 * 16; }
 
-  static Matrix empty(int64_t rows, int64_t cols, const at::Device& device) {
-    const auto o = at::TensorOptions().device(device);
-    const int64_t ld = (cols + 15) / 16 * 16;
-    Tensor codes = at::empty({rows, ld}, o.dtype(kCodes));
-    if (ld != cols) codes = codes.narrow(1, 0, cols);
-    return {codes, at::empty({(rows + 127) / 128, (cols + 511) / 512, 32, 4, 4}, o.dtype(kScales))};
+  // On the current device, codes and scales in one allocation and without the dispatcher: 4 us of host as two calls of
+  // at::empty and one of narrow.
+  static Matrix empty(int64_t rows, int64_t cols) {
+    const int64_t ld = (cols + 15) / 16 * 16, tiles = (rows + 127) / 128, groups = (cols + 511) / 512;
+    const int64_t scales_at = (rows * ld + 255) / 256 * 256;
+    const c10::Storage storage(c10::make_intrusive<c10::StorageImpl>(c10::StorageImpl::use_byte_size_t(),
+                                                                     scales_at + tiles * groups * 512,
+                                                                     c10::cuda::CUDACachingAllocator::get(), false));
+    auto view = [&](at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides, int64_t offset) {
+      Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(storage), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                                          c10::scalarTypeToTypeMeta(type));
+      t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides, offset);
+      return t;
+    };
+    return {view(kCodes, {rows, cols}, {ld, 1}, 0),
+            view(kScales, {tiles, groups, 32, 4, 4}, {groups * 512, 512, 16, 4, 1}, scales_at)};
   }
   static Matrix checked(PyObject* c, PyObject* s) {
     Matrix m{tensor_of(c, "codes"), tensor_of(s, "scales")};
@@ -200,8 +212,8 @@ struct Matrix {
 // x as it lies and its transpose, where asked for.
 void quantize(const Tensor& x, bool square, Matrix* q, Matrix* qt) {
   const int64_t rows = x.size(0), cols = x.size(1);
-  if (q) *q = Matrix::empty(rows, cols, x.device());
-  if (qt) *qt = Matrix::empty(cols, rows, x.device());
+  if (q) *q = Matrix::empty(rows, cols);
+  if (qt) *qt = Matrix::empty(cols, rows);
   check(mpadam_e4m3_quantize(x.const_data_ptr(), type_of(x), rows, cols, rows > 1 ? std::max(x.stride(0), cols) : cols, square,
                              q ? q->q() : nullptr, q ? q->s() : nullptr, q ? q->ld() : 0, qt ? qt->q() : nullptr,
                              qt ? qt->s() : nullptr, qt ? qt->ld() : 0, current_stream(x)));
@@ -289,42 +301,42 @@ Tensor with_shape(const Tensor& y, const Tensor& x) {
   return y.view(shape);
 }
 
-struct Linear : torch::autograd::Function<Linear> {
-  static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, bool need_x, bool need_w,
-                        const c10::optional<Tensor>& grad_w) {
-    const c10::cuda::CUDAGuard guard(x.device());
-    const Tensor m = rows_of(x);
-    Matrix q, qt, qw, qwt;
-    quantize(m, false, &q, need_w ? &qt : nullptr);
-    quantize(rows_of(w), true, &qw, need_x ? &qwt : nullptr);
-    ctx->save_for_backward({qt.codes, qt.scales, qwt.codes, qwt.scales});
-    ctx->saved_data["need_x"] = need_x;
-    ctx->saved_data["need_w"] = need_w;
-    ctx->saved_data["x_type"] = (int64_t)x.scalar_type();
-    ctx->saved_data["w_type"] = (int64_t)w.scalar_type();
-    ctx->saved_data["shape"] = x.sizes();
-    if (grad_w) ctx->saved_data["grad_w"] = *grad_w;
-    return with_shape(product(q, qw, x.scalar_type()), x);
-  }
+// The layer's node in the graph.  It holds what the backward pass takes as members: as a torch::autograd::Function, with a
+// context that keeps them by name, forward and backward of a small layer took 198 us of host, so 160 (torch's own
+// linear: 207).
+struct LinearBackward : torch::autograd::Node {
+  Matrix qt, qwt;  // x's transpose, w's
+  Tensor grad_w;
+  std::vector<int64_t> x_shape;
+  at::ScalarType x_type, w_type;
+  bool need_x, need_w, released = false;
 
-  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+  variable_list apply(variable_list&& grads) override {
     TORCH_CHECK(!at::GradMode::is_enabled(), "the 8-bit linear layer is differentiable once: no create_graph");
+    TORCH_CHECK(!released, "backward through the same 8-bit linear layer a second time: give retain_graph=True the first time");
     const Tensor& dy = grads[0];
-    const bool need_x = ctx->saved_data["need_x"].toBool(), need_w = ctx->saved_data["need_w"].toBool();
-    const auto saved = ctx->get_saved_variables();
-    const Matrix qt{saved[0], saved[1]}, qwt{saved[2], saved[3]};
+    if (!dy.defined()) return {Tensor(), Tensor()};
     const c10::cuda::CUDAGuard guard(dy.device());
     Matrix q, qdt;
     quantize(rows_of(dy), false, need_x ? &q : nullptr, need_w ? &qdt : nullptr);
     Tensor dx, dw;
-    if (need_x) dx = product(q, qwt, (at::ScalarType)ctx->saved_data["x_type"].toInt()).view(ctx->saved_data["shape"].toIntVector());
-    if (need_w) {
-      const auto held = ctx->saved_data.find("grad_w");
-      if (held != ctx->saved_data.end()) multiply(qdt, qt, held->second.toTensor(), true);
-      else dw = product(qdt, qt, (at::ScalarType)ctx->saved_data["w_type"].toInt());
+    if (need_x) {
+      dx = product(q, qwt, x_type);
+      if (x_shape.size() != 2) dx = dx.view(x_shape);
     }
-    return {dx, dw, Tensor(), Tensor(), Tensor()};
+    if (need_w) {
+      if (grad_w.defined()) multiply(qdt, qt, grad_w, true);
+      else dw = product(qdt, qt, w_type);
+    }
+    return {dx, dw};
   }
+  void release_variables() override {
+    qt = Matrix();
+    qwt = Matrix();
+    grad_w = Tensor();
+    released = true;
+  }
+  std::string name() const override { return "E4M3LinearBackward"; }
 };
 
 void check_activations(const Tensor& x) {
@@ -347,12 +359,26 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
                       "grad_w must be a float32 tensor of w's shape beside it");
   }
   const bool on = at::GradMode::is_enabled(), need_x = on && x.requires_grad(), need_w = on && w.requires_grad();
-  if (need_x || need_w) return THPVariable_Wrap(Linear::apply(x, w, need_x, need_w, grad_w));
   const c10::cuda::CUDAGuard guard(x.device());
-  Matrix q, qw;
-  quantize(rows_of(x), false, &q, nullptr);
-  quantize(rows_of(w), true, &qw, nullptr);
-  return THPVariable_Wrap(with_shape(product(q, qw, x.scalar_type()), x));
+  Matrix q, qt, qw, qwt;
+  Tensor y;
+  {
+    const at::AutoDispatchBelowADInplaceOrView below;  // what follows is the layer's own: no graph of its parts
+    quantize(rows_of(x), false, &q, need_w ? &qt : nullptr);
+    quantize(rows_of(w), true, &qw, need_x ? &qwt : nullptr);
+    y = with_shape(product(q, qw, x.scalar_type()), x);
+  }
+  if (need_x || need_w) {
+    const std::shared_ptr<LinearBackward> node(new LinearBackward(), torch::autograd::deleteNode);
+    node->qt = qt, node->qwt = qwt;
+    if (grad_w) node->grad_w = *grad_w;
+    node->x_shape = x.sizes().vec();
+    node->x_type = x.scalar_type(), node->w_type = w.scalar_type();
+    node->need_x = need_x, node->need_w = need_w;
+    node->set_next_edges(torch::autograd::collect_next_edges(x, w));
+    torch::autograd::set_history(y, node);
+  }
+  return THPVariable_Wrap(y);
   END_HANDLE_TH_ERRORS
 }
 

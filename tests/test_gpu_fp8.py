@@ -241,6 +241,25 @@ def test_linear_adds_to_the_weight_gradient_it_is_given():
     assert bool(((total.cpu().double() - 0.5 - 2 * want).abs() <= 1e-5 * (1 + want.abs().max())).all())
 
 
+def test_graphs_of_the_layer():
+    """A second backward pass needs the graph to be retained; a second derivative is refused; an unused output's gradient
+    is none; what autograd sees is one node whose inputs are x and w."""
+    x, w, dy = _layer(8, 96, 40, 1)
+    y = fp8.linear(x, w)
+    first = torch.autograd.grad(y, (x, w), dy, retain_graph=True)
+    second = torch.autograd.grad(y, (x, w), dy)
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(y, (x, w), dy)
+    with pytest.raises(RuntimeError, match="differentiable once"):
+        torch.autograd.grad(fp8.linear(x, w).float().square().sum(), x, create_graph=True)
+    assert y.grad_fn.name() == "E4M3LinearBackward" and len(y.grad_fn.next_functions) == 2
+    h = fp8.linear(x, w)
+    z = fp8.linear(torch.nn.functional.gelu(h), w.detach().t().contiguous())  # through another layer
+    z.sum().backward()
+    assert x.grad is not None and w.grad is not None and z.requires_grad and not fp8.linear(x.detach(), w.detach()).requires_grad
+
+
 def test_linear_of_no_tokens():
     x, w, dy = _layer(0, 96, 40, 1)
     for shape in ((0, 96), (2, 0, 96)):
