@@ -102,12 +102,14 @@ struct Pointers {
     TORCH_CHECK_VALUE((size_t)n == s.numel.size(), n, " gradients for ", s.numel.size(), " tensors");
     p.resize(n ? n : 1);
     PyObject** items = PySequence_Fast_ITEMS(seq);
+    const caffe2::TypeMeta type = c10::scalarTypeToTypeMeta(s.type);
+    const c10::Device device(c10::DeviceType::CUDA, (c10::DeviceIndex)s.device);
     for (Py_ssize_t i = 0; i < n; ++i) {
       const Tensor& t = tensor_of(items[i], "a gradient");
-      TORCH_CHECK_VALUE(t.scalar_type() == s.type && t.numel() == s.numel[i] && t.is_cuda() && t.get_device() == s.device &&
-                            t.is_contiguous(),
+      const c10::TensorImpl& x = *t.unsafeGetTensorImpl();
+      TORCH_CHECK_VALUE(x.dtype() == type && x.numel() == s.numel[i] && x.device() == device && x.is_contiguous(),
                         "gradients must be contiguous ", s.type, " tensors on cuda:", s.device, ", as large as their weights");
-      p[i] = t.const_data_ptr();
+      p[i] = x.data();
     }
   }
 };
