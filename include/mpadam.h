@@ -643,6 +643,15 @@ typedef struct {
 
 int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, struct CUstream_st* stream);
 
+/* mpadam_e4m3_quantize of x (device, [m, k], row stride ldx) into p->a and
+ * p->a_scale, which the call writes, by rows, then mpadam_e4m3_matmul of p: one
+ * token or a batch through a weight held in 8 bits.  The same results; where
+ * few tokens make the weight's bytes the cost, their copies begin while x is
+ * quantised.  x, p->a and p->a_scale must not overlap b, its scales or d.
+ * Errors: as the two. */
+int32_t mpadam_e4m3_quantize_matmul(const void* x, int32_t x_dtype, int64_t ldx, const mpadam_e4m3_product* p,
+                                    struct CUstream_st* stream);
+
 /* Host only, no GPU: how a product of this shape is cut up: plan[0] = rows of a
  * per tile (columns of d^T), plan[1] = CTAs that share a tile's k, plan[2] = 1
  * when pairs of CTAs make tiles of 256 rows of b, 0 when single ones make tiles

@@ -30,6 +30,7 @@ EXPORTED = ["mpadam_create", "mpadam_create_ex", "mpadam_fp8_init", "mpadam_step
             "mpadam_debug_tile_schedule", "mpadam_debug_pool_rule", "mpadam_debug_ring_layout",
             "mpadam_adamw_create", "mpadam_adamw_step", "mpadam_adamw_status", "mpadam_adamw_destroy", "mpadam_grad_norm_create",
             "mpadam_grad_norm", "mpadam_grad_norm_destroy", "mpadam_e4m3_quantize", "mpadam_e4m3_matmul",
+            "mpadam_e4m3_quantize_matmul",
             "mpadam_e4m3_status", "mpadam_debug_e4m3_plan"]
 
 
@@ -162,6 +163,7 @@ def lib() -> ctypes.CDLL:
             "mpadam_grad_norm_destroy": [P],
             "mpadam_e4m3_quantize": [P, i32, i64, i64, i64, i32, P, P, i64, P, P, i64, P],
             "mpadam_e4m3_matmul": [P, P],
+            "mpadam_e4m3_quantize_matmul": [P, i32, i64, P, P],
             "mpadam_e4m3_status": [P, P],
             "mpadam_debug_e4m3_plan": [i64, i64, i64, P],
         }
@@ -473,6 +475,12 @@ def mpadam_e4m3_quantize(x: int, x_dtype: int, rows: int, cols: int, ld: int, sq
 
 def mpadam_e4m3_matmul(product: mpadam_e4m3_product, stream: int = 0) -> None:
     status = lib().mpadam_e4m3_matmul(ctypes.byref(product), stream or None)
+    if status:
+        _check(status)
+
+
+def mpadam_e4m3_quantize_matmul(x: int, x_dtype: int, ldx: int, product: mpadam_e4m3_product, stream: int = 0) -> None:
+    status = lib().mpadam_e4m3_quantize_matmul(x or None, x_dtype, ldx, ctypes.byref(product), stream or None)
     if status:
         _check(status)
 

@@ -45,6 +45,7 @@ struct MatmulArgs {
   int32_t m, n, k;
   int32_t f32, accumulate;
   int32_t split;
+  int32_t b_early;             // b was complete before the kernel that this launch follows, which writes a (not for pairs)
   int32_t* err;                // device error word
 };
 

@@ -188,7 +188,9 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
   const uint32_t tmem_scales = tmem + TM;
-  wait_for_earlier_kernels();
+  // After a's quantisation, which lets this kernel begin once it has itself waited for all before it, only a has to be
+  // waited for, by the thread that copies it (d is not touched before a has been used).
+  if (!p.b_early) wait_for_earlier_kernels();
 
   const int tiles_m = (p.m + TM - 1) / TM;
   const int tile = blockIdx.x / p.split, rank = blockIdx.x % p.split;
@@ -199,21 +201,34 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
 
   if (warp == 0) {
     if (lane == 0) {
-      int s = 0;
-      uint32_t phase = 0;
+      auto load_b = [&](int s, int k) {
+        const uint32_t st = smem + s * S::kStageBytes;
+        mbar_arrive_tx(full(s), (kTileN + TM) * kTileK + ((k & 3) == 0 ? S::kScaleBytes : 0));
+        tma_load_2d(st, &p.b, k * kTileK, tn * kTileN, full(s));
+        if ((k & 3) == 0)
+          bulk_load(st + (kTileN + TM) * kTileK, p.sb + ((int64_t)tn * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
+      };
+      auto load_a = [&](int s, int k) {
+        const uint32_t st = smem + s * S::kStageBytes;
+        tma_load_2d(st + kTileN * kTileK, &p.a, k * kTileK, tm * TM, full(s));
+        if ((k & 3) == 0)
+          bulk_load(st + (kTileN + TM) * kTileK + kScaleTile, p.sa + ((int64_t)tm * groups + (k >> 2)) * kScaleTile, kScaleTile,
+                    full(s));
+      };
       int k = k0;
+      if (p.b_early) {
+        const int ahead = min(S::kStages, k1 - k0);
+        for (int i = 0; i < ahead; ++i) load_b(i, k0 + i);
+        wait_for_earlier_kernels();
+        for (int i = 0; i < ahead; ++i) load_a(i, k0 + i);
+        k += ahead;
+      }
+      int s = (k - k0) % S::kStages;
+      uint32_t phase = (k - k0) / S::kStages;
       for (; k < k1; ++k) {
         if (!mbar_wait(empty(s), phase ^ 1)) break;
-        const uint32_t st = smem + s * S::kStageBytes;
-        const bool scales = (k & 3) == 0;
-        mbar_arrive_tx(full(s), (kTileN + TM) * kTileK + (scales ? S::kScaleBytes : 0));
-        tma_load_2d(st, &p.b, k * kTileK, tn * kTileN, full(s));
-        tma_load_2d(st + kTileN * kTileK, &p.a, k * kTileK, tm * TM, full(s));
-        if (scales) {
-          const uint32_t sc = st + (kTileN + TM) * kTileK;
-          bulk_load(sc, p.sb + ((int64_t)tn * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
-          bulk_load(sc + kScaleTile, p.sa + ((int64_t)tm * groups + (k >> 2)) * kScaleTile, kScaleTile, full(s));
-        }
+        load_b(s, k);
+        load_a(s, k);
         if (++s == S::kStages) { s = 0; phase ^= 1; }
       }
       if (k < k1) {

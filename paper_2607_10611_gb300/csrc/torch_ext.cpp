@@ -221,7 +221,7 @@ void quantize(const Tensor& x, bool square, Matrix* q, Matrix* qt) {
                              qt ? qt->s() : nullptr, qt ? qt->ld() : 0, current_stream(x)));
 }
 
-void multiply(const Matrix& a, const Matrix& b, const Tensor& out, bool accumulate) {
+mpadam_e4m3_product product_of(const Matrix& a, const Matrix& b, const Tensor& out, bool accumulate) {
   mpadam_e4m3_product p{};
   p.a = a.q(), p.a_scale = a.s(), p.lda = a.ld();
   p.b = b.q(), p.b_scale = b.s(), p.ldb = b.ld();
@@ -230,6 +230,10 @@ void multiply(const Matrix& a, const Matrix& b, const Tensor& out, bool accumula
   p.ldd = p.m > 1 ? std::max(out.stride(0), p.n) : p.n;
   p.d_dtype = type_of(out);
   p.accumulate = accumulate;
+  return p;
+}
+void multiply(const Matrix& a, const Matrix& b, const Tensor& out, bool accumulate) {
+  const mpadam_e4m3_product p = product_of(a, b, out, accumulate);
   check(mpadam_e4m3_matmul(&p, current_stream(out)));
 }
 
@@ -396,9 +400,13 @@ PyObject* linear_held(PyObject*, PyObject* const* a, Py_ssize_t n) {
   TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && x.requires_grad()),
                     "a quantised weight passes no gradient: give linear() the weight itself");
   const c10::cuda::CUDAGuard guard(x.device());
-  Matrix q;
-  quantize(rows_of(x), false, &q, nullptr);
-  return THPVariable_Wrap(with_shape(product(q, w, x.scalar_type()), x));
+  const Tensor m = rows_of(x);
+  const Matrix q = Matrix::empty(m.size(0), m.size(1));
+  const Tensor y = at::empty({q.rows(), w.rows()}, m.options());
+  const mpadam_e4m3_product p = product_of(q, w, y, false);
+  check(mpadam_e4m3_quantize_matmul(m.const_data_ptr(), type_of(m), q.rows() > 1 ? std::max(m.stride(0), q.cols()) : q.cols(), &p,
+                                    current_stream(m)));
+  return THPVariable_Wrap(with_shape(y, x));
   END_HANDLE_TH_ERRORS
 }
 

@@ -384,7 +384,10 @@ bool code_map(CUtensorMap* map, const uint8_t* q, int64_t rows, int64_t k, int64
 
 }  // namespace
 
-extern "C" int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, cudaStream_t stream) {
+namespace {
+
+// A product's arguments.
+int32_t check_product(const mpadam_e4m3_product* p) {
   if (!p) return fail(MPADAM_EINVAL, "product is NULL");
   if (p->m < 0 || p->n < 0 || p->k < 0 || p->m > kMatmulMax || p->n > kMatmulMax || p->k > kMatmulMax)
     return fail(MPADAM_EINVAL, "m, n and k must be in [0, 2^31 - 1024]");
@@ -393,19 +396,26 @@ extern "C" int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, cudaStream_t
   if (p->accumulate != 0 && p->accumulate != 1) return fail(MPADAM_EINVAL, "accumulate must be 0 or 1");
   if (p->accumulate && p->d_dtype != MPADAM_F32) return fail(MPADAM_EINVAL, "accumulation needs a binary32 d");
   if (p->m == 0 || p->n == 0) return MPADAM_OK;
-  const size_t dsz = p->d_dtype == MPADAM_F32 ? 4 : 2;
-  if (!p->d || !is_aligned(p->d, dsz)) return fail(MPADAM_EINVAL, "d NULL or misaligned");
+  if (!p->d || !is_aligned(p->d, p->d_dtype == MPADAM_F32 ? 4 : 2)) return fail(MPADAM_EINVAL, "d NULL or misaligned");
   if (p->ldd < p->n) return fail(MPADAM_EINVAL, "ldd must be >= n");
-  if (p->k == 0) {
-    if (p->accumulate) return MPADAM_OK;
-    const cudaError_t e = cudaMemset2DAsync(p->d, (size_t)p->ldd * dsz, 0, (size_t)p->n * dsz, (size_t)p->m, stream);
-    return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "clearing d");
-  }
+  if (p->k == 0) return MPADAM_OK;
   if (!p->a || !p->b || !p->a_scale || !p->b_scale || !is_aligned(p->a, 16) || !is_aligned(p->b, 16) ||
       !is_aligned(p->a_scale, 16) || !is_aligned(p->b_scale, 16))
     return fail(MPADAM_EINVAL, "codes and scales must be 16-byte aligned and not NULL");
   if (p->lda < p->k || p->ldb < p->k || p->lda % 16 || p->ldb % 16)
     return fail(MPADAM_EINVAL, "lda and ldb must be multiples of 16, >= k");
+  return MPADAM_OK;
+}
+
+// Of checked arguments; b_early: the launch follows a's quantisation on the stream.
+int32_t multiply(const mpadam_e4m3_product* p, bool b_early, cudaStream_t stream) {
+  if (p->m == 0 || p->n == 0) return MPADAM_OK;
+  const size_t dsz = p->d_dtype == MPADAM_F32 ? 4 : 2;
+  if (p->k == 0) {
+    if (p->accumulate) return MPADAM_OK;
+    const cudaError_t e = cudaMemset2DAsync(p->d, (size_t)p->ldd * dsz, 0, (size_t)p->n * dsz, (size_t)p->m, stream);
+    return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "clearing d");
+  }
   MatmulArgs a;
   const MatmulPlan plan = matmul_plan(p->m, p->n, p->k);
   if (!encode_tiled()) return fail(MPADAM_EUNSUPPORTED, "the driver offers no cuTensorMapEncodeTiled");
@@ -421,11 +431,28 @@ extern "C" int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, cudaStream_t
   a.k = (int32_t)p->k;
   a.f32 = p->d_dtype == MPADAM_F32;
   a.accumulate = p->accumulate;
+  a.b_early = b_early && !plan.pair;
   cudaError_t e = matmul_error_word(&a.err);
   if (e != cudaSuccess) return cuda_fail(e, "the products' error word");
   e = launch_matmul(a, plan, stream);
   if (e != cudaSuccess) return cuda_fail(e, "launch of the product");
   return MPADAM_OK;
+}
+
+}  // namespace
+
+extern "C" int32_t mpadam_e4m3_matmul(const mpadam_e4m3_product* p, cudaStream_t stream) {
+  const int32_t rc = check_product(p);
+  return rc ? rc : multiply(p, false, stream);
+}
+
+extern "C" int32_t mpadam_e4m3_quantize_matmul(const void* x, int32_t x_dtype, int64_t ldx, const mpadam_e4m3_product* p,
+                                               cudaStream_t stream) {
+  int32_t rc = check_product(p);
+  if (rc) return rc;
+  rc = mpadam_e4m3_quantize(x, x_dtype, p->m, p->k, ldx, 0, const_cast<uint8_t*>(p->a), const_cast<uint8_t*>(p->a_scale), p->lda,
+                            nullptr, nullptr, 0, stream);
+  return rc ? rc : multiply(p, p->m > 0 && p->k > 0, stream);
 }
 
 extern "C" int32_t mpadam_e4m3_status(cudaStream_t stream, int32_t* code) {

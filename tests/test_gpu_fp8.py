@@ -277,6 +277,26 @@ def test_serving_with_a_held_weight_gives_the_same(tokens):
         assert torch.equal(fp8.linear(x, held), fp8.linear(x, w))
 
 
+@pytest.mark.parametrize("tokens,k,n", [(1, 4096, 1024), (20, 512, 3000), (100, 2048, 500)])
+def test_a_weight_written_just_before_it_serves(tokens, k, n):
+    """The weight's copies begin while the tokens are quantised, not before what wrote the weight has ended; and what
+    follows on the stream sees the product."""
+    x, w, _ = _layer(tokens, k, n, 6)
+    x, w = x.detach(), w.detach()
+    got, want = [], []
+    for i in range(30):
+        w = w.roll(1, 0)
+        held = fp8.quantize(w, square=True)
+        got.append(fp8.linear(x, held))
+        got[-1] += 1.0
+    torch.cuda.synchronize()
+    for i in range(30):
+        w = w.roll(-1, 0) if i else w
+        want.insert(0, fp8.linear(x, w) + 1.0)
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_other_streams_and_graphs():
     x, w, _ = _layer(70, 256, 200, 4)
     x, w = x.detach(), w.detach()

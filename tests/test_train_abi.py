@@ -85,6 +85,17 @@ def test_matmul_refuses(N, bad):
     refused(N, N.mpadam_e4m3_matmul, N.mpadam_e4m3_product(**{**PRODUCT, **bad}))
 
 
+@pytest.mark.parametrize("bad", [dict(ldx=39), dict(x_dtype=2), dict(x=0), dict(a=None), dict(a_scale=None), dict(lda=47),
+                                 dict(b=None), dict(b=0x3008), dict(ldb=40), dict(d=None), dict(ldd=8), dict(d_dtype=3),
+                                 dict(accumulate=1, d_dtype=1), dict(m=-1)])
+def test_quantize_matmul_refuses(N, bad):
+    """All before its first launch, the product's arguments too."""
+    call = dict(x=0x9000, x_dtype=0, ldx=40)
+    call.update({k: v for k, v in bad.items() if k in call})
+    product = N.mpadam_e4m3_product(**{**PRODUCT, **{k: v for k, v in bad.items() if k not in call}})
+    refused(N, N.mpadam_e4m3_quantize_matmul, **call, product=product)
+
+
 def test_sizes_of_zero_need_no_pointers(N):
     N.mpadam_e4m3_quantize(**{**QUANT, "rows": 0, "x": 0, "q": 0, "qt": 0})
     N.mpadam_e4m3_matmul(N.mpadam_e4m3_product(**{**PRODUCT, "m": 0, "a": None, "d": None}))
