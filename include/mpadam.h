@@ -531,8 +531,7 @@ typedef struct {
 } mpadam_adamw_tensor;
 
 /* Valid ranges (else MPADAM_EINVAL): 0 <= beta1, beta2 < 1; eps > 0 finite;
- * weight_decay >= 0 finite; state_rounding stochastic only with E4M3 states;
- * rounding stochastic only with BF16 weights. */
+ * weight_decay >= 0 finite; state_rounding stochastic only with E4M3 states. */
 typedef struct {
   float beta1, beta2;
   float eps;
@@ -540,7 +539,7 @@ typedef struct {
   int32_t weight_dtype;    /* MPADAM_F32 or MPADAM_BF16 */
   int32_t grad_dtype;      /* MPADAM_F32 or MPADAM_BF16 */
   int32_t state_dtype;     /* MPADAM_F32 or MPADAM_E4M3 */
-  int32_t rounding;        /* mpadam_rounding of BF16 weights */
+  int32_t rounding;        /* mpadam_rounding of BF16 weights (binary32 ones need none) */
   int32_t state_rounding;  /* mpadam_rounding of E4M3 states */
   int32_t reserved;        /* must be 0 */
   uint64_t seed;

@@ -29,6 +29,7 @@ class AdamW:
     (state_dtype "e4m3") float8_e4m3fn tensors of the same sizes with m_scales
     and v_scales, float8_e8m0fnu tensors of ceil(numel / 128) scales each; v then
     holds the second moment's square root.  init_state() makes either.
+    rounding is that of BF16 weights (binary32 ones need none).
     compute: with binary32 weights, BF16 tensors that every step overwrites with
     the rounded weights (entries may be None).  The tensors' memory has to stay
     where it is; the object keeps references to them.

@@ -141,8 +141,6 @@ extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32
   for (int32_t r : {c.rounding, c.state_rounding})
     if (r != MPADAM_ROUND_NEAREST && r != MPADAM_ROUND_STOCHASTIC)
       return fail(MPADAM_EINVAL, "rounding must be nearest (0) or stochastic (1) (got %d)", r);
-  if (c.rounding == MPADAM_ROUND_STOCHASTIC && c.weight_dtype != MPADAM_BF16)
-    return fail(MPADAM_EINVAL, "stochastic rounding is for BF16 weights");
   if (c.state_rounding == MPADAM_ROUND_STOCHASTIC && c.state_dtype != MPADAM_E4M3)
     return fail(MPADAM_EINVAL, "stochastic state rounding is for E4M3 states");
   if (c.reserved != 0) return fail(MPADAM_EINVAL, "reserved must be 0");

@@ -124,6 +124,7 @@ class Problem:
 @pytest.mark.parametrize("grads", ["f32", "bf16"])
 @pytest.mark.parametrize("weights,rounding,state,state_rounding", [
     ("f32", "nearest", "f32", "nearest"), ("bf16", "nearest", "f32", "nearest"), ("bf16", "stochastic", "f32", "nearest"),
+    ("f32", "stochastic", "f32", "nearest"), ("f32", "stochastic", "e4m3", "stochastic"),  # (a BF16 weight's rounding)
     ("f32", "nearest", "e4m3", "nearest"), ("f32", "nearest", "e4m3", "stochastic"), ("bf16", "nearest", "e4m3", "nearest"),
     ("bf16", "stochastic", "e4m3", "nearest"), ("bf16", "nearest", "e4m3", "stochastic"),
     ("bf16", "stochastic", "e4m3", "stochastic")])
@@ -365,7 +366,7 @@ def test_refusals():
                 dict(weight_dtype="bf16"), dict(compute=[w]), dict(v=[])):
         with pytest.raises(ValueError):
             make(**bad)
-    for bad in (dict(beta1=1.0), dict(eps=0.0), dict(weight_decay=-1.0), dict(rounding="stochastic")):
+    for bad in (dict(beta1=1.0), dict(eps=0.0), dict(weight_decay=-1.0)):
         with pytest.raises(RuntimeError):
             make(**bad)
     g = torch.zeros(256, device="cuda")

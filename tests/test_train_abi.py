@@ -33,7 +33,7 @@ GOOD = (0x1000, 0x2000, 0x3000, 0x4000, 0x5000, 0, 256)
 @pytest.mark.parametrize("bad", [
     dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=math.nan), dict(eps=0.0), dict(eps=math.inf), dict(weight_decay=-1.0),
     dict(weight_dtype=2), dict(grad_dtype=2), dict(state_dtype=1), dict(rounding=2), dict(state_rounding=-1),
-    dict(reserved=1), dict(weight_dtype=0, rounding=1), dict(state_dtype=0, state_rounding=1)])
+    dict(reserved=1), dict(state_dtype=0, state_rounding=1)])
 def test_adamw_refuses_bad_configs(N, bad):
     refused(N, N.mpadam_adamw_create, [GOOD], _config(N, **bad))
 
