@@ -1,9 +1,12 @@
-"""GB300-native fused M+Adam optimizer step (arxiv 2607.10611).
+"""GB300-native fused M+Adam optimizer step (arxiv 2607.10611), and what trains
+a layer in 8 bits next to it: AdamW with moments in binary32 or 8 bits, the
+gradients' norm, block-of-128 E4M3 matrices, their product and a linear layer.
 
-The step runs in one hand-written sm_103a CUDA kernel behind the C ABI of
-include/mpadam.h; this package holds that library's sources (csrc/), its
-build script and a thin ctypes binding with the C entry points' names.
-PyTorch is used only for device memory and streams.
+The kernels are hand-written for sm_103a behind the C ABI of include/mpadam.h;
+this package holds that library's sources (csrc/), its build script, a thin
+ctypes binding with the C entry points' names and classes on torch tensors
+(MPAdam, AdamW, GradNorm, fp8).  PyTorch is used for device memory, streams and
+the layer's place in the graph.
 """
 from .builder import build  # noqa: F401
 

@@ -153,7 +153,10 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], int k, const uint3
 // place, its pointers and its blocks' scales beside them, whose addresses need
 // not be aligned); the consumer warps update 8 elements a thread and store
 // straight to global memory.  Arrays that are off a 16-byte boundary, and ends
-// that do not fill one, are read by the consumers themselves.
+// that do not fill one, are read by the consumers themselves.  With binary32
+// moments memory bounds it: GPT-2 with binary32 weights and the BF16 copy (28
+// bytes an element) takes 555 us (6.3 TB/s, 0.94 of the copy's rate), 537 of them
+// between a launch's first access and its last.
 // ---------------------------------------------------------------------------
 template <bool LOW>
 struct StepShape {
@@ -260,7 +263,12 @@ __device__ __noinline__ float slow_weight(float w, float m, float r, float ka, f
 // ---------------------------------------------------------------------------
 // The update of 8 weights with 8-bit moments, where an element has 10 bytes (with
 // BF16 weights) and instructions are the bound: the same results, bit for bit,
-// with two thirds of the instructions.
+// with two thirds of the instructions.  A 7B-width shard of 667 M weights, all
+// rounded stochastically, takes 2327 us (2.9 TB/s; 2970 by the general code; its
+// bytes alone would take 1003): 89 instructions an element, of which the three
+// Philox blocks of 8 elements are 22 and the widest, with the multiplier pipe busy
+// 63 % of the time, the integer pipe 50 % and 64 % of issue slots taken (packed and
+// wide instructions take two).
 //
 // Two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
 // powers of two and a code's square has 8 bits, so b1 (code s) = (b1 s) code and
@@ -603,6 +611,9 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
 // loads in flight at once, and adds squares in eight binary32 sums a thread;
 // these meet in binary64, a partial sum per CTA, which the CTA that comes last
 // adds up in order.  The runs depend on the list alone, so the result's bits do.
+// Memory bounds it: 405 M BF16 gradients take 120 us (6.8 TB/s, 1.01 of the copy's
+// rate; by CTAs of 2048 elements in turn, a chain of loads each, 234), 4000 ragged
+// tensors of 86 M 33 (5.2 TB/s) behind 46 of the caller's look at them.
 // ---------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
 constexpr int kNormWarps = kNormThreads / 32;
