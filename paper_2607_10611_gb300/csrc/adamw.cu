@@ -169,16 +169,18 @@ struct StepShape {
 };
 constexpr int kStepMaxStages = 8;
 
-// What the consumers need to know of a stage's tile.
+// What the consumers need to know of a stage's tile.  Pointers are to its first element or block.
 struct TileHead {
-  const void* grad;
+  const uint8_t* grad;
   uint8_t *w, *m, *v;
   uint16_t* compute;
   uint8_t *m_scale, *v_scale;
-  int64_t at, left, goff;  // the tile's first element, the elements from there to the tensor's end, its global index
-  int32_t staged[4];       // elements of w, g, m, v that are in the stage
-  uint32_t vec;            // 1: w, m, v, compute on 16-byte boundaries; 2: the gradient; 4: w, m, v on 32-byte ones
-  int32_t pad[3];
+  int64_t left, goff;  // the elements from here to the tensor's end, the first one's global index
+  int32_t staged[4];   // elements of w, g, m, v that are in the stage
+  // 1: w, m, v, compute on 16-byte boundaries; 2: the gradient; 4: w, m, v on 32-byte ones; 8: the tile is full, all of it
+  // is in the stage, and every store can be a vector's
+  uint32_t flags;
+  int32_t pad;
   uint8_t scales[2][32];
 };
 
@@ -196,8 +198,7 @@ struct StepRing {
 
 // 8 values of an array: from the stage where they are whole in it, else from memory.
 template <bool F32>
-__device__ __forceinline__ void take8(uint32_t stage, int in, int staged, const void* p, int64_t at, int64_t left, bool vec,
-                                      float (&x)[8]) {
+__device__ __forceinline__ void take8(uint32_t stage, int in, int staged, const void* p, int64_t left, bool vec, float (&x)[8]) {
   if (in + 8 <= staged) {
     uint32_t a[4];
     if (F32) {
@@ -212,11 +213,11 @@ __device__ __forceinline__ void take8(uint32_t stage, int in, int staged, const 
       for (int j = 0; j < 4; ++j) x[2 * j] = bf16_lo(a[j]), x[2 * j + 1] = bf16_hi(a[j]);
     }
   } else {
-    load8<F32>(p, at, left, vec, x);
+    load8<F32>(p, in, left, vec, x);
   }
 }
 __device__ __forceinline__ uint2 take8_codes(uint32_t stage, int in, int staged, const uint8_t* p, int64_t left, bool vec) {
-  if (in + 8 > staged) return load8_codes(p, left, vec);
+  if (in + 8 > staged) return load8_codes(p + in, left, vec);
   uint32_t a[2];
   lds2(stage + in, a);
   return make_uint2(a[0], a[1]);
@@ -285,7 +286,7 @@ __device__ __noinline__ float slow_weight(float w, float m, float r, float ka, f
 // such) takes the general encoder.
 // ---------------------------------------------------------------------------
 template <bool W32, bool SR, bool STATE_SR>
-__device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t at, int64_t left, bool vec,
+__device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t left, bool vec, bool vec32,
                                             const float (&w)[8], const float (&g)[8], const float (&m0)[8],
                                             const float (&r0)[8], uint32_t km0, uint32_t kr0, const TileHead& h,
                                             uint32_t stage_w, int in) {
@@ -324,7 +325,7 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
   }
   if (am != 0.0f && __fmul_rn(lm, c.ka) < 0x1p-100f && c.ka != 0.0f) {
     float y[8];
-    take8<W32>(stage_w, in, h.staged[0], h.w, at, left, vec, y);
+    take8<W32>(stage_w, in, h.staged[0], h.w, left, vec, y);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = slow_weight(y[j], m[j], r[j], c.ka, c.c2, c.eps, c.kwd);
   }
@@ -341,10 +342,10 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     for (int j = 0; j < 4; ++j) u[j] = bf16x2_rn(x[2 * j], x[2 * j + 1]);
   }
   if (W32) {
-    store8_f32(h.w, at, left, h.vec & 4, x);
-    if (h.compute) store8_bf16(h.compute, at, left, vec, u);
+    store8_f32(h.w, in, left, vec32, x);
+    if (h.compute) store8_bf16(h.compute, in, left, vec, u);
   } else {
-    store8_bf16(h.w, at, left, vec, u);
+    store8_bf16(h.w, in, left, vec, u);
   }
 
   uint32_t lanes[8] = {};
@@ -381,11 +382,11 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
       b[j] = e4m3x2(z0, z1);
     }
   }
-  store8_codes(h.m + at, left, vec, make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)));
-  store8_codes(h.v + at, left, vec, make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410)));
+  store8_codes(h.m + in, left, vec, make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)));
+  store8_codes(h.v + in, left, vec, make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410)));
   if ((threadIdx.x & 15) == 0 && left > 0) {
-    h.m_scale[at / 128] = (uint8_t)(km + 127);
-    h.v_scale[at / 128] = (uint8_t)(kr + 127);
+    h.m_scale[threadIdx.x >> 4] = (uint8_t)(km + 127);
+    h.v_scale[threadIdx.x >> 4] = (uint8_t)(kr + 127);
   }
   return true;
 }
@@ -476,13 +477,14 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
         auto whole = [&](const void* q, int size) { return (reinterpret_cast<uintptr_t>(q) & 15) ? 0 : n * size / 16 * 16; };
         const uint8_t *w = d.w + d.at * R::kW, *g = d.grad + d.at * R::kG, *m = d.m + d.at * R::kS, *v = d.v + d.at * R::kS;
         const int bw = whole(w, R::kW), bg = whole(g, R::kG), bm = whole(m, R::kS), bv = whole(v, R::kS);
-        h.grad = d.grad;
-        h.w = d.w, h.m = d.m, h.v = d.v;
-        h.compute = d.compute;
-        h.m_scale = d.ms, h.v_scale = d.vs;
-        h.at = d.at, h.left = d.left, h.goff = d.goff;
+        h.grad = g;
+        h.w = const_cast<uint8_t*>(w), h.m = const_cast<uint8_t*>(m), h.v = const_cast<uint8_t*>(v);
+        h.compute = d.compute ? d.compute + d.at : nullptr;
+        h.m_scale = d.ms + d.at / 128, h.v_scale = d.vs + d.at / 128;
+        h.left = d.left, h.goff = d.goff + d.at;
         h.staged[0] = bw / R::kW, h.staged[1] = bg / R::kG, h.staged[2] = bm / R::kS, h.staged[3] = bv / R::kS;
-        h.vec = d.vec;
+        const bool full_tile = n == kTile && bw == kTile * R::kW && bg == kTile * R::kG && bm == kTile * R::kS && bv == kTile * R::kS;
+        h.flags = d.vec | (full_tile && (d.vec & 3) == 3 && (!W32 || (d.vec & 4)) ? 8u : 0u);
         const uint32_t st = smem + s * R::kBytes;
         mbar_expect_tx(full(s), bw + bg + bm + bv);
         if (bw) tma_load(st + R::kOffW, w, bw, full(s), policy);
@@ -524,25 +526,24 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
       if (++s == R::kStages) { s = 0; phase ^= 1; }
       continue;
     }
-    const int64_t at = h.at + in;
-    const bool vec = h.vec & 1, gvec = h.vec & 2, vec32 = h.vec & 4;
+    const uint32_t flags = h.flags;
+    const bool vec = flags & 1, gvec = flags & 2, vec32 = flags & 4;
+    const int64_t gi = h.goff + in;
     uint32_t km0 = 127, kr0 = 127;
     float w[8], g[8], m[8], v[8];
-    auto take_all = [&] {
-      take8<G32>(st + R::kOffG, in, h.staged[1], h.grad, at, left, gvec, g);
-      take8<W32>(st + R::kOffW, in, h.staged[0], h.w, at, left, vec, w);
+    auto take_all = [&](const int (&staged)[4]) {
+      take8<G32>(st + R::kOffG, in, staged[1], h.grad, left, gvec, g);
+      take8<W32>(st + R::kOffW, in, staged[0], h.w, left, vec, w);
       if (LOW) {
-        decode8(take8_codes(st + R::kOffM, in, h.staged[2], h.m + at, left, vec), m);
-        decode8(take8_codes(st + R::kOffV, in, h.staged[3], h.v + at, left, vec), v);
+        decode8(take8_codes(st + R::kOffM, in, staged[2], h.m, left, vec), m);
+        decode8(take8_codes(st + R::kOffV, in, staged[3], h.v, left, vec), v);
         km0 = h.scales[0][threadIdx.x >> 4];
         kr0 = h.scales[1][threadIdx.x >> 4];
       } else {
-        take8<true>(st + R::kOffM, in, h.staged[2], h.m, at, left, vec, m);
-        take8<true>(st + R::kOffV, in, h.staged[3], h.v, at, left, vec, v);
+        take8<true>(st + R::kOffM, in, staged[2], h.m, left, vec, m);
+        take8<true>(st + R::kOffV, in, staged[3], h.v, left, vec, v);
       }
     };
-    take_all();
-    const int64_t gi = h.goff + at;
     // With 8-bit moments the stage is kept to the end: what is needed again is read from it again, not kept in registers.
     auto release = [&] {
       __syncwarp();
@@ -550,12 +551,23 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
       if (++s == R::kStages) { s = 0; phase ^= 1; }
     };
     if constexpr (LOW) {
-      if (p.plain && fast_update<W32, SR, STATE_SR>(p, mult, gi, at, left, vec, w, g, m, v, km0, kr0, h, st + R::kOffW, in)) {
-        release();
-        continue;
+      if (p.plain) {
+        bool done;
+        if (flags & 8) {  // no look at the tile's end or at alignments
+          constexpr int kAll[4] = {1 << 30, 1 << 30, 1 << 30, 1 << 30};
+          take_all(kAll);
+          done = fast_update<W32, SR, STATE_SR>(p, mult, gi, 8, true, true, w, g, m, v, km0, kr0, h, st + R::kOffW, in);
+        } else {
+          take_all(h.staged);
+          done = fast_update<W32, SR, STATE_SR>(p, mult, gi, left, vec, vec32, w, g, m, v, km0, kr0, h, st + R::kOffW, in);
+        }
+        if (done) {
+          release();
+          continue;
+        }
       }
-      take_all();
     }
+    take_all(h.staged);
     uint8_t *const hw = h.w, *const hm = h.m, *const hv = h.v, *const ms = h.m_scale, *const vs = h.v_scale;
     uint16_t* const compute = h.compute;
     if constexpr (!LOW) release();
@@ -577,17 +589,17 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
       uint32_t lanes[8] = {};
       if (STATE_SR) state_lanes(p, gi, lanes);
       const int km = block_exponent(m), kv = block_exponent(r);
-      store8_codes(hm + at, left, vec, encode8<STATE_SR, false>(m, km, lanes, 0));
-      store8_codes(hv + at, left, vec, encode8<STATE_SR, true>(r, kv, lanes, 16));
+      store8_codes(hm + in, left, vec, encode8<STATE_SR, false>(m, km, lanes, 0));
+      store8_codes(hv + in, left, vec, encode8<STATE_SR, true>(r, kv, lanes, 16));
       if ((threadIdx.x & 15) == 0 && left > 0) {
-        ms[at / 128] = (uint8_t)(km + 127);
-        vs[at / 128] = (uint8_t)(kv + 127);
+        ms[threadIdx.x >> 4] = (uint8_t)(km + 127);
+        vs[threadIdx.x >> 4] = (uint8_t)(kv + 127);
       }
     } else {
-      store8_f32(hm, at, left, vec32, m);
-      store8_f32(hv, at, left, vec32, v);
+      store8_f32(hm, in, left, vec32, m);
+      store8_f32(hv, in, left, vec32, v);
     }
-    if (W32) store8_f32(hw, at, left, vec32, w);
+    if (W32) store8_f32(hw, in, left, vec32, w);
     if (!W32 || compute) {
       uint32_t u[4];
       if (!W32 && SR) {
@@ -599,8 +611,8 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[j] = bf16x2_rn(w[2 * j], w[2 * j + 1]);
       }
-      if (!W32) store8_bf16(hw, at, left, vec, u);
-      else store8_bf16(compute, at, left, vec, u);
+      if (!W32) store8_bf16(hw, in, left, vec, u);
+      else store8_bf16(compute, in, left, vec, u);
     }
     if constexpr (LOW) release();
   }
