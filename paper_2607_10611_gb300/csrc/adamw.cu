@@ -265,10 +265,10 @@ __device__ __noinline__ float slow_weight(float w, float m, float r, float ka, f
 // The update of 8 weights with 8-bit moments, where an element has 10 bytes (with
 // BF16 weights) and instructions are the bound: the same results, bit for bit,
 // with two thirds of the instructions.  A 7B-width shard of 667 M weights, all
-// rounded stochastically, takes 2327 us (2.9 TB/s; 2970 by the general code; its
-// bytes alone would take 1003): 89 instructions an element, of which the three
+// rounded stochastically, takes 2216 us (3.0 TB/s; 2970 by the general code; its
+// bytes alone would take 1003): 85 instructions an element, of which the three
 // Philox blocks of 8 elements are 22 and the widest, with the multiplier pipe busy
-// 63 % of the time, the integer pipe 50 % and 64 % of issue slots taken (packed and
+// 64 % of the time, the integer pipe 51 % and 63 % of issue slots taken (packed and
 // wide instructions take two).
 //
 // Two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
