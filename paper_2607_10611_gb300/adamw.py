@@ -4,21 +4,15 @@ What every call does with its list of gradients is csrc/torch_ext.cpp's.
 """
 from __future__ import annotations
 
+import ctypes
 from typing import Optional, Sequence
 
 import torch
 
 from . import _native as N
 
-_FLOAT = {"f32": torch.float32, "bf16": torch.bfloat16}
 _STATE = {"f32": torch.float32, "e4m3": torch.float8_e4m3fn}
 BLOCK = 128  # elements that share a scale of 8-bit moments
-
-
-def _check(tensors, dtype, what):
-    for t in tensors:
-        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-            raise ValueError(f"{what}: expected contiguous CUDA tensors of {dtype}")
 
 
 class AdamW:
@@ -43,42 +37,16 @@ class AdamW:
                  state_rounding: Optional[str] = None, seed: int = 0, beta1: float = 0.9, beta2: float = 0.999,
                  eps: float = 1e-8, weight_decay: float = 0.01):
         self.w, self.m, self.v = list(w), list(m), list(v)
-        n = len(self.w)
-        low = state_dtype == "e4m3"
-        if low and (m_scales is None or v_scales is None):
-            raise ValueError("8-bit moments need m_scales and v_scales")
-        if not low and (m_scales is not None or v_scales is not None):
-            raise ValueError("binary32 moments have no scales")
-        self.m_scales, self.v_scales = (list(m_scales), list(v_scales)) if low else ([None] * n, [None] * n)
-        self.compute = list(compute) if compute is not None else [None] * n
-        if not (len(self.m) == len(self.v) == len(self.m_scales) == len(self.v_scales) == len(self.compute) == n):
-            raise ValueError("one entry per tensor in every list")
-        _check(self.w, _FLOAT[weight_dtype], "weights")
-        _check(self.m + self.v, _STATE[state_dtype], "moments")
-        copies = [c for c in self.compute if c is not None]
-        _check(copies, torch.bfloat16, "compute copies")
-        scales = self.m_scales + self.v_scales if low else []
-        _check(scales, torch.float8_e8m0fnu, "scales")
-        self.device = self.w[0].device if n else torch.device("cuda", torch.cuda.current_device())
-        if any(t.device != self.device for t in self.w + self.m + self.v + copies + scales):
-            raise ValueError("all tensors of a list must be on one device")
-        self.numels = [t.numel() for t in self.w]
-        for k, size in enumerate(self.numels):
-            if self.m[k].numel() != size or self.v[k].numel() != size:
-                raise ValueError(f"tensor {k}: moments differ in size from the weights")
-            if self.compute[k] is not None and self.compute[k].numel() != size:
-                raise ValueError(f"tensor {k}: the compute copy differs in size from the weights")
-            if low and not self.m_scales[k].numel() == self.v_scales[k].numel() == -(-size // BLOCK):
-                raise ValueError(f"tensor {k}: needs one scale per {BLOCK} elements")
+        given = lambda x: list(x) if x is not None else None
+        self.m_scales, self.v_scales, self.compute = given(m_scales), given(v_scales), given(compute)
         if state_rounding is None:
-            state_rounding = "stochastic" if low else "nearest"
+            state_rounding = "stochastic" if state_dtype == "e4m3" else "nearest"
         cfg = N.mpadam_adamw_config(beta1, beta2, eps, weight_decay, N.DTYPE[weight_dtype], N.DTYPE[grad_dtype],
                                     N.DTYPE[state_dtype], N.ROUNDING[rounding], N.ROUNDING[state_rounding], 0, seed)
-        ptr = lambda t: t.data_ptr() if t is not None else 0
-        with torch.cuda.device(self.device):
-            self.state = N.mpadam_adamw_create(
-                [tuple(map(ptr, row)) + (size,) for *row, size in
-                 zip(self.w, self.m, self.v, self.m_scales, self.v_scales, self.compute, self.numels)], cfg)
+        self.state = N.ext().adamw_create(ctypes.addressof(cfg), self.w, self.m, self.v, self.m_scales, self.v_scales,
+                                          self.compute)
+        self.device = self.w[0].device if self.w else torch.device("cuda", torch.cuda.current_device())
+        self.numels = [t.numel() for t in self.w]
         self._spec = N.ext().list_spec(self.numels, grad_dtype == "f32", self.device.index)
         self._step = N.ext().adamw_step
 

@@ -114,6 +114,56 @@ struct Pointers {
   }
 };
 
+// adamw_create(config's address, w, m, v, m scales or None, v scales or None, compute or None) -> state: lists of tensors
+// whose types, sizes and devices are checked here; compute's entries may be None.
+PyObject* adamw_create(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 7, "adamw_create takes 7 arguments");
+  const auto* cfg = static_cast<const mpadam_adamw_config*>(PyLong_AsVoidPtr(a[0]));
+  if (PyErr_Occurred()) return nullptr;
+  for (int i = 1; i < 7; ++i) TORCH_CHECK_VALUE(PyList_Check(a[i]) || (i > 3 && a[i] == Py_None), "the tensors come in lists");
+  const bool low = cfg->state_dtype == MPADAM_E4M3;
+  TORCH_CHECK_VALUE(!low || (a[4] != Py_None && a[5] != Py_None), "8-bit moments need m_scales and v_scales");
+  TORCH_CHECK_VALUE(low || (a[4] == Py_None && a[5] == Py_None), "binary32 moments have no scales");
+  const Py_ssize_t count = PyList_GET_SIZE(a[1]);
+  for (int i = 2; i < 7; ++i)
+    TORCH_CHECK_VALUE(a[i] == Py_None || PyList_GET_SIZE(a[i]) == count, "one entry per tensor in every list");
+  std::vector<mpadam_adamw_tensor> list((size_t)count + 1);
+  c10::optional<c10::Device> device;
+  auto take = [&](int i, Py_ssize_t k, at::ScalarType type, const char* what) {
+    const Tensor& t = tensor_of(PyList_GET_ITEM(a[i], k), what);
+    TORCH_CHECK_VALUE(t.scalar_type() == type && t.is_cuda() && t.is_contiguous(), what, ": expected contiguous CUDA tensors of ",
+                      type);
+    if (!device) device = t.device();
+    TORCH_CHECK_VALUE(t.device() == *device, "all tensors of a list must be on one device");
+    return t;
+  };
+  const auto wt = cfg->weight_dtype == MPADAM_F32 ? at::kFloat : at::kBFloat16, st = low ? kCodes : at::kFloat;
+  for (Py_ssize_t k = 0; k < count; ++k) {
+    mpadam_adamw_tensor& x = list[k];
+    const Tensor w = take(1, k, wt, "weights"), m = take(2, k, st, "moments"), v = take(3, k, st, "moments");
+    x = {w.data_ptr(), m.data_ptr(), v.data_ptr(), nullptr, nullptr, nullptr, w.numel()};
+    TORCH_CHECK_VALUE(m.numel() == x.numel && v.numel() == x.numel, "tensor ", k, ": moments differ in size from the weights");
+    if (low) {
+      const Tensor ms = take(4, k, kScales, "scales"), vs = take(5, k, kScales, "scales");
+      TORCH_CHECK_VALUE(ms.numel() == (x.numel + 127) / 128 && vs.numel() == ms.numel(), "tensor ", k,
+                        ": needs one scale per 128 elements");
+      x.m_scale = static_cast<uint8_t*>(ms.data_ptr());
+      x.v_scale = static_cast<uint8_t*>(vs.data_ptr());
+    }
+    if (a[6] != Py_None && PyList_GET_ITEM(a[6], k) != Py_None) {
+      const Tensor c = take(6, k, at::kBFloat16, "compute copies");
+      TORCH_CHECK_VALUE(c.numel() == x.numel, "tensor ", k, ": the compute copy differs in size from the weights");
+      x.compute = static_cast<uint16_t*>(c.data_ptr());
+    }
+  }
+  const c10::cuda::OptionalCUDAGuard guard(device);
+  mpadam_adamw_state* state = nullptr;
+  if (const int32_t rc = mpadam_adamw_create(list.data(), (int32_t)count, cfg, &state)) return raise(rc);
+  return PyLong_FromVoidPtr(state);
+  END_HANDLE_TH_ERRORS
+}
+
 cudaStream_t stream_of(PyObject* o, int device) {
   return o == Py_None ? c10::cuda::getCurrentCUDAStream(device).stream() : reinterpret_cast<cudaStream_t>(PyLong_AsSize_t(o));
 }
@@ -418,6 +468,7 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define MPADAM_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef kMethods[] = {{"list_spec", MPADAM_FAST(list_spec)},
+                          {"adamw_create", MPADAM_FAST(adamw_create)},
                           {"adamw_step", MPADAM_FAST(adamw_step)},
                           {"grad_norm", MPADAM_FAST(grad_norm)},
                           {"check_matrix", MPADAM_FAST(check_matrix)},

@@ -31,21 +31,19 @@ struct List {
   int64_t tiles = 0;
   size_t grad_size = 4;
   std::vector<int64_t> numel;
+  uint8_t* memory = nullptr;  // one allocation: the tables below, then what the operator asked for, zeroed
   ListTensor* d_tensors = nullptr;
   int32_t* d_tile_tensor = nullptr;
   const void** d_grads = nullptr;
+  void* extra = nullptr;
   std::vector<const void*> last;  // what d_grads holds
   bool last_known = false, captured = false;
 
   List() = default;
   List(const List&) = delete;
-  ~List() {
-    cudaFree(d_tensors);
-    cudaFree(d_tile_tensor);
-    cudaFree(d_grads);
-  }
+  ~List() { cudaFree(memory); }
 
-  int32_t build(std::vector<ListTensor>& t, int32_t tile) {
+  int32_t build(std::vector<ListTensor>& t, int32_t tile, size_t extra_bytes) {
     n = (int32_t)t.size();
     int64_t goff = 0;
     for (auto& x : t) {
@@ -58,19 +56,29 @@ struct List {
     if (tiles >= INT32_MAX) return fail(MPADAM_EINVAL, "the list has too many elements");
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-    if (!tiles) return MPADAM_OK;
-    std::vector<int32_t> owner((size_t)tiles);
-    for (int32_t k = 0; k < n; ++k)
-      std::fill_n(owner.begin() + t[k].tile0, (t[k].numel + tile - 1) / tile, k);
-    if (dev_malloc(&d_tensors, sizeof(ListTensor) * n) != cudaSuccess ||
-        dev_malloc(&d_tile_tensor, sizeof(int32_t) * tiles) != cudaSuccess ||
-        (n > kInlineGrads && dev_malloc(&d_grads, sizeof(void*) * n) != cudaSuccess)) {
+    auto pad = [](size_t x) { return (x + 255) / 256 * 256; };
+    const size_t tensors_at = 0, extra_at = pad(sizeof(ListTensor) * n), owner_at = extra_at + pad(extra_bytes);
+    const size_t upload = owner_at + sizeof(int32_t) * tiles, grads_at = pad(upload);
+    const size_t bytes = grads_at + (n > kInlineGrads ? sizeof(void*) * n : 0);
+    std::vector<uint8_t> host(upload);
+    if (n) std::memcpy(host.data() + tensors_at, t.data(), sizeof(ListTensor) * n);
+    int32_t* owner = reinterpret_cast<int32_t*>(host.data() + owner_at);
+    for (int32_t k = 0; k < n; ++k) std::fill_n(owner + t[k].tile0, (t[k].numel + tile - 1) / tile, k);
+    if (dev_malloc(&memory, std::max<size_t>(bytes, 256)) != cudaSuccess) {
+      memory = nullptr;
       cudaGetLastError();
       return fail(MPADAM_EALLOC, "allocation of the list's tables failed");
     }
-    e = cudaMemcpy(d_tensors, t.data(), sizeof(ListTensor) * n, cudaMemcpyHostToDevice);
-    if (e == cudaSuccess) e = cudaMemcpy(d_tile_tensor, owner.data(), sizeof(int32_t) * tiles, cudaMemcpyHostToDevice);
-    if (e != cudaSuccess) return cuda_fail(e, "upload of the list's tables");
+    if (upload) {
+      e = cudaMemcpy(memory, host.data(), upload, cudaMemcpyHostToDevice);
+      // a copy from pageable memory may return before it has arrived, and steps run on any stream
+      if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);
+      if (e != cudaSuccess) return cuda_fail(e, "upload of the list's tables");
+    }
+    d_tensors = reinterpret_cast<ListTensor*>(memory + tensors_at);
+    d_tile_tensor = reinterpret_cast<int32_t*>(memory + owner_at);
+    d_grads = reinterpret_cast<const void**>(memory + grads_at);
+    extra = memory + extra_at;
     return MPADAM_OK;
   }
 
@@ -118,12 +126,10 @@ struct mpadam_adamw_state {
   AdamwKind kind;
   int32_t sms = 0;
   AdamwArgs args{};
-  ~mpadam_adamw_state() { cudaFree(args.err); }
 };
 struct mpadam_grad_norm_state {
   List list;
   NormArgs args{};
-  ~mpadam_grad_norm_state() { cudaFree(args.partial); }
 };
 
 extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32_t n, const mpadam_adamw_config* cfg,
@@ -169,18 +175,13 @@ extern "C" int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32
     std::unique_ptr<mpadam_adamw_state> s(new mpadam_adamw_state());
     s->cfg = c;
     s->list.grad_size = c.grad_dtype == MPADAM_F32 ? 4 : 2;
-    const int32_t rc = s->list.build(list, adamw_tile(c.state_dtype == MPADAM_E4M3));
+    const int32_t rc = s->list.build(list, adamw_tile(c.state_dtype == MPADAM_E4M3), sizeof(int32_t));
     if (rc) return rc;
     s->kind = {c.weight_dtype == MPADAM_F32, c.grad_dtype == MPADAM_F32, c.state_dtype == MPADAM_E4M3,
                c.rounding == MPADAM_ROUND_STOCHASTIC, c.state_rounding == MPADAM_ROUND_STOCHASTIC};
-    cudaError_t e = prepare_adamw(s->kind, &s->sms);
+    const cudaError_t e = prepare_adamw(s->kind, &s->sms);
     if (e != cudaSuccess) return cuda_fail(e, "preparing the AdamW step");
-    if (dev_malloc(&s->args.err, sizeof(int32_t)) != cudaSuccess) {
-      cudaGetLastError();
-      return fail(MPADAM_EALLOC, "allocation of the error word failed");
-    }
-    e = cudaMemset(s->args.err, 0, sizeof(int32_t));
-    if (e != cudaSuccess) return cuda_fail(e, "cudaMemset");
+    s->args.err = static_cast<int32_t*>(s->list.extra);
     s->args.tensors = s->list.d_tensors;
     s->args.tile_tensor = s->list.d_tile_tensor;
     s->args.tiles = s->list.tiles;
@@ -265,20 +266,12 @@ extern "C" int32_t mpadam_grad_norm_create(const int64_t* numel, int32_t n, int3
     }
     std::unique_ptr<mpadam_grad_norm_state> s(new mpadam_grad_norm_state());
     s->list.grad_size = grad_dtype == MPADAM_F32 ? 4 : 2;
-    int32_t rc = s->list.build(list, kNormTile);
-    NormArgs& a = s->args;
-    if (!rc) {
-      // the partial sums, and the count of CTAs behind them
-      if (dev_malloc(&a.partial, sizeof(double) * (kNormCtas + 1)) != cudaSuccess) {
-        cudaGetLastError();
-        rc = fail(MPADAM_EALLOC, "allocation of the partial sums failed");
-      } else {
-        a.done = reinterpret_cast<uint32_t*>(a.partial + kNormCtas);
-        const cudaError_t e = cudaMemset(a.done, 0, sizeof(uint32_t));
-        if (e != cudaSuccess) rc = cuda_fail(e, "cudaMemset");
-      }
-    }
+    // the partial sums, and the count of CTAs behind them
+    const int32_t rc = s->list.build(list, kNormTile, sizeof(double) * (kNormCtas + 1));
     if (rc) return rc;
+    NormArgs& a = s->args;
+    a.partial = static_cast<double*>(s->list.extra);
+    a.done = reinterpret_cast<uint32_t*>(a.partial + kNormCtas);
     a.tensors = s->list.d_tensors;
     a.tile_tensor = s->list.d_tile_tensor;
     a.tiles = s->list.tiles;
