@@ -385,6 +385,23 @@ def test_refusals():
         norm([g], out=torch.zeros(1, device="cuda"))
 
 
+def test_refused_lists():
+    """What a list's creation refuses, whatever tensor of it is at fault."""
+    ws = [torch.zeros(k, device="cuda") for k in (5, 0, 300)]
+    zeros = lambda: [torch.zeros_like(w) for w in ws]
+    args = dict(weight_dtype="f32", grad_dtype="f32", state_dtype="f32")
+    AdamW(ws, zeros(), zeros(), compute=[None, None, torch.zeros(300, device="cuda", dtype=torch.bfloat16)], **args)
+    low = AdamW.init_state(ws)
+    for m, kw in ((zeros()[:2], {}), ([*zeros()[:2], None], {}), ([*zeros()[:2], torch.zeros(300)], {}),
+                  ([*zeros()[:2], torch.zeros(600, device="cuda")[::2]], {}), ([*zeros()[:2], zeros()[2].bfloat16()], {}),
+                  (zeros(), dict(m_scales=low["m_scales"])), (zeros(), dict(compute=[None] * 2)),
+                  (zeros(), dict(compute=[None, None, torch.zeros(299, device="cuda", dtype=torch.bfloat16)]))):
+        with pytest.raises(ValueError):
+            AdamW(ws, m, zeros(), **args, **kw)
+    with pytest.raises(ValueError):
+        AdamW(ws, **{**low, "v_scales": low["v_scales"][:2]}, weight_dtype="f32", grad_dtype="f32")
+
+
 @pytest.fixture(scope="module")
 def probe(tmp_path_factory):
     from paper_2607_10611_gb300 import builder as B

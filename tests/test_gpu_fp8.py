@@ -260,6 +260,30 @@ def test_graphs_of_the_layer():
     assert x.grad is not None and w.grad is not None and z.requires_grad and not fp8.linear(x.detach(), w.detach()).requires_grad
 
 
+@pytest.mark.parametrize("xt,wt", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+def test_activations_and_weights_of_different_types(xt, wt):
+    """The result and dx have x's type, dw has w's; each rounds once from the same binary32 product."""
+    x, w, dy = _layer(40, 160, 56, 4, torch.float32)
+    x, w = x.detach().to(xt).requires_grad_(), w.detach().to(wt).requires_grad_()
+    dy = dy.to(xt)
+    y = fp8.linear(x, w)
+    dx, dw = torch.autograd.grad(y, (x, w), dy)
+    assert (y.dtype, dx.dtype, dw.dtype) == (xt, xt, wt)
+    x32, w32 = x.detach().float().requires_grad_(), w.detach().float().requires_grad_()
+    y32 = fp8.linear(x32, w32)
+    dx32, dw32 = torch.autograd.grad(y32, (x32, w32), dy.float())
+    assert torch.equal(y, y32.to(xt)) and torch.equal(dx, dx32.to(xt)) and torch.equal(dw, dw32.to(wt))
+
+
+def test_inference_mode_gives_the_same():
+    x, w, _ = _layer(24, 160, 56, 4)
+    want = fp8.linear(x, w).detach()
+    with torch.inference_mode():
+        held = fp8.quantize(w, square=True)
+        assert torch.equal(fp8.linear(x, w), want) and torch.equal(fp8.linear(x, held), want)
+        assert torch.equal(fp8.linear(x.clone(), w.clone()), want)
+
+
 def test_linear_of_no_tokens():
     x, w, dy = _layer(0, 96, 40, 1)
     for shape in ((0, 96), (2, 0, 96)):
