@@ -247,15 +247,7 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
   return __fsub_rn(c.kwd != 0.0f ? __fsub_rn(w, __fmul_rn(w, c.kwd)) : w, u);
 }
 
-// A moment's code and a weight off the fast path.  They take and give values, so that nothing of the fast path has to
-// live in memory.
-template <bool SR, bool KEEP>
-__device__ __noinline__ uint32_t slow_code(float x, float inv, uint32_t r) {
-  float y = __fmul_rn(x, inv);
-  if (SR) y = e4m3_stochastic(y, r);
-  if (KEEP && x > 0.0f) y = fmaxf(y, 0x1p-9f);
-  return e4m3x2(y, 0.0f) & 0xFFu;
-}
+// A weight off the fast path.  It takes and gives values, so that nothing of the fast path has to live in memory.
 __device__ __noinline__ float slow_weight(float w, float m, float r, float ka, float c2, float eps, float kwd) {
   const AdamwScalars c{0.0f, 0.0f, 0.0f, 0.0f, ka, c2, eps, kwd};
   return new_weight(c, w, m, r);
@@ -334,9 +326,7 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     uint32_t rnd[4];
     weight_lanes(p, gi, rnd);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)  // (finite: no look for NaN)
-      u[j] = __byte_perm(__float_as_uint(x[2 * j]) + (~rnd[j] & 0xFFFFu), __float_as_uint(x[2 * j + 1]) + 0xFFFFu - (rnd[j] >> 16),
-                         0x7632);
+    for (int j = 0; j < 4; ++j) u[j] = rs_bf16x2(x[2 * j], x[2 * j + 1], ~rnd[j]);
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) u[j] = bf16x2_rn(x[2 * j], x[2 * j + 1]);
@@ -356,30 +346,30 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
   for (int d = 1; d < 16; d <<= 1) k2 = __vmaxu2(k2, __shfl_xor_sync(~0u, k2, d));
   const int km = (k2 & 0xFFFFu) ? (int)(k2 & 0xFFFFu) - 135 : 0, kr = k2 >> 16 ? (int)(k2 >> 16) - 135 : 0;
   const float im = __uint_as_float((uint32_t)(127 - km) << 23), ir = __uint_as_float((uint32_t)(127 - kr) << 23);
-  uint32_t a[4], b[4];
-  if (STATE_SR ? (am != 0.0f && __fmul_rn(lm, im) < 0x1p-6f) || (ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-6f)
-               : ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-9f) {
+  const bool small = STATE_SR ? (am != 0.0f && __fmul_rn(lm, im) < 0x1p-6f) || (ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-6f)
+                              : ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-9f;
+  float y[8], z[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      a[j] = slow_code<STATE_SR, false>(m[2 * j], im, lanes[2 * j] & 0xFFFFu) |
-             slow_code<STATE_SR, false>(m[2 * j + 1], im, lanes[2 * j + 1] & 0xFFFFu) << 8;
-      b[j] = slow_code<STATE_SR, true>(r[2 * j], ir, lanes[2 * j] >> 16) |
-             slow_code<STATE_SR, true>(r[2 * j + 1], ir, lanes[2 * j + 1] >> 16) << 8;
+  for (int j = 0; j < 8; j += 2) {
+    unpk(mul2_rn(pk(m[j], m[j + 1]), both(im)), y[j], y[j + 1]);
+    unpk(mul2_rn(pk(r[j], r[j + 1]), both(ir)), z[j], z[j + 1]);
+  }
+  if (small) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (STATE_SR) y[j] = settle(y[j]), z[j] = settle(z[j]);
+      if (r[j] > 0.0f) z[j] = fmaxf(z[j], 0x1p-9f);  // never stored as 0
     }
-  } else {
+  }
+  uint32_t a[4], b[4];  // two codes each, in the low bytes
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float y0, y1, z0, z1;
-      unpk(mul2_rn(pk(m[2 * j], m[2 * j + 1]), both(im)), y0, y1);
-      unpk(mul2_rn(pk(r[2 * j], r[2 * j + 1]), both(ir)), z0, z1);
-      if (STATE_SR) {
-        y0 = __uint_as_float((__float_as_uint(y0) + (lanes[2 * j] & 0xFFFFu) * 16u) & ~0xFFFFFu);
-        y1 = __uint_as_float((__float_as_uint(y1) + (lanes[2 * j + 1] & 0xFFFFu) * 16u) & ~0xFFFFFu);
-        z0 = __uint_as_float((__float_as_uint(z0) + (lanes[2 * j] >> 16) * 16u) & ~0xFFFFFu);
-        z1 = __uint_as_float((__float_as_uint(z1) + (lanes[2 * j + 1] >> 16) * 16u) & ~0xFFFFFu);
-      }
-      a[j] = e4m3x2(y0, y1);
-      b[j] = e4m3x2(z0, z1);
+  for (int j = 0; j < 4; ++j) {
+    if (STATE_SR) {
+      a[j] = __byte_perm(rs_codes(y[2 * j], z[2 * j], lanes[2 * j]), rs_codes(y[2 * j + 1], z[2 * j + 1], lanes[2 * j + 1]), 0x6240);
+      b[j] = a[j] >> 16;
+    } else {
+      a[j] = e4m3x2(y[2 * j], y[2 * j + 1]);
+      b[j] = e4m3x2(z[2 * j], z[2 * j + 1]);
     }
   }
   store8_codes(h.m + in, left, vec, make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)));

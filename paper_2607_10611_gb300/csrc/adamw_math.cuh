@@ -55,4 +55,28 @@ __device__ __forceinline__ f32x2 quotient2(f32x2 a, f32x2 nd) {
   return fma2_rn(fma2_rn(nd, q, a), y, q);
 }
 
+// Stochastic rounding by the hardware's conversions: the random bits are added
+// below the result's last bit and the rest is cut off.  These two are what the
+// step defines (and what its general code computes in integers) for finite BF16
+// results, and for E4M3 ones of values up to 448 that are 0, at least 2^-6, or
+// multiples of 2^-29 below that; tested for every such value
+// (tests/test_gpu_adamw.py).  rs_bf16x2: lo by the random word's low half, hi by
+// its high half.  rs_codes: a code in byte 0 by the low half, one in byte 2 by
+// the high half; the other two bytes are 0.
+__device__ __forceinline__ uint32_t rs_bf16x2(float lo, float hi, uint32_t rnd) {
+  uint32_t d;
+  asm("cvt.rs.bf16x2.f32 %0, %1, %2, %3;" : "=r"(d) : "f"(hi), "f"(lo), "r"(rnd));
+  return d;
+}
+__device__ __forceinline__ uint32_t rs_codes(float lo, float hi, uint32_t rnd) {
+  uint32_t d;
+  asm("cvt.rs.satfinite.e4m3x4.f32 %0, {%3, %1, %3, %2}, %4;" : "=r"(d) : "f"(hi), "f"(lo), "f"(0.0f), "r"(rnd));
+  return d;
+}
+// Values below 2^-6 onto the multiples of 2^-29, as the sum with 2^-6 rounds them.
+__device__ __forceinline__ float settle(float y) {
+  const float a = fabsf(y);
+  return a < 0x1p-6f ? copysignf(__fsub_rn(__fadd_rn(a, 0x1p-6f), 0x1p-6f), y) : y;
+}
+
 }  // namespace mpadam

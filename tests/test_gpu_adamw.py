@@ -446,3 +446,22 @@ def test_quotient_is_the_correctly_rounded_one(probe):
         wrong = torch.zeros(1, dtype=torch.int64, device="cuda")
         assert probe.quotient_probe(a.data_ptr(), d.data_ptr(), n, wrong.data_ptr()) == 0
         assert int(wrong) == 0, int(wrong)
+
+
+@pytest.fixture(scope="module")
+def rounding_probe(tmp_path_factory):
+    from paper_2607_10611_gb300 import builder as B
+    out = tmp_path_factory.mktemp("rounding") / "librounding_probe.so"
+    subprocess.run([B.nvcc(), *B.NVCC_FLAGS, "-shared", str(Path(__file__).parent / "cuda" / "rounding_probe.cu"), "-o", str(out)],
+                   check=True)
+    lib = ctypes.CDLL(str(out))
+    lib.codes_probe.argtypes = lib.pairs_probe.argtypes = [ctypes.c_void_p]
+    return lib
+
+
+@pytest.mark.parametrize("which", ["codes", "pairs"])
+def test_stochastic_conversions_are_the_definition_everywhere(rounding_probe, which):
+    """Codes for every value up to 448 and pairs for every finite one."""
+    wrong = torch.zeros(1, dtype=torch.int64, device="cuda")
+    assert getattr(rounding_probe, which + "_probe")(wrong.data_ptr()) == 0
+    assert int(wrong) == 0, int(wrong)
