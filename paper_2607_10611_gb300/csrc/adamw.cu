@@ -247,21 +247,14 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
   return __fsub_rn(c.kwd != 0.0f ? __fsub_rn(w, __fmul_rn(w, c.kwd)) : w, u);
 }
 
-// A weight off the fast path.  It takes and gives values, so that nothing of the fast path has to live in memory.
-__device__ __noinline__ float slow_weight(float w, float m, float r, float ka, float c2, float eps, float kwd) {
-  const AdamwScalars c{0.0f, 0.0f, 0.0f, 0.0f, ka, c2, eps, kwd};
-  return new_weight(c, w, m, r);
-}
-
 // ---------------------------------------------------------------------------
 // The update of 8 weights with 8-bit moments, where an element has 10 bytes (with
 // BF16 weights) and instructions are the bound: the same results, bit for bit,
-// with two thirds of the instructions.  A 7B-width shard of 667 M weights, all
-// rounded stochastically, takes 2216 us (3.0 TB/s; 2970 by the general code; its
-// bytes alone would take 1003): 85 instructions an element, of which the three
-// Philox blocks of 8 elements are 22 and the widest, with the multiplier pipe busy
-// 64 % of the time, the integer pipe 51 % and 63 % of issue slots taken (packed and
-// wide instructions take two).
+// with 0.6 of the instructions.  A 7B-width shard of 667 M weights, all rounded
+// stochastically, takes 1886 us (3.5 TB/s; 2970 by the general code; its bytes
+// alone would take 1003): three quarters of issue slots are taken (packed and wide
+// instructions take two), a fourth of them by the three Philox blocks of 8
+// elements, whose wide products keep the multiplier pipe busiest.
 //
 // Two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
 // powers of two and a code's square has 8 bits, so b1 (code s) = (b1 s) code and
@@ -269,29 +262,44 @@ __device__ __noinline__ float slow_weight(float w, float m, float r, float ka, f
 // where nothing is subnormal or overflows.  Other scales, weights that are not
 // finite (as where a moment is not) and second moments from 2^32 on send the warp
 // to the general code (false).  Quotients are correctly rounded where the first
-// moment times the rate is at least 2^-100; a thread that has a smaller one beside
-// others takes the general division.
+// moment times the rate is at least 2^-100.  A smaller one's quotient is off by
+// less than 2^-99 / eps, which no weight of 2^-70 / eps or more notices: it stays
+// as the decay left it.  Smaller weights beside such moments (zeros beside zeros
+// among them, whose sign counts) send the warp to the general code, too.
 //
-// Codes of the moments: on E4M3's normal range, adding 16 random bits below the
-// grid and cutting off is two integer operations.  A thread with a non-zero value
-// below 2^-6 of its block's scale (about 1 in 500; zeros beside others count as
-// such) takes the general encoder.
+// Branches around single operations (a gradient multiplier, weight decay, weights
+// off the common range) stand before or after the loop over pairs, never in it, and
+// call nothing: 677 us of a 202 M shard's step were 631 with the rounding
+// conversions, 611 with one branch a loop, 576 without a call.
+//
+// Codes of the moments come from the rounding conversions (adamw_math.cuh).  A
+// thread with a value below 2^-6 of its block's scale (about 1 in 500; zeros count)
+// settles its values first.
 // ---------------------------------------------------------------------------
 template <bool W32, bool SR, bool STATE_SR>
 __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t left, bool vec, bool vec32,
                                             const float (&w)[8], const float (&g)[8], const float (&m0)[8],
-                                            const float (&r0)[8], uint32_t km0, uint32_t kr0, const TileHead& h,
-                                            uint32_t stage_w, int in) {
+                                            const float (&r0)[8], uint32_t km0, uint32_t kr0, const TileHead& h, int in) {
   const AdamwScalars& c = p.s;
   float m[8], r[8], x[8];
   f32x2 fin = 0;
   const float sm = scale_value(km0), sr = scale_value(kr0);
   const f32x2 b1 = both(__fmul_rn(c.b1, sm)), b2 = both(__fmul_rn(c.b2, __fmul_rn(sr, sr)));
   const f32x2 nz = p.minus_zero, mult2 = both(mult), nkwd = both(-c.kwd), nka = both(-c.ka);
+  f32x2 gs[4], bs[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) gs[j] = pk(g[2 * j], g[2 * j + 1]), bs[j] = pk(w[2 * j], w[2 * j + 1]);
+  if (p.grad_scale) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) gs[j] = mul2_rn(gs[j], mult2);
+  }
+  if (c.kwd != 0.0f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bs[j] = add2_rn(bs[j], prod2(bs[j], nkwd, nz));
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    f32x2 gg = pk(g[2 * j], g[2 * j + 1]);
-    if (p.grad_scale) gg = mul2_rn(gg, mult2);
+    const f32x2 gg = gs[j];
     const f32x2 mm = add2_rn(prod2(pk(m0[2 * j], m0[2 * j + 1]), b1, nz), prod2(gg, both(c.omb1), nz));
     const f32x2 ro = pk(r0[2 * j], r0[2 * j + 1]);
     const f32x2 vv = add2_rn(prod2(mul2_rn(ro, ro), b2, nz), prod2(mul2_rn(gg, gg), both(c.omb2), nz));
@@ -299,13 +307,11 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     unpk(mm, m[2 * j], m[2 * j + 1]);
     unpk(rr, r[2 * j], r[2 * j + 1]);
     const f32x2 nd = add2_rn(prod2(rr, both(-c.c2), nz), both(-c.eps));
-    f32x2 base = pk(w[2 * j], w[2 * j + 1]);
-    if (c.kwd != 0.0f) base = add2_rn(base, prod2(base, nkwd, nz));
+    const f32x2 base = bs[j];
     const f32x2 wn = add2_rn(base, quotient2(mul2_rn(mm, nka), nd));
     fin = fma2_rn(wn, 0ull, fin);
     unpk(wn, x[2 * j], x[2 * j + 1]);
   }
-  if (__any_sync(~0u, cert_not_finite(fin) || min(km0, kr0) < 80u || max(km0, kr0) > 150u)) return false;
   // Both blocks' exponents from the 16 lanes' maxima, as 16-bit halves of a word: 0 where all are 0, else k + 135.
   float am = 0.0f, ar = 0.0f, lm = __uint_as_float(0x7F800000u), lr = lm;
 #pragma unroll
@@ -315,12 +321,14 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
     lm = fminf(fminf(lm, fabsf(m[j])), fabsf(m[j + 1]));
     lr = fminf(fminf(lr, r[j]), r[j + 1]);
   }
-  if (am != 0.0f && __fmul_rn(lm, c.ka) < 0x1p-100f && c.ka != 0.0f) {
-    float y[8];
-    take8<W32>(stage_w, in, h.staged[0], h.w, left, vec, y);
+  bool odd = cert_not_finite(fin) || min(km0, kr0) < 80u || max(km0, kr0) > 150u;
+  if (__fmul_rn(lm, c.ka) < 0x1p-100f) {
+    float lx = fabsf(x[0]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = slow_weight(y[j], m[j], r[j], c.ka, c.c2, c.eps, c.kwd);
+    for (int j = 1; j < 8; ++j) lx = fminf(lx, fabsf(x[j]));
+    odd |= __fmul_rn(lx, c.eps) < 0x1p-70f;
   }
+  if (__any_sync(~0u, odd)) return false;
   uint32_t u[4];
   if (!W32 && SR) {
     uint32_t rnd[4];
@@ -346,8 +354,7 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
   for (int d = 1; d < 16; d <<= 1) k2 = __vmaxu2(k2, __shfl_xor_sync(~0u, k2, d));
   const int km = (k2 & 0xFFFFu) ? (int)(k2 & 0xFFFFu) - 135 : 0, kr = k2 >> 16 ? (int)(k2 >> 16) - 135 : 0;
   const float im = __uint_as_float((uint32_t)(127 - km) << 23), ir = __uint_as_float((uint32_t)(127 - kr) << 23);
-  const bool small = STATE_SR ? (am != 0.0f && __fmul_rn(lm, im) < 0x1p-6f) || (ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-6f)
-                              : ar != 0.0f && __fmul_rn(lr, ir) < 0x1p-9f;
+  const bool small = STATE_SR ? fminf(__fmul_rn(lm, im), __fmul_rn(lr, ir)) < 0x1p-6f : __fmul_rn(lr, ir) < 0x1p-9f;
   float y[8], z[8];
 #pragma unroll
   for (int j = 0; j < 8; j += 2) {
@@ -361,19 +368,20 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
       if (r[j] > 0.0f) z[j] = fmaxf(z[j], 0x1p-9f);  // never stored as 0
     }
   }
-  uint32_t a[4], b[4];  // two codes each, in the low bytes
+  uint32_t a[4], b[4];  // two codes each, in the low bytes (of b, with stochastic rounding, the high ones)
+  constexpr uint32_t kHalves = STATE_SR ? 0x7632 : 0x5410;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if (STATE_SR) {
-      a[j] = __byte_perm(rs_codes(y[2 * j], z[2 * j], lanes[2 * j]), rs_codes(y[2 * j + 1], z[2 * j + 1], lanes[2 * j + 1]), 0x6240);
-      b[j] = a[j] >> 16;
+      a[j] = b[j] = __byte_perm(rs_codes(y[2 * j], z[2 * j], lanes[2 * j]), rs_codes(y[2 * j + 1], z[2 * j + 1], lanes[2 * j + 1]),
+                                0x6240);
     } else {
       a[j] = e4m3x2(y[2 * j], y[2 * j + 1]);
       b[j] = e4m3x2(z[2 * j], z[2 * j + 1]);
     }
   }
   store8_codes(h.m + in, left, vec, make_uint2(__byte_perm(a[0], a[1], 0x5410), __byte_perm(a[2], a[3], 0x5410)));
-  store8_codes(h.v + in, left, vec, make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410)));
+  store8_codes(h.v + in, left, vec, make_uint2(__byte_perm(b[0], b[1], kHalves), __byte_perm(b[2], b[3], kHalves)));
   if ((threadIdx.x & 15) == 0 && left > 0) {
     h.m_scale[threadIdx.x >> 4] = (uint8_t)(km + 127);
     h.v_scale[threadIdx.x >> 4] = (uint8_t)(kr + 127);
@@ -502,7 +510,8 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
   const int in = threadIdx.x * 8;
   int s = 0;
   uint32_t phase = 0;
-  for (int64_t i = 0; i < count; ++i) {
+  const int n32 = (int)count;
+  for (int i = 0; i < n32; ++i) {
     if (!mbar_wait(full(s), phase)) {
       if (lane == 0) atomicOr(p.err, 2);
       return;
@@ -546,10 +555,10 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
         if (flags & 8) {  // no look at the tile's end or at alignments
           constexpr int kAll[4] = {1 << 30, 1 << 30, 1 << 30, 1 << 30};
           take_all(kAll);
-          done = fast_update<W32, SR, STATE_SR>(p, mult, gi, 8, true, true, w, g, m, v, km0, kr0, h, st + R::kOffW, in);
+          done = fast_update<W32, SR, STATE_SR>(p, mult, gi, 8, true, true, w, g, m, v, km0, kr0, h, in);
         } else {
           take_all(h.staged);
-          done = fast_update<W32, SR, STATE_SR>(p, mult, gi, left, vec, vec32, w, g, m, v, km0, kr0, h, st + R::kOffW, in);
+          done = fast_update<W32, SR, STATE_SR>(p, mult, gi, left, vec, vec32, w, g, m, v, km0, kr0, h, in);
         }
         if (done) {
           release();

@@ -174,6 +174,38 @@ def test_every_range_bit_for_bit(kw, weights):
         p.check()
 
 
+@pytest.mark.parametrize("weights", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(weight_decay=0.0), dict(), dict(eps=1.0), dict(eps=1e-30, weight_decay=0.0), dict(lr=0.0)])
+def test_small_weights_beside_small_moments_bit_for_bit(kw, weights):
+    """Zeros of either sign, subnormal and small weights, each beside gradients and moments that are zero, subnormal or
+    small: the quotient's tiny results, and the sign of what they leave."""
+    hp = {**HP, **kw}
+    p = Problem([256 * 60, 1000], weights, "f32", "e4m3", seed=12)
+    for i, n in enumerate(p.sizes):
+        w = np.exp2(p.rng.uniform(-150, 2, n)).astype(np.float32) * np.where(p.rng.random(n) < 0.5, -1, 1).astype(np.float32)
+        w[p.rng.random(n) < 0.2] = 0.0
+        w[p.rng.random(n) < 0.2] = -0.0
+        w[256 * 3:256 * 5] = np.float32(0.5)  # parts without a small weight
+        p.w[i] = w if weights == "f32" else R.bf16_value(R.bf16_nearest(w))
+        p.gw[i].copy_(torch.from_numpy(p.w[i]))
+        for codes, gpu in ((p.m[i], p.gm[i]), (p.v[i], p.gv[i])):
+            codes[p.rng.random(n) < 0.3] = 0
+            gpu.view(torch.uint8).copy_(torch.from_numpy(codes))
+    opt = p.optimizer(rounding="nearest", seed=9, **{k: v for k, v in hp.items() if k != "lr"})
+    for t in (1, 2, 3):
+        host, dev = p.grads()
+        for i, n in enumerate(p.sizes):
+            g = host[i] * np.exp2(p.rng.uniform(-130, 0, n)).astype(np.float32)
+            g[p.rng.random(n) < 0.3] = 0.0
+            host[i] = g
+            dev[i].copy_(torch.from_numpy(g))
+        opt.step(dev, t, hp["lr"])
+        p.reference_step(host, t, 9, "nearest", "stochastic", hp=hp)
+        p.check()
+        for gpu, w in zip(p.gw, p.w):
+            np.testing.assert_array_equal(np.signbit(gpu.float().cpu().numpy()), np.signbit(w))
+
+
 @pytest.mark.parametrize("decay", [0.0, 0.3])
 def test_update_in_64_bits(decay):
     """u = lr m^ / (sqrt(v^) + eps) from nine roundings of binary32 (five of them under the root or in m with at most a
