@@ -94,6 +94,19 @@ __device__ __forceinline__ void decode8(uint2 c, float (&x)[8]) {
   const uint32_t u[2] = {c.x, c.y};
   e4m3x8_to_f32(u, x);
 }
+// The squares of 8 E4M3 codes' values, exactly: one product of half-precision operands each, in binary32.
+__device__ __forceinline__ void decode8_squares(uint2 c, float (&x)[8]) {
+  const uint32_t u[2] = {c.x, c.y};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    asm("{\n .reg .b16 a, b, lo, hi;\n .reg .b32 p, q;\n mov.b32 {a, b}, %4;\n"
+        " cvt.rn.f16x2.e4m3x2 p, a;\n cvt.rn.f16x2.e4m3x2 q, b;\n"
+        " mov.b32 {lo, hi}, p;\n fma.rn.f32.f16 %0, lo, lo, 0f00000000;\n fma.rn.f32.f16 %1, hi, hi, 0f00000000;\n"
+        " mov.b32 {lo, hi}, q;\n fma.rn.f32.f16 %2, lo, lo, 0f00000000;\n fma.rn.f32.f16 %3, hi, hi, 0f00000000;\n}"
+        : "=f"(x[4 * i]), "=f"(x[4 * i + 1]), "=f"(x[4 * i + 2]), "=f"(x[4 * i + 3])
+        : "r"(u[i]));
+  }
+}
 __device__ __forceinline__ float scale_value(uint32_t scale) { return __uint_as_float(scale == 0 ? 0x00400000u : scale << 23); }
 
 // The largest finite |x| (as bits) of the 16 lanes that own a block of 128, and the block's exponent from it: the
@@ -279,7 +292,7 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
 template <bool W32, bool SR, bool STATE_SR>
 __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int64_t gi, int64_t left, bool vec, bool vec32,
                                             const float (&w)[8], const float (&g)[8], const float (&m0)[8],
-                                            const float (&r0)[8], uint32_t km0, uint32_t kr0, const TileHead& h, int in) {
+                                            const float (&q0)[8], uint32_t km0, uint32_t kr0, const TileHead& h, int in) {
   const AdamwScalars& c = p.s;
   float m[8], r[8], x[8];
   f32x2 fin = 0;
@@ -301,8 +314,7 @@ __device__ __forceinline__ bool fast_update(const AdamwArgs& p, float mult, int6
   for (int j = 0; j < 4; ++j) {
     const f32x2 gg = gs[j];
     const f32x2 mm = add2_rn(prod2(pk(m0[2 * j], m0[2 * j + 1]), b1, nz), prod2(gg, both(c.omb1), nz));
-    const f32x2 ro = pk(r0[2 * j], r0[2 * j + 1]);
-    const f32x2 vv = add2_rn(prod2(mul2_rn(ro, ro), b2, nz), prod2(mul2_rn(gg, gg), both(c.omb2), nz));
+    const f32x2 vv = add2_rn(prod2(pk(q0[2 * j], q0[2 * j + 1]), b2, nz), prod2(mul2_rn(gg, gg), both(c.omb2), nz));
     const f32x2 rr = root2(vv);
     unpk(mm, m[2 * j], m[2 * j + 1]);
     unpk(rr, r[2 * j], r[2 * j + 1]);
@@ -530,12 +542,14 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
     const int64_t gi = h.goff + in;
     uint32_t km0 = 127, kr0 = 127;
     float w[8], g[8], m[8], v[8];
-    auto take_all = [&](const int (&staged)[4]) {
+    auto take_all = [&](const int (&staged)[4], bool squares) {  // (squares: v as its codes' squares)
       take8<G32>(st + R::kOffG, in, staged[1], h.grad, left, gvec, g);
       take8<W32>(st + R::kOffW, in, staged[0], h.w, left, vec, w);
       if (LOW) {
         decode8(take8_codes(st + R::kOffM, in, staged[2], h.m, left, vec), m);
-        decode8(take8_codes(st + R::kOffV, in, staged[3], h.v, left, vec), v);
+        const uint2 codes = take8_codes(st + R::kOffV, in, staged[3], h.v, left, vec);
+        if (squares) decode8_squares(codes, v);
+        else decode8(codes, v);
         km0 = h.scales[0][threadIdx.x >> 4];
         kr0 = h.scales[1][threadIdx.x >> 4];
       } else {
@@ -554,10 +568,10 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
         bool done;
         if (flags & 8) {  // no look at the tile's end or at alignments
           constexpr int kAll[4] = {1 << 30, 1 << 30, 1 << 30, 1 << 30};
-          take_all(kAll);
+          take_all(kAll, true);
           done = fast_update<W32, SR, STATE_SR>(p, mult, gi, 8, true, true, w, g, m, v, km0, kr0, h, in);
         } else {
-          take_all(h.staged);
+          take_all(h.staged, true);
           done = fast_update<W32, SR, STATE_SR>(p, mult, gi, left, vec, vec32, w, g, m, v, km0, kr0, h, in);
         }
         if (done) {
@@ -566,7 +580,7 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
         }
       }
     }
-    take_all(h.staged);
+    take_all(h.staged, false);
     uint8_t *const hw = h.w, *const hm = h.m, *const hv = h.v, *const ms = h.m_scale, *const vs = h.v_scale;
     uint16_t* const compute = h.compute;
     if constexpr (!LOW) release();
