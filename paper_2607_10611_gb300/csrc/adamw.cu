@@ -236,17 +236,32 @@ __device__ __forceinline__ uint2 take8_codes(uint32_t stage, int in, int staged,
   return make_uint2(a[0], a[1]);
 }
 
+// Philox4x32-10 of the step's counters {lo, hi, t}.  What the first two rounds make of t alone comes with the launch,
+// so that it takes no registers: with them, fewer of the loop's values are spilled.
+__device__ __forceinline__ uint4 philox_of_step(const AdamwArgs& p, uint32_t lo, uint32_t hi) {
+  const uint64_t a = (uint64_t)lo * kPhiloxM0, c = (uint64_t)(p.round1[0] ^ hi) * kPhiloxM0;
+  const uint64_t b = (uint64_t)((uint32_t)(a >> 32) ^ p.round1[1]) * kPhiloxM1;
+  uint32_t x0 = (uint32_t)(b >> 32) ^ p.round1[2], x1 = (uint32_t)b, x2 = (uint32_t)(c >> 32) ^ (uint32_t)a ^ p.rk1[1], x3 = (uint32_t)c;
+#pragma unroll
+  for (int r = 2; r < kPhiloxRounds; ++r) {
+    const uint64_t pa = (uint64_t)x0 * kPhiloxM0, pb = (uint64_t)x2 * kPhiloxM1;
+    x0 = (uint32_t)(pb >> 32) ^ x1 ^ p.rk0[r];
+    x2 = (uint32_t)(pa >> 32) ^ x3 ^ p.rk1[r];
+    x1 = (uint32_t)pb, x3 = (uint32_t)pa;
+  }
+  return make_uint4(x0, x1, x2, x3);
+}
 // The 16 random bits of 8 weights, two to a word, and the 32 of 8 elements' moments (gi: the first one's global index).
 __device__ __forceinline__ void weight_lanes(const AdamwArgs& p, int64_t gi, uint32_t (&r)[4]) {
   const uint64_t b = (uint64_t)gi >> 3;
-  const uint4 x = philox4x32_10((uint32_t)b, (uint32_t)(b >> 32), p.t_lo, p.t_hi, p.rk0, p.rk1);
+  const uint4 x = philox_of_step(p, (uint32_t)b, (uint32_t)(b >> 32));
   r[0] = x.x, r[1] = x.y, r[2] = x.z, r[3] = x.w;
 }
 __device__ __forceinline__ void state_lanes(const AdamwArgs& p, int64_t gi, uint32_t (&r)[8]) {
   const uint64_t b = (uint64_t)gi >> 2;  // even: both blocks have the same high word
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint4 x = philox4x32_10((uint32_t)b + i, (uint32_t)(b >> 32) | 0x80000000u, p.t_lo, p.t_hi, p.rk0, p.rk1);
+    const uint4 x = philox_of_step(p, (uint32_t)b + i, (uint32_t)(b >> 32) | 0x80000000u);
     r[4 * i] = x.x, r[4 * i + 1] = x.y, r[4 * i + 2] = x.z, r[4 * i + 3] = x.w;
   }
 }
@@ -264,7 +279,7 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
 // The update of 8 weights with 8-bit moments, where an element has 10 bytes (with
 // BF16 weights) and instructions are the bound: the same results, bit for bit,
 // with 0.6 of the instructions.  A 7B-width shard of 667 M weights, all rounded
-// stochastically, takes 1886 us (3.5 TB/s; 2970 by the general code; its bytes
+// stochastically, takes 1847 us (3.6 TB/s; 2970 by the general code; its bytes
 // alone would take 1003): three quarters of issue slots are taken (packed and wide
 // instructions take two), a fourth of them by the three Philox blocks of 8
 // elements, whose wide products keep the multiplier pipe busiest.

@@ -13,6 +13,7 @@ namespace mpadam {
 // Elements per tile; a tensor's last tile may be short.  A CTA takes a tile of a
 // step (of this size by the moments' type), a warp one of the norm.
 constexpr int adamw_tile(bool state_e4m3) { return state_e4m3 ? 2816 : 3840; }
+constexpr uint32_t kPhiloxM0 = 0xD2511F53u, kPhiloxM1 = 0xCD9E8D57u;
 constexpr int kNormTile = 2048;
 constexpr int kInlineGrads = 448;    // gradient pointers that travel with one launch
 
@@ -51,7 +52,9 @@ struct AdamwArgs {
   const float* grad_scale;     // device multiplier of the gradients, or nullptr
   int32_t* err;                // device error word
   uint32_t rk0[kPhiloxRounds], rk1[kPhiloxRounds];
-  uint32_t t_lo, t_hi;
+  // the first Philox round's share of step t: the high word of t_lo M1 and t_hi, each with the round's key, and the low
+  // word with the next round's
+  uint32_t round1[3];
   GradTable g;
 };
 

@@ -225,8 +225,10 @@ extern "C" int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* g
   // r' < 2^16 on the fast path: denominators lie in [2^-100, 2^25], and quotients of 2^-100 and more are not subnormal
   s->args.plain = c.eps >= 0x1p-100f && c.eps <= 0x1p20f && q.c2 <= 0x1p8f;
   s->args.grad_scale = grad_scale;
-  s->args.t_lo = (uint32_t)(uint64_t)step;
-  s->args.t_hi = (uint32_t)((uint64_t)step >> 32);
+  const uint64_t first = (uint64_t)(uint32_t)step * kPhiloxM1;
+  s->args.round1[0] = (uint32_t)(first >> 32) ^ s->args.rk0[0];
+  s->args.round1[1] = (uint32_t)((uint64_t)step >> 32) ^ s->args.rk1[0];
+  s->args.round1[2] = (uint32_t)first ^ s->args.rk0[1];
   const cudaError_t e = launch_adamw(s->args, s->kind, s->sms, stream);
   if (e != cudaSuccess) return cuda_fail(e, "launch of the AdamW step");
   return MPADAM_OK;
