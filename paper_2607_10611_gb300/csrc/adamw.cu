@@ -278,11 +278,12 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
 // ---------------------------------------------------------------------------
 // The update of 8 weights with 8-bit moments, where an element has 10 bytes (with
 // BF16 weights) and instructions are the bound: the same results, bit for bit,
-// with 0.6 of the instructions.  A 7B-width shard of 667 M weights, all rounded
-// stochastically, takes 1847 us (3.6 TB/s; 2970 by the general code; its bytes
-// alone would take 1003): three quarters of issue slots are taken (packed and wide
-// instructions take two), a fourth of them by the three Philox blocks of 8
-// elements, whose wide products keep the multiplier pipe busiest.
+// with little more than half of the instructions.  A 7B-width shard of 667 M
+// weights, all rounded stochastically, takes 1847 us (3.6 TB/s; 2970 by the general
+// code; its bytes alone would take 1003): 71 instructions an element, of which 14
+// are the three Philox blocks of 8 elements and 14 packed.  Both take two issue
+// slots, or the multiplier pipe for two cycles: 63 % of cycles issue, and four
+// fifths of the slots are taken.
 //
 // Two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
 // powers of two and a code's square has 8 bits, so b1 (code s) = (b1 s) code and
@@ -297,8 +298,11 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
 //
 // Branches around single operations (a gradient multiplier, weight decay, weights
 // off the common range) stand before or after the loop over pairs, never in it, and
-// call nothing: 677 us of a 202 M shard's step were 631 with the rounding
-// conversions, 611 with one branch a loop, 576 without a call.
+// call nothing.  A step over 202 M weights: 677 us, with the rounding conversions
+// 631, one branch around each loop 611, no call 572, squares from half-precision
+// products 566, Philox's first rounds from the launch 561.  No gain: the root's
+// scaling folded into its neighbours, parts of tiles claimed by whichever warp is
+// free (5 % slower), tiles of 2048 to 2560 with more registers a thread.
 //
 // Codes of the moments come from the rounding conversions (adamw_math.cuh).  A
 // thread with a value below 2^-6 of its block's scale (about 1 in 500; zeros count)
