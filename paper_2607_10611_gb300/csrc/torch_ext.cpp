@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -395,8 +396,14 @@ struct LinearBackward : torch::autograd::Node {
   std::string name() const override { return "E4M3LinearBackward"; }
 };
 
+// A tangent would be lost, which forward mode takes as a derivative of zero.
+void refuse_tangent(const Tensor& t, const char* what) {
+  TORCH_CHECK(!c10::AutogradState::get_tls_state().get_fw_grad_mode() || !t._fw_grad(0).defined(), what,
+              " has a tangent: the 8-bit linear layer has no forward-mode derivative");
+}
 void check_activations(const Tensor& x) {
   TORCH_CHECK_VALUE(x.dim() >= 1 && is_real(x), "x must be a CUDA float32 or bfloat16 tensor");
+  refuse_tangent(x, "x");
 }
 
 // linear(x, w, grad_w or None) -> y
@@ -407,6 +414,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   check_activations(x);
   TORCH_CHECK_VALUE(w.dim() == 2 && is_real(w) && w.device() == x.device(), "w must be a float32 or bfloat16 matrix beside x");
   TORCH_CHECK_VALUE(w.size(1) == x.size(-1), "inner sizes differ: ", x.size(-1), " and ", w.size(1));
+  refuse_tangent(w, "w");
   c10::optional<Tensor> grad_w;
   if (a[2] != Py_None) {
     grad_w = tensor_of(a[2], "grad_w");

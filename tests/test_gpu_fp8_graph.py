@@ -1,0 +1,39 @@
+"""The 8-bit linear layer's place in torch's graph: what it refuses, what it computes when only a part of its gradients
+is asked for, what saved-tensor hooks see of it, and on which streams its results are ready."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2607_10611_gb300 import fp8  # noqa: E402
+
+
+@pytest.fixture(autouse=True)
+def waits_held():
+    yield
+    if torch.cuda.is_available():
+        assert fp8.device_status() == 0
+
+
+def _layer(tokens=24, k=96, n=40, seed=0, dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(tokens, k, generator=g).to(dtype).cuda().requires_grad_()
+    w = (0.05 * torch.randn(n, k, generator=g)).to(dtype).cuda().requires_grad_()
+    return x, w, torch.randn(tokens, n, generator=g).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("which", ["x", "w", "held"])
+def test_tangents_are_refused(which):
+    """A result without a tangent stands for a derivative of zero in forward mode."""
+    x, w, _ = _layer()
+    x, w = x.detach(), w.detach()
+    held = fp8.quantize(w, square=True)
+    want = fp8.linear(x, w)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(w if which == "w" else x, torch.ones_like(w if which == "w" else x))
+        call = {"x": lambda: fp8.linear(dual, w), "w": lambda: fp8.linear(x, dual), "held": lambda: fp8.linear(dual, held)}[which]
+        with pytest.raises(RuntimeError, match="forward"):
+            call()
+        with torch.autograd.forward_ad._set_fwd_grad_enabled(False):  # tangents are of no matter here, to torch either
+            assert torch.equal(call(), want)
+        assert torch.equal(fp8.linear(x, w), want)
