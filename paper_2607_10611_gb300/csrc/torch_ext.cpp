@@ -373,15 +373,17 @@ struct LinearBackward : torch::autograd::Node {
     TORCH_CHECK(!released, "backward through the same 8-bit linear layer a second time: give retain_graph=True the first time");
     const Tensor& dy = grads[0];
     if (!dy.defined()) return {Tensor(), Tensor()};
+    // What this pass asks for may be less than what could be had (torch.autograd.grad, inputs=): grad_w is then left alone.
+    const bool want_x = need_x && task_should_compute_output(0), want_w = need_w && task_should_compute_output(1);
     const c10::cuda::CUDAGuard guard(dy.device());
     Matrix q, qdt;
-    quantize(rows_of(dy), false, need_x ? &q : nullptr, need_w ? &qdt : nullptr);
+    quantize(rows_of(dy), false, want_x ? &q : nullptr, want_w ? &qdt : nullptr);
     Tensor dx, dw;
-    if (need_x) {
+    if (want_x) {
       dx = product(q, qwt, x_type);
       if (x_shape.size() != 2) dx = dx.view(x_shape);
     }
-    if (need_w) {
+    if (want_w) {
       if (grad_w.defined()) multiply(qdt, qt, grad_w, true);
       else dw = product(qdt, qt, w_type);
     }

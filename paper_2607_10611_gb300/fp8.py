@@ -95,8 +95,8 @@ def device_status(device=None, stream: Optional[torch.cuda.Stream] = None) -> in
 def linear(x: torch.Tensor, w: Union[torch.Tensor, E4M3Matrix], *, grad_w: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [..., k] times w [n, k] transposed, in 8 bits, [..., n] of x's type (float32 or bfloat16), on the current
     stream.  w: float32 or bfloat16, quantised in squares here, or (for serving, without gradients) an E4M3Matrix that
-    quantize(w, square=True) made once.  Differentiable once in x and w, backwards only; grad_w: a float32 [n, k] to which the
-    backward pass adds w's gradient instead of returning it."""
+    quantize(w, square=True) made once.  Differentiable once in x and w, backwards only; grad_w: a float32 [n, k] to which a
+    backward pass that asks for w's gradient adds it instead of returning it."""
     if isinstance(w, E4M3Matrix):
         if grad_w is not None:
             raise ValueError("a quantised weight passes no gradient")

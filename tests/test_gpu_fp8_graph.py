@@ -37,3 +37,36 @@ def test_tangents_are_refused(which):
         with torch.autograd.forward_ad._set_fwd_grad_enabled(False):  # tangents are of no matter here, to torch either
             assert torch.equal(call(), want)
         assert torch.equal(fp8.linear(x, w), want)
+
+
+def test_only_the_gradients_that_are_asked_for():
+    """With a buffer for w's gradient: asking for x's leaves the buffer alone, and a following pass adds once."""
+    x, w, dy = _layer(130)
+    once = torch.zeros(40, 96, device="cuda")
+    fp8.linear(x, w, grad_w=once).backward(dy)
+    total = torch.zeros(40, 96, device="cuda")
+    y = fp8.linear(x, w, grad_w=total)
+    dx, = torch.autograd.grad(y, x, dy, retain_graph=True)
+    assert torch.equal(total, torch.zeros_like(total))
+    x.grad = None
+    torch.autograd.backward(y, dy, inputs=[x], retain_graph=True)
+    assert torch.equal(total, torch.zeros_like(total)) and torch.equal(x.grad, dx)
+    y.backward(dy)
+    assert torch.equal(total, once) and torch.equal(x.grad, dx + dx)
+
+
+def test_no_product_is_made_for_a_gradient_nobody_asks_for():
+    """By the memory that a backward pass takes: dx is 32 MiB here, dw 32 KiB."""
+    x, w, dy = _layer(16384, 1024, 16)
+    for asked, other in ((w, x), (x, w)):
+        y = fp8.linear(x, w)
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        got, = torch.autograd.grad(y, asked, dy)
+        taken = torch.cuda.max_memory_allocated() - before
+        if asked is w:
+            assert taken < x.numel() * x.element_size()  # no dx
+        assert got.shape == asked.shape
+        both = torch.autograd.grad(fp8.linear(x, w), (asked, other), dy)
+        assert torch.equal(got, both[0])
