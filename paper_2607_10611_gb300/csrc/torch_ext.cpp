@@ -425,6 +425,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
                       "grad_w must be a float32 tensor of w's shape beside it");
   }
   const bool on = at::GradMode::is_enabled(), need_x = on && x.requires_grad(), need_w = on && w.requires_grad();
+  TORCH_CHECK_VALUE(!on || !grad_w || need_w, "grad_w would never be added to: w requires no gradient");
   const c10::cuda::CUDAGuard guard(x.device());
   Matrix q, qt, qw, qwt;
   Tensor y;

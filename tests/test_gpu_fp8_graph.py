@@ -70,3 +70,15 @@ def test_no_product_is_made_for_a_gradient_nobody_asks_for():
         assert got.shape == asked.shape
         both = torch.autograd.grad(fp8.linear(x, w), (asked, other), dy)
         assert torch.equal(got, both[0])
+
+
+def test_a_buffer_for_the_gradient_of_a_weight_without_one_is_refused():
+    x, w, dy = _layer()
+    total = torch.zeros(40, 96, device="cuda")
+    with pytest.raises(ValueError, match="grad_w"):
+        fp8.linear(x, w.detach(), grad_w=total)
+    with pytest.raises(ValueError, match="grad_w"):
+        fp8.linear(x.detach(), w.detach(), grad_w=total)
+    with torch.no_grad():  # nothing is differentiated here
+        assert torch.equal(fp8.linear(x, w, grad_w=total), fp8.linear(x, w.detach()))
+    assert torch.equal(total, torch.zeros_like(total))
