@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/saved_variable.h>
 
 #include <memory>
 #include <string>
@@ -232,23 +233,34 @@ struct Matrix {
   // A single row's stride is of no matter, so its codes may have any.
   int64_t ld() const { return rows() > 1 ? codes.stride(0) : (cols() + 15) / 16 * 16; }
 
+  // Where codes and scales lie in one allocation.
+  struct Layout {
+    int64_t ld, tiles, groups, scales_at, bytes;
+    Layout(int64_t rows, int64_t cols)
+        : ld((cols + 15) / 16 * 16), tiles((rows + 127) / 128), groups((cols + 511) / 512),
+          scales_at((rows * ld + 255) / 256 * 256), bytes(scales_at + tiles * groups * 512) {}
+  };
+  static Tensor view(const c10::Storage& s, at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides, int64_t offset) {
+    Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(s), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                                        c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides, offset);
+    return t;
+  }
+  // `first`: the byte of the storage that the layout begins at.
+  static Matrix over(const c10::Storage& s, int64_t first, int64_t rows, int64_t cols) {
+    const Layout l(rows, cols);
+    return {view(s, kCodes, {rows, cols}, {l.ld, 1}, first),
+            view(s, kScales, {l.tiles, l.groups, 32, 4, 4}, {l.groups * 512, 512, 16, 4, 1}, first + l.scales_at)};
+  }
   // On the current device, codes and scales in one allocation and without the dispatcher: 4 us of host as two calls of
   // at::empty and one of narrow.
   static Matrix empty(int64_t rows, int64_t cols) {
-    const int64_t ld = (cols + 15) / 16 * 16, tiles = (rows + 127) / 128, groups = (cols + 511) / 512;
-    const int64_t scales_at = (rows * ld + 255) / 256 * 256;
-    const c10::Storage storage(c10::make_intrusive<c10::StorageImpl>(c10::StorageImpl::use_byte_size_t(),
-                                                                     scales_at + tiles * groups * 512,
+    const c10::Storage storage(c10::make_intrusive<c10::StorageImpl>(c10::StorageImpl::use_byte_size_t(), Layout(rows, cols).bytes,
                                                                      c10::cuda::CUDACachingAllocator::get(), false));
-    auto view = [&](at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides, int64_t offset) {
-      Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(storage), c10::DispatchKeySet(c10::DispatchKey::CUDA),
-                                                          c10::scalarTypeToTypeMeta(type));
-      t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides, offset);
-      return t;
-    };
-    return {view(kCodes, {rows, cols}, {ld, 1}, 0),
-            view(kScales, {tiles, groups, 32, 4, 4}, {groups * 512, 512, 16, 4, 1}, scales_at)};
+    return over(storage, 0, rows, cols);
   }
+  // All of what empty() made, as one tensor.
+  Tensor bytes() const { return view(codes.storage(), at::kByte, {Layout(rows(), cols()).bytes}, {1}, 0); }
   static Matrix checked(PyObject* c, PyObject* s) {
     Matrix m{tensor_of(c, "codes"), tensor_of(s, "scales")};
     TORCH_CHECK_VALUE(m.codes.scalar_type() == kCodes && m.codes.dim() == 2 && m.codes.is_cuda(),
@@ -358,11 +370,30 @@ Tensor with_shape(const Tensor& y, const Tensor& x) {
   return y.view(shape);
 }
 
+// A matrix that the backward pass takes, kept the way torch keeps tensors: saved-tensor hooks see it, and may hold it
+// elsewhere or make it again.
+struct SavedMatrix {
+  torch::autograd::SavedVariable bytes;
+  int64_t rows = 0, cols = 0;
+  void save(const Matrix& m) {
+    bytes = torch::autograd::SavedVariable(m.bytes(), false);
+    rows = m.rows(), cols = m.cols();
+  }
+  Matrix unpack(const c10::Device& device) const {
+    const Tensor b = bytes.unpack();
+    TORCH_CHECK(b.scalar_type() == at::kByte && b.device() == device && b.dim() == 1 &&
+                    b.numel() == Matrix::Layout(rows, cols).bytes && b.is_contiguous() &&
+                    reinterpret_cast<uintptr_t>(b.const_data_ptr()) % 16 == 0,
+                "a saved-tensor hook gave the 8-bit linear layer something else back than it was given");
+    return Matrix::over(b.storage(), b.storage_offset(), rows, cols);
+  }
+};
+
 // The layer's node in the graph.  It holds what the backward pass takes as members: as a torch::autograd::Function, with a
 // context that keeps them by name, forward and backward of a small layer took 198 us of host, so 160 (torch's own
 // linear: 207).
 struct LinearBackward : torch::autograd::Node {
-  Matrix qt, qwt;  // x's transpose, w's
+  SavedMatrix qt, qwt;  // x's transpose, w's
   Tensor grad_w;
   std::vector<int64_t> x_shape;
   at::ScalarType x_type, w_type;
@@ -380,18 +411,19 @@ struct LinearBackward : torch::autograd::Node {
     quantize(rows_of(dy), false, want_x ? &q : nullptr, want_w ? &qdt : nullptr);
     Tensor dx, dw;
     if (want_x) {
-      dx = product(q, qwt, x_type);
+      dx = product(q, qwt.unpack(dy.device()), x_type);
       if (x_shape.size() != 2) dx = dx.view(x_shape);
     }
     if (want_w) {
-      if (grad_w.defined()) multiply(qdt, qt, grad_w, true);
-      else dw = product(qdt, qt, w_type);
+      const Matrix x = qt.unpack(dy.device());
+      if (grad_w.defined()) multiply(qdt, x, grad_w, true);
+      else dw = product(qdt, x, w_type);
     }
     return {dx, dw};
   }
   void release_variables() override {
-    qt = Matrix();
-    qwt = Matrix();
+    qt.bytes.reset_data();
+    qwt.bytes.reset_data();
     grad_w = Tensor();
     released = true;
   }
@@ -437,7 +469,8 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   if (need_x || need_w) {
     const std::shared_ptr<LinearBackward> node(new LinearBackward(), torch::autograd::deleteNode);
-    node->qt = qt, node->qwt = qwt;
+    if (need_w) node->qt.save(qt);
+    if (need_x) node->qwt.save(qwt);
     if (grad_w) node->grad_w = *grad_w;
     node->x_shape = x.sizes().vec();
     node->x_type = x.scalar_type(), node->w_type = w.scalar_type();

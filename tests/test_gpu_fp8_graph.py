@@ -82,3 +82,49 @@ def test_a_buffer_for_the_gradient_of_a_weight_without_one_is_refused():
     with torch.no_grad():  # nothing is differentiated here
         assert torch.equal(fp8.linear(x, w, grad_w=total), fp8.linear(x, w.detach()))
     assert torch.equal(total, torch.zeros_like(total))
+
+
+def test_saved_tensor_hooks_see_what_the_backward_pass_takes():
+    x, w, dy = _layer(512, 1000, 400)
+    want = torch.autograd.grad(fp8.linear(x, w), (x, w), dy)
+    packed = []
+
+    def pack(t):
+        packed.append(t.numel() * t.element_size())
+        return t.cpu()
+
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.cuda()):
+        y = fp8.linear(x, w)
+    held = torch.cuda.memory_allocated() - before - 512 * 400 * 2
+    assert len(packed) == 2 and sum(packed) >= 512 * 1000 + 1000 * 400  # x's and w's transposes in 8 bits
+    assert held < 4096  # nothing of them stays on the GPU
+    for _ in range(2):
+        got = torch.autograd.grad(y, (x, w), dy, retain_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with torch.autograd.graph.save_on_cpu():
+        y = fp8.linear(x, w)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, (x, w), dy), want))
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(y, (x, w), dy)
+
+
+def test_a_hook_that_gives_something_else_back_is_refused():
+    x, w, dy = _layer()
+    for other in (lambda t: t[:-1], lambda t: t.cpu(), lambda t: t.float(), lambda t: t.view(1, -1)):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, other):
+            y = fp8.linear(x, w)
+        with pytest.raises(RuntimeError, match="hook"):
+            torch.autograd.grad(y, (x, w), dy)
+
+
+def test_a_recomputed_layer_saves_nothing_and_gives_the_same():
+    x, w, dy = _layer(512, 1000, 400)
+    want = torch.autograd.grad(torch.nn.functional.gelu(fp8.linear(x, w)), (x, w), dy)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    y = torch.utils.checkpoint.checkpoint(lambda a: torch.nn.functional.gelu(fp8.linear(a, w)), x, use_reentrant=False)
+    assert torch.cuda.memory_allocated() - before < 512 * 400 * 2 + 4096
+    got = torch.autograd.grad(y, (x, w), dy)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
