@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/AutogradState.h>
+#include <c10/core/Event.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -416,8 +417,20 @@ struct LinearBackward : torch::autograd::Node {
     }
     if (want_w) {
       const Matrix x = qt.unpack(dy.device());
-      if (grad_w.defined()) multiply(qdt, x, grad_w, true);
-      else dw = product(qdt, x, w_type);
+      if (grad_w.defined()) {
+        multiply(qdt, x, grad_w, true);
+        // Torch orders streams by the gradients that nodes pass on, and this one passes none: the stream that w's would have
+        // gone to, for which the caller of backward() waits, is made to wait here.
+        const c10::Stream here = c10::cuda::getCurrentCUDAStream(dy.get_device()).unwrap();
+        const auto there = next_edge(1).function->stream();
+        if (there && *there != here) {
+          c10::Event done(c10::DeviceType::CUDA);
+          done.record(here);
+          done.block(*there);
+        }
+      } else {
+        dw = product(qdt, x, w_type);
+      }
     }
     return {dx, dw};
   }

@@ -128,3 +128,24 @@ def test_a_recomputed_layer_saves_nothing_and_gives_the_same():
     assert torch.cuda.memory_allocated() - before < 512 * 400 * 2 + 4096
     got = torch.autograd.grad(y, (x, w), dy)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_buffer_for_the_gradient_is_ready_where_the_backward_call_returns():
+    """The layer runs on another stream, which is busy, and w's place in the graph was made on this one: what reads the
+    buffer here next has to see the sum."""
+    x, w, dy = _layer(512, 1000, 400)
+    x = x.detach()
+    once = torch.zeros(400, 1000, device="cuda")
+    fp8.linear(x, w, grad_w=once).backward(dy)
+    accumulator = w.expand_as(w).grad_fn.next_functions[0][0]
+    total = torch.zeros(400, 1000, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y = fp8.linear(x, w, grad_w=total)
+        assert y.grad_fn.next_functions[1][0] is accumulator
+        torch.cuda._sleep(100_000_000)  # about 50 ms
+    y.backward(dy)
+    got = total.clone()
+    torch.cuda.synchronize()
+    assert torch.equal(got, once) and w.grad is None
