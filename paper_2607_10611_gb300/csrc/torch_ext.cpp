@@ -361,7 +361,8 @@ PyObject* py_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ---------------------------------------------------------------------------
 // x as a matrix of its last dimension, with contiguous rows.
 Tensor rows_of(const Tensor& x) {
-  const Tensor m = x.dim() == 2 ? x : x.reshape({-1, x.size(-1)});
+  // (a size of -1 would be ambiguous where there are no columns)
+  const Tensor m = x.dim() == 2 ? x : x.reshape({c10::multiply_integers(x.sizes().slice(0, x.dim() - 1)), x.size(-1)});
   return has_rows(m) ? m : m.contiguous();
 }
 Tensor with_shape(const Tensor& y, const Tensor& x) {

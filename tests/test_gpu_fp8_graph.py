@@ -149,3 +149,16 @@ def test_a_buffer_for_the_gradient_is_ready_where_the_backward_call_returns():
     got = total.clone()
     torch.cuda.synchronize()
     assert torch.equal(got, once) and w.grad is None
+
+
+@pytest.mark.parametrize("shape,n", [((2, 3, 0), 5), ((4, 0), 5), ((0,), 5), ((0, 3, 0), 5), ((2, 3, 16), 0), ((16,), 0)])
+def test_widths_of_zero(shape, n):
+    """As torch's own linear: a sum of nothing is zero, and so is its gradient."""
+    x = torch.ones(shape, device="cuda", requires_grad=True)
+    w = torch.ones(n, shape[-1], device="cuda", requires_grad=True)
+    y = fp8.linear(x, w)
+    assert y.shape == (*shape[:-1], n) and torch.equal(y, torch.zeros_like(y))
+    dx, dw = torch.autograd.grad(y, (x, w), torch.ones_like(y))
+    assert torch.equal(dx, torch.zeros_like(x)) and torch.equal(dw, torch.zeros_like(w))
+    with torch.no_grad():
+        assert torch.equal(fp8.linear(x, fp8.quantize(w, square=True)), torch.zeros_like(y))
