@@ -42,7 +42,7 @@ class E4M3Matrix:
     def row_scales(self) -> torch.Tensor:
         """Scales as float32 [rows, blocks of 128]."""
         rows, cols = self.codes.shape
-        s = self.scales.float().permute(0, 3, 2, 1, 4).reshape(self.scales.shape[0] * BLOCK, -1)
+        s = self.scales.float().permute(0, 3, 2, 1, 4).reshape(self.scales.shape[0] * BLOCK, self.scales.shape[1] * 4)
         return s[:rows, :-(-cols // BLOCK)]
 
     def dequantize(self) -> torch.Tensor:

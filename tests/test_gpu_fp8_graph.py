@@ -162,3 +162,9 @@ def test_widths_of_zero(shape, n):
     assert torch.equal(dx, torch.zeros_like(x)) and torch.equal(dw, torch.zeros_like(w))
     with torch.no_grad():
         assert torch.equal(fp8.linear(x, fp8.quantize(w, square=True)), torch.zeros_like(y))
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 5), (5, 0), (0, 0), (0, 600)])
+def test_values_of_empty_matrices(rows, cols):
+    q = fp8.quantize(torch.ones(rows, cols, device="cuda"))
+    assert q.row_scales().shape == (rows, -(-cols // 128)) and q.dequantize().shape == (rows, cols)
