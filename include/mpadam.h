@@ -583,9 +583,10 @@ int32_t mpadam_grad_norm_create(const int64_t* numel, int32_t n, int32_t grad_dt
 /* out (device, two binary32): the 2-norm over all gradients, and the
  * multiplier that clips them to max_norm (> 0; +INFINITY: never):
  * min(1, max_norm / norm), NaN when the norm is not finite.  Squares are
- * summed in binary32 within a thread and in binary64 across threads, in an
+ * summed in binary32 up to 64 at a time and in binary64 from there on, in an
  * order that depends on the list alone, so the same gradients give the same
- * bits; a gradient above about 1.8e19 overflows its square and makes the norm
+ * bits, and the norm is within 6.5 * 2^-24 of itself however many there are;
+ * a gradient above about 1.8e19 overflows its square and makes the norm
  * infinite.  Asynchronous on `stream`; one launch (lists of more than 448
  * tensors as for mpadam_adamw_step).  Errors: EINVAL, ECUDA. */
 int32_t mpadam_grad_norm(mpadam_grad_norm_state* s, const void* const* grads, float max_norm, float* out,

@@ -46,8 +46,8 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, int64_t left, b
 }
 
 // vec32: the array is on a 32-byte boundary, so that a thread's 8 values go in one access and fill a sector; vec: on a
-// 16-byte one, as views of flat buffers may be: two accesses.  GPT-2's step takes 557 us
-// in the first way, 562 in the second, 1030 in single words.
+// 16-byte one, as views of flat buffers may be: two accesses.  GPT-2's step takes 557 us in
+// the first way, 562 in the second, 1030 in single words.
 __device__ __forceinline__ void store8_f32(void* p, int64_t at, int64_t left, bool vec, bool vec32, const float (&x)[8]) {
   float* q = static_cast<float*>(p) + at;
   if (vec32 && left >= 8) {
@@ -656,9 +656,11 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
 
 // ---------------------------------------------------------------------------
 // The norm.  Each warp walks a run of tiles of 2048 elements, all of a tile's
-// loads in flight at once, and adds squares in eight binary32 sums a thread;
-// these meet in binary64, a partial sum per CTA, which the CTA that comes last
-// adds up in order.  The runs depend on the list alone, so the result's bits do.
+// loads in flight at once, and adds a tile's squares in eight binary32 sums a
+// thread, eight to each; these meet in binary64, with a partial sum per CTA, which
+// the CTA that comes last adds up in order.  (Over a whole run in binary32, small
+// squares of BF16 lost more to rounding than they gained: a norm over 4.3 10^9
+// gradients came out 2 10^-6 too small.)  The runs depend on the list alone, so the result's bits do.
 // Memory bounds it: 405 M BF16 gradients take 120 us (6.8 TB/s, 1.01 of the copy's
 // rate; by CTAs of 2048 elements in turn, a chain of loads each, 234), 4000 ragged
 // tensors of 86 M 33 (5.2 TB/s) behind 46 of the caller's look at them.
@@ -674,7 +676,7 @@ __global__ void __launch_bounds__(kNormThreads, 5) grad_norm_kernel(const __grid
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t walker = (int64_t)blockIdx.x * kNormWarps + warp, walkers = (int64_t)gridDim.x * kNormWarps;
   const int64_t t0 = p.tiles * walker / walkers, t1 = p.tiles * (walker + 1) / walkers;
-  float acc[8] = {};
+  double sum = 0.0;
   constexpr int kSize = G32 ? 4 : 2, kPer = 16 / kSize, kRow = 32 * kPer, kLoads = kNormTile / kRow;
   for (int64_t base = t0; base < t1; base += 32) {
     // Each lane looks up one of the next 32 tiles: where it starts, and how many elements it has.
@@ -691,6 +693,7 @@ __global__ void __launch_bounds__(kNormThreads, 5) grad_norm_kernel(const __grid
       const uint8_t* q = reinterpret_cast<const uint8_t*>(__shfl_sync(~0u, reinterpret_cast<uint64_t>(at), i));
       const int n = __shfl_sync(~0u, elements, i);
       const bool vec = (reinterpret_cast<uintptr_t>(q) & 15) == 0;
+      float acc[8] = {};
       // The squares of a lane's vector r.
       auto add = [&](const uint4& x, int r) {
         const uint32_t u[4] = {x.x, x.y, x.z, x.w};
@@ -738,6 +741,8 @@ __global__ void __launch_bounds__(kNormThreads, 5) grad_norm_kernel(const __grid
           for (int r = 0; r < 4; ++r) add(x[r], r);
         }
       }
+      sum += (double)__fadd_rn(__fadd_rn(__fadd_rn(acc[0], acc[1]), __fadd_rn(acc[2], acc[3])),
+                               __fadd_rn(__fadd_rn(acc[4], acc[5]), __fadd_rn(acc[6], acc[7])));
     }
   }
   auto block_sum = [&](double x) {
@@ -750,9 +755,6 @@ __global__ void __launch_bounds__(kNormThreads, 5) grad_norm_kernel(const __grid
     for (int w = 0; w < kNormWarps; ++w) x += part[w];
     return x;
   };
-  double sum = 0.0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) sum += (double)acc[j];
   const double mine = block_sum(sum);
   if (threadIdx.x == 0) {
     p.partial[blockIdx.x] = mine;

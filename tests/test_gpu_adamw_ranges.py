@@ -1,4 +1,4 @@
-"""Where the AdamW step leaves its common ranges: arrays on 16-byte boundaries."""
+"""Where the AdamW step and the norm leave their common ranges: arrays on 16-byte boundaries, long lists."""
 import numpy as np
 import pytest
 import torch
@@ -7,7 +7,7 @@ from test_gpu_adamw import HP, Problem
 
 pytestmark = pytest.mark.gpu
 
-from paper_2607_10611_gb300.adamw import AdamW  # noqa: E402
+from paper_2607_10611_gb300.adamw import AdamW, GradNorm  # noqa: E402
 
 
 @pytest.mark.parametrize("grads", ["f32", "bf16"])
@@ -42,3 +42,19 @@ def test_arrays_on_16_byte_boundaries_are_stored_in_vectors():
         times[offset] = start.elapsed_time(end)
         assert opt.device_status() == 0
     assert times[4] < 1.3 * times[0], times
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_of_a_long_list(dtype):
+    """Sixteen times the same 2^28 gradients, 4.3 10^9 in all.  Eight squares at most are added in binary32 (each with the
+    square's own rounding, fused), their eight sums in three levels, and the rest in binary64: a sum of squares within 11
+    units of 2^-24 of itself, so a norm within 6, and its own rounding to binary32, half of one."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randn(1 << 28, generator=gen, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    total = sum(float(part.double().square().sum()) for part in x.split(1 << 25)) * 16
+    norm = GradNorm([x.numel()] * 16, dtype)
+    got = norm([x] * 16, 1.0).cpu().double()
+    want = total ** 0.5
+    print(f"{dtype}: relative error {float(got[0]) / want - 1:.2e}")
+    assert abs(float(got[0]) - want) <= 6.5 * 2.0 ** -24 * want
+    assert abs(float(got[1]) - 1.0 / want) <= 7 * 2.0 ** -24 / want
