@@ -660,8 +660,8 @@ int32_t mpadam_debug_e4m3_plan(int64_t m, int64_t n, int64_t k, int32_t* plan);
 
 /* Device-side status of the products on the current device: waits for
  * `stream`, returns in *code the error bits that their kernels recorded since
- * the last read (non-zero: a bounded wait gave up, and that product's results
- * are incomplete), and clears them.  Errors: EINVAL, ECUDA. */
+ * the last read (non-zero: a bounded wait gave up, and parts of that product's
+ * d were left as they were), and clears them.  Errors: EINVAL, ECUDA. */
 int32_t mpadam_e4m3_status(struct CUstream_st* stream, int32_t* code);
 
 #ifdef __cplusplus

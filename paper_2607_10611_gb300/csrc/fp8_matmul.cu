@@ -110,6 +110,8 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
+// mbar_wait for a whole warp: false in every lane where one gave up.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(~0u, mbar_wait(bar, parity)); }
 // The address of `addr` in the cluster's CTA `rank`.
 __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
   uint32_t r;
@@ -142,6 +144,9 @@ __device__ __forceinline__ float4 lds_cluster(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
   return v;
 }
+__device__ __forceinline__ void sts_cluster(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 // Sums of all CTAs of a cluster over four neighbouring lanes, in the CTAs' order; all loads in flight at once.
 template <int SPLIT>
 __device__ __forceinline__ float4 cluster_sum(uint32_t addr) {
@@ -160,7 +165,7 @@ template <int TM, bool F32>
 __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_constant__ MatmulArgs p) {
   using S = Shape<TM>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ alignas(8) uint64_t bars[2 * S::kStages + 1];
+  __shared__ alignas(8) uint64_t bars[2 * S::kStages + 2];
   __shared__ uint32_t tmem_base_s;
   __shared__ int32_t failed;
   const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -168,7 +173,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
   const uint32_t bar0 = smem_addr(bars);
   auto full = [&](int s) { return bar0 + 8u * s; };
   auto empty = [&](int s) { return bar0 + 8u * (S::kStages + s); };
-  const uint32_t acc_full = bar0 + 8u * (2 * S::kStages);
+  const uint32_t acc_full = bar0 + 8u * (2 * S::kStages), drained = acc_full + 8;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) {
@@ -176,6 +181,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
       mbar_init(empty(s), 1);
     }
     mbar_init(acc_full, 1);
+    mbar_init(drained, 1);
     failed = 0;
     mbar_init_fence();
   }
@@ -245,19 +251,18 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
       }
     }
   } else if (warp == 1) {
-    // The whole warp walks the stages, so that addresses stay in uniform registers, and one lane issues.  After a wait
-    // that gave up it goes on without waiting; what it then computes is not used.
+    // The whole warp walks the stages, so that addresses stay in uniform registers, and one lane issues.
     const bool issue = elected();
     const uint32_t low0 = desc_low(smem);
     int s = 0;
     uint32_t phase = 0;
-    bool ok = true;
-    for (int kg = k0; kg < k1; kg += 4) {
+    int at = k1;  // the step whose operands were given up
+    for (int kg = k0; kg < at; kg += 4) {
       const uint32_t sb = tmem_scales + ((kg >> 2) & 1) * S::kScaleCols, sa = sb + 4;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (kg + j >= k1) break;
-        if (ok) ok = mbar_wait(full(s), phase);
+        if (!warp_wait(full(s), phase)) { at = kg + j; break; }
         tc_fence_after();
         if (issue) {
           const uint32_t low = low0 + s * (S::kStageBytes >> 4);
@@ -275,21 +280,31 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
         if (++s == S::kStages) { s = 0; phase ^= 1; }
       }
     }
-    if (issue) {
-      mma_commit(acc_full);
-      if (!ok) atomicOr(p.err, kErrCopy);
-    }
-    if (!ok) {
-      *stop = 1;
-      mbar_wait(acc_full, 0);  // the products in flight, before their memory goes
+    if (at == k1) {
+      if (issue) mma_commit(acc_full);
+    } else {
+      // The products and copies in flight, before their memory goes (once the products are done, the producer fills every
+      // stage again); then the epilogue is woken up to find that it has nothing to store.
+      if (issue) {
+        atomicOr(p.err, kErrCopy);
+        mma_commit(drained);
+      }
+      warp_wait(drained, 0);
+      for (const int end = min(k1, at + S::kStages); at < end; ++at) {
+        warp_wait(full(s), phase);
+        if (++s == S::kStages) { s = 0; phase ^= 1; }
+      }
+      if (issue) {
+        *stop = 1;
+        mbar_arrive(acc_full);
+      }
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2;
     constexpr int kHalf = TM / 2 >= 16 ? TM / 2 : 16;  // columns of one warp
-    if (!mbar_wait(acc_full, 0)) {
+    if (!warp_wait(acc_full, 0)) {
       if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
-    } else if (half * kHalf < TM) {
-      __syncwarp();
+    } else if (!*stop && half * kHalf < TM) {
       tc_fence_after();
       const int n = tn * kTileN + quarter * 32 + lane;
       for (int c = half * kHalf; c < half * kHalf + kHalf; c += 16) {
@@ -334,8 +349,11 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::kCols) : "memory");
   if (p.split > 1) {
+    if (threadIdx.x == 0 && *stop) {  // no sum without this CTA's share
+      for (int s = 0; s < p.split; ++s) sts_cluster(peer_addr(smem_addr(&failed), s), 1);
+    }
     cluster_sync();
-    const int width = kTileN / p.split, rows = min(TM, p.m - tm * TM);
+    const int width = kTileN / p.split, rows = *stop ? 0 : min(TM, p.m - tm * TM);
 #pragma unroll 2
     for (int e = threadIdx.x; e < rows * width / 4; e += kMatmulThreads) {
       const int j = 4 * e / width, l = rank * width + 4 * e % width, n = tn * kTileN + l;
@@ -436,6 +454,9 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
   }
   return false;
 }
+__device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity) {
+  return __all_sync(~0u, mbar_wait_cluster(bar, parity));
+}
 // 32 columns of this warp's 32 lanes.
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
   asm volatile(
@@ -501,7 +522,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
 
   const int tiles_n = (p.n + kPairTileN - 1) / kPairTileN, tiles_m = (p.m + TM - 1) / TM;
   const int tiles = tiles_n * tiles_m, pairs = gridDim.x / 2;
-  const int steps = (p.k + kTileK - 1) / kTileK, groups = (steps + 3) / 4;
+  const int steps = (p.k + kTileK - 1) / kTileK;
   volatile int32_t* stop = &failed;
 
   if (warp == 0) {
@@ -545,21 +566,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
     const uint32_t low0 = desc_low(smem);
     int s = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
-    bool ok = true;
-    for (int t = blockIdx.x / 2; t < tiles; t += pairs) {
-      if (ok) ok = mbar_wait_cluster(acc_free(acc), acc_phase ^ 1);
+    int t = blockIdx.x / 2, at = steps;  // the tile, and its step whose operands were given up
+    for (; t < tiles; t += pairs) {
+      if (!warp_wait_cluster(acc_free(acc), acc_phase ^ 1)) { at = 0; break; }
       tc_fence_after();
       const uint32_t d = tmem + acc * TM;
       int tm, tn;
       pair_place(t, tiles_m, tiles_n, tm, tn);
       const uint32_t col = (uint32_t)(tm * TM % 128) / 32;  // 0 or 2
-      for (int g = 0; g < groups; ++g) {
+      for (int g = 0; 4 * g < at; ++g) {
         const uint32_t sb = tmem + S::kAccs * TM + (g & 1) * S::kScaleCols, sa = sb + 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int k = 4 * g + j;
           if (k >= steps) break;
-          if (ok) ok = mbar_wait(full(s), phase);
+          if (!warp_wait(full(s), phase)) { at = k; break; }
           tc_fence_after();
           if (issue) {
             const uint32_t low = low0 + s * (S::kStageBytes >> 4);
@@ -581,16 +602,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
           if (++s == kPairStages) { s = 0; phase ^= 1; }
         }
       }
+      if (at < steps) break;
       if (issue) pair_commit(acc_full(acc));
       if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
     }
-    if (!ok) {  // the products in flight, before their memory goes
-      *stop = 1;
+    if (at < steps) {
+      // As in matmul_kernel, for both CTAs: their copies arrive here.
       if (issue) {
         atomicOr(p.err, kErrCopy);
         pair_commit(drained);
       }
-      mbar_wait(drained, 0);
+      warp_wait(drained, 0);
+      const int64_t left = (int64_t)((tiles - 1 - t) / pairs) * steps + steps - at;
+      for (int i = 0; i < (int)min(left, (int64_t)kPairStages); ++i) {
+        warp_wait(full(s), phase);
+        if (++s == kPairStages) { s = 0; phase ^= 1; }
+      }
+      if (issue) {
+        for (uint32_t r = 0; r < 2; ++r) {
+          sts_cluster(peer_addr(smem_addr(&failed), r), 1);
+          mbar_arrive_cluster(peer_addr(acc_full(acc), r));
+        }
+      }
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -598,11 +631,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int t = blockIdx.x / 2; t < tiles; t += pairs) {
-      if (*stop || !mbar_wait_cluster(acc_full(acc), acc_phase)) {
+      if (!warp_wait_cluster(acc_full(acc), acc_phase) || *stop) {
         if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
         break;
       }
-      __syncwarp();
       tc_fence_after();
       int tm, tn;
       pair_place(t, tiles_m, tiles_n, tm, tn);
