@@ -291,8 +291,8 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
 //
 // Two elements at a time.  Old codes' scales go into beta1 and beta2: scales are
 // powers of two and a code's square has 8 bits, so b1 (code s) = (b1 s) code and
-// b2 (code s)^2 = (b2 s^2) code^2 bit for bit, for scales from 2^-47 to 2^23,
-// where nothing is subnormal or overflows.  Other scales, weights that are not
+// b2 (code s)^2 = (b2 s^2) code^2 bit for bit, for scales from 2^-47 to 2^23
+// and betas of 0 or at least 2^-30, where nothing is subnormal or overflows.  Other scales, weights that are not
 // finite (as where a moment is not) and second moments from 2^32 on send the warp
 // to the general code (false).  Quotients are correctly rounded where the first
 // moment times the rate is at least 2^-100.  A smaller one's quotient is off by

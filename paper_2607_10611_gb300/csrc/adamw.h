@@ -48,7 +48,7 @@ struct AdamwArgs {
   int64_t tiles;
   AdamwScalars s;
   uint64_t minus_zero;         // two binary32 -0 (see prod2)
-  int32_t plain;               // denominators are in quotient2's range (see fast_update)
+  int32_t plain;               // eps and betas are in fast_update's range
   const float* grad_scale;     // device multiplier of the gradients, or nullptr
   int32_t* err;                // device error word
   uint32_t rk0[kPhiloxRounds], rk1[kPhiloxRounds];

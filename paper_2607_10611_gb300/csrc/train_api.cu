@@ -223,7 +223,9 @@ extern "C" int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* g
   q.eps = c.eps;
   q.kwd = (float)((double)lr * (double)c.weight_decay);
   // r' < 2^16 on the fast path: denominators lie in [2^-100, 2^25], and quotients of 2^-100 and more are not subnormal
-  s->args.plain = c.eps >= 0x1p-100f && c.eps <= 0x1p20f && q.c2 <= 0x1p8f;
+  // betas of 2^-30 and more keep all their bits when old scales (2^-47 at least; the root's enters squared) go into them
+  auto holds = [](float beta) { return beta == 0.0f || beta >= 0x1p-30f; };
+  s->args.plain = c.eps >= 0x1p-100f && c.eps <= 0x1p20f && q.c2 <= 0x1p8f && holds(c.beta1) && holds(c.beta2);
   s->args.grad_scale = grad_scale;
   const uint64_t first = (uint64_t)(uint32_t)step * kPhiloxM1;
   s->args.round1[0] = (uint32_t)(first >> 32) ^ s->args.rk0[0];

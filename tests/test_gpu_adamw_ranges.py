@@ -1,4 +1,4 @@
-"""Where the AdamW step and the norm leave their common ranges: arrays on 16-byte boundaries, long lists."""
+"""Where the AdamW step and the norm leave their common ranges: arrays on 16-byte boundaries, long lists, small betas."""
 import numpy as np
 import pytest
 import torch
@@ -58,3 +58,23 @@ def test_norm_of_a_long_list(dtype):
     print(f"{dtype}: relative error {float(got[0]) / want - 1:.2e}")
     assert abs(float(got[0]) - want) <= 6.5 * 2.0 ** -24 * want
     assert abs(float(got[1]) - 1.0 / want) <= 7 * 2.0 ** -24 / want
+
+
+@pytest.mark.parametrize("kw", [dict(beta1=0.5, beta2=1.234567e-12, eps=1e-30), dict(beta1=0.5, beta2=3e-11, eps=1e-30),
+                                dict(beta1=0.5, beta2=2.0 ** -30, eps=1e-30), dict(beta2=1e-30, eps=1e-30), dict(beta1=1e-30), dict(beta1=2.0 ** -81), dict(beta1=2.0 ** -30),
+                                dict(beta1=1e-38, beta2=1e-38)])
+def test_small_betas_bit_for_bit(kw):
+    """Old scales down to 2^-47 times betas that make the product subnormal: gradients of the first step put the scales
+    there, the second step's are zero, so that all there is comes of the decayed moments."""
+    hp = {**HP, "weight_decay": 0.0, **kw}
+    p = Problem([128 * 48, 1000], "f32", "f32", "e4m3", seed=21)
+    opt = p.optimizer(seed=3, **{k: v for k, v in hp.items() if k != "lr"})
+    for t in (1, 2, 3):
+        host, dev = p.grads()
+        for i, n in enumerate(p.sizes):
+            scale = np.exp2(-np.arange(-(-n // 128)) % 44.0).repeat(128)[:n] if t == 1 else np.zeros(n)
+            host[i] = (host[i] * scale).astype(np.float32)
+            dev[i].copy_(torch.from_numpy(host[i]))
+        opt.step(dev, t, hp["lr"])
+        p.reference_step(host, t, 3, "nearest", "stochastic", hp=hp)
+        p.check()
