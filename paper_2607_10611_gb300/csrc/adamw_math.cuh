@@ -38,7 +38,8 @@ __device__ __forceinline__ f32x2 root2(f32x2 v) {
 }
 
 // a / d rounded correctly, for nd = -d with d in [2^-100, 2^100], and a = 0 or
-// |a| >= 2^-100, in the same paper's way: y, the reciprocal after one Newton
+// |a| >= 2^-100 with a quotient that is neither subnormal nor too large (a
+// quotient that overflows comes out as no finite value), in the same paper's way: y, the reciprocal after one Newton
 // step, is the correctly rounded one (tested for every mantissa,
 // tests/test_gpu_adamw.py); a quotient within one unit that is corrected with its
 // exact remainder and such a reciprocal then is too.  Six instructions for two

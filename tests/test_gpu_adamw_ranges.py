@@ -1,9 +1,10 @@
-"""Where the AdamW step and the norm leave their common ranges: arrays on 16-byte boundaries, long lists, small betas."""
+"""Where the AdamW step and the norm leave their common ranges: arrays on 16-byte boundaries, long lists, small betas,
+quotients at either end."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_adamw import HP, Problem
+from test_gpu_adamw import HP, Problem, probe  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +79,24 @@ def test_small_betas_bit_for_bit(kw):
         opt.step(dev, t, hp["lr"])
         p.reference_step(host, t, 3, "nearest", "stochastic", hp=hp)
         p.check()
+
+
+@pytest.mark.parametrize("near", [False, True])
+def test_quotients_over_the_whole_range_of_the_step(probe, near):
+    """Denominators in [2^-100, 2^25), numerators from 2^-100 up to where the quotient is still below 2^127; near: mantissas
+    at either end, where quotients come closest to ties."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    n = 1 << 26
+    below = lambda top: (torch.rand(n, generator=g, device="cuda", dtype=torch.float64) * top).to(torch.int32)
+
+    def value(exponent):
+        mantissa = torch.where(below(2) == 1, below(64), (1 << 23) - 1 - below(64)) if near else below(1 << 23)
+        return ((exponent + 127) << 23 | mantissa).view(torch.float32)
+
+    e = below(125) - 100
+    top = (e + 125).clamp(max=126)
+    a, d = value(-100 + below(top + 101)), value(e)
+    assert float(a.min()) >= 2.0 ** -100 and float((a.double() / d.double()).min()) >= 2.0 ** -126
+    wrong = torch.zeros(1, dtype=torch.int64, device="cuda")
+    assert probe.quotient_probe(a.data_ptr(), d.data_ptr(), n, wrong.data_ptr()) == 0
+    assert int(wrong) == 0, int(wrong)
