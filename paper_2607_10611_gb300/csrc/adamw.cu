@@ -17,6 +17,14 @@ namespace {
 
 __device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// mbar_wait for a whole warp, which goes on or leaves with all its lanes.  (With the vote behind the lanes' loops, a 7B-width
+// shard's step in 8 bits takes 1906 us, so 1851, with waits of each lane for itself 1845.)
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kSpinLimit; ++i)
+    if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
+  return false;
+}
+
 __device__ __forceinline__ const void* grad_of(const GradTable& g, int k) { return g.grads ? g.grads[k] : g.inline_grads[k]; }
 
 // 8 values at p[at ..], `left` of them inside; whole and aligned ones in vector loads.
@@ -497,7 +505,7 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
           vs = reinterpret_cast<const uint8_t*>(vp)[lane];
         }
       }
-      if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
+      if (!warp_wait(empty(s), phase ^ 1)) { ok = false; break; }
       TileHead& h = *reinterpret_cast<TileHead*>(ring + s * R::kBytes);
       if (LOW) {
         h.scales[0][lane] = (uint8_t)ms;
@@ -547,7 +555,7 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
   uint32_t phase = 0;
   const int n32 = (int)count;
   for (int i = 0; i < n32; ++i) {
-    if (!mbar_wait(full(s), phase)) {
+    if (!warp_wait(full(s), phase)) {
       if (lane == 0) atomicOr(p.err, 2);
       return;
     }
