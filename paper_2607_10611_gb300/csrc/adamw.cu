@@ -18,7 +18,7 @@ namespace {
 __device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // mbar_wait for a whole warp, which goes on or leaves with all its lanes.  (With the vote behind the lanes' loops, a 7B-width
-// shard's step in 8 bits takes 1906 us, so 1851, with waits of each lane for itself 1845.)
+// shard's step in 8 bits takes 1906 us, so 1845.)
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
   for (uint32_t i = 0; i < kSpinLimit; ++i)
     if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
@@ -557,6 +557,11 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
   for (int i = 0; i < n32; ++i) {
     if (!warp_wait(full(s), phase)) {
       if (lane == 0) atomicOr(p.err, 2);
+      // the copies in flight, before the block's memory goes: the producer may be done, with every stage filled
+      for (int n = min(n32 - i, R::kStages); n > 0; --n) {
+        warp_wait(full(s), phase);
+        if (++s == R::kStages) { s = 0; phase ^= 1; }
+      }
       return;
     }
     const TileHead& h = *reinterpret_cast<const TileHead*>(ring + s * R::kBytes);

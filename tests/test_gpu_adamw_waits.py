@@ -70,3 +70,29 @@ def test_a_warp_gives_up_as_a_whole(probe, state, lane):
                 assert np.array_equal(got[at], old.cpu().numpy()[at])
                 got[at] = want[at]
             assert np.array_equal(got, want)
+
+
+def test_a_warp_that_gives_up_waits_for_the_stages_ahead(probe):
+    """200 tensors of one tile on 152 CTAs: block 1 has tiles 1 and 153 in its ring when its third warp gives up, and leaves
+    both; everything else is stepped."""
+    from paper_2607_10611_gb300 import _native as N
+    n, count = 1000, 200
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert sms < count - 1 < 2 * sms
+    w, m, v, g = (torch.full((count, 1024), x, device="cuda") for x in (0.5, 0.0, 0.0, 1.0))
+    rows = [N.mpadam_adamw_tensor(w[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr(), None, None, None, n) for i in range(count)]
+    cfg = N.mpadam_adamw_config(0.9, 0.999, 1e-8, 0.0, N.MPADAM_F32, N.MPADAM_F32, N.MPADAM_F32, 0, 0, 0, 0)
+    state, code = ctypes.c_void_p(), ctypes.c_int32()
+    assert probe.mpadam_adamw_create((N.mpadam_adamw_tensor * count)(*rows), count, ctypes.addressof(cfg), ctypes.byref(state)) == 0
+    try:
+        assert probe.give_up(1, 2, 7, 0) == 0
+        pointers = (ctypes.c_void_p * count)(*[x.data_ptr() for x in g])
+        assert probe.mpadam_adamw_step(state, pointers, 1, 0.25, None, torch.cuda.current_stream().cuda_stream) == 0
+        assert probe.mpadam_adamw_status(state, ctypes.byref(code)) == 0 and code.value == 2
+    finally:
+        probe.give_up(-1, 0, 0, 0)
+        probe.mpadam_adamw_destroy(state)
+    left = torch.zeros(count, 1024, dtype=torch.bool, device="cuda")
+    left[:, n:] = True
+    left[[1, 1 + sms], 512:768] = True
+    assert torch.equal(w == 0.5, left) and torch.equal(m == 0.0, left) and torch.equal(v == 0.0, left)
