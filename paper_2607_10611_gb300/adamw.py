@@ -69,11 +69,13 @@ class AdamW:
 
     def device_status(self) -> int:
         """Device error bits of the steps so far (0 = none); synchronises."""
-        return N.mpadam_adamw_status(self.state)
+        with torch.cuda.device(self.device):
+            return N.mpadam_adamw_status(self.state)
 
     def close(self):
         if getattr(self, "state", None):
-            N.mpadam_adamw_destroy(self.state)
+            with torch.cuda.device(self.device):
+                N.mpadam_adamw_destroy(self.state)
             self.state = None
 
     def __del__(self):
@@ -107,7 +109,8 @@ class GradNorm:
 
     def close(self):
         if getattr(self, "state", None):
-            N.mpadam_grad_norm_destroy(self.state)
+            with torch.cuda.device(self.device):
+                N.mpadam_grad_norm_destroy(self.state)
             self.state = None
 
     def __del__(self):
