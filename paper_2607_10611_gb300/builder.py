@@ -108,6 +108,7 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    EXT_TORCH.unlink(missing_ok=True)  # until EXT is linked against this LIB, the build is not done
     os.replace(tmp, LIB)
     tmp = OUT_DIR / f".mpadam_torch.{os.getpid()}.so"
     cmd = [os.environ.get("CXX", "g++"), "-shared", "-o", str(tmp), str(ext_obj), f"-L{_torch_dir() / 'lib'}",

@@ -35,3 +35,35 @@ def test_a_handles_calls_are_made_on_its_own_device(monkeypatch, devices):
     opt.close()  # once is enough
     assert seen == [("mpadam_adamw_status", 11, 1), ("mpadam_adamw_destroy", 11, 1), ("mpadam_grad_norm_destroy", 12, 2)]
     assert opt.state is None and norm.state is None
+
+
+def test_a_failed_link_of_the_torch_module_is_not_a_finished_build(monkeypatch, tmp_path):
+    """An older module beside a new library would read the library's structs by their old layout."""
+    from pathlib import Path
+    from types import SimpleNamespace
+    from paper_2607_10611_gb300 import builder as B
+    for name, file in (("OUT_DIR", "."), ("LIB", B.LIB.name), ("EXT", B.EXT.name), ("EXT_TORCH", B.EXT_TORCH.name)):
+        monkeypatch.setattr(B, name, tmp_path / file)
+    state = {"fails": False, "made": 0}
+
+    def run(cmd, **kw):
+        out = Path(cmd[cmd.index("-o") + 1])
+        if state["fails"] and "-ltorch_python" in cmd:
+            return SimpleNamespace(returncode=1, stdout="", stderr="no space left")
+        state["made"] += 1
+        out.write_text(str(state["made"]))
+        return SimpleNamespace(returncode=0, stdout="", stderr="")
+
+    monkeypatch.setattr(B.subprocess, "run", run)
+    B.build()
+    assert not B.needs_build()
+    old = B.EXT.read_text()
+    state["fails"] = True
+    with pytest.raises(RuntimeError, match="no space left"):
+        B.build(force=True)
+    assert B.EXT.read_text() == old and B.needs_build()
+    with pytest.raises(RuntimeError, match="no space left"):
+        B.build()
+    state["fails"] = False
+    B.build()
+    assert B.EXT.read_text() != old and not B.needs_build()
