@@ -47,13 +47,15 @@ struct List {
     n = (int32_t)t.size();
     int64_t goff = 0;
     for (auto& x : t) {
+      // checked before it is rounded up, and the sum after each: nothing here overflows
+      const int64_t own = x.numel <= (int64_t)INT32_MAX * tile ? (x.numel + tile - 1) / tile : INT32_MAX;
+      if (tiles + own >= INT32_MAX) return fail(MPADAM_EINVAL, "the list has too many elements");
       x.goff = goff;
       x.tile0 = tiles;
       goff += (x.numel + 127) / 128 * 128;
-      tiles += (x.numel + tile - 1) / tile;
+      tiles += own;
       numel.push_back(x.numel);
     }
-    if (tiles >= INT32_MAX) return fail(MPADAM_EINVAL, "the list has too many elements");
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
     auto pad = [](size_t x) { return (x + 255) / 256 * 256; };

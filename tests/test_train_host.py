@@ -67,3 +67,20 @@ def test_a_failed_link_of_the_torch_module_is_not_a_finished_build(monkeypatch, 
     state["fails"] = False
     B.build()
     assert B.EXT.read_text() != old and not B.needs_build()
+
+
+TOP = (1 << 63) - 1
+
+
+@pytest.mark.parametrize("sizes", [[TOP], [TOP - 500], [5, TOP - 3000], [1 << 62] * 3, [TOP - 3000, 1 << 62, 5],
+                                   [(1 << 31) * 4000], [1 << 41] * 8, [-(-TOP // 4), -(-TOP // 4), -(-TOP // 4), -(-TOP // 4), 7]])
+def test_sizes_that_no_list_can_have_are_refused(sizes):
+    """Before any arithmetic on them could overflow."""
+    from paper_2607_10611_gb300 import _native as N, build
+    build()
+    cfg = N.mpadam_adamw_config(0.9, 0.999, 1e-8, 0.0, N.MPADAM_BF16, N.MPADAM_F32, N.MPADAM_E4M3, 0, 0, 0, 0)
+    for create in (lambda: N.mpadam_grad_norm_create(sizes, N.MPADAM_F32),
+                   lambda: N.mpadam_adamw_create([(0x1000, 0x2000, 0x3000, 0x4000, 0x5000, 0, n) for n in sizes], cfg)):
+        with pytest.raises(N.MPAdamError) as e:
+            create()
+        assert e.value.status == N.MPADAM_EINVAL and "too many elements" in str(e.value)
