@@ -168,3 +168,15 @@ def test_widths_of_zero(shape, n):
 def test_values_of_empty_matrices(rows, cols):
     q = fp8.quantize(torch.ones(rows, cols, device="cuda"))
     assert q.row_scales().shape == (rows, -(-cols // 128)) and q.dequantize().shape == (rows, cols)
+
+
+@pytest.mark.parametrize("tokens,k,n", [(129, 512, 700), (300, 130, 257), (1500, 1000, 2600), (4096, 256, 1100)])
+def test_prompts_through_a_held_weight(tokens, k, n):
+    """More tokens than one tile of a, by single CTAs and by pairs: bit for bit what the weight itself gives."""
+    x, w, _ = _layer(tokens, k, n, 5)
+    with torch.no_grad():
+        held = fp8.quantize(w, square=True)
+        want = fp8.linear(x, w)
+        assert torch.equal(fp8.linear(x, held), want)
+        assert torch.equal(fp8.linear(x.view(1, tokens, k), held), want[None])
+        assert torch.equal(fp8.linear(x[3:4], held), want[3:4])
