@@ -548,7 +548,9 @@ typedef struct {
 typedef struct mpadam_adamw_state mpadam_adamw_state;
 
 /* Copies the list, validates, and uploads its tables (synchronously, on the
- * current device).  Errors: EINVAL, EALLOC, ECUDA.  On error *out is NULL. */
+ * current device): 0.13 ms for 98 tensors and 0.9 for 4000, so a state is for
+ * a list that many steps take.  Errors: EINVAL, EALLOC, ECUDA.  On error *out
+ * is NULL. */
 int32_t mpadam_adamw_create(const mpadam_adamw_tensor* tensors, int32_t n, const mpadam_adamw_config* cfg,
                             mpadam_adamw_state** out);
 
@@ -564,8 +566,9 @@ int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* grads, int64
 
 /* Device-side status of the steps issued so far: synchronises the device,
  * returns in *code the error bits that they recorded (0 = none; non-zero: a
- * bounded wait gave up, and that step's results are incomplete) and clears
- * them.  Errors: EINVAL, ECUDA. */
+ * bounded wait gave up, and some of that step's elements were left as they
+ * were) and clears them.  Nothing else tells of it: ask now and then.  Errors:
+ * EINVAL, ECUDA. */
 int32_t mpadam_adamw_status(mpadam_adamw_state* s, int32_t* code);
 
 /* Synchronises the device and frees the library's tables; NULL is a no-op. */
@@ -576,8 +579,9 @@ int32_t mpadam_adamw_destroy(mpadam_adamw_state* s);
  * ------------------------------------------------------------------------ */
 typedef struct mpadam_grad_norm_state mpadam_grad_norm_state;
 
-/* For a list of n tensors of numel[k] gradients each.  Errors: EINVAL,
- * EALLOC, ECUDA.  On error *out is NULL. */
+/* For a list of n tensors of numel[k] gradients each; costs about what
+ * mpadam_adamw_create does.  Errors: EINVAL, EALLOC, ECUDA.  On error *out is
+ * NULL. */
 int32_t mpadam_grad_norm_create(const int64_t* numel, int32_t n, int32_t grad_dtype, mpadam_grad_norm_state** out);
 
 /* out (device, two binary32): the 2-norm over all gradients, and the
@@ -624,7 +628,11 @@ int32_t mpadam_e4m3_quantize(const void* x, int32_t x_dtype, int64_t rows, int64
 /* d[m, n] = a b^T, or d += a b^T (accumulate != 0; binary32 d only), for a [m, k]
  * and b [n, k] stored as above: sums over k of the codes' products times both
  * scales in binary32 on the tensor cores, rounded once into d (d_dtype
- * MPADAM_F32 or MPADAM_BF16, row stride ldd >= n elements).  k = 0 gives 0.
+ * MPADAM_F32 or MPADAM_BF16, row stride ldd >= n elements).  The tensor cores
+ * add 32 values of k at a time, each time with at most one rounding or
+ * truncation of the sum and of the aligned addends: a sum is within
+ * (2 ceil(k / 32) + 1) 2^-23 of the sum of its addends' magnitudes, and the same
+ * from call to call.  k = 0 gives 0.
  * m, n, k <= 2^31 - 1024.  Asynchronous on `stream`.  Errors: EINVAL, EUNSUPPORTED (no
  * driver entry for tensor maps), ECUDA. */
 typedef struct {
@@ -661,7 +669,8 @@ int32_t mpadam_debug_e4m3_plan(int64_t m, int64_t n, int64_t k, int32_t* plan);
 /* Device-side status of the products on the current device: waits for
  * `stream`, returns in *code the error bits that their kernels recorded since
  * the last read (non-zero: a bounded wait gave up, and parts of that product's
- * d were left as they were), and clears them.  Errors: EINVAL, ECUDA. */
+ * d were left as they were), and clears them.  Nothing else tells of it.
+ * Errors: EINVAL, ECUDA. */
 int32_t mpadam_e4m3_status(struct CUstream_st* stream, int32_t* code);
 
 #ifdef __cplusplus

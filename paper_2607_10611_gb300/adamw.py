@@ -86,7 +86,8 @@ class AdamW:
 
 
 class GradNorm:
-    """The global 2-norm of a list of gradients with the given sizes, and the multiplier that clips them."""
+    """The global 2-norm of a list of gradients with the given sizes, and the multiplier that clips them.  Its partial
+    sums are the object's, so calls on several streams have to be ordered, as AdamW's have to be."""
 
     def __init__(self, numels: Sequence[int], grad_dtype: str = "bf16", device: Optional[torch.device] = None):
         self.numels = [int(n) for n in numels]

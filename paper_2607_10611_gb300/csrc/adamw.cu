@@ -292,7 +292,7 @@ __device__ __forceinline__ float new_weight(const AdamwScalars& c, float w, floa
 // BF16 weights) and instructions are the bound: the same results, bit for bit,
 // with little more than half of the instructions.  A 7B-width shard of 667 M
 // weights, all rounded stochastically, takes 1847 us (3.6 TB/s; 2970 by the general
-// code; its bytes alone would take 1003): 71 instructions an element, of which 14
+// code; its bytes alone would take 1003): 70 instructions an element, of which 14
 // are the three Philox blocks of 8 elements and 14 packed.  Both take two issue
 // slots, or the multiplier pipe for two cycles: 63 % of cycles issue, and four
 // fifths of the slots are taken.
@@ -673,7 +673,8 @@ __global__ void __launch_bounds__(StepShape<LOW>::kThreads, StepShape<LOW>::kCta
 // thread, eight to each; these meet in binary64, with a partial sum per CTA, which
 // the CTA that comes last adds up in order.  (Over a whole run in binary32, small
 // squares of BF16 lost more to rounding than they gained: a norm over 4.3 10^9
-// gradients came out 2 10^-6 too small.)  The runs depend on the list alone, so the result's bits do.
+// gradients came out 2 10^-6 too small.)  The runs depend on the list alone, so the
+// result's bits do.
 // Memory bounds it: 405 M BF16 gradients take 120 us (6.8 TB/s, 1.01 of the copy's
 // rate; by CTAs of 2048 elements in turn, a chain of loads each, 234), 4000 ragged
 // tensors of 86 M 33 (5.2 TB/s) behind 46 of the caller's look at them.

@@ -752,8 +752,10 @@ MatmulPlan matmul_plan(int64_t m, int64_t n, int64_t k) {
   // Pairs of CTAs from 40 tiles of 256 x 256 on, about half of what runs at once (36 tiles, 1023 x 2304 x 768: 8.2 us
   // by pairs, 6.8 by single CTAs; 40, 1280 x 2048 x 4096: 15.0 and 15.9; 43, 256 x 11008 x 4096: 17.3 and 19.2).  Else
   // tiles of 128 x up to 128, a tile's k shared out among CTAs while all of them run at once with one an SM: an SM takes
-  // in about 60 GB/s, so idle ones cost (1 x 4096 x 4096 10.3 us by 32 CTAs, 6.2 by 128), but with a second CTA on some
-  // SMs the others wait (1024 x 2048 x 2048 8.9 us by 128, 12.3 by 256).
+  // in about 60 GB/s, so idle ones cost (1 x 4096 x 4096 10.3 us by 32 CTAs, 6.2 by 128), but with a second CTA on many
+  // SMs the others wait (1024 x 2048 x 2048 8.9 us by 128, 12.3 by 256).  Eight SMs with two are worth it up to 64 rows of
+  // a or with a long k: 1 x 5120 x 4096 6.1 us by 160 CTAs, 7.4 by 80; 1 x 10240 x 4096 7.8 and 9.5; 128 x 10240 x 11008
+  // 28.7 and 35.9; they cost where sums of 128 rows are joined after a short k (128 x 2560 x 4096 11.1 and 7.9).
   const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
   if (m > 128 && large >= 40) return {pair_tile(m, n, k), 1, true};
   const int tile = m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
