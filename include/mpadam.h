@@ -673,6 +673,94 @@ int32_t mpadam_debug_e4m3_plan(int64_t m, int64_t n, int64_t k, int32_t* plan);
  * Errors: EINVAL, ECUDA. */
 int32_t mpadam_e4m3_status(struct CUstream_st* stream, int32_t* code);
 
+/* ------------------------------------------------------------------------
+ * Layer normalisation over the rows of a matrix, forward and backward.
+ *
+ * Per row of cols values, in binary32 (one rounding at the end where x is BF16):
+ *   n = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ *   y = n w + b           (w = 1 where w is NULL, b = 0 where b is NULL)
+ * and backwards, with dn = dy w:
+ *   dx = (dn - mean(dn) - n mean(dn n)) rstd
+ *   dw = sum over rows of dy n,  db = sum over rows of dy
+ * The order of every sum depends on the sizes and on 16-byte alignment alone:
+ * the same call gives the same bits.  A row whose sums or squared deviations
+ * pass binary32's range gives what binary32 makes of it.  Rows of up to 8192 values are read from
+ * memory once; wider ones are right, and read two or three times.  Rows of x,
+ * y, dy, dx on 16-byte boundaries with whole 16 bytes of values take the
+ * vectorised path.  x and y have x_dtype (MPADAM_F32 or MPADAM_BF16), and so
+ * have dy and dx; w, b, dw and db have w_dtype, binary32 or x's.  Row strides are in
+ * elements, >= cols.  rows, cols < 2^31.  Outputs must not overlap inputs.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  const void* x;
+  int64_t ldx;
+  const void* w;     /* cols, or NULL */
+  const void* b;     /* cols, or NULL */
+  void* y;
+  int64_t ldy;
+  float* mean;       /* rows each, for the backward pass, or both NULL */
+  float* rstd;
+  int64_t rows, cols;
+  int32_t x_dtype, w_dtype;
+  float eps;         /* finite, >= 0 */
+  int32_t reserved;  /* must be 0 */
+} mpadam_layer_norm;
+
+/* Asynchronous on `stream`, one launch.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_layer_norm_forward(const mpadam_layer_norm* p, struct CUstream_st* stream);
+
+typedef struct {
+  const void* x;
+  int64_t ldx;
+  const void* dy;
+  int64_t lddy;
+  const void* w;            /* as forward */
+  const float* mean;        /* as forward left them */
+  const float* rstd;
+  void* dx;                 /* or NULL: not wanted */
+  int64_t lddx;
+  void* dw;                 /* cols each, or NULL: not wanted */
+  void* db;
+  void* workspace;          /* 16-byte aligned; NULL when neither dw nor db is wanted */
+  int64_t workspace_bytes;  /* at least mpadam_layer_norm_workspace's */
+  int64_t rows, cols;
+  int32_t x_dtype, w_dtype;
+} mpadam_layer_norm_grad;
+
+/* Host only: bytes of workspace that dw and db of these sizes need.  Errors: EINVAL. */
+int32_t mpadam_layer_norm_workspace(int64_t rows, int64_t cols, int64_t* bytes);
+
+/* Asynchronous on `stream`: one launch, and one where dw or db is wanted.  With
+ * no rows, dw and db are 0.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_layer_norm_backward(const mpadam_layer_norm_grad* p, struct CUstream_st* stream);
+
+/* ------------------------------------------------------------------------
+ * Tokens times a weight in NVFP4, as mpadam_step leaves one (MPADAM_NVFP4): the
+ * product that serves what the step trains.
+ * ------------------------------------------------------------------------ */
+
+/* [rows, cols] as one flat tensor: codes (ceil(rows cols / 2) bytes, element 2i
+ * in the low nibble of byte i), scales (E4M3, one per 16 consecutive elements of
+ * the flat tensor), and the tensor's scale G (finite, > 0). */
+typedef struct {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int64_t rows, cols;
+  float global_scale;
+  int32_t reserved;      /* must be 0 */
+} mpadam_nvfp4_matrix;
+
+/* y[t, i] = G sum over j of x[t, j] q[i, j] s[i, j], rounded once: x and y have
+ * x_dtype (MPADAM_F32 or MPADAM_BF16) and row strides ldx >= cols and ldy >=
+ * rows.  Products are exact and summed in binary32, in an order that depends on
+ * the sizes and alignment alone.  cols a multiple of 32, codes 16-byte and
+ * scales 2-byte aligned take the tensor cores; else every product is one
+ * multiply-add.  0 <= tokens <= 65536; made for few: the weight is read once
+ * for every 8 to 32 tokens.  cols = 0 gives 0.  y must not overlap x.
+ * Asynchronous on `stream`, one launch.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_nvfp4_linear(const void* x, int32_t x_dtype, int64_t tokens, int64_t ldx, const mpadam_nvfp4_matrix* w,
+                            void* y, int64_t ldy, struct CUstream_st* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,7 @@ the layer's place in the graph.
 """
 from .builder import build  # noqa: F401
 
-__all__ = ["build", "native", "MPAdam", "AdamW", "GradNorm", "fp8"]
+__all__ = ["build", "native", "MPAdam", "AdamW", "GradNorm", "fp8", "fp4", "layer_norm"]
 
 
 def __getattr__(name):
@@ -23,7 +23,10 @@ def __getattr__(name):
     if name in ("AdamW", "GradNorm"):
         from . import adamw
         return getattr(adamw, name)
-    if name == "fp8":
+    if name in ("fp8", "fp4"):
         import importlib
-        return importlib.import_module(".fp8", __name__)
+        return importlib.import_module("." + name, __name__)
+    if name == "layer_norm":
+        from .norm import layer_norm
+        return layer_norm
     raise AttributeError(name)

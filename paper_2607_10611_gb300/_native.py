@@ -31,7 +31,8 @@ EXPORTED = ["mpadam_create", "mpadam_create_ex", "mpadam_fp8_init", "mpadam_step
             "mpadam_adamw_create", "mpadam_adamw_step", "mpadam_adamw_status", "mpadam_adamw_destroy", "mpadam_grad_norm_create",
             "mpadam_grad_norm", "mpadam_grad_norm_destroy", "mpadam_e4m3_quantize", "mpadam_e4m3_matmul",
             "mpadam_e4m3_quantize_matmul",
-            "mpadam_e4m3_status", "mpadam_debug_e4m3_plan"]
+            "mpadam_e4m3_status", "mpadam_debug_e4m3_plan",
+            "mpadam_layer_norm_forward", "mpadam_layer_norm_workspace", "mpadam_layer_norm_backward", "mpadam_nvfp4_linear"]
 
 
 class MPAdamError(RuntimeError):
@@ -90,6 +91,26 @@ class mpadam_e4m3_product(ctypes.Structure):
                 ("b", ctypes.c_void_p), ("b_scale", ctypes.c_void_p), ("ldb", ctypes.c_int64),
                 ("d", ctypes.c_void_p), ("ldd", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64),
                 ("k", ctypes.c_int64), ("d_dtype", ctypes.c_int32), ("accumulate", ctypes.c_int32)]
+
+
+class mpadam_layer_norm(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("w", ctypes.c_void_p), ("b", ctypes.c_void_p),
+                ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64), ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("x_dtype", ctypes.c_int32),
+                ("w_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class mpadam_layer_norm_grad(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("dy", ctypes.c_void_p), ("lddy", ctypes.c_int64),
+                ("w", ctypes.c_void_p), ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+                ("lddx", ctypes.c_int64), ("dw", ctypes.c_void_p), ("db", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("x_dtype", ctypes.c_int32), ("w_dtype", ctypes.c_int32)]
+
+
+class mpadam_nvfp4_matrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("global_scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 TOY_MODES = {"additive": 0, "multiplicative": 1, "combined": 2}
@@ -166,6 +187,10 @@ def lib() -> ctypes.CDLL:
             "mpadam_e4m3_quantize_matmul": [P, i32, i64, P, P],
             "mpadam_e4m3_status": [P, P],
             "mpadam_debug_e4m3_plan": [i64, i64, i64, P],
+            "mpadam_layer_norm_forward": [P, P],
+            "mpadam_layer_norm_workspace": [i64, i64, P],
+            "mpadam_layer_norm_backward": [P, P],
+            "mpadam_nvfp4_linear": [P, i32, i64, i64, P, P, i64, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -497,3 +522,22 @@ def mpadam_debug_e4m3_plan(m: int, n: int, k: int) -> tuple:
     out = (ctypes.c_int32 * 3)()
     _check(lib().mpadam_debug_e4m3_plan(m, n, k, out))
     return out[0], out[1], bool(out[2])
+
+
+def mpadam_layer_norm_forward(norm: mpadam_layer_norm, stream: int = 0) -> None:
+    _check(lib().mpadam_layer_norm_forward(ctypes.byref(norm), stream or None))
+
+
+def mpadam_layer_norm_workspace(rows: int, cols: int) -> int:
+    out = ctypes.c_int64()
+    _check(lib().mpadam_layer_norm_workspace(rows, cols, ctypes.byref(out)))
+    return out.value
+
+
+def mpadam_layer_norm_backward(grad: mpadam_layer_norm_grad, stream: int = 0) -> None:
+    _check(lib().mpadam_layer_norm_backward(ctypes.byref(grad), stream or None))
+
+
+def mpadam_nvfp4_linear(x: int, x_dtype: int, tokens: int, ldx: int, w: mpadam_nvfp4_matrix, y: int, ldy: int,
+                        stream: int = 0) -> None:
+    _check(lib().mpadam_nvfp4_linear(x or None, x_dtype, tokens, ldx, ctypes.byref(w), y or None, ldy, stream or None))

@@ -689,24 +689,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-// Lets a kernel use `bytes` of shared memory on the current device, once.
-template <typename K>
-cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>& ready) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const uint64_t bit = 1ull << (dev & 63);
-  if (ready.load(std::memory_order_relaxed) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) ready.fetch_or(bit);
-  return e;
-}
-
 template <int TM, bool F32>
 cudaError_t launch_pair(const MatmulArgs& a, cudaStream_t stream) {
   using S = PairShape<TM>;
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem(matmul_pair_kernel<TM, F32>, S::kDynSmem, ready);
+  const cudaError_t e = allow_smem((const void*)matmul_pair_kernel<TM, F32>, S::kDynSmem, ready);
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)((a.n + kPairTileN - 1) / kPairTileN) * ((a.m + TM - 1) / TM);
   return launch_dependent((const void*)matmul_pair_kernel<TM, F32>, 2 * (unsigned)std::min<int64_t>(tiles, kSms / 2), kMatmulThreads,
@@ -722,7 +709,7 @@ template <int TM, bool F32>
 cudaError_t launch(const MatmulArgs& a, cudaStream_t stream) {
   using S = Shape<TM>;
   static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem(matmul_kernel<TM, F32>, S::kDynSmem, ready);
+  const cudaError_t e = allow_smem((const void*)matmul_kernel<TM, F32>, S::kDynSmem, ready);
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)((a.n + kTileN - 1) / kTileN) * ((a.m + TM - 1) / TM);
   return launch_dependent((const void*)matmul_kernel<TM, F32>, (unsigned)(tiles * a.split), kMatmulThreads, a.split, S::kDynSmem, &a,

@@ -1,0 +1,447 @@
+// layer_norm.cu -- layer normalisation of rows, forward and backward:
+//   n = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps),  y = n w + b
+//   dn = dy w,  dx = (dn - mean(dn) - n mean(dn n)) rstd
+//   dw = sum over rows of dy n,  db = sum over rows of dy
+// Everything is in binary32 from the load to the store; the variance is taken
+// around the mean, so that a mean far from 0 costs no bits.
+#include <algorithm>
+
+#include "launch.h"
+#include "layer_norm.h"
+#include "step_kernel.cuh"
+
+namespace mpadam {
+
+namespace {
+
+constexpr int kSms = 152;        // GB300
+constexpr int kRowWarps = 8;     // rows of a block where a row is one warp's
+constexpr int kMaxThreads = 512; // of a row that a block shares
+constexpr int kWideThreads = 512;
+
+__device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_later_kernels_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+__device__ __forceinline__ float get(const float* p, int64_t i) { return p[i]; }
+__device__ __forceinline__ float get(const uint16_t* p, int64_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
+__device__ __forceinline__ void put(float* p, int64_t i, float x) { p[i] = x; }
+__device__ __forceinline__ void put(uint16_t* p, int64_t i, float x) { p[i] = (uint16_t)bf16x2_rn(x, 0.0f); }
+
+// 16 bytes of values, as they lie.
+template <typename T>
+struct Pack;
+template <>
+struct Pack<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ void open(const uint4& r, float* x) {
+    x[0] = __uint_as_float(r.x), x[1] = __uint_as_float(r.y), x[2] = __uint_as_float(r.z), x[3] = __uint_as_float(r.w);
+  }
+  static __device__ __forceinline__ uint4 close(const float* x) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+template <>
+struct Pack<uint16_t> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void open(const uint4& r, float* x) {
+    const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+  static __device__ __forceinline__ uint4 close(const float* x) {
+    return make_uint4(bf16x2_rn(x[0], x[1]), bf16x2_rn(x[2], x[3]), bf16x2_rn(x[4], x[5]), bf16x2_rn(x[6], x[7]));
+  }
+};
+
+// A thread's E values of a row of T values, shared out among `threads`: VEC:
+// packs of 16 bytes, the threads' packs next to one another; else single
+// values.  raw[] holds them as they lie, so that a row fetched ahead takes few registers.
+template <typename T, bool VEC, int E>
+struct Slice {
+  static constexpr int kN = VEC ? Pack<T>::kN : 1, kSlots = E / kN, kWords = VEC ? 4 * kSlots : kSlots;
+  static_assert(E % kN == 0, "whole packs");
+  static __device__ __forceinline__ int64_t at(int slot, int t, int threads) { return (int64_t)(slot * threads + t) * kN; }
+  static __device__ __forceinline__ void fetch(const T* p, int64_t cols, int t, int threads, uint32_t* raw) {
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const int64_t c = at(s, t, threads);
+      if constexpr (VEC) {
+        const uint4 v = c < cols ? *reinterpret_cast<const uint4*>(p + c) : make_uint4(0, 0, 0, 0);
+        raw[4 * s] = v.x, raw[4 * s + 1] = v.y, raw[4 * s + 2] = v.z, raw[4 * s + 3] = v.w;
+      } else {
+        raw[s] = c < cols ? __float_as_uint(get(p, c)) : 0u;
+      }
+    }
+  }
+  static __device__ __forceinline__ void open(const uint32_t* raw, float* x) {
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      if constexpr (VEC) Pack<T>::open(make_uint4(raw[4 * s], raw[4 * s + 1], raw[4 * s + 2], raw[4 * s + 3]), x + s * kN);
+      else x[s] = __uint_as_float(raw[s]);
+    }
+  }
+  static __device__ __forceinline__ void store(T* p, int64_t cols, int t, int threads, const float* x) {
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const int64_t c = at(s, t, threads);
+      if (c >= cols) continue;
+      if constexpr (VEC) *reinterpret_cast<uint4*>(p + c) = Pack<T>::close(x + s * kN);
+      else put(p, c, x[0 + s]);
+    }
+  }
+  // The same columns of a vector of another type (`absent` where there is none).
+  template <typename W>
+  static __device__ __forceinline__ void vector(const W* p, float absent, int64_t cols, int t, int threads, float* x) {
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const int64_t c = at(s, t, threads);
+      if constexpr (VEC) {
+        if (p && c < cols) {
+#pragma unroll
+          for (int h = 0; h < kN; h += Pack<W>::kN) {
+            float v[Pack<W>::kN];
+            Pack<W>::open(*reinterpret_cast<const uint4*>(p + c + h), v);
+#pragma unroll
+            for (int i = 0; i < Pack<W>::kN && h + i < kN; ++i) x[s * kN + h + i] = v[i];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kN; ++i) x[s * kN + i] = absent;
+        }
+      } else {
+        x[s] = p && c < cols ? get(p, c) : absent;
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) x = __fadd_rn(x, __shfl_xor_sync(~0u, x, d));
+  return x;
+}
+
+// Sums of `x` over a block's warps, the same in every thread; `slots` (2 x 32
+// values) alternate between calls, so that one barrier a call is enough: a
+// warp that is two calls ahead would have passed the barrier between them.
+struct BlockSum {
+  float (*slots)[32];
+  int turn = 0;
+  __device__ __forceinline__ float operator()(float x) {
+    x = warp_sum(x);
+    float* s = slots[turn];
+    turn ^= 1;
+    const int warps = blockDim.x / 32;
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
+    __syncthreads();
+    float sum = 0.0f;
+    for (int i = 0; i < warps; ++i) sum = __fadd_rn(sum, s[i]);
+    return sum;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Forward: a row in the registers of a warp (ONE) or of a block.
+// ---------------------------------------------------------------------------
+template <typename X, typename W, bool VEC, int E, bool ONE>
+__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads) forward_kernel(const __grid_constant__ NormForwardArgs p) {
+  using S = Slice<X, VEC, E>;
+  __shared__ float slots[2][32];
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+  const int t = ONE ? threadIdx.x & 31 : threadIdx.x, threads = ONE ? 32 : blockDim.x;
+  const int64_t row = ONE ? (int64_t)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5) : blockIdx.x;
+  if (row >= p.rows) return;
+  BlockSum block{slots};
+  auto sum = [&](float x) { return ONE ? warp_sum(x) : block(x); };
+  uint32_t raw[S::kWords];
+  float x[E];
+  S::fetch(static_cast<const X*>(p.x) + row * p.ldx, p.cols, t, threads, raw);
+  S::open(raw, x);
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < E; ++i) s = __fadd_rn(s, x[i]);
+  const float mean = __fmul_rn(sum(s), p.inv_cols);
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    x[i] = __fsub_rn(x[i], mean);
+    if (S::at(i / S::kN, t, threads) < p.cols) s = __fmaf_rn(x[i], x[i], s);
+  }
+  const float rstd = 1.0f / sqrtf(__fmaf_rn(sum(s), p.inv_cols, p.eps));
+  if (t == 0 && p.mean) p.mean[row] = mean, p.rstd[row] = rstd;
+  float w[E], b[E];
+  S::vector(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
+  S::vector(static_cast<const W*>(p.b), 0.0f, p.cols, t, threads, b);
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = __fmaf_rn(__fmul_rn(x[i], rstd), w[i], b[i]);
+  S::store(static_cast<X*>(p.y) + row * p.ldy, p.cols, t, threads, x);
+}
+
+// Rows of any width, read three times.
+template <typename X, typename W>
+__global__ void __launch_bounds__(kWideThreads) forward_wide_kernel(const __grid_constant__ NormForwardArgs p) {
+  __shared__ float slots[2][32];
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+  BlockSum sum{slots};
+  const X* x = static_cast<const X*>(p.x) + blockIdx.x * p.ldx;
+  X* y = static_cast<X*>(p.y) + blockIdx.x * p.ldy;
+  const W *w = static_cast<const W*>(p.w), *b = static_cast<const W*>(p.b);
+  float s = 0.0f;
+  for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) s = __fadd_rn(s, get(x, c));
+  const float mean = __fmul_rn(sum(s), p.inv_cols);
+  s = 0.0f;
+  for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) {
+    const float d = __fsub_rn(get(x, c), mean);
+    s = __fmaf_rn(d, d, s);
+  }
+  const float rstd = 1.0f / sqrtf(__fmaf_rn(sum(s), p.inv_cols, p.eps));
+  if (threadIdx.x == 0 && p.mean) p.mean[blockIdx.x] = mean, p.rstd[blockIdx.x] = rstd;
+  for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads)
+    put(y, c, __fmaf_rn(__fmul_rn(__fsub_rn(get(x, c), mean), rstd), w ? get(w, c) : 1.0f, b ? get(b, c) : 0.0f));
+}
+
+// ---------------------------------------------------------------------------
+// Backward: a row in the registers of a warp (ONE) or of a block, rows in turn;
+// each thread keeps the sums over its rows of dy n and dy for its columns.  The
+// next row is fetched before the sums over this one are exchanged.
+// ---------------------------------------------------------------------------
+template <typename X, typename W, bool VEC, int E, bool ONE>
+__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, 1)
+    backward_kernel(const __grid_constant__ NormBackwardArgs p) {
+  using S = Slice<X, VEC, E>;
+  extern __shared__ float joined[];  // ONE: [2][cols]
+  __shared__ float2 slots[2][32];
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
+  const int t = ONE ? lane : threadIdx.x, threads = ONE ? 32 : blockDim.x;
+  const int64_t stride = ONE ? (int64_t)gridDim.x * warps : gridDim.x;
+  int64_t row = ONE ? (int64_t)blockIdx.x * warps + warp : blockIdx.x;
+  const X *x = static_cast<const X*>(p.x), *dy = static_cast<const X*>(p.dy);
+  float w[E], dw[E], db[E];
+  S::vector(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
+#pragma unroll
+  for (int i = 0; i < E; ++i) dw[i] = db[i] = 0.0f;
+  uint32_t raw_x[S::kWords], raw_dy[S::kWords];
+  float mean = 0.0f, rstd = 0.0f;
+  auto fetch = [&](int64_t r) {
+    S::fetch(x + r * p.ldx, p.cols, t, threads, raw_x);
+    S::fetch(dy + r * p.lddy, p.cols, t, threads, raw_dy);
+    mean = p.mean[r], rstd = p.rstd[r];
+  };
+  if (row < p.rows) fetch(row);
+  int turn = 0;
+  for (; row < p.rows; row += stride) {
+    float n[E], dn[E];
+    S::open(raw_x, n);
+    S::open(raw_dy, dn);
+    const float scale = rstd;
+    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      // (columns past the last have dy = 0, and n = 0 whatever the mean: they add nothing)
+      n[i] = S::at(i / S::kN, t, threads) < p.cols ? __fmul_rn(__fsub_rn(n[i], mean), scale) : 0.0f;
+      dw[i] = __fmaf_rn(dn[i], n[i], dw[i]);
+      db[i] = __fadd_rn(db[i], dn[i]);
+      dn[i] = __fmul_rn(dn[i], w[i]);
+      s0 = __fadd_rn(s0, dn[i]);
+      s1 = __fmaf_rn(dn[i], n[i], s1);
+    }
+    if (row + stride < p.rows) fetch(row + stride);
+    if (!p.dx) continue;
+    s0 = warp_sum(s0), s1 = warp_sum(s1);
+    if (!ONE) {
+      if (lane == 0) slots[turn][warp] = make_float2(s0, s1);
+      __syncthreads();
+      s0 = s1 = 0.0f;
+      for (int i = 0; i < warps; ++i) s0 = __fadd_rn(s0, slots[turn][i].x), s1 = __fadd_rn(s1, slots[turn][i].y);
+      turn ^= 1;
+    }
+    s0 = __fmul_rn(s0, p.inv_cols), s1 = __fmul_rn(s1, p.inv_cols);
+#pragma unroll
+    for (int i = 0; i < E; ++i) dn[i] = __fmul_rn(__fsub_rn(__fsub_rn(dn[i], s0), __fmul_rn(n[i], s1)), scale);
+    S::store(static_cast<X*>(p.dx) + row * p.lddx, p.cols, t, threads, dn);
+  }
+  if (!p.partial) return;
+  if (ONE) {  // the warps' sums one after another
+    for (int k = 0; k < warps; ++k) {
+      if (warp == k) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const int64_t c = S::at(i / S::kN, t, threads) + i % S::kN;
+          if (c >= p.cols) continue;
+          joined[c] = k ? __fadd_rn(joined[c], dw[i]) : dw[i];
+          joined[p.cols + c] = k ? __fadd_rn(joined[p.cols + c], db[i]) : db[i];
+        }
+      }
+      __syncthreads();
+    }
+    for (int64_t c = threadIdx.x; c < 2 * p.cols; c += blockDim.x) p.partial[blockIdx.x * 2 * p.cols + c] = joined[c];
+  } else {
+    float* out = p.partial + blockIdx.x * 2 * p.cols;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int64_t c = S::at(i / S::kN, t, threads) + i % S::kN;
+      if (c < p.cols) out[c] = dw[i], out[p.cols + c] = db[i];
+    }
+  }
+}
+
+// Rows of any width: dx, read twice.
+template <typename X, typename W>
+__global__ void __launch_bounds__(kWideThreads) backward_wide_kernel(const __grid_constant__ NormBackwardArgs p) {
+  __shared__ float slots[2][32];
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+  BlockSum sum{slots};
+  const int64_t row = blockIdx.x;
+  const X *x = static_cast<const X*>(p.x) + row * p.ldx, *dy = static_cast<const X*>(p.dy) + row * p.lddy;
+  X* dx = static_cast<X*>(p.dx) + row * p.lddx;
+  const W* w = static_cast<const W*>(p.w);
+  const float mean = p.mean[row], rstd = p.rstd[row];
+  float s0 = 0.0f, s1 = 0.0f;
+  for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) {
+    const float n = __fmul_rn(__fsub_rn(get(x, c), mean), rstd), dn = __fmul_rn(get(dy, c), w ? get(w, c) : 1.0f);
+    s0 = __fadd_rn(s0, dn);
+    s1 = __fmaf_rn(dn, n, s1);
+  }
+  s0 = __fmul_rn(sum(s0), p.inv_cols);
+  s1 = __fmul_rn(sum(s1), p.inv_cols);
+  for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) {
+    const float n = __fmul_rn(__fsub_rn(get(x, c), mean), rstd), dn = __fmul_rn(get(dy, c), w ? get(w, c) : 1.0f);
+    put(dx, c, __fmul_rn(__fsub_rn(__fsub_rn(dn, s0), __fmul_rn(n, s1)), rstd));
+  }
+}
+
+// ... and the sums over each part's rows, a column a thread.
+template <typename X>
+__global__ void __launch_bounds__(kWideThreads) wide_sums_kernel(const __grid_constant__ NormBackwardArgs p) {
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+  const X *x = static_cast<const X*>(p.x), *dy = static_cast<const X*>(p.dy);
+  const int64_t tiles = (p.cols + kWideThreads - 1) / kWideThreads;
+  const int64_t part = blockIdx.x / tiles, c = blockIdx.x % tiles * kWideThreads + threadIdx.x;
+  if (c >= p.cols) return;
+  float dw = 0.0f, db = 0.0f;
+  for (int64_t r = part; r < p.rows; r += p.parts) {
+    const float d = get(dy, r * p.lddy + c);
+    dw = __fmaf_rn(d, __fmul_rn(__fsub_rn(get(x, r * p.ldx + c), p.mean[r]), p.rstd[r]), dw);
+    db = __fadd_rn(db, d);
+  }
+  p.partial[part * 2 * p.cols + c] = dw;
+  p.partial[part * 2 * p.cols + p.cols + c] = db;
+}
+
+// The parts' sums: 32 columns a block, 32 rows of threads that take every 32nd
+// part each and are joined in order.
+template <typename W>
+__global__ void __launch_bounds__(1024) sums_kernel(const __grid_constant__ NormSumArgs p) {
+  __shared__ float joined[32][33];
+  wait_for_earlier_kernels();
+  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+  const int64_t tiles = (p.cols + 31) / 32;
+  const bool second = blockIdx.x >= tiles;
+  const int64_t c = (blockIdx.x - (second ? tiles : 0)) * 32 + lane;
+  void* out = second ? p.db : p.dw;
+  if (!out) return;
+  float s = 0.0f;
+  if (c < p.cols) {
+    const float* from = p.partial + (second ? p.cols : 0) + c;
+#pragma unroll 8
+    for (int i = group; i < p.parts; i += 32) s = __fadd_rn(s, from[(int64_t)i * 2 * p.cols]);
+  }
+  joined[group][lane] = s;
+  __syncthreads();
+  if (group || c >= p.cols) return;
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) s = __fadd_rn(s, joined[i][lane]);
+  put(static_cast<W*>(out), c, s);
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+constexpr int64_t kOneCols = 32 * 32;           // widest row of a warp
+constexpr int64_t kBlockCols = 16 * kMaxThreads; // and of a block
+
+bool whole_packs(const void* p, int64_t ld, int64_t rows, int64_t size) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows == 1 || ld * size % 16 == 0);
+}
+
+int threads_for(int64_t cols, int each) { return (int)((cols + 32 * each - 1) / (32 * each)) * 32; }
+
+template <typename X, typename W, bool VEC>
+cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
+  auto one = [&](auto* kernel) {
+    return launch_dependent((const void*)kernel, (unsigned)((a.rows + kRowWarps - 1) / kRowWarps), 32 * kRowWarps, 0, 0, &a, stream);
+  };
+  auto block = [&](auto* kernel, int each) {
+    return launch_dependent((const void*)kernel, (unsigned)a.rows, threads_for(a.cols, each), 0, 0, &a, stream);
+  };
+  // Few rows: as many threads to a row as there are packs, for its latency.
+  if (a.rows <= 2 * kSms && a.cols > 256 && a.cols <= 8 * kMaxThreads) return block(forward_kernel<X, W, VEC, 8, false>, 8);
+  if (a.cols <= 256) return one(forward_kernel<X, W, VEC, 8, true>);
+  if (a.cols <= 512) return one(forward_kernel<X, W, VEC, 16, true>);
+  if (a.cols <= 768) return one(forward_kernel<X, W, VEC, 24, true>);
+  if (a.cols <= kOneCols) return one(forward_kernel<X, W, VEC, 32, true>);
+  if (a.cols <= kBlockCols) return block(forward_kernel<X, W, VEC, 16, false>, 16);
+  return launch_dependent((const void*)forward_wide_kernel<X, W>, (unsigned)a.rows, kWideThreads, 0, 0, &a, stream);
+}
+
+template <typename X, typename W, bool VEC>
+cudaError_t launch_backward(const NormBackwardArgs& a, cudaStream_t stream) {
+  auto one = [&](auto* kernel) {
+    return launch_dependent((const void*)kernel, (unsigned)a.parts, 32 * kRowWarps, 0, (int)(2 * a.cols * sizeof(float)), &a, stream);
+  };
+  if (a.cols <= 256) return one(backward_kernel<X, W, VEC, 8, true>);
+  if (a.cols <= 512) return one(backward_kernel<X, W, VEC, 16, true>);
+  if (a.cols <= 768) return one(backward_kernel<X, W, VEC, 24, true>);
+  if (a.cols <= kOneCols) return one(backward_kernel<X, W, VEC, 32, true>);
+  if (a.cols <= kBlockCols)
+    return launch_dependent((const void*)backward_kernel<X, W, VEC, 16, false>, (unsigned)a.parts, threads_for(a.cols, 16), 0, 0, &a,
+                            stream);
+  if (a.dx) {
+    const cudaError_t e = launch_dependent((const void*)backward_wide_kernel<X, W>, (unsigned)a.rows, kWideThreads, 0, 0, &a, stream);
+    if (e != cudaSuccess) return e;
+  }
+  if (!a.partial) return cudaSuccess;
+  const int64_t tiles = (a.cols + kWideThreads - 1) / kWideThreads;
+  return launch_dependent((const void*)wide_sums_kernel<X>, (unsigned)(tiles * a.parts), kWideThreads, 0, 0, &a, stream);
+}
+
+}  // namespace
+
+int norm_parts(int64_t rows, int64_t cols) {
+  if (cols <= kOneCols) return (int)std::min<int64_t>((rows + kRowWarps - 1) / kRowWarps, 2 * kSms);
+  if (cols <= kBlockCols) return (int)std::min<int64_t>(rows, kSms * std::max<int64_t>(1, std::min<int64_t>(4, 8192 / cols)));
+  return (int)std::min<int64_t>(rows, 32);
+}
+
+cudaError_t launch_norm_forward(const NormForwardArgs& a, cudaStream_t stream) {
+  const int64_t xs = a.x_f32 ? 4 : 2;
+  const bool vec = a.cols % (16 / xs) == 0 && whole_packs(a.x, a.ldx, a.rows, xs) && whole_packs(a.y, a.ldy, a.rows, xs) &&
+                   whole_packs(a.w, 0, 1, 1) && whole_packs(a.b, 0, 1, 1);
+  if (a.x_f32) return vec ? launch_forward<float, float, true>(a, stream) : launch_forward<float, float, false>(a, stream);
+  if (a.w_f32) return vec ? launch_forward<uint16_t, float, true>(a, stream) : launch_forward<uint16_t, float, false>(a, stream);
+  return vec ? launch_forward<uint16_t, uint16_t, true>(a, stream) : launch_forward<uint16_t, uint16_t, false>(a, stream);
+}
+
+cudaError_t launch_norm_backward(const NormBackwardArgs& a, cudaStream_t stream) {
+  const int64_t xs = a.x_f32 ? 4 : 2;
+  const bool vec = a.cols % (16 / xs) == 0 && whole_packs(a.x, a.ldx, a.rows, xs) && whole_packs(a.dy, a.lddy, a.rows, xs) &&
+                   whole_packs(a.dx, a.lddx, a.rows, xs) && whole_packs(a.w, 0, 1, 1);
+  if (a.x_f32) return vec ? launch_backward<float, float, true>(a, stream) : launch_backward<float, float, false>(a, stream);
+  if (a.w_f32) return vec ? launch_backward<uint16_t, float, true>(a, stream) : launch_backward<uint16_t, float, false>(a, stream);
+  return vec ? launch_backward<uint16_t, uint16_t, true>(a, stream) : launch_backward<uint16_t, uint16_t, false>(a, stream);
+}
+
+cudaError_t launch_norm_sums(const NormSumArgs& a, cudaStream_t stream) {
+  const unsigned grid = (unsigned)(2 * ((a.cols + 31) / 32));
+  return a.w_f32 ? launch_dependent((const void*)sums_kernel<float>, grid, 1024, 0, 0, &a, stream)
+                 : launch_dependent((const void*)sums_kernel<uint16_t>, grid, 1024, 0, 0, &a, stream);
+}
+
+}  // namespace mpadam

@@ -446,9 +446,9 @@ struct LinearBackward : torch::autograd::Node {
 };
 
 // A tangent would be lost, which forward mode takes as a derivative of zero.
-void refuse_tangent(const Tensor& t, const char* what) {
+void refuse_tangent(const Tensor& t, const char* what, const char* by = "the 8-bit linear layer") {
   TORCH_CHECK(!c10::AutogradState::get_tls_state().get_fw_grad_mode() || !t._fw_grad(0).defined(), what,
-              " has a tangent: the 8-bit linear layer has no forward-mode derivative");
+              " has a tangent: ", by, " has no forward-mode derivative");
 }
 void check_activations(const Tensor& x) {
   TORCH_CHECK_VALUE(x.dim() >= 1 && is_real(x), "x must be a CUDA float32 or bfloat16 tensor");
@@ -519,6 +519,181 @@ PyObject* linear_held(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------
+// Layer normalisation
+// ---------------------------------------------------------------------------
+int64_t row_stride(const Tensor& m) { return m.size(0) > 1 ? std::max(m.stride(0), m.size(1)) : m.size(1); }
+const void* pointer(const Tensor& t) { return t.defined() ? t.const_data_ptr() : nullptr; }
+
+// The norm's node in the graph, of the same make as the linear layer's.  x and w are kept as inputs (torch then refuses a
+// backward pass after one of them was written to), the rows' means and 1 / sigmas as one tensor.
+struct LayerNormBackward : torch::autograd::Node {
+  torch::autograd::SavedVariable x, w, stats;
+  at::ScalarType w_type;
+  bool has_w, has_b, need_x, need_w, need_b, released = false;
+
+  variable_list apply(variable_list&& grads) override {
+    TORCH_CHECK(!at::GradMode::is_enabled(), "layer_norm is differentiable once: no create_graph");
+    TORCH_CHECK(!released, "backward through the same layer_norm a second time: give retain_graph=True the first time");
+    const Tensor& dy = grads[0];
+    if (!dy.defined()) return {Tensor(), Tensor(), Tensor()};
+    const bool want_x = need_x && task_should_compute_output(0), want_w = need_w && task_should_compute_output(1),
+               want_b = need_b && task_should_compute_output(2);
+    if (!want_x && !want_w && !want_b) return {Tensor(), Tensor(), Tensor()};
+    const c10::cuda::CUDAGuard guard(dy.device());
+    const Tensor in = x.unpack(), weight = has_w ? w.unpack() : Tensor(), st = stats.unpack();
+    const Tensor mx = rows_of(in), md = rows_of(dy);
+    const int64_t rows = mx.size(0), cols = mx.size(1);
+    TORCH_CHECK(in.device() == dy.device() && in.sizes() == dy.sizes() && in.scalar_type() == dy.scalar_type() && st.dim() == 2 &&
+                    st.size(0) == 2 && st.size(1) == rows && st.scalar_type() == at::kFloat && st.is_contiguous() &&
+                    st.device() == dy.device() &&
+                    (!has_w || (weight.scalar_type() == w_type && weight.numel() == cols && weight.device() == dy.device())),
+                "a saved-tensor hook gave layer_norm something else back than it was given");
+    const Tensor mw = has_w ? weight.contiguous() : Tensor();
+    Tensor dx, dw, db, work;
+    mpadam_layer_norm_grad p{};
+    p.x = mx.const_data_ptr(), p.ldx = row_stride(mx);
+    p.dy = md.const_data_ptr(), p.lddy = row_stride(md);
+    p.w = pointer(mw);
+    p.mean = st.const_data_ptr<float>(), p.rstd = p.mean + rows;
+    p.rows = rows, p.cols = cols;
+    p.x_dtype = type_of(mx);
+    p.w_dtype = has_w || has_b ? (w_type == at::kFloat ? MPADAM_F32 : MPADAM_BF16) : MPADAM_F32;
+    if (want_x) {
+      dx = at::empty(in.sizes(), in.options());
+      p.dx = dx.data_ptr(), p.lddx = cols;
+    }
+    const auto vector = md.options().dtype(w_type);
+    if (want_w) dw = at::empty({cols}, vector), p.dw = dw.data_ptr();
+    if (want_b) db = at::empty({cols}, vector), p.db = db.data_ptr();
+    if (want_w || want_b) {
+      check(mpadam_layer_norm_workspace(rows, cols, &p.workspace_bytes));
+      work = at::empty({p.workspace_bytes}, md.options().dtype(at::kByte));
+      p.workspace = work.data_ptr();
+    }
+    check(mpadam_layer_norm_backward(&p, current_stream(md)));
+    return {dx, dw, db};
+  }
+  void release_variables() override {
+    x.reset_data();
+    w.reset_data();
+    stats.reset_data();
+    released = true;
+  }
+  std::string name() const override { return "LayerNormRowsBackward"; }
+};
+
+// layer_norm(x, w or None, b or None, eps) -> y
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 4, "layer_norm takes 4 arguments");
+  const Tensor& x = tensor_of(a[0], "x");
+  TORCH_CHECK_VALUE(x.dim() >= 1 && is_real(x), "x must be a CUDA float32 or bfloat16 tensor");
+  const double eps = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred()) return nullptr;
+  refuse_tangent(x, "x", "layer_norm");
+  const int64_t cols = x.size(-1);
+  Tensor w, b;
+  auto vector = [&](PyObject* o, const char* what) {
+    const Tensor& v = tensor_of(o, what);
+    TORCH_CHECK_VALUE(v.dim() == 1 && v.size(0) == cols && v.device() == x.device() &&
+                          (v.scalar_type() == at::kFloat || v.scalar_type() == x.scalar_type()),
+                      what, " must be a tensor of ", cols, " elements beside x, float32 or of x's type");
+    refuse_tangent(v, what, "layer_norm");
+    return v;
+  };
+  if (a[1] != Py_None) w = vector(a[1], "weight");
+  if (a[2] != Py_None) b = vector(a[2], "bias");
+  TORCH_CHECK_VALUE(!w.defined() || !b.defined() || w.scalar_type() == b.scalar_type(), "weight and bias differ in their type");
+  const auto w_type = w.defined() ? w.scalar_type() : b.defined() ? b.scalar_type() : at::kFloat;
+  const bool on = at::GradMode::is_enabled(), need_x = on && x.requires_grad(),
+             need_w = on && w.defined() && w.requires_grad(), need_b = on && b.defined() && b.requires_grad();
+  const bool need = need_x || need_w || need_b;
+  const c10::cuda::CUDAGuard guard(x.device());
+  Tensor y, stats;
+  {
+    const at::AutoDispatchBelowADInplaceOrView below;
+    const Tensor m = rows_of(x), mw = w.defined() ? w.contiguous() : w, mb = b.defined() ? b.contiguous() : b;
+    y = at::empty(x.sizes(), x.options());
+    mpadam_layer_norm p{};
+    if (need) {
+      stats = at::empty({2, m.size(0)}, x.options().dtype(at::kFloat));
+      p.mean = stats.data_ptr<float>(), p.rstd = p.mean + m.size(0);
+    }
+    p.x = m.const_data_ptr(), p.ldx = row_stride(m);
+    p.w = pointer(mw), p.b = pointer(mb);
+    p.y = y.data_ptr(), p.ldy = cols;
+    p.rows = m.size(0), p.cols = cols;
+    p.x_dtype = type_of(m), p.w_dtype = w_type == at::kFloat ? MPADAM_F32 : MPADAM_BF16;
+    p.eps = (float)eps;
+    check(mpadam_layer_norm_forward(&p, current_stream(m)));
+  }
+  if (need) {
+    const std::shared_ptr<LayerNormBackward> node(new LayerNormBackward(), torch::autograd::deleteNode);
+    node->x = torch::autograd::SavedVariable(x, false);
+    if (w.defined()) node->w = torch::autograd::SavedVariable(w, false);
+    node->stats = torch::autograd::SavedVariable(stats, false);
+    node->w_type = w_type;
+    node->has_w = w.defined(), node->has_b = b.defined();
+    node->need_x = need_x, node->need_w = need_w, node->need_b = need_b;
+    node->set_next_edges(torch::autograd::collect_next_edges(x, w, b));
+    torch::autograd::set_history(y, node);
+  }
+  return THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// ---------------------------------------------------------------------------
+// Weights in NVFP4
+// ---------------------------------------------------------------------------
+// The matrix that codes, scales, a scale and a shape make up.
+mpadam_nvfp4_matrix nvfp4_of(PyObject* c, PyObject* s, PyObject* scale, PyObject* rows, PyObject* cols) {
+  const Tensor &codes = tensor_of(c, "codes"), &scales = tensor_of(s, "scales");
+  mpadam_nvfp4_matrix w{};
+  w.rows = PyLong_AsLongLong(rows), w.cols = PyLong_AsLongLong(cols);
+  w.global_scale = (float)PyFloat_AsDouble(scale);
+  if (PyErr_Occurred()) throw python_error();
+  TORCH_CHECK_VALUE(w.rows >= 0 && w.cols >= 0 && w.rows <= INT32_MAX && w.cols <= INT32_MAX, "rows and columns must be in [0, 2^31)");
+  const int64_t numel = w.rows * w.cols;
+  TORCH_CHECK_VALUE(codes.scalar_type() == at::kByte && codes.is_cuda() && codes.is_contiguous() && codes.numel() == (numel + 1) / 2,
+                    "codes must be a contiguous CUDA uint8 tensor of ", (numel + 1) / 2, " bytes, two codes each");
+  TORCH_CHECK_VALUE((scales.scalar_type() == at::kByte || scales.scalar_type() == kCodes) && scales.device() == codes.device() &&
+                        scales.is_contiguous() && scales.numel() == (numel + 15) / 16,
+                    "scales must be a contiguous tensor of ", (numel + 15) / 16, " E4M3 codes (uint8 or float8_e4m3fn) beside the codes");
+  TORCH_CHECK_VALUE(w.global_scale > 0.0f && w.global_scale <= 3.402823466e38f, "global_scale must be a finite binary32 above 0");
+  w.codes = static_cast<const uint8_t*>(codes.const_data_ptr());
+  w.scales = static_cast<const uint8_t*>(scales.const_data_ptr());
+  return w;
+}
+
+// check_nvfp4(codes, scales, global scale, rows, cols)
+PyObject* check_nvfp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 5, "check_nvfp4 takes 5 arguments");
+  nvfp4_of(a[0], a[1], a[2], a[3], a[4]);
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// nvfp4_linear(x, codes, scales, global scale, rows, cols) -> y
+PyObject* nvfp4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 6, "nvfp4_linear takes 6 arguments");
+  const Tensor& x = tensor_of(a[0], "x");
+  TORCH_CHECK_VALUE(x.dim() >= 1 && is_real(x), "x must be a CUDA float32 or bfloat16 tensor");
+  refuse_tangent(x, "x", "a product with an NVFP4 weight");
+  const mpadam_nvfp4_matrix w = nvfp4_of(a[1], a[2], a[3], a[4], a[5]);
+  TORCH_CHECK_VALUE(tensor_of(a[1], "codes").device() == x.device(), "the weight is on another device than x");
+  TORCH_CHECK_VALUE(w.cols == x.size(-1), "inner sizes differ: ", x.size(-1), " and ", w.cols);
+  TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && x.requires_grad()), "an NVFP4 weight passes no gradient");
+  const c10::cuda::CUDAGuard guard(x.device());
+  const Tensor m = rows_of(x);
+  const Tensor y = at::empty({m.size(0), w.rows}, m.options());
+  check(mpadam_nvfp4_linear(m.const_data_ptr(), type_of(m), m.size(0), row_stride(m), &w, y.data_ptr(), w.rows, current_stream(m)));
+  return THPVariable_Wrap(with_shape(y, x));
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_INCREF(cls);
   Py_XSETREF(g_error, cls);
@@ -535,6 +710,9 @@ PyMethodDef kMethods[] = {{"list_spec", MPADAM_FAST(list_spec)},
                           {"matmul", MPADAM_FAST(py_matmul)},
                           {"linear", MPADAM_FAST(linear)},
                           {"linear_held", MPADAM_FAST(linear_held)},
+                          {"layer_norm", MPADAM_FAST(layer_norm)},
+                          {"check_nvfp4", MPADAM_FAST(check_nvfp4)},
+                          {"nvfp4_linear", MPADAM_FAST(nvfp4_linear)},
                           {"set_error", set_error, METH_O, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_mpadam_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
