@@ -761,6 +761,111 @@ typedef struct {
 int32_t mpadam_nvfp4_linear(const void* x, int32_t x_dtype, int64_t tokens, int64_t ldx, const mpadam_nvfp4_matrix* w,
                             void* y, int64_t ldy, struct CUstream_st* stream);
 
+/* ------------------------------------------------------------------------
+ * Orthogonalisation of matrices by Newton-Schulz steps, and Muon, the optimizer
+ * that orthogonalises its updates with them (K. Jordan et al., "Muon: An
+ * optimizer for hidden layers in neural networks", 2024).
+ *
+ * For a matrix U, on the side with fewer rows (a matrix with more rows than
+ * columns is taken as its transpose):
+ *   X = U / |U|_F (0 where U is 0),  then `steps` times
+ *   A = X X^T,  B = b A + c A A,  X <- a X + B X,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * which takes singular values above about 1/500 of the norm to between 0.68 and
+ * 1.21 in five steps.  The norm is right for any finite U, however large or
+ * small.  Products are of FP16 values, summed in binary32 on the tensor cores: X
+ * is held as the sum of two FP16 values, of which products take the first, A and
+ * B as one, all times 2^14.  The error of the result, relative in the 2-norm, is
+ * about 1.4e-3 for a random matrix and less for one that a few directions
+ * dominate.  A matrix with a value that is not finite gives NaN.  The same call
+ * gives the same bits.
+ * ------------------------------------------------------------------------ */
+typedef struct mpadam_orthogonal_state mpadam_orthogonal_state;
+
+/* For a list of n matrices [rows[k], cols[k]], contiguous, of dtype (MPADAM_F32
+ * or MPADAM_BF16); 1 <= steps <= 32; sides up to 2^20.  Allocates, on the current
+ * device, a workspace of about 6 bytes an element and 4 per element of the
+ * shorter side's square, for as many matrices at once as stay below 6 GiB (and
+ * for the largest).  Errors: EINVAL, EALLOC, ECUDA, EUNSUPPORTED (no driver entry
+ * for tensor maps).  On error *out is NULL. */
+int32_t mpadam_orthogonal_create(const int64_t* rows, const int64_t* cols, int32_t n, int32_t dtype, int32_t steps,
+                                 mpadam_orthogonal_state** out);
+
+/* out[k] = x[k] orthogonalised, rounded to the nearest; x, out: host arrays of n
+ * device pointers; out[k] may be x[k], and must not overlap another x.
+ * Asynchronous on `stream`; 3 + 3 steps launches for as many matrices as share
+ * the workspace.  A captured call may be replayed.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_orthogonalize(mpadam_orthogonal_state* s, const void* const* x, void* const* out, struct CUstream_st* stream);
+
+/* Device-side status of the calls issued so far: synchronises the device, returns
+ * in *code the error bits that they recorded (non-zero: a bounded wait gave up)
+ * and clears them.  From such a call on until the bits are cleared nothing is
+ * written to out.  Nothing else tells of it.  Errors: EINVAL, ECUDA. */
+int32_t mpadam_orthogonal_status(mpadam_orthogonal_state* s, int32_t* code);
+
+/* Synchronises the device and frees tables and workspace; NULL is a no-op. */
+int32_t mpadam_orthogonal_destroy(mpadam_orthogonal_state* s);
+
+/* Muon.  Per matrix, with g' = g s when the step is given a multiplier s, else g,
+ * in binary32, every operation rounded on its own:
+ *   m' = b m + (1-b) g'         U = b m' + (1-b) g' (nesterov), else m'
+ *   w' = (w - kwd w) - ka O     O = U orthogonalised, as above
+ * (w - ka O when kwd = 0) with kwd = lr * weight_decay, and ka = lr times 0.2
+ * sqrt(max(rows, cols)) (MPADAM_SCALE_RMS: updates as large as AdamW's usually
+ * are) or sqrt(max(1, rows / cols)) (MPADAM_SCALE_SPECTRAL).  U comes from m'
+ * before it is rounded for storage.  BF16 weights are rounded to the nearest or
+ * stochastically, with the random lanes of mpadam_adamw_step; the global element
+ * index too is that of an AdamW list of the same sizes. */
+typedef enum { MPADAM_SCALE_RMS = 0, MPADAM_SCALE_SPECTRAL = 1 } mpadam_muon_scale;
+
+/* One matrix: w has the config's weight_dtype, m its momentum_dtype; compute:
+ * optional BF16 copy of binary32 weights (nearest), overwritten every step, or
+ * NULL.  Contiguous, aligned to the element size; where all are 16-byte aligned
+ * and cols is a multiple of 8, accesses are vectors. */
+typedef struct {
+  void* w;
+  void* m;
+  uint16_t* compute;
+  int64_t rows, cols;
+} mpadam_muon_tensor;
+
+/* Valid ranges (else MPADAM_EINVAL): 0 <= momentum < 1; weight_decay >= 0 finite;
+ * 1 <= steps <= 32. */
+typedef struct {
+  float momentum;
+  float weight_decay;      /* decoupled: w -= lr * weight_decay * w */
+  int32_t nesterov;        /* 0 or 1 */
+  int32_t steps;           /* 5 as a rule */
+  int32_t scale;           /* mpadam_muon_scale */
+  int32_t weight_dtype;    /* MPADAM_F32 or MPADAM_BF16 */
+  int32_t grad_dtype;      /* MPADAM_F32 or MPADAM_BF16 */
+  int32_t momentum_dtype;  /* MPADAM_F32 or MPADAM_BF16 */
+  int32_t rounding;        /* mpadam_rounding of BF16 weights (binary32 ones need none) */
+  int32_t reserved;        /* must be 0 */
+  uint64_t seed;
+} mpadam_muon_config;
+
+typedef struct mpadam_muon_state mpadam_muon_state;
+
+/* Copies the list, validates, allocates and uploads as mpadam_orthogonal_create
+ * does.  Errors: EINVAL, EALLOC, ECUDA, EUNSUPPORTED.  On error *out is NULL. */
+int32_t mpadam_muon_create(const mpadam_muon_tensor* tensors, int32_t n, const mpadam_muon_config* cfg, mpadam_muon_state** out);
+
+/* Step t (>= 1, for the random lanes) with learning rate lr (finite, >= 0) over
+ * every matrix, asynchronously on `stream`; launches as mpadam_orthogonalize's.
+ * grads: host array of n device pointers of grad_dtype.  grad_scale: device
+ * binary32 that multiplies every gradient (see mpadam_grad_norm), or NULL; where
+ * it is NaN the step changes nothing.  A captured step may be replayed.  Errors:
+ * EINVAL, ECUDA. */
+int32_t mpadam_muon_step(mpadam_muon_state* s, const void* const* grads, int64_t step, float lr, const float* grad_scale,
+                         struct CUstream_st* stream);
+
+/* As mpadam_orthogonal_status; from a step whose wait gave up on until the bits
+ * are cleared weights are left as they are (momentum is not). */
+int32_t mpadam_muon_status(mpadam_muon_state* s, int32_t* code);
+
+/* Synchronises the device and frees tables and workspace; NULL is a no-op. */
+int32_t mpadam_muon_destroy(mpadam_muon_state* s);
+
 #ifdef __cplusplus
 }
 #endif

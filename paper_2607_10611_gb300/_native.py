@@ -32,7 +32,9 @@ EXPORTED = ["mpadam_create", "mpadam_create_ex", "mpadam_fp8_init", "mpadam_step
             "mpadam_grad_norm", "mpadam_grad_norm_destroy", "mpadam_e4m3_quantize", "mpadam_e4m3_matmul",
             "mpadam_e4m3_quantize_matmul",
             "mpadam_e4m3_status", "mpadam_debug_e4m3_plan",
-            "mpadam_layer_norm_forward", "mpadam_layer_norm_workspace", "mpadam_layer_norm_backward", "mpadam_nvfp4_linear"]
+            "mpadam_layer_norm_forward", "mpadam_layer_norm_workspace", "mpadam_layer_norm_backward", "mpadam_nvfp4_linear",
+            "mpadam_orthogonal_create", "mpadam_orthogonalize", "mpadam_orthogonal_status", "mpadam_orthogonal_destroy",
+            "mpadam_muon_create", "mpadam_muon_step", "mpadam_muon_status", "mpadam_muon_destroy"]
 
 
 class MPAdamError(RuntimeError):
@@ -113,6 +115,19 @@ class mpadam_nvfp4_matrix(ctypes.Structure):
                 ("global_scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
+class mpadam_muon_tensor(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("m", ctypes.c_void_p), ("compute", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
+
+
+class mpadam_muon_config(ctypes.Structure):
+    _fields_ = [("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("scale", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("momentum_dtype", ctypes.c_int32), ("rounding", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("seed", ctypes.c_uint64)]
+
+
+MUON_SCALES = {"rms": 0, "spectral": 1}
 TOY_MODES = {"additive": 0, "multiplicative": 1, "combined": 2}
 
 
@@ -191,6 +206,14 @@ def lib() -> ctypes.CDLL:
             "mpadam_layer_norm_workspace": [i64, i64, P],
             "mpadam_layer_norm_backward": [P, P],
             "mpadam_nvfp4_linear": [P, i32, i64, i64, P, P, i64, P],
+            "mpadam_orthogonal_create": [P, P, i32, i32, i32, P],
+            "mpadam_orthogonalize": [P, P, P, P],
+            "mpadam_orthogonal_status": [P, P],
+            "mpadam_orthogonal_destroy": [P],
+            "mpadam_muon_create": [P, i32, P, P],
+            "mpadam_muon_step": [P, P, i64, ctypes.c_float, P, P],
+            "mpadam_muon_status": [P, P],
+            "mpadam_muon_destroy": [P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -541,3 +564,54 @@ def mpadam_layer_norm_backward(grad: mpadam_layer_norm_grad, stream: int = 0) ->
 def mpadam_nvfp4_linear(x: int, x_dtype: int, tokens: int, ldx: int, w: mpadam_nvfp4_matrix, y: int, ldy: int,
                         stream: int = 0) -> None:
     _check(lib().mpadam_nvfp4_linear(x or None, x_dtype, tokens, ldx, ctypes.byref(w), y or None, ldy, stream or None))
+
+
+def mpadam_orthogonal_create(shapes: Sequence[tuple], dtype: int, steps: int = 5) -> int:
+    """shapes: (rows, columns) per matrix.  Returns the state handle."""
+    rows = (ctypes.c_int64 * max(1, len(shapes)))(*(r for r, _ in shapes))
+    cols = (ctypes.c_int64 * max(1, len(shapes)))(*(c for _, c in shapes))
+    out = ctypes.c_void_p()
+    _check(lib().mpadam_orthogonal_create(rows, cols, len(shapes), dtype, steps, ctypes.byref(out)))
+    return out.value
+
+
+def mpadam_orthogonalize(state: int, x: Sequence[int], out: Sequence[int], stream: int = 0) -> None:
+    a, b = _ptr_array(x), _ptr_array(out)
+    _check(lib().mpadam_orthogonalize(state or None, a.buffer_info()[0], b.buffer_info()[0], stream or None))
+
+
+def mpadam_orthogonal_status(state: int) -> int:
+    """Synchronises; returns and clears the calls' device error bits (0: no bounded wait gave up)."""
+    out = ctypes.c_int32()
+    _check(lib().mpadam_orthogonal_status(state or None, ctypes.byref(out)))
+    return out.value
+
+
+def mpadam_orthogonal_destroy(state: int) -> None:
+    _check(lib().mpadam_orthogonal_destroy(state or None))
+
+
+def mpadam_muon_create(tensors: Sequence[tuple], cfg: mpadam_muon_config) -> int:
+    """tensors: (w, m, compute, rows, columns) per matrix, pointers as ints (0 = NULL)."""
+    arr = (mpadam_muon_tensor * max(1, len(tensors)))()
+    for i, (w, m, c, rows, cols) in enumerate(tensors):
+        arr[i] = mpadam_muon_tensor(w or None, m or None, c or None, rows, cols)
+    out = ctypes.c_void_p()
+    _check(lib().mpadam_muon_create(arr, len(tensors), ctypes.byref(cfg), ctypes.byref(out)))
+    return out.value
+
+
+def mpadam_muon_step(state: int, grads: Sequence[int], step: int, lr: float, grad_scale: int = 0, stream: int = 0) -> None:
+    g = _ptr_array(grads)
+    _check(lib().mpadam_muon_step(state or None, g.buffer_info()[0], step, lr, grad_scale or None, stream or None))
+
+
+def mpadam_muon_status(state: int) -> int:
+    """Synchronises; returns and clears the steps' device error bits (0: no bounded wait gave up)."""
+    out = ctypes.c_int32()
+    _check(lib().mpadam_muon_status(state or None, ctypes.byref(out)))
+    return out.value
+
+
+def mpadam_muon_destroy(state: int) -> None:
+    _check(lib().mpadam_muon_destroy(state or None))

@@ -28,8 +28,10 @@ EXT_SOURCE = "torch_ext.cpp"
 EXT_TORCH = OUT_DIR / "torch_version"  # the torch that EXT was built for
 
 SOURCES = ["mpadam_api.cu", "step_bf16.cu", "step_e4m3.cu", "step_e4m3b.cu", "step_nvfp4.cu", "toy.cu",
-           "train_api.cu", "adamw.cu", "fp8_quant.cu", "fp8_matmul.cu", "layer_api.cu", "layer_norm.cu", "fp4_linear.cu"]
-HEADERS = ["step_args.h", "step_kernel.cuh", "toy.h", "host.h", "adamw.h", "adamw_math.cuh", "fp8.h", "launch.h", "layer_norm.h", "fp4.h"]
+           "train_api.cu", "adamw.cu", "fp8_quant.cu", "fp8_matmul.cu", "layer_api.cu", "layer_norm.cu", "fp4_linear.cu",
+           "muon_api.cu", "muon_step.cu", "muon_products.cu"]
+HEADERS = ["step_args.h", "step_kernel.cuh", "toy.h", "host.h", "adamw.h", "adamw_math.cuh", "fp8.h", "launch.h", "layer_norm.h", "fp4.h", "list.h",
+           "muon.h", "tcgen05.cuh"]
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + [

@@ -75,6 +75,7 @@ bool has_rows(const Tensor& t) {
 // What the gradients of a list have to be.
 struct Spec {
   std::vector<int64_t> numel;
+  std::vector<int64_t> rows, cols;  // of matrices; else empty
   at::ScalarType type;
   int device;
 };
@@ -86,6 +87,24 @@ PyObject* list_spec(PyObject*, PyObject* const* a, Py_ssize_t n) {
   TORCH_CHECK_VALUE(n == 3 && PyList_Check(a[0]), "list_spec(list of sizes, binary32, device)");
   auto s = std::make_unique<Spec>();
   for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[0]); ++i) s->numel.push_back(PyLong_AsLongLong(PyList_GET_ITEM(a[0], i)));
+  s->type = PyObject_IsTrue(a[1]) ? at::kFloat : at::kBFloat16;
+  s->device = (int)PyLong_AsLong(a[2]);
+  if (PyErr_Occurred()) return nullptr;
+  return PyCapsule_New(s.release(), kSpecName,
+                       [](PyObject* c) { delete static_cast<Spec*>(PyCapsule_GetPointer(c, kSpecName)); });
+  END_HANDLE_TH_ERRORS
+}
+
+// matrix_spec(shapes, binary32?, device index) -> capsule: shapes are tuples (rows, columns)
+PyObject* matrix_spec(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 3 && PyList_Check(a[0]), "matrix_spec(list of shapes, binary32, device)");
+  auto s = std::make_unique<Spec>();
+  for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[0]); ++i) {
+    long long r, c;
+    if (!PyArg_ParseTuple(PyList_GET_ITEM(a[0], i), "LL", &r, &c)) return nullptr;
+    s->rows.push_back(r), s->cols.push_back(c), s->numel.push_back(r * c);
+  }
   s->type = PyObject_IsTrue(a[1]) ? at::kFloat : at::kBFloat16;
   s->device = (int)PyLong_AsLong(a[2]);
   if (PyErr_Occurred()) return nullptr;
@@ -112,6 +131,8 @@ struct Pointers {
       const c10::TensorImpl& x = *t.unsafeGetTensorImpl();
       TORCH_CHECK_VALUE(x.dtype() == type && x.numel() == s.numel[i] && x.device() == device && x.is_contiguous(),
                         "gradients must be contiguous ", s.type, " tensors on cuda:", s.device, ", as large as their weights");
+      TORCH_CHECK_VALUE(s.rows.empty() || (t.dim() == 2 && t.size(0) == s.rows[i] && t.size(1) == s.cols[i]), "matrix ", i,
+                        " of the list must be [", s.rows[i], ", ", s.cols[i], "]");
       p[i] = x.data();
     }
   }
@@ -171,11 +192,10 @@ cudaStream_t stream_of(PyObject* o, int device) {
   return o == Py_None ? c10::cuda::getCurrentCUDAStream(device).stream() : reinterpret_cast<cudaStream_t>(PyLong_AsSize_t(o));
 }
 
-// adamw_step(state, spec, grads, t, lr, grad_scale or None, stream or None)
-PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  HANDLE_TH_ERRORS
-  TORCH_CHECK_VALUE(n == 7, "adamw_step takes 7 arguments");
-  auto* state = static_cast<mpadam_adamw_state*>(PyLong_AsVoidPtr(a[0]));
+// A step's arguments (state, spec, grads, t, lr, grad_scale or None, stream or None), handed to `step`.
+template <typename F>
+PyObject* list_step(PyObject* const* a, F step) {
+  void* state = PyLong_AsVoidPtr(a[0]);
   auto* spec = static_cast<Spec*>(PyCapsule_GetPointer(a[1], kSpecName));
   const int64_t t = PyLong_AsLongLong(a[3]);
   const double lr = PyFloat_AsDouble(a[4]);
@@ -191,8 +211,17 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     scale = x.const_data_ptr<float>();
   }
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)spec->device);
-  if (const int32_t rc = mpadam_adamw_step(state, g.p.data(), t, (float)lr, scale, stream)) return raise(rc);
+  if (const int32_t rc = step(state, g.p.data(), t, (float)lr, scale, stream)) return raise(rc);
   Py_RETURN_NONE;
+}
+
+// adamw_step(state, spec, grads, t, lr, grad_scale or None, stream or None)
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 7, "adamw_step takes 7 arguments");
+  return list_step(a, [](void* state, const void* const* g, int64_t t, float lr, const float* scale, cudaStream_t stream) {
+    return mpadam_adamw_step(static_cast<mpadam_adamw_state*>(state), g, t, lr, scale, stream);
+  });
   END_HANDLE_TH_ERRORS
 }
 
@@ -219,6 +248,89 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   if (const int32_t rc = mpadam_grad_norm(state, g.p.data(), (float)max_norm, out.data_ptr<float>(), stream)) return raise(rc);
   return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// ---------------------------------------------------------------------------
+// Lists of matrices
+// ---------------------------------------------------------------------------
+// muon_create(config's address, w, m, compute or None) -> state: lists of matrices whose types, sizes and devices are
+// checked here; compute's entries may be None.
+PyObject* muon_create(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 4, "muon_create takes 4 arguments");
+  const auto* cfg = static_cast<const mpadam_muon_config*>(PyLong_AsVoidPtr(a[0]));
+  if (PyErr_Occurred()) return nullptr;
+  for (int i = 1; i < 4; ++i) TORCH_CHECK_VALUE(PyList_Check(a[i]) || (i == 3 && a[i] == Py_None), "the matrices come in lists");
+  const Py_ssize_t count = PyList_GET_SIZE(a[1]);
+  for (int i = 2; i < 4; ++i)
+    TORCH_CHECK_VALUE(a[i] == Py_None || PyList_GET_SIZE(a[i]) == count, "one entry per matrix in every list");
+  std::vector<mpadam_muon_tensor> list((size_t)count + 1);
+  c10::optional<c10::Device> device;
+  auto take = [&](int i, Py_ssize_t k, int32_t dtype, const char* what) {
+    const auto type = dtype == MPADAM_F32 ? at::kFloat : at::kBFloat16;
+    const Tensor& t = tensor_of(PyList_GET_ITEM(a[i], k), what);
+    TORCH_CHECK_VALUE(t.scalar_type() == type && t.dim() == 2 && t.is_cuda() && t.is_contiguous(), what,
+                      ": expected contiguous CUDA matrices of ", type);
+    if (!device) device = t.device();
+    TORCH_CHECK_VALUE(t.device() == *device, "all matrices of a list must be on one device");
+    return t;
+  };
+  for (Py_ssize_t k = 0; k < count; ++k) {
+    const Tensor w = take(1, k, cfg->weight_dtype, "weights"), m = take(2, k, cfg->momentum_dtype, "momentum");
+    TORCH_CHECK_VALUE(m.sizes() == w.sizes(), "matrix ", k, ": the momentum differs in shape from the weights");
+    list[k] = {w.data_ptr(), m.data_ptr(), nullptr, w.size(0), w.size(1)};
+    if (a[3] != Py_None && PyList_GET_ITEM(a[3], k) != Py_None) {
+      const Tensor c = take(3, k, MPADAM_BF16, "compute copies");
+      TORCH_CHECK_VALUE(c.sizes() == w.sizes(), "matrix ", k, ": the compute copy differs in shape from the weights");
+      list[k].compute = static_cast<uint16_t*>(c.data_ptr());
+    }
+  }
+  const c10::cuda::OptionalCUDAGuard guard(device);
+  mpadam_muon_state* state = nullptr;
+  if (const int32_t rc = mpadam_muon_create(list.data(), (int32_t)count, cfg, &state)) return raise(rc);
+  return PyLong_FromVoidPtr(state);
+  END_HANDLE_TH_ERRORS
+}
+
+// muon_step(state, spec, grads, t, lr, grad_scale or None, stream or None)
+PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 7, "muon_step takes 7 arguments");
+  return list_step(a, [](void* state, const void* const* g, int64_t t, float lr, const float* scale, cudaStream_t stream) {
+    return mpadam_muon_step(static_cast<mpadam_muon_state*>(state), g, t, lr, scale, stream);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// orthogonalize(state, spec, x, out or None, stream or None) -> list of results
+PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_VALUE(n == 5, "orthogonalize takes 5 arguments");
+  auto* state = static_cast<mpadam_orthogonal_state*>(PyLong_AsVoidPtr(a[0]));
+  auto* spec = static_cast<Spec*>(PyCapsule_GetPointer(a[1], kSpecName));
+  if (PyErr_Occurred()) return nullptr;
+  const cudaStream_t stream = stream_of(a[4], spec->device);
+  if (PyErr_Occurred()) return nullptr;
+  const Pointers x(a[2], *spec);
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)spec->device);
+  const Py_ssize_t count = (Py_ssize_t)spec->numel.size();
+  std::unique_ptr<PyObject, void (*)(PyObject*)> out(nullptr, [](PyObject* o) { Py_XDECREF(o); });
+  if (a[3] != Py_None) {
+    out.reset(PySequence_List(a[3]));
+  } else {
+    out.reset(PyList_New(count));
+    const auto options = at::TensorOptions().dtype(spec->type).device(at::kCUDA, (c10::DeviceIndex)spec->device);
+    for (Py_ssize_t i = 0; out && i < count; ++i) {
+      PyObject* t = THPVariable_Wrap(at::empty({spec->rows[i], spec->cols[i]}, options));
+      if (!t) throw python_error();
+      PyList_SET_ITEM(out.get(), i, t);
+    }
+  }
+  if (!out) throw python_error();
+  const Pointers y(out.get(), *spec);
+  if (const int32_t rc = mpadam_orthogonalize(state, x.p.data(), const_cast<void* const*>(y.p.data()), stream)) return raise(rc);
+  return out.release();
   END_HANDLE_TH_ERRORS
 }
 
@@ -702,9 +814,13 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define MPADAM_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef kMethods[] = {{"list_spec", MPADAM_FAST(list_spec)},
+                          {"matrix_spec", MPADAM_FAST(matrix_spec)},
                           {"adamw_create", MPADAM_FAST(adamw_create)},
                           {"adamw_step", MPADAM_FAST(adamw_step)},
                           {"grad_norm", MPADAM_FAST(grad_norm)},
+                          {"muon_create", MPADAM_FAST(muon_create)},
+                          {"muon_step", MPADAM_FAST(muon_step)},
+                          {"orthogonalize", MPADAM_FAST(orthogonalize)},
                           {"check_matrix", MPADAM_FAST(check_matrix)},
                           {"quantize", MPADAM_FAST(py_quantize)},
                           {"matmul", MPADAM_FAST(py_matmul)},

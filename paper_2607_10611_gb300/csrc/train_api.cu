@@ -10,18 +10,11 @@
 #include "adamw.h"
 #include "fp8.h"
 #include "host.h"
+#include "list.h"
 
 using namespace mpadam;
 
 namespace {
-
-int32_t check_device(int device) {
-  int dev = -1;
-  const cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-  if (dev != device) return fail(MPADAM_EINVAL, "current device %d differs from the state's device %d", dev, device);
-  return MPADAM_OK;
-}
 
 // What both list operators keep on the device: the tensors, each tile's tensor,
 // and gradient pointers where they do not fit a launch.
@@ -34,10 +27,8 @@ struct List {
   uint8_t* memory = nullptr;  // one allocation: the tables below, then what the operator asked for, zeroed
   ListTensor* d_tensors = nullptr;
   int32_t* d_tile_tensor = nullptr;
-  const void** d_grads = nullptr;
+  PointerTable grads;
   void* extra = nullptr;
-  std::vector<const void*> last;  // what d_grads holds
-  bool last_known = false, captured = false;
 
   List() = default;
   List(const List&) = delete;
@@ -79,7 +70,7 @@ struct List {
     }
     d_tensors = reinterpret_cast<ListTensor*>(memory + tensors_at);
     d_tile_tensor = reinterpret_cast<int32_t*>(memory + owner_at);
-    d_grads = reinterpret_cast<const void**>(memory + grads_at);
+    grads.table = reinterpret_cast<const void**>(memory + grads_at);
     extra = memory + extra_at;
     return MPADAM_OK;
   }
@@ -91,31 +82,6 @@ struct List {
       if (!grads[k]) return fail(MPADAM_EINVAL, "grads[%d] is NULL", k);
       if (!is_aligned(grads[k], grad_size)) return fail(MPADAM_EINVAL, "grads[%d] not aligned to its element size", k);
     }
-    return MPADAM_OK;
-  }
-
-  // Gradient pointers for a launch on `stream`: with it, or through the device
-  // table, refilled when they changed.  A replayed graph fills the table as it
-  // was captured, so once a fill was captured the table's content is not known.
-  int32_t grads_for(GradTable* g, const void* const* grads, cudaStream_t stream) {
-    g->grads = nullptr;
-    if (n <= kInlineGrads) {
-      std::memcpy(g->inline_grads, grads, sizeof(void*) * n);
-      return MPADAM_OK;
-    }
-    g->grads = d_grads;
-    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
-    cudaError_t e = cudaStreamIsCapturing(stream, &st);
-    if (e != cudaSuccess) return cuda_fail(e, "cudaStreamIsCapturing");
-    if (st != cudaStreamCaptureStatusNone) captured = true;
-    if (!captured && last_known && std::memcmp(last.data(), grads, sizeof(void*) * n) == 0) return MPADAM_OK;
-    last_known = false;
-    for (int32_t i = 0; i < n; i += kInlineGrads) {
-      e = fill_grads(d_grads, grads + i, i, std::min(kInlineGrads, n - i), stream);
-      if (e != cudaSuccess) return cuda_fail(e, "launch of the gradient table's fill");
-    }
-    last.assign(grads, grads + n);
-    last_known = true;
     return MPADAM_OK;
   }
 };
@@ -208,7 +174,7 @@ extern "C" int32_t mpadam_adamw_step(mpadam_adamw_state* s, const void* const* g
   rc = check_device(s->list.device);
   if (rc) return rc;
   try {
-    rc = s->list.grads_for(&s->args.g, grads, stream);
+    rc = s->list.grads.for_launch(&s->args.g, grads, s->list.n, stream);
   } catch (const std::bad_alloc&) {
     return fail(MPADAM_EALLOC, "host allocation failed");
   }
@@ -300,7 +266,7 @@ extern "C" int32_t mpadam_grad_norm(mpadam_grad_norm_state* s, const void* const
   if (rc) return rc;
   if (s->list.tiles) {
     try {
-      rc = s->list.grads_for(&s->args.g, grads, stream);
+      rc = s->list.grads.for_launch(&s->args.g, grads, s->list.n, stream);
     } catch (const std::bad_alloc&) {
       return fail(MPADAM_EALLOC, "host allocation failed");
     }
@@ -345,20 +311,6 @@ extern "C" int32_t mpadam_e4m3_quantize(const void* x, int32_t x_dtype, int64_t 
 namespace {
 
 constexpr int64_t kMatmulMax = INT32_MAX - 1023;  // the kernels round sizes up to tiles in 32 bits
-
-using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
-
-EncodeTiled encode_tiled() {
-  static const EncodeTiled f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-        r != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeTiled>(p);
-  }();
-  return f;
-}
 
 // Tensor map of scales, [row tiles, groups, 128 words], boxes of `box` row tiles of one group.
 bool scale_map(CUtensorMap* map, const uint8_t* s, int64_t rows, int64_t k, int box) {
