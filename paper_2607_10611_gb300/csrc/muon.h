@@ -4,10 +4,10 @@
 //
 // Every matrix is worked on lying down, [r, c] with r <= c (a tall one as its
 // transpose), and held in FP16 times 2^14: X in two parts, a value's FP16 and the
-// FP16 of what that leaves, A = X X^T and B = b A + c A A in one.  The steps'
-// polynomial keeps X's singular values, and so its values, below 1.21, A's below
-// 1.45 and B's below 2.81, so nothing reaches 65504, and what lies below FP16's
-// normal numbers is below 2^-28.  FP16 is as fast as BF16 on the tensor cores and
+// FP16 of what that leaves, A = X X^T and B = a I + b A + c A A in one.  The
+// steps' polynomial keeps X's singular values, and so its values, below 1.21, A's
+// below 1.45 and B's between 0.63 and 3.45, so nothing reaches 65504, and what
+// lies below FP16's normal numbers is below 2^-28.  FP16 is as fast as BF16 on the tensor cores and
 // rounds 8 times finer; X's second part, which only the sum a X takes, keeps the
 // small singular values of matrices that a few large ones dominate: a 768 x 768
 // of rank 32 and 1 % noise comes out with a relative error of 6e-4 after five
@@ -55,7 +55,7 @@ struct ProductArgs {
   int32_t* err;
 };
 
-// The three products of a step: A = X X^T, B = b A + c A A, X = a X + B X.
+// The three products of a step: A = X X^T, B = a I + b A + c A A, X = B X and a times X's second part.
 cudaError_t launch_product(int which, const ProductArgs& a, cudaStream_t stream);
 
 // A matrix as the element-wise kernels see it.
@@ -79,11 +79,20 @@ struct MuonMatrix {
   uint32_t aligned;    // w, m and compute on 16-byte boundaries
 };
 
+// 1 / |U| times 2^14, as three factors that take a value of U to X's without
+// leaving binary32's range on the way; and the chunks whose squares are summed (0
+// between launches).
+struct MuonNorm {
+  float down0, down1, rest;
+  uint32_t done;
+};
+
 struct MuonArgs {
   const MuonMatrix* matrices;
   const int32_t* owner;      // the matrix of each tile, or of each chunk
   int32_t count;
   double* partial;           // sums of squares, a chunk each
+  MuonNorm* norms;           // of each matrix
   const float* grad_scale;   // or nullptr
   int32_t* err;              // the products' error word
   float beta, rest, lr, decay;

@@ -172,7 +172,8 @@ struct Newton {
     const size_t newton_at = 0, matrices_at = newton_at + round_up(sizeof(NewtonMatrix) * newton.size(), 256);
     const size_t tiles_at = matrices_at + round_up(sizeof(MuonMatrix) * matrices.size(), 256);
     const size_t owners_at = tiles_at + round_up(sizeof(NewtonTile) * tiles.size(), 256);
-    const size_t err_at = owners_at + round_up(sizeof(int32_t) * owners.size(), 256), upload = err_at + 256;
+    const size_t err_at = owners_at + round_up(sizeof(int32_t) * owners.size(), 256), norms_at = err_at + 256;
+    const size_t upload = norms_at + round_up(sizeof(MuonNorm) * matrices.size(), 256);
     const size_t partial_at = upload, pointers_at = partial_at + round_up(sizeof(double) * chunks_most, 256);
     const size_t bytes = pointers_at + (n > kInlineGrads ? 2 * sizeof(void*) * n : 0);
     std::vector<uint8_t> host(upload);
@@ -198,6 +199,7 @@ struct Newton {
     args.matrices = reinterpret_cast<const MuonMatrix*>(memory + matrices_at);
     args.partial = reinterpret_cast<double*>(memory + partial_at);
     args.err = reinterpret_cast<int32_t*>(memory + err_at);
+    args.norms = reinterpret_cast<MuonNorm*>(memory + norms_at);
     args.last = steps & 1;
     in.table = reinterpret_cast<const void**>(memory + pointers_at);
     out.table = in.table + n;

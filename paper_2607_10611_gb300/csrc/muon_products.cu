@@ -1,8 +1,9 @@
 // muon_products.cu -- the three products of a Newton-Schulz step (muon.h) over a
 // list of matrices, one launch each:
-//   A = X X^T,   B = b A + c A A,   X <- a X + B X
-// A and B are symmetric: their tiles on and below the diagonal are computed and
-// stored in both places.
+//   A = X X^T,   B = a I + b A + c A A,   X <- B X
+// of X's first part; a times its second part is added to the last.  A and B are
+// symmetric: their tiles on and below the diagonal are computed and stored in
+// both places.
 #include <algorithm>
 #include <atomic>
 
@@ -197,51 +198,68 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int i = blockIdx.x / 2; i < p.count; i += pairs) {
+      const NewtonTile t = p.tiles[i];
+      const NewtonMatrix& q = p.matrices[t.matrix];
+      const int m = t.tm * kNewtonTile + (int)rank * 128 + quarter * 32 + lane, n0 = t.tn * kNewtonTile + half * 128;
+      const int rows = q.r, last_m = WHICH == 3 ? q.c : q.r;
+      const int64_t ld = WHICH == 3 ? q.ld : q.lda;
+      // What is added to the sums, X's second part or A, a column of the tile at a time: fetched ahead, whatever is in the
+      // way of the stores.
+      const uint16_t* addend = WHICH == 3 ? q.lo : q.ga;
+      const bool adds = WHICH == 2 || (WHICH == 3 && p.use_lo);
+      uint16_t ahead[32];
+      auto fetch = [&](int c) {
+        const uint16_t* from = addend + (int64_t)(n0 + c) * ld + m;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) ahead[j] = adds && m < last_m && n0 + c + j < rows ? from[j * ld] : (uint16_t)0;
+      };
+      if (WHICH != 1) fetch(0);
       if (!warp_wait_cluster(acc_full(acc), acc_phase) || *stop) {
         if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
         break;
       }
       tc_fence_after();
-      const NewtonTile t = p.tiles[i];
-      const NewtonMatrix& q = p.matrices[t.matrix];
-      const int m = t.tm * kNewtonTile + (int)rank * 128 + quarter * 32 + lane, n0 = t.tn * kNewtonTile + half * 128;
-      const int rows = q.r, last_m = WHICH == 3 ? q.c : q.r;
       const uint32_t from = tmem + acc * kNewtonTile + half * 128 + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
       for (int c = 0; c < 128; c += 32) {
         uint32_t r[32];
+        uint16_t add[32];
         __syncwarp();
         tmem_load32(from + c, r);
+        if (WHICH != 1) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) add[j] = ahead[j];
+          if (c + 32 < 128) fetch(c + 32);
+        }
         tmem_wait_load();
         const int n = n0 + c, here = min(32, rows - n);  // columns of the tile: rows of the result
         if (here <= 0 || m >= last_m) continue;
+        const int64_t at = (int64_t)n * ld + m;
         if (WHICH == 3) {
-          const int64_t at = (int64_t)n * q.ld + m;
-          const uint16_t *hi = q.hi[p.from] + at, *lo = q.lo + at;
-          uint16_t *hi_out = q.hi[p.from ^ 1] + at, *lo_out = q.lo + at;
+          uint16_t *hi = q.hi[p.from ^ 1] + at, *lo = q.lo + at;
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             if (j >= here) break;
-            float x = of_half(hi[j * q.ld]);
-            if (p.use_lo) x = __fadd_rn(x, of_half(lo[j * q.ld]));
-            const float y = __fmaf_rn(kA, x, __fmul_rn(__uint_as_float(r[j]), kFromHeld));
+            const float y = __fmaf_rn(kA, of_half(add[j]), __fmul_rn(__uint_as_float(r[j]), kFromHeld));
             const uint16_t h = half_of(y);
-            hi_out[j * q.ld] = h;
-            if (p.keep_lo) lo_out[j * q.ld] = half_of(__fsub_rn(y, of_half(h)));
+            hi[j * ld] = h;
+            if (p.keep_lo) lo[j * ld] = half_of(__fsub_rn(y, of_half(h)));
           }
         } else {
           uint16_t* out = WHICH == 1 ? q.ga : q.gb;
-          uint16_t* below = out + (int64_t)n * q.lda + m;
           uint16_t h[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             float y = __fmul_rn(__uint_as_float(r[j]), kFromHeld);
-            if (WHICH == 2) y = __fmaf_rn(kC, y, j < here ? __fmul_rn(kB, of_half(q.ga[(int64_t)(n + j) * q.lda + m])) : 0.0f);
+            if (WHICH == 2) {
+              y = __fmaf_rn(kC, y, __fmul_rn(kB, of_half(add[j])));
+              if (n + j == m) y = __fadd_rn(y, kA * kHeld);
+            }
             h[j] = half_of(y);
-            if (j < here) below[j * q.lda] = h[j];
+            if (j < here) out[at + j * ld] = h[j];
           }
           if (t.tm != t.tn) {  // (the row's padding has room for whole vectors)
-            uint4* row = reinterpret_cast<uint4*>(out + (int64_t)m * q.lda + n);
+            uint4* row = reinterpret_cast<uint4*>(out + (int64_t)m * ld + n);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               if (8 * j >= here) break;

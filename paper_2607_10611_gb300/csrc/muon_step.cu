@@ -7,6 +7,7 @@
 // Every operation rounds on its own, in binary32; the squares' sums are in
 // binary64 above 64 of them.
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 #include "muon.h"
@@ -136,15 +137,16 @@ __global__ void __launch_bounds__(kStepThreads) squares_kernel(const __grid_cons
   const int64_t end = min(numel, first + q.chunk);
   const bool vec = on_16(in) && (!STEP || q.aligned);
   double sum = 0.0;
-  for (int64_t base = first; base < end; base += kSquaresPass) {
+  auto pass = [&](int64_t base, auto whole_pass) {
+    constexpr bool all = decltype(whole_pass)::value;  // of vectors
     float u[8][8];
 #pragma unroll
     for (int v = 0; v < 8; ++v) {
       const int64_t at = base + (v * kStepThreads + threadIdx.x) * 8;
-      const int count = (int)max((int64_t)0, min((int64_t)8, end - at));
+      const int count = all ? 8 : (int)max((int64_t)0, min((int64_t)8, end - at));
       float m[8];
-      if (count) {
-        update8<STEP, G32, M32>(p, q, in, at, count, vec && count == 8, scale, m, u[v]);
+      if (all || count) {
+        update8<STEP, G32, M32>(p, q, in, at, count, all || (vec && count == 8), scale, m, u[v]);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[v][i] = 0.0f;
@@ -166,24 +168,36 @@ __global__ void __launch_bounds__(kStepThreads) squares_kernel(const __grid_cons
         s[i & 3] = __fmaf_rn(x, x, s[i & 3]);
       }
     sum += (double)__fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3])) * pow2d(2 * e);
+  };
+  for (int64_t base = first; base < end; base += kSquaresPass) {
+    if (vec && end - base >= kSquaresPass) pass(base, std::true_type());
+    else pass(base, std::false_type());
   }
+  // The last of a matrix's blocks sums up, in the chunks' order, and leaves the count as it was.
+  __shared__ bool last;
   sum = block_sum(sum);
-  if (threadIdx.x == 0) p.partial[blockIdx.x] = sum;
-}
-
-// 1 / |U| times 2^14, as three factors that take a value of U to X's without leaving binary32's range on the way.
-struct Inverse {
-  float down0, down1, rest;
-  __device__ __forceinline__ float operator()(float u) const { return __fmul_rn(__fmul_rn(__fmul_rn(u, down0), down1), rest); }
-};
-__device__ __forceinline__ Inverse inverse_norm(const double* partial, int chunks) {
-  double s = 0.0;
-  for (int i = threadIdx.x; i < chunks; i += kStepThreads) s += partial[i];
-  const double norm = sqrt(block_sum(s));
-  if (norm == 0.0) return {0.0f, 0.0f, 0.0f};
-  if (!(norm <= 1e300)) return {1.0f, 1.0f, __uint_as_float(0x7FC00000u)};  // no direction
-  const int e = (int)(__double_as_longlong(norm) >> 52) - 1023, half = e / 2;  // |e| < 200: U has less than 2^60 elements
-  return {pow2f(-half), pow2f(-(e - half)), (float)((double)kHeld / (norm * pow2d(-e)))};
+  if (threadIdx.x == 0) {
+    p.partial[blockIdx.x] = sum;
+    __threadfence();
+    last = atomicAdd(&p.norms[k].done, 1u) == (uint32_t)q.chunks - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!last) return;
+  sum = 0.0;
+  for (int i = threadIdx.x; i < q.chunks; i += kStepThreads) sum += __ldcg(p.partial + q.chunk0 + i);
+  sum = block_sum(sum);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(sum);
+    MuonNorm n{0.0f, 0.0f, 0.0f, 0u};
+    if (!(norm <= 1e300)) {
+      n = {1.0f, 1.0f, __uint_as_float(0x7FC00000u), 0u};  // no direction
+    } else if (norm > 0.0) {  // |e| < 200: U has less than 2^41 elements
+      const int e = (int)(__double_as_longlong(norm) >> 52) - 1023, half = e / 2;
+      n = {pow2f(-half), pow2f(-(e - half)), (float)((double)kHeld / (norm * pow2d(-e))), 0u};
+    }
+    p.norms[k] = n;
+  }
 }
 
 // A block takes a tile of 64 x 64 of the caller's matrix; a thread 8 neighbours
@@ -198,38 +212,47 @@ __global__ void __launch_bounds__(kStepThreads) begin_kernel(const __grid_consta
   const void* in = pointer_of(p.in, q.index);
   const int tile = blockIdx.x - q.tile0, i0 = tile / q.tiles_across * kElementTile, j0 = tile % q.tiles_across * kElementTile;
   const bool vec = q.cols % 8 == 0 && on_16(in) && (!STEP || q.aligned);
-  const Inverse inverse = inverse_norm(p.partial + q.chunk0, q.chunks);
+  const MuonNorm norm = p.norms[p.owner[blockIdx.x]];
   const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+  auto take = [&](auto whole_tile) {
+    constexpr bool all = decltype(whole_tile)::value;  // of vectors
+    float m[2][8], u[2][8];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int i = i0 + r + 32 * h, j = j0 + c, count = i < q.rows ? max(0, min(8, q.cols - j)) : 0;
-    uint32_t held[8] = {};
-    if (count) {
-      const int64_t at = (int64_t)i * q.cols + j;
-      const bool whole = vec && count == 8;
-      float m[8], u[8];
-      update8<STEP, G32, M32>(p, q, in, at, count, whole, scale, m, u);
-      if (STEP) store8<M32>(q.m, at, count, whole, m);
+    for (int h = 0; h < 2; ++h) {
+      const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+      if (all || count) update8<STEP, G32, M32>(p, q, in, (int64_t)i * q.cols + j, count, all || (vec && count == 8), scale, m[h], u[h]);
+    }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float x = inverse(u[k]);
-        const uint16_t hi = half_of(x);
-        held[k] = hi | (uint32_t)half_of(__fsub_rn(x, of_half(hi))) << 16;
+    for (int h = 0; h < 2; ++h) {
+      const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+      uint32_t held[8] = {};
+      if (all || count) {
+        const int64_t at = (int64_t)i * q.cols + j;
+        const bool whole = all || (vec && count == 8);
+        if (STEP) store8<M32>(q.m, at, count, whole, m[h]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float x = __fmul_rn(__fmul_rn(__fmul_rn(u[h][k], norm.down0), norm.down1), norm.rest);
+          const uint16_t hi = half_of(x);
+          held[k] = hi | (uint32_t)half_of(__fsub_rn(x, of_half(hi))) << 16;
+        }
+        if (!q.tall) {  // (rows' padding has room for whole vectors)
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) hi[k] = __byte_perm(held[2 * k], held[2 * k + 1], 0x5410), lo[k] = __byte_perm(held[2 * k], held[2 * k + 1], 0x7632);
+          const int64_t to = (int64_t)i * q.ld + j;
+          *reinterpret_cast<uint4*>(q.hi[0] + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(q.lo + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
       }
-      if (!q.tall) {  // (rows' padding has room for whole vectors)
-        uint32_t hi[4], lo[4];
+      if (q.tall) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) hi[k] = __byte_perm(held[2 * k], held[2 * k + 1], 0x5410), lo[k] = __byte_perm(held[2 * k], held[2 * k + 1], 0x7632);
-        const int64_t to = (int64_t)i * q.ld + j;
-        *reinterpret_cast<uint4*>(q.hi[0] + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(q.lo + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        for (int k = 0; k < 8; ++k) turned[r + 32 * h][c + k] = held[k];
       }
     }
-    if (q.tall) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) turned[r + 32 * h][c + k] = held[k];
-    }
-  }
+  };
+  if (vec && i0 + kElementTile <= q.rows && j0 + kElementTile <= q.cols) take(std::true_type());
+  else take(std::false_type());
   if (!q.tall) return;
   __syncthreads();
 #pragma unroll
@@ -247,20 +270,28 @@ __global__ void __launch_bounds__(kStepThreads) begin_kernel(const __grid_consta
   }
 }
 
-// The 16 random bits of the elements e to e + 7 of the list.
-__device__ __forceinline__ void random_lanes(const MuonArgs& p, int64_t e, uint32_t (&bits)[8]) {
-  const uint32_t lo = (uint32_t)p.step, hi = (uint32_t)((uint64_t)p.step >> 32);
-  uint4 r = make_uint4(0, 0, 0, 0);
+// The 16 random bits of the elements e to e + 7 of the list, e a multiple of 8.
+__device__ __forceinline__ void random_block(const MuonArgs& p, int64_t e, uint32_t* bits) {
+  const uint64_t b = (uint64_t)e / 8;
+  const uint4 r = philox4x32_10((uint32_t)b, (uint32_t)(b >> 32), (uint32_t)p.step, (uint32_t)((uint64_t)p.step >> 32), p.rk0, p.rk1);
+  const uint32_t u[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i == 0 || (e + i) % 8 == 0) {
-      const uint64_t b = (uint64_t)(e + i) / 8;
-      r = philox4x32_10((uint32_t)b, (uint32_t)(b >> 32), lo, hi, p.rk0, p.rk1);
+  for (int i = 0; i < 8; ++i) bits[i] = i & 1 ? u[i / 2] >> 16 : u[i / 2] & 0xFFFFu;
+}
+// The same of any e: from the two blocks that they lie in.
+__device__ __forceinline__ void random_lanes(const MuonArgs& p, int64_t e, uint32_t (&bits)[8]) {
+  uint32_t two[16];
+  random_block(p, e & ~(int64_t)7, two);
+  random_block(p, (e & ~(int64_t)7) + 8, two + 8);
+  // shifted down by e mod 8, in steps of 4, 2 and 1, so that the array stays in registers
+#pragma unroll
+  for (int d = 4; d; d >>= 1)
+    if (e & d) {
+#pragma unroll
+      for (int i = 0; i + d < 16; ++i) two[i] = two[i + d];
     }
-    const int l = (int)((e + i) & 7);
-    const uint32_t word = l < 4 ? (l < 2 ? r.x : r.y) : (l < 6 ? r.z : r.w);
-    bits[i] = l & 1 ? word >> 16 : word & 0xFFFFu;
-  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) bits[i] = two[i];
 }
 
 template <bool STEP, bool W32, bool SR>
@@ -287,44 +318,57 @@ __global__ void __launch_bounds__(kStepThreads) finish_kernel(const __grid_const
   void* out = STEP ? nullptr : const_cast<void*>(pointer_of(p.out, q.index));
   const bool vec = q.cols % 8 == 0 && (STEP ? q.aligned != 0 : on_16(out));
   const float ka = __fmul_rn(p.lr, q.factor);
+  auto take = [&](auto whole_tile) {
+    constexpr bool all = decltype(whole_tile)::value;  // of vectors
+    float weights[2][8];
+    if (STEP) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int i = i0 + r + 32 * h, j = j0 + c, count = i < q.rows ? max(0, min(8, q.cols - j)) : 0;
-    if (!count) continue;
-    const int64_t at = (int64_t)i * q.cols + j;
-    const bool whole = vec && count == 8;
-    float o[8];
-    if (q.tall) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = of_half(turned[r + 32 * h][c + k]);
-    } else {
-      const uint4 v = *reinterpret_cast<const uint4*>(x + (int64_t)i * q.ld + j);
-      const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = of_half((uint16_t)(u[k / 2] >> 16 * (k & 1)));
+      for (int h = 0; h < 2; ++h) {
+        const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+        if (all || count) load8<W32>(q.w, (int64_t)i * q.cols + j, count, all || (vec && count == 8), weights[h]);
+      }
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = __fmul_rn(o[k], kFromHeld);
-    if (!STEP) {
-      store8<W32>(out, at, count, whole, o);
-      continue;
-    }
-    float w[8];
-    load8<W32>(q.w, at, count, whole, w);
+    for (int h = 0; h < 2; ++h) {
+      const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+      if (!all && !count) continue;
+      const int64_t at = (int64_t)i * q.cols + j;
+      const bool whole = all || (vec && count == 8);
+      float o[8];
+      if (q.tall) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float kept = p.decay != 0.0f ? __fsub_rn(w[k], __fmul_rn(w[k], p.decay)) : w[k];
-      w[k] = __fsub_rn(kept, __fmul_rn(o[k], ka));
-    }
-    if (SR) {
-      uint32_t bits[8];
-      random_lanes(p, q.goff + at, bits);
+        for (int k = 0; k < 8; ++k) o[k] = of_half(turned[r + 32 * h][c + k]);
+      } else {
+        const uint4 v = *reinterpret_cast<const uint4*>(x + (int64_t)i * q.ld + j);
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = bf16_value((uint16_t)(bf16_sr_sum(w[k], ~bits[k] & 0xFFFFu) >> 16));
+        for (int k = 0; k < 8; ++k) o[k] = of_half((uint16_t)(u[k / 2] >> 16 * (k & 1)));
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = __fmul_rn(o[k], kFromHeld);
+      if (!STEP) {
+        store8<W32>(out, at, count, whole, o);
+        continue;
+      }
+      float (&w)[8] = weights[h];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float kept = p.decay != 0.0f ? __fsub_rn(w[k], __fmul_rn(w[k], p.decay)) : w[k];
+        w[k] = __fsub_rn(kept, __fmul_rn(o[k], ka));
+      }
+      if (SR) {
+        uint32_t bits[8];
+        if (all) random_block(p, q.goff + at, bits);  // (rows start at multiples of 8)
+        else random_lanes(p, q.goff + at, bits);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = bf16_value((uint16_t)(bf16_sr_sum(w[k], ~bits[k] & 0xFFFFu) >> 16));
+      }
+      store8<W32>(q.w, at, count, whole, w);
+      if (W32 && q.compute) store8<false>(q.compute, at, count, whole, w);
     }
-    store8<W32>(q.w, at, count, whole, w);
-    if (W32 && q.compute) store8<false>(q.compute, at, count, whole, w);
-  }
+  };
+  if (vec && i0 + kElementTile <= q.rows && j0 + kElementTile <= q.cols) take(std::true_type());
+  else take(std::false_type());
 }
 
 template <bool STEP, bool G32, bool M32>
