@@ -31,7 +31,7 @@ SOURCES = ["mpadam_api.cu", "step_bf16.cu", "step_e4m3.cu", "step_e4m3b.cu", "st
            "train_api.cu", "adamw.cu", "fp8_quant.cu", "fp8_matmul.cu", "layer_api.cu", "layer_norm.cu", "fp4_linear.cu",
            "muon_api.cu", "muon_step.cu", "muon_products.cu"]
 HEADERS = ["step_args.h", "step_kernel.cuh", "toy.h", "host.h", "adamw.h", "adamw_math.cuh", "fp8.h", "launch.h", "layer_norm.h", "fp4.h", "list.h",
-           "muon.h", "tcgen05.cuh"]
+           "muon.h", "muon_schedule.h", "tcgen05.cuh"]
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + [

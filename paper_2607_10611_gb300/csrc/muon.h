@@ -25,38 +25,61 @@ namespace mpadam {
 constexpr float kHeld = 0x1p14f, kFromHeld = 0x1p-14f;
 
 constexpr int kNewtonTile = 256;   // rows and columns of a product's tile, by a pair of CTAs
-constexpr int kElementTile = 64;   // rows and columns of a tile of the element-wise kernels
-constexpr int kSquaresPass = 16384; // elements that a block squares at once
+constexpr int kNewtonStepK = 64;   // values of k that are copied and multiplied at once
+constexpr int kNewtonPairs = 76;   // GB300: two SMs each
+constexpr int kTileRows = 64;      // rows and columns of a tile of the element-wise kernels
+constexpr int kTileCols = 128;
+constexpr int kSquaresPass = 8192; // elements that a block squares at once
 constexpr int kMaxChunks = 1024;   // partial sums of a matrix's squares
 
 // A matrix as the products see it.
 struct alignas(128) NewtonMatrix {
-  CUtensorMap x[2];    // X before and after an odd step, boxes of 64 x 64
+  CUtensorMap x[2];    // X's first part before and after an odd step, A and B: a product's operands, boxes of 128 rows of 64
   CUtensorMap a, b;
+  CUtensorMap x_along[2], a_along, b_along;            // the same where k runs along their columns: boxes of 64 x 64
+  CUtensorMap x_patch[2], lo_patch, a_patch, b_patch;  // boxes of 32 rows of 64, what an epilogue's warp handles at once
   uint16_t* hi[2];     // X's first part, row stride ld
   uint16_t* lo;        // and its second
   uint16_t* ga;        // A and B, row stride lda
   uint16_t* gb;
   int64_t ld, lda;
   int32_t r, c;
+  int32_t row0;        // its first counter: one for every 256 rows
 };
 
-struct NewtonTile {
-  int32_t matrix, tm, tn, pad;
+// A tile of a product: rows 256 tm and columns 256 tn of its result.
+struct alignas(16) NewtonTile {
+  int32_t matrix;
+  uint16_t tm, tn;
+  int32_t steps;   // of 64 values of k, times 32; and which product it is of (1, 2, 3), which X the step reads, whether something
+                   // is added to the sums (A, X's second part), whether X's second part is stored
+  uint32_t need;   // how far its operands' rows have to be: kSignals for every tile that was made of them
+
+  static NewtonTile make(int32_t matrix, int tm, int tn, int steps, int which, int from, bool adds, bool keep_lo, uint32_t need) {
+    return {matrix, (uint16_t)tm, (uint16_t)tn, steps << 5 | which << 3 | from << 2 | (int)adds << 1 | (int)keep_lo, need};
+  }
+  __host__ __device__ int steps_k() const { return steps >> 5; }
+  __host__ __device__ int which() const { return steps >> 3 & 3; }
+  __host__ __device__ int from() const { return steps >> 2 & 1; }
+  __host__ __device__ bool adds() const { return steps >> 1 & 1; }
+  __host__ __device__ bool keep_lo() const { return steps & 1; }
+  // Products 2 and 3 read rows `tile` of A and B up to the diagonal's tile; from this step of k on, what lies above the
+  // diagonal, they read what is below it, turned: k runs along its columns then.
+  __host__ __device__ static int turned_from(int tile) { return (tile + 1) * (kNewtonTile / kNewtonStepK); }
 };
+constexpr uint32_t kSignals = 16;
 
 struct ProductArgs {
   const NewtonMatrix* matrices;
   const NewtonTile* tiles;
   int32_t count;
-  int32_t from;        // which of a matrix's two X the step reads
-  int32_t keep_lo;     // the third product writes X's second part
-  int32_t use_lo;      // and reads it
+  uint32_t* progress;  // of every 256 rows; 0 when the launch begins, and so is
+  uint32_t* taken;     // the number of tiles that were taken
   int32_t* err;
 };
 
-// The three products of a step: A = X X^T, B = a I + b A + c A A, X = B X and a times X's second part.
-cudaError_t launch_product(int which, const ProductArgs& a, cudaStream_t stream);
+// All products of the list: A = X X^T, B = a I + b A + c A A, X = B X and a times X's second part, step after step.
+cudaError_t launch_products(const ProductArgs& a, cudaStream_t stream);
 
 // A matrix as the element-wise kernels see it.
 struct MuonMatrix {
@@ -95,6 +118,8 @@ struct MuonArgs {
   MuonNorm* norms;           // of each matrix
   const float* grad_scale;   // or nullptr
   int32_t* err;              // the products' error word
+  uint32_t* progress;        // the products' counters, which begin clears: `counters` of them
+  int32_t counters;
   float beta, rest, lr, decay;
   int32_t nesterov, last;    // last: which X holds the result
   int64_t step;

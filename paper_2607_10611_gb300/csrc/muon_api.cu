@@ -9,6 +9,7 @@
 
 #include "list.h"
 #include "muon.h"
+#include "muon_schedule.h"
 
 using namespace mpadam;
 
@@ -27,18 +28,28 @@ struct Matrix {
 
 // Matrices whose products run together, and where their entries in the tables begin.
 struct Group {
-  int64_t chunk_owner = 0, tile_owner = 0, symmetric = 0, full = 0;
-  int32_t chunks = 0, tiles = 0, symmetric_tiles = 0, full_tiles = 0;
+  int64_t chunk_owner = 0, tile_owner = 0, product = 0;
+  int32_t chunks = 0, tiles = 0, product_tiles = 0;
 };
 
 int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
-bool matrix_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld) {
+bool matrix_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t boxes[2] = {64, 64}, steps[2] = {1, 1};
+  const cuuint32_t boxes[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
   return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool matrix_maps(NewtonMatrix* m) {
+  constexpr int kOperand = kNewtonTile / 2, kAlong = kNewtonStepK, kPatch = 32;
+  auto x = [&](CUtensorMap* map, const void* p, int box_rows) { return matrix_map(map, p, m->r, m->c, m->ld, box_rows); };
+  auto a = [&](CUtensorMap* map, const void* p, int box_rows) { return matrix_map(map, p, m->r, m->r, m->lda, box_rows); };
+  bool ok = x(&m->lo_patch, m->lo, kPatch);
+  for (int i = 0; i < 2; ++i)
+    ok = ok && x(&m->x[i], m->hi[i], kOperand) && x(&m->x_along[i], m->hi[i], kAlong) && x(&m->x_patch[i], m->hi[i], kPatch);
+  ok = ok && a(&m->a, m->ga, kOperand) && a(&m->a_along, m->ga, kAlong) && a(&m->a_patch, m->ga, kPatch);
+  return ok && a(&m->b, m->gb, kOperand) && a(&m->b_along, m->gb, kAlong) && a(&m->b_patch, m->gb, kPatch);
 }
 
 // What both operators keep: the list, its tables on the device, the workspace.
@@ -73,7 +84,7 @@ struct Newton {
     std::vector<int32_t> owners;
     std::vector<NewtonTile> tiles;
     std::vector<int64_t> offsets;  // of each matrix in the workspace
-    int64_t goff = 0, used = 0, most = 0, chunks_most = 0;
+    int64_t goff = 0, used = 0, most = 0, chunks_most = 0, counters = 0;
     std::vector<std::pair<int32_t, int32_t>> members;  // of each group: first and last + 1
     for (int32_t k = 0; k < n; ++k) {
       const Matrix& x = list[k];
@@ -91,11 +102,13 @@ struct Newton {
       q.aligned = is_aligned(x.w, 16) && is_aligned(x.m, 16) && is_aligned(x.compute, 16);
       q.chunk = (int32_t)round_up((count + kMaxChunks - 1) / kMaxChunks, kSquaresPass);
       q.chunks = (int32_t)((count + q.chunk - 1) / q.chunk);
-      q.tiles_across = (int32_t)((x.cols + kElementTile - 1) / kElementTile);
+      q.tiles_across = (int32_t)((x.cols + kTileCols - 1) / kTileCols);
       NewtonMatrix m{};
       m.r = std::min(q.rows, q.cols), m.c = std::max(q.rows, q.cols);
       m.ld = q.ld = round_up(m.c, 64);
       m.lda = round_up(m.r, 64);
+      m.row0 = (int32_t)counters;
+      counters += newton_across(m.r);
       const int64_t bytes = 3 * round_up(2 * m.r * m.ld, 1024) + 2 * round_up(2 * m.r * m.lda, 1024);
       if (members.empty() || used + bytes > kWorkspace) {
         members.push_back({(int32_t)matrices.size(), (int32_t)matrices.size()});
@@ -108,47 +121,38 @@ struct Newton {
       matrices.push_back(q);
       newton.push_back(m);
     }
+    if (!encode_tiled() && !matrices.empty()) return fail(MPADAM_EUNSUPPORTED, "the driver offers no cuTensorMapEncodeTiled");
+    if (most && dev_malloc(&workspace, (size_t)most) != cudaSuccess) {
+      workspace = nullptr;
+      cudaGetLastError();
+      return fail(MPADAM_EALLOC, "allocation of a workspace of %lld bytes failed", (long long)most);
+    }
     for (const auto& member : members) {
       Group g;
-      std::vector<int32_t> order;  // long runs of k first, for an even end
-      for (int32_t k = member.first; k < member.second; ++k) order.push_back(k);
       g.chunk_owner = (int64_t)owners.size();
-      for (int32_t k : order) {
+      for (int32_t k = member.first; k < member.second; ++k) {
         matrices[k].chunk0 = (int64_t)owners.size() - g.chunk_owner;
         owners.insert(owners.end(), matrices[k].chunks, k);
       }
       g.chunks = (int32_t)(owners.size() - g.chunk_owner);
       chunks_most = std::max<int64_t>(chunks_most, g.chunks);
       g.tile_owner = (int64_t)owners.size();
-      for (int32_t k : order) {
-        const int64_t down = (matrices[k].rows + kElementTile - 1) / kElementTile;
+      for (int32_t k = member.first; k < member.second; ++k) {
+        const int64_t down = (matrices[k].rows + kTileRows - 1) / kTileRows;
         const int64_t first = (int64_t)owners.size() - g.tile_owner;
         if (first + down * matrices[k].tiles_across >= INT32_MAX) return fail(MPADAM_EINVAL, "the list has too many elements");
         matrices[k].tile0 = (int32_t)first;
         owners.insert(owners.end(), down * matrices[k].tiles_across, k);
       }
       g.tiles = (int32_t)(owners.size() - g.tile_owner);
-      auto across = [](int32_t n) { return (n + kNewtonTile - 1) / kNewtonTile; };
-      std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return newton[a].c > newton[b].c; });
-      g.symmetric = (int64_t)tiles.size();
-      for (int32_t k : order)
-        for (int32_t tm = 0; tm < across(newton[k].r); ++tm)
-          for (int32_t tn = 0; tn <= tm; ++tn) tiles.push_back({k, tm, tn, 0});
-      g.symmetric_tiles = (int32_t)(tiles.size() - g.symmetric);
-      std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return newton[a].r > newton[b].r; });
-      g.full = (int64_t)tiles.size();
-      for (int32_t k : order)  // 8 rows of tiles at a time, so that neighbours in time meet in L2
-        for (int32_t t0 = 0; t0 < across(newton[k].r); t0 += 8)
-          for (int32_t tm = 0; tm < across(newton[k].c); ++tm)
-            for (int32_t tn = t0; tn < std::min(across(newton[k].r), t0 + 8); ++tn) tiles.push_back({k, tm, tn, 0});
-      g.full_tiles = (int32_t)(tiles.size() - g.full);
+      int64_t count = 0;
+      for (int32_t k = member.first; k < member.second; ++k)
+        for (int which = 1; which <= 3; ++which) count += steps * newton_tiles(which, newton[k].r, newton[k].c);
+      if (count >= INT32_MAX / (2 * kSignals)) return fail(MPADAM_EINVAL, "the list has too many elements");
+      g.product = (int64_t)tiles.size();
+      g.product_tiles = (int32_t)count;
+      newton_schedule(newton, member.first, member.second, steps, kNewtonPairs, &tiles);
       groups.push_back(g);
-    }
-    if (!encode_tiled() && !matrices.empty()) return fail(MPADAM_EUNSUPPORTED, "the driver offers no cuTensorMapEncodeTiled");
-    if (most && dev_malloc(&workspace, (size_t)most) != cudaSuccess) {
-      workspace = nullptr;
-      cudaGetLastError();
-      return fail(MPADAM_EALLOC, "allocation of a workspace of %lld bytes failed", (long long)most);
     }
     for (size_t k = 0; k < matrices.size(); ++k) {
       NewtonMatrix& m = newton[k];
@@ -160,20 +164,17 @@ struct Newton {
         return p;
       };
       m.hi[0] = next(x), m.hi[1] = next(x), m.lo = next(x), m.ga = next(a), m.gb = next(a);
-      for (int i = 0; i < 2; ++i) {
-        matrices[k].hi[i] = m.hi[i];
-        if (!matrix_map(&m.x[i], m.hi[i], m.r, m.c, m.ld)) return fail(MPADAM_EINVAL, "no tensor map for a matrix of this size");
-      }
+      matrices[k].hi[0] = m.hi[0], matrices[k].hi[1] = m.hi[1];
       matrices[k].lo = m.lo;
-      if (!matrix_map(&m.a, m.ga, m.r, m.r, m.lda) || !matrix_map(&m.b, m.gb, m.r, m.r, m.lda))
-        return fail(MPADAM_EINVAL, "no tensor map for a matrix of this size");
+      if (!matrix_maps(&m)) return fail(MPADAM_EINVAL, "no tensor map for a matrix of this size");
     }
     // one allocation: what is uploaded, then the partial sums, the error word and the tables of pointers
     const size_t newton_at = 0, matrices_at = newton_at + round_up(sizeof(NewtonMatrix) * newton.size(), 256);
     const size_t tiles_at = matrices_at + round_up(sizeof(MuonMatrix) * matrices.size(), 256);
     const size_t owners_at = tiles_at + round_up(sizeof(NewtonTile) * tiles.size(), 256);
     const size_t err_at = owners_at + round_up(sizeof(int32_t) * owners.size(), 256), norms_at = err_at + 256;
-    const size_t upload = norms_at + round_up(sizeof(MuonNorm) * matrices.size(), 256);
+    const size_t progress_at = norms_at + round_up(sizeof(MuonNorm) * matrices.size(), 256);
+    const size_t upload = progress_at + round_up(sizeof(uint32_t) * (counters + 1), 256);
     const size_t partial_at = upload, pointers_at = partial_at + round_up(sizeof(double) * chunks_most, 256);
     const size_t bytes = pointers_at + (n > kInlineGrads ? 2 * sizeof(void*) * n : 0);
     std::vector<uint8_t> host(upload);
@@ -200,6 +201,8 @@ struct Newton {
     args.partial = reinterpret_cast<double*>(memory + partial_at);
     args.err = reinterpret_cast<int32_t*>(memory + err_at);
     args.norms = reinterpret_cast<MuonNorm*>(memory + norms_at);
+    args.progress = reinterpret_cast<uint32_t*>(memory + progress_at);
+    args.counters = (int32_t)counters + 1;
     args.last = steps & 1;
     in.table = reinterpret_cast<const void**>(memory + pointers_at);
     out.table = in.table + n;
@@ -225,15 +228,8 @@ struct Newton {
       args.owner = d_owners + g.tile_owner;
       args.count = g.tiles;
       if (e == cudaSuccess) e = launch_begin(args, kind, stream);
-      for (int32_t s = 0; s < steps; ++s) {
-        // X's second part is for the sum a X of all steps but the last, in which it no longer matters.
-        ProductArgs p{d_newton, d_tiles + g.symmetric, g.symmetric_tiles, s & 1, s + 2 < steps, s + 1 < steps, args.err};
-        if (e == cudaSuccess) e = launch_product(1, p, stream);
-        if (e == cudaSuccess) e = launch_product(2, p, stream);
-        p.tiles = d_tiles + g.full;
-        p.count = g.full_tiles;
-        if (e == cudaSuccess) e = launch_product(3, p, stream);
-      }
+      const ProductArgs p{d_newton, d_tiles + g.product, g.product_tiles, args.progress, args.progress + args.counters - 1, args.err};
+      if (e == cudaSuccess) e = launch_products(p, stream);
       if (e == cudaSuccess) e = launch_finish(args, kind, stream);
       if (e != cudaSuccess) return cuda_fail(e, "launch of the Newton-Schulz steps");
     }

@@ -1,11 +1,27 @@
-// muon_products.cu -- the three products of a Newton-Schulz step (muon.h) over a
-// list of matrices, one launch each:
+// muon_products.cu -- the products of all Newton-Schulz steps (muon.h) over a
+// list of matrices, in one launch:
 //   A = X X^T,   B = a I + b A + c A A,   X <- B X
 // of X's first part; a times its second part is added to the last.  A and B are
-// symmetric: their tiles on and below the diagonal are computed and stored in
-// both places.
+// symmetric: only their tiles on and below the diagonal are computed and stored, and
+// read as they lie or turned (an operand of the tensor cores may run along either of
+// its sides).
+//
+// The host lists every tile of every product in an order in which it can be made
+// (muon_schedule.h), and pairs of CTAs take them from that list one after another
+// by a counter.  Every 256 rows of a matrix have a counter of their own, which every
+// warp that has stored a part of a result in them raises, and a tile says how far
+// those of its operands' rows have to be; who takes it waits for that (bounded).
+//   A's tile (i, j) waits for rows i and j of X, B's for rows i and j of A, X's
+//   tile (i, n) for row i of B, and so for all that B's row was made of.
+// What a tile writes over was read only by tiles that those rows waited for.
+// Whatever a tile waits for is ahead of it in the list and taken by a pair that
+// runs, so the first tile that is not done can always go on, however many pairs run
+// at once.  One launch a product left the last wave of each to itself, 10 us of
+// launch, first copies and last stores each time, and X, A and B of a whole list out
+// of L2 in between.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "launch.h"
 #include "muon.h"
@@ -15,22 +31,28 @@ namespace mpadam {
 
 namespace {
 
-constexpr int kPairs = 76;      // GB300: two SMs each
-constexpr int kStepK = 64;      // values of k per stage: a row of one 128-byte swizzle atom
-constexpr int kStages = 6;
+constexpr int kStepK = kNewtonStepK;  // a row of one 128-byte swizzle atom
+constexpr int kStages = 5;
 constexpr int kBoxBytes = 64 * 64 * 2;
 constexpr int kStageBytes = 4 * kBoxBytes;  // 128 rows of either operand
-constexpr int kDynSmem = kStages * kStageBytes + 1024;
 constexpr uint32_t kStageTx = 2 * kStageBytes;  // of both CTAs
 constexpr int kEpiWarps = 8;
-constexpr int kProductThreads = 32 * (4 + kEpiWarps);  // a producer and an issuing warp (and two idle ones), then the epilogue
+static_assert(2 * kEpiWarps == kSignals, "every epilogue warp of a pair says when it has stored its part");
+constexpr int kPatchBytes = 32 * 64 * 2;        // rows of one 128-byte swizzle atom
+constexpr int kPatches = 2;                     // of a warp, in a tile
+constexpr int kEpiBytes = kPatches * kPatchBytes;
+static_assert(64 * kPatches * 2 == kNewtonTile, "two warps side by side");
+constexpr int kDynSmem = kStages * kStageBytes + kEpiWarps * kEpiBytes + 1024;
+constexpr int kProductThreads = 32 * (4 + kEpiWarps);  // producer, issuer, the one who takes tiles, an idle one, then the epilogue
+constexpr int kSlots = 3;                       // tiles that a pair has taken ahead of its epilogue
+constexpr int kReaders = 2 * kEpiWarps + 3;     // of a slot: epilogue warps and a producer in both CTAs, the issuer
 
-enum ProductError : int32_t { kErrCopy = 1, kErrStage = 2, kErrAcc = 4 };
+enum ProductError : int32_t { kErrCopy = 1, kErrStage = 2, kErrAcc = 4, kErrSlot = 8, kErrTurn = 16 };
 
 // The steps' coefficients (K. Jordan et al., "Muon: An optimizer for hidden layers in neural networks", 2024).
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 
-// An operand whose rows run along m (or n) instead of k: chunks of 64 of them 8192 bytes apart, groups of 8 values of k 1024.
+// An operand whose rows run along n instead of k: chunks of 64 of them 8192 bytes apart, groups of 8 values of k 1024.
 __device__ __forceinline__ uint32_t desc_low_mn(uint32_t addr) { return addr >> 4 | (uint32_t)(kBoxBytes >> 4) << 16; }
 
 __device__ __forceinline__ void pair_mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
@@ -41,26 +63,66 @@ __device__ __forceinline__ void pair_mma_f16(uint32_t d, uint64_t a, uint64_t b,
       : "memory");
 }
 
-__device__ __forceinline__ uint16_t half_of(float x) {
-  uint16_t h;
-  asm("cvt.rn.f16.f32 %0, %1;" : "=h"(h) : "f"(x));
+__device__ __forceinline__ void sts_v4(uint32_t addr, const uint32_t (&v)[4]) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ uint4 lds_v4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+// What this thread wrote to shared memory may be read by copies from here on.
+__device__ __forceinline__ void fence_for_copies() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+               : "memory");
+}
+__device__ __forceinline__ void commit_stores() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// This thread's stores, but for the last LEFT groups, have read what they store; or all have stored it.
+template <int LEFT>
+__device__ __forceinline__ void wait_for_reads() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void wait_for_stores() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
   return h;
 }
-__device__ __forceinline__ float of_half(uint16_t h) {
-  float x;
-  asm("cvt.f32.f16 %0, %1;" : "=f"(x) : "h"(h));
+__device__ __forceinline__ float2 of_half2(uint32_t h) {
+  float2 x;
+  asm("{\n .reg .f16 lo, hi;\n mov.b32 {lo, hi}, %2;\n cvt.f32.f16 %0, lo;\n cvt.f32.f16 %1, hi;\n}" : "=f"(x.x), "=f"(x.y) : "r"(h));
   return x;
 }
 
-// WHICH: 1, 2, 3, the product.  A tile is [256 rows m, 256 columns n] of
-//   1: X X^T, 2: A A, 3: X^T B (B is symmetric: the transpose of B X, whose rows then run along the lanes)
-// Lane m of a warp holds column by column n: stores of a column go to 32
-// neighbouring elements of the row n of the result (of the transposed place in a
-// symmetric one).
-template <int WHICH>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductArgs p) {
+
+__device__ __forceinline__ uint32_t load_relaxed(const uint32_t* p) {
+  uint32_t v;
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
+__device__ __forceinline__ void add_one_release(uint32_t* p) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory"); }
+// Between this thread's ordinary accesses to global memory and copies: in either direction.
+__device__ __forceinline__ void fence_copies_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+
+// A tile is 256 rows m by 256 columns n of a product's result, by a pair of CTAs;
+// a warp of the epilogue takes 32 rows, a row a lane, and 128 columns, in two
+// patches.  What is added to a patch's sums (A, or X's second part) is copied to
+// shared memory as the tile begins, the results take its place there and are copied
+// out; X's second part is held in registers until the first has gone.  Copies know
+// the matrix's edges (nothing lies beyond them, nothing is stored there).  Shared
+// memory's bandwidth is what this competes for: the products read 64 bytes a cycle
+// of it and the operands' copies write as many.  A row a lane straight from and to
+// memory (a line of L1 for 16 bytes), and results stored turned as well, took 8 us of
+// a warp's time a tile; this takes 3, and half of GPT-2's hidden matrices 800 us
+// instead of 1080.
+// One lane of the pair takes tiles and waits for their rows, so that nobody else has
+// to look.
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) newton_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ alignas(8) uint64_t bars[2 * kStages + 5];
+  __shared__ alignas(8) uint64_t bars[2 * kStages + 5 + 2 * kSlots + kEpiWarps];
+  __shared__ alignas(16) int4 slots[kSlots];
   __shared__ uint32_t tmem_base_s;
   __shared__ int32_t failed;
   const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -72,6 +134,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   auto acc_full = [&](int a) { return bar0 + 8u * (2 * kStages + a); };
   auto acc_free = [&](int a) { return bar0 + 8u * (2 * kStages + 2 + a); };
   const uint32_t drained = bar0 + 8u * (2 * kStages + 4);
+  auto slot_full = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + s); };           // each CTA's own
+  auto slot_free = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + kSlots + s); };  // the leader's alone
+  auto addend_full = [&](int w) { return bar0 + 8u * (2 * kStages + 5 + 2 * kSlots + w); };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -83,6 +148,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
       mbar_init(acc_free(a), 2 * kEpiWarps);
     }
     mbar_init(drained, 1);
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(slot_full(s), 1);
+      mbar_init(slot_free(s), kReaders);
+    }
+    for (int w = 0; w < kEpiWarps; ++w) mbar_init(addend_full(w), 1);
     failed = 0;
     mbar_init_fence();
   }
@@ -98,43 +168,113 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   const uint32_t tmem = tmem_base_s;
   wait_for_earlier_kernels();
 
-  const int pairs = gridDim.x / 2;
   volatile int32_t* stop = &failed;
-  auto steps_of = [&](const NewtonTile& t) {
-    const NewtonMatrix& q = p.matrices[t.matrix];
-    return ((WHICH == 1 ? q.c : q.r) + kStepK - 1) / kStepK;
+  // Nobody waits for long once someone of the pair has given up.
+  auto stop_both = [&] {
+    for (uint32_t r = 0; r < 2; ++r) sts_cluster(peer_addr(smem_addr(&failed), r), 1);
+  };
+  auto give_up = [&](int32_t why) {
+    atomicOr(p.err, why);
+    stop_both();
+  };
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+      if (mbar_try_wait(bar, parity)) return true;
+      if (*stop) return false;
+    }
+    return false;
+  };
+  auto wait_cluster = [&](uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+      if (mbar_try_wait_cluster(bar, parity)) return true;
+      if (*stop) return false;
+    }
+    return false;
+  };
+  auto tile_of = [](int4 v) {
+    return NewtonTile{v.x, (uint16_t)v.y, (uint16_t)((uint32_t)v.y >> 16), v.z, (uint32_t)v.w};
+  };
+  // The pair's n-th tile; matrix < 0: there are no more.  By whole warps, or by one lane (whole = false).
+  auto read_slot = [&](int n, NewtonTile& t, bool whole) {
+    const int s = n % kSlots;
+    bool ok = wait_cluster(slot_full(s), (uint32_t)(n / kSlots) & 1);
+    if (whole) ok = __all_sync(~0u, ok);
+    if (!ok) return false;
+    const volatile int4& v = slots[s];
+    t = tile_of(make_int4(v.x, v.y, v.z, v.w));
+    if (whole) __syncwarp();
+    if (!whole || lane == 0) mbar_arrive_cluster(peer_addr(slot_free(s), 0));
+    return true;
+  };
+  // Until the rows that the tile is made of have come as far as they have to.
+  auto wait_turn = [&](const NewtonTile& t) {
+    const uint32_t* count = p.progress + __ldg(&p.matrices[t.matrix].row0);
+    const uint32_t *one = count + t.tm, *two = t.which() == 3 ? one : count + t.tn;
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+      const uint32_t a = load_relaxed(one), b = load_relaxed(two);
+      if (a >= t.need && b >= t.need) {  // (loads that acquire empty L1 every time)
+        fence_gpu();
+        return true;
+      }
+      if (*stop || ((i & 63) == 63 && *static_cast<volatile int32_t*>(p.err))) return false;
+    }
+    return false;
   };
 
   if (warp == 0) {
     if (lane == 0) {
+      const uint32_t full0 = peer_addr(full(0), 0);
       int s = 0, issued = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int i = blockIdx.x / 2; i < p.count && ok; i += pairs) {
-        if (*stop) { ok = false; break; }
-        const NewtonTile t = p.tiles[i];
+      for (int n = 0; ok; ++n) {
+        NewtonTile t;
+        if (!read_slot(n, t, false)) { give_up(kErrSlot); ok = false; break; }
+        if (t.matrix < 0) break;
         const NewtonMatrix& q = p.matrices[t.matrix];
-        const CUtensorMap* first = WHICH == 2 ? &q.a : &q.x[p.from];
-        const CUtensorMap* second = WHICH == 1 ? &q.x[p.from] : WHICH == 2 ? &q.a : &q.b;
-        const int m0 = t.tm * kNewtonTile + (int)rank * 128, n0 = t.tn * kNewtonTile + (int)rank * 128, steps = steps_of(t);
-        for (int k = 0; k < steps; ++k) {
-          if (!mbar_wait(empty(s), phase ^ 1)) { ok = false; break; }
-          const uint32_t st = smem + s * kStageBytes, bar = peer_addr(full(s), 0);
-          if (rank == 0) mbar_arrive_tx(full(s), kStageTx);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (WHICH == 3) pair_load_2d(st + h * kBoxBytes, first, m0 + 64 * h, k * kStepK, bar);
-            else pair_load_2d(st + h * kBoxBytes, first, k * kStepK, m0 + 64 * h, bar);
-            pair_load_2d(st + (2 + h) * kBoxBytes, second, k * kStepK, n0 + 64 * h, bar);
+        const int which = t.which(), from = t.from(), steps = t.steps_k();
+        const CUtensorMap* first = which == 1 ? &q.x[from] : which == 2 ? &q.a : &q.b;
+        const CUtensorMap* turned = which == 2 ? &q.a_along : &q.b_along;
+        const CUtensorMap* second = which == 2 ? turned : &q.x_along[from];
+        prefetch_map(first);
+        if (which != 1) prefetch_map(turned);
+        if (which == 3) prefetch_map(second);
+        fence_copies_global();  // what others stored, and the slot's writer waited for, before what is copied here
+        const int m0 = t.tm * kNewtonTile + (int)rank * 128, n0 = t.tn * kNewtonTile + (int)rank * 128;
+        // (Loops of their own: a choice of maps within one took 130 cycles more a step.)
+        auto load = [&](int k, int end, auto first_turned, auto second_turned) {
+          for (; k < end && ok; ++k) {
+            if (!wait(empty(s), phase ^ 1)) { give_up(kErrStage); ok = false; break; }
+            const uint32_t st = smem + s * kStageBytes, to = st + kStageBytes / 2, bar = full0 + 8u * s;
+            const int x = k * kStepK;
+            if (rank == 0) mbar_arrive_tx(full(s), kStageTx);
+            if (decltype(first_turned)::value) {
+              pair_load_2d(st, turned, m0, x, bar);
+              pair_load_2d(st + kBoxBytes, turned, m0 + 64, x, bar);
+            } else {
+              pair_load_2d(st, first, x, m0, bar);
+            }
+            if (decltype(second_turned)::value) {
+              pair_load_2d(to, second, n0, x, bar);
+              pair_load_2d(to + kBoxBytes, second, n0 + 64, x, bar);
+            } else {
+              pair_load_2d(to, first, x, n0, bar);
+            }
+            ++issued;
+            if (++s == kStages) { s = 0; phase ^= 1; }
           }
-          ++issued;
-          if (++s == kStages) { s = 0; phase ^= 1; }
-        }
+        };
+        constexpr std::true_type yes;
+        constexpr std::false_type no;
+        const int plain = which == 1 ? steps : which == 2 ? min(steps, t.turned_from(t.tn)) : 0;
+        const int half = which == 1 ? steps : min(steps, t.turned_from(t.tm));
+        load(0, plain, no, no);
+        load(plain, half, no, yes);
+        load(half, steps, yes, yes);
       }
       if (!ok) {
-        *stop = 1;
-        atomicOr(p.err, kErrStage);
-        // the copies in flight: the leader sees both CTAs' last stages arrive, the other one waits for it in the end
+        // The copies in flight, before the block's memory goes: the leader sees both CTAs' last stages arrive (or waits its
+        // time), the other one waits for it in the end.
         for (int i = 0; i < min(issued, kStages); ++i) {
           if (s == 0) { s = kStages; phase ^= 1; }
           --s;
@@ -142,140 +282,193 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
         }
       }
     }
+  } else if (warp == 2 && rank == 0) {
+    if (lane == 0) {
+      for (int n = 0;; ++n) {
+        const int s = n % kSlots;
+        if (!wait_cluster(slot_free(s), (uint32_t)(n / kSlots) & 1 ^ 1)) { give_up(kErrSlot); break; }
+        const uint32_t i = atomicAdd(p.taken, 1u);
+        const bool more = i < (uint32_t)p.count;
+        const int4 v = more ? __ldg(reinterpret_cast<const int4*>(p.tiles) + i) : make_int4(-1, 0, 0, 0);
+        if (more && !wait_turn(tile_of(v))) { give_up(kErrTurn); break; }
+        for (uint32_t r = 0; r < 2; ++r) {
+          const uint32_t to = peer_addr(smem_addr(&slots[s]), r);
+          sts_cluster(to, (uint32_t)v.x), sts_cluster(to + 4, (uint32_t)v.y), sts_cluster(to + 8, (uint32_t)v.z), sts_cluster(to + 12, (uint32_t)v.w);
+          mbar_arrive_cluster(peer_addr(slot_full(s), r));
+        }
+        if (!more) break;
+      }
+    }
   } else if (warp == 1 && rank == 0) {
     const bool issue = elected();
-    // FP16 operands, binary32 sums, 256 x 256; product 3's first operand runs along m
-    constexpr uint32_t id = 1u << 4 | (WHICH == 3 ? 1u << 15 : 0u) | (uint32_t)(kNewtonTile >> 3) << 17 | (uint32_t)(kNewtonTile >> 4) << 24;
+    // FP16 operands, binary32 sums, 256 x 256
+    constexpr uint32_t kInstr = 1u << 4 | (uint32_t)(kNewtonTile >> 3) << 17 | (uint32_t)(kNewtonTile >> 4) << 24;
     int s = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
-    int i = blockIdx.x / 2, at = -1;  // the tile, and its step whose operands were given up
-    for (; i < p.count; i += pairs) {
-      const int steps = steps_of(p.tiles[i]);
-      if (!warp_wait_cluster(acc_free(acc), acc_phase ^ 1)) { at = 0; break; }
+    bool ok = true;
+    for (int n = 0; ok; ++n) {
+      NewtonTile t;
+      if (!read_slot(n, t, true)) { ok = false; break; }
+      if (t.matrix < 0) break;
+      const int steps = t.steps_k();
+      if (!__all_sync(~0u, wait_cluster(acc_free(acc), acc_phase ^ 1))) { ok = false; break; }
       tc_fence_after();
       const uint32_t d = tmem + acc * kNewtonTile;
       for (int k = 0; k < steps; ++k) {
-        if (!warp_wait(full(s), phase)) { at = k; break; }
+        if (!__all_sync(~0u, wait(full(s), phase))) { ok = false; break; }
         tc_fence_after();
         if (issue) {
-          const uint32_t st = smem + s * kStageBytes;
-          const uint32_t first = WHICH == 3 ? desc_low_mn(st) : desc_low(st), second = desc_low(st + 2 * kBoxBytes);
-          constexpr uint32_t kAdvance = WHICH == 3 ? 2048 >> 4 : 32 >> 4;  // 16 values of k
+          const uint32_t st = smem + s * kStageBytes, second_at = st + kStageBytes / 2;
+          const bool first_along = t.which() != 1 && k >= t.turned_from(t.tm);
+          const bool second_along = t.which() == 3 || (t.which() == 2 && k >= t.turned_from(t.tn));
+          const uint32_t first = first_along ? desc_low_mn(st) : desc_low(st), second = second_along ? desc_low_mn(second_at) : desc_low(second_at);
+          const uint32_t on1 = first_along ? 2048 >> 4 : 32 >> 4, on2 = second_along ? 2048 >> 4 : 32 >> 4;  // 16 values of k
+          const uint32_t id = kInstr | (first_along ? 1u << 15 : 0u) | (second_along ? 1u << 16 : 0u);
 #pragma unroll
           for (int j = 0; j < kStepK / 16; ++j)
-            pair_mma_f16(d, desc(first + kAdvance * j, kOperandHigh), desc(second + 2 * j, kOperandHigh), id, j > 0 || k > 0);
+            pair_mma_f16(d, desc(first + on1 * j, kOperandHigh), desc(second + on2 * j, kOperandHigh), id, j > 0 || k > 0);
           pair_commit(empty(s));
         }
         if (++s == kStages) { s = 0; phase ^= 1; }
       }
-      if (at >= 0) break;
+      if (!ok) break;
       if (issue) pair_commit(acc_full(acc));
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }
-    if (at >= 0) {
-      // The products in flight, then both CTAs' copies that are still to come (the producers fill every stage again, unless
-      // they have seen the stop), before their memory goes; then the epilogue is woken up to find that it has nothing to store.
+    if (!ok) {  // the products in flight, before their operands' memory goes (the producer waits for the copies)
       if (issue) {
-        atomicOr(p.err, kErrCopy);
+        give_up(kErrCopy);
         pair_commit(drained);
       }
-      warp_wait(drained, 0);
-      int64_t left = -at;
-      for (int t = i; t < p.count && left < kStages; t += pairs) left += steps_of(p.tiles[t]);
-      for (int n = 0; n < (int)min(left, (int64_t)kStages); ++n) {
-        warp_wait(full(s), phase);
-        if (++s == kStages) { s = 0; phase ^= 1; }
-      }
-      if (issue) {
-        for (uint32_t r = 0; r < 2; ++r) {
-          sts_cluster(peer_addr(smem_addr(&failed), r), 1);
-          mbar_arrive_cluster(peer_addr(acc_full(acc), r));
-        }
-      }
+      for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(drained, 0); ++i) {}
     }
   } else if (warp >= 4) {
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const int quarter = warp & 3, half = (warp - 4) >> 2, who = warp - 4;
+    const uint32_t places = smem + kStages * kStageBytes + who * kEpiBytes;
     int acc = 0;
-    uint32_t acc_phase = 0;
-    for (int i = blockIdx.x / 2; i < p.count; i += pairs) {
-      const NewtonTile t = p.tiles[i];
+    uint32_t acc_phase = 0, addend_phase = 0;
+    for (int at = 0;; ++at) {
+      NewtonTile t;
+      if (!read_slot(at, t, true)) { if (lane == 0) give_up(kErrSlot); break; }
+      if (t.matrix < 0) break;
       const NewtonMatrix& q = p.matrices[t.matrix];
-      const int m = t.tm * kNewtonTile + (int)rank * 128 + quarter * 32 + lane, n0 = t.tn * kNewtonTile + half * 128;
-      const int rows = q.r, last_m = WHICH == 3 ? q.c : q.r;
-      const int64_t ld = WHICH == 3 ? q.ld : q.lda;
-      // What is added to the sums, X's second part or A, a column of the tile at a time: fetched ahead, whatever is in the
-      // way of the stores.
-      const uint16_t* addend = WHICH == 3 ? q.lo : q.ga;
-      const bool adds = WHICH == 2 || (WHICH == 3 && p.use_lo);
-      uint16_t ahead[32];
-      auto fetch = [&](int c) {
-        const uint16_t* from = addend + (int64_t)(n0 + c) * ld + m;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) ahead[j] = adds && m < last_m && n0 + c + j < rows ? from[j * ld] : (uint16_t)0;
-      };
-      if (WHICH != 1) fetch(0);
-      if (!warp_wait_cluster(acc_full(acc), acc_phase) || *stop) {
-        if (lane == 0) { atomicOr(p.err, kErrAcc); *stop = 1; }
+      const int from = t.from();
+      const int m = t.tm * kNewtonTile + (int)rank * 128 + quarter * 32, n0 = t.tn * kNewtonTile + half * 128;
+      const int rows = q.r, cols = t.which() == 3 ? q.c : q.r, row0 = q.row0;
+      const int patches = m < rows ? min(kPatches, (max(cols - n0, 0) + 63) / 64) : 0;
+      const uint32_t sums = tmem + acc * kNewtonTile + half * 128 + ((uint32_t)(quarter * 32) << 16);
+      const bool fetches = t.adds() && patches > 0;
+      if (fetches && lane == 0) {  // (the places are free: the last tile's stores are done)
+        fence_copies_global();
+        mbar_arrive_tx(addend_full(who), patches * kPatchBytes);
+        for (int b = 0; b < patches; ++b)
+          tma_load_2d(places + b * kPatchBytes, t.which() == 2 ? &q.a_patch : &q.lo_patch, n0 + 64 * b, m, addend_full(who));
+      }
+      __syncwarp();
+      bool ok = __all_sync(~0u, wait_cluster(acc_full(acc), acc_phase));
+      if (fetches) {  // (seen to its end in any case: the copies are in flight)
+        ok = __all_sync(~0u, mbar_wait(addend_full(who), addend_phase)) && ok;
+        addend_phase ^= 1;
+      }
+      if (!ok) {
+        if (lane == 0) give_up(kErrAcc);
         break;
       }
       tc_fence_after();
-      const uint32_t from = tmem + acc * kNewtonTile + half * 128 + ((uint32_t)(quarter * 32) << 16);
-#pragma unroll 1
-      for (int c = 0; c < 128; c += 32) {
-        uint32_t r[32];
-        uint16_t add[32];
+      auto freed = [&] {  // the sums are read
+        tc_fence_before();
         __syncwarp();
-        tmem_load32(from + c, r);
-        if (WHICH != 1) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) add[j] = ahead[j];
-          if (c + 32 < 128) fetch(c + 32);
+        if (lane == 0) mbar_arrive_cluster(peer_addr(acc_free(acc), 0));
+      };
+      auto store = [&](const CUtensorMap* map, int b) {
+        fence_for_copies();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_2d(map, n0 + 64 * b, m, places + b * kPatchBytes);
+          commit_stores();
         }
-        tmem_wait_load();
-        const int n = n0 + c, here = min(32, rows - n);  // columns of the tile: rows of the result
-        if (here <= 0 || m >= last_m) continue;
-        const int64_t at = (int64_t)n * ld + m;
-        if (WHICH == 3) {
-          uint16_t *hi = q.hi[p.from ^ 1] + at, *lo = q.lo + at;
+      };
+      // 8 columns are 16 bytes of a row, in the copies' swizzle.
+      auto place = [&](int b, int g) { return places + b * kPatchBytes + lane * 128 + (g ^ (lane & 7)) * 16; };
+      auto make = [&](auto product, auto adding, auto keeping) {
+        constexpr int kWhich = decltype(product)::value;
+        constexpr bool kAdds = decltype(adding)::value, kKeepLo = decltype(keeping)::value;
+        uint32_t rest[kPatches][32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            if (j >= here) break;
-            const float y = __fmaf_rn(kA, of_half(add[j]), __fmul_rn(__uint_as_float(r[j]), kFromHeld));
-            const uint16_t h = half_of(y);
-            hi[j * ld] = h;
-            if (p.keep_lo) lo[j * ld] = half_of(__fsub_rn(y, of_half(h)));
-          }
-        } else {
-          uint16_t* out = WHICH == 1 ? q.ga : q.gb;
-          uint16_t h[32];
+        for (int b = 0; b < kPatches; ++b) {
+          if (b >= patches) break;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            float y = __fmul_rn(__uint_as_float(r[j]), kFromHeld);
-            if (WHICH == 2) {
-              y = __fmaf_rn(kC, y, __fmul_rn(kB, of_half(add[j])));
-              if (n + j == m) y = __fadd_rn(y, kA * kHeld);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[32];
+            tmem_load32(sums + 64 * b + 32 * h, r);
+            tmem_wait_load();
+            const bool diagonal = kWhich == 2 && n0 + 64 * b + 32 * h == m;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const uint32_t to = place(b, 4 * h + g);
+              uint4 add = make_uint4(0, 0, 0, 0);
+              if (kAdds) add = lds_v4(to);
+              const uint32_t old[4] = {add.x, add.y, add.z, add.w};
+              uint32_t sum[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int k = 8 * g + 2 * j;
+                float y0 = __fmul_rn(__uint_as_float(r[k]), kFromHeld), y1 = __fmul_rn(__uint_as_float(r[k + 1]), kFromHeld);
+                const float2 a = of_half2(old[j]);
+                if (kWhich == 2) {
+                  y0 = __fmaf_rn(kC, y0, __fmul_rn(kB, a.x)), y1 = __fmaf_rn(kC, y1, __fmul_rn(kB, a.y));
+                  if (diagonal) {
+                    if (lane == k) y0 = __fadd_rn(y0, kA * kHeld);
+                    if (lane == k + 1) y1 = __fadd_rn(y1, kA * kHeld);
+                  }
+                }
+                if (kWhich == 3 && kAdds) y0 = __fmaf_rn(kA, a.x, y0), y1 = __fmaf_rn(kA, a.y, y1);
+                sum[j] = half2_of(y0, y1);
+                if (kKeepLo) {
+                  const float2 held = of_half2(sum[j]);
+                  rest[b][16 * h + 4 * g + j] = half2_of(__fsub_rn(y0, held.x), __fsub_rn(y1, held.y));
+                }
+              }
+              sts_v4(to, sum);
             }
-            h[j] = half_of(y);
-            if (j < here) out[at + j * ld] = h[j];
           }
-          if (t.tm != t.tn) {  // (the row's padding has room for whole vectors)
-            uint4* row = reinterpret_cast<uint4*>(out + (int64_t)m * ld + n);
+          store(kWhich == 1 ? &q.a_patch : kWhich == 2 ? &q.b_patch : &q.x_patch[from ^ 1], b);
+        }
+        freed();
+        if (kKeepLo) {  // X's second part takes the first's place once that has been read
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (8 * j >= here) break;
-              uint32_t u[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) u[k] = h[8 * j + 2 * k] | (uint32_t)h[8 * j + 2 * k + 1] << 16;
-              row[j] = make_uint4(u[0], u[1], u[2], u[3]);
+          for (int b = 0; b < kPatches; ++b) {
+            if (b >= patches) break;
+            if (lane == 0) {
+              if (b + 1 < patches) wait_for_reads<1>();
+              else wait_for_reads<0>();
             }
+            __syncwarp();
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+              const uint32_t some[4] = {rest[b][4 * g], rest[b][4 * g + 1], rest[b][4 * g + 2], rest[b][4 * g + 3]};
+              sts_v4(place(b, g), some);
+            }
+            store(&q.lo_patch, b);
           }
         }
+      };
+      constexpr std::true_type yes;
+      constexpr std::false_type no;
+      if (t.which() == 1) make(std::integral_constant<int, 1>(), no, no);
+      else if (t.which() == 2) make(std::integral_constant<int, 2>(), yes, no);
+      else if (t.keep_lo()) make(std::integral_constant<int, 3>(), yes, yes);
+      else if (t.adds()) make(std::integral_constant<int, 3>(), yes, no);
+      else make(std::integral_constant<int, 3>(), no, no);
+      if (lane == 0) {
+        wait_for_stores();  // in memory now: its rows are that much further
+        fence_copies_global();
+        add_one_release(p.progress + row0 + t.tm);
+        if (t.which() != 3 && t.tm != t.tn) add_one_release(p.progress + row0 + t.tn);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(peer_addr(acc_free(acc), 0));
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }
+    if (lane == 0) wait_for_stores();
   }
   __syncwarp();
   tc_fence_before();
@@ -285,19 +478,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-template <int WHICH>
-cudaError_t launch(const ProductArgs& a, cudaStream_t stream) {
-  static std::atomic<uint64_t> ready{0};
-  const cudaError_t e = allow_smem((const void*)product_kernel<WHICH>, kDynSmem, ready);
-  if (e != cudaSuccess) return e;
-  return launch_dependent((const void*)product_kernel<WHICH>, 2 * (unsigned)std::min(a.count, kPairs), kProductThreads, 0, kDynSmem, &a,
-                          stream);
-}
-
 }  // namespace
 
-cudaError_t launch_product(int which, const ProductArgs& a, cudaStream_t stream) {
-  return which == 1 ? launch<1>(a, stream) : which == 2 ? launch<2>(a, stream) : launch<3>(a, stream);
+cudaError_t launch_products(const ProductArgs& a, cudaStream_t stream) {
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = allow_smem((const void*)newton_kernel, kDynSmem, ready);
+  if (e != cudaSuccess) return e;
+  return launch_dependent((const void*)newton_kernel, 2 * (unsigned)std::min(a.count, kNewtonPairs), kProductThreads, 0, kDynSmem, &a, stream);
 }
 
 }  // namespace mpadam

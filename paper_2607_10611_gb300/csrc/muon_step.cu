@@ -5,7 +5,7 @@
 //   begin:   m' is stored, and X = U / |U| in two parts (muon.h)
 //   finish:  w' = (w - kwd w) - ka O, rounded; or O is written out
 // Every operation rounds on its own, in binary32; the squares' sums are in
-// binary64 above 64 of them.
+// binary64 above 32 of them.
 #include <algorithm>
 #include <type_traits>
 
@@ -18,6 +18,11 @@ namespace mpadam {
 namespace {
 
 constexpr int kStepThreads = 256;
+constexpr int kVectors = kSquaresPass / kStepThreads / 8;
+// A tile's vectors of 8 across, the rows that a block takes at once, and how often.
+constexpr int kAcross = kTileCols / 8, kDown = kStepThreads / kAcross, kTimes = kTileRows / kDown;
+// Turned: the same of its columns.
+constexpr int kAcrossT = kTileRows / 8, kDownT = kStepThreads / kAcrossT, kTimesT = kTileCols / kDownT;
 
 __device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -122,11 +127,11 @@ __device__ __forceinline__ double block_sum(double x) {
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 __device__ __forceinline__ double pow2d(int e) { return __longlong_as_double((long long)(e + 1023) << 52); }
 
-// A block takes a chunk of a matrix, 64 elements a thread at once.  Those are
+// A block takes a chunk of a matrix, 32 elements a thread at once.  Those are
 // scaled by a power of two so that no square leaves binary32's range: momentum
 // that decays without gradients keeps its direction down to its last bits.
 template <bool STEP, bool G32, bool M32>
-__global__ void __launch_bounds__(kStepThreads) squares_kernel(const __grid_constant__ MuonArgs p) {
+__global__ void __launch_bounds__(kStepThreads, 4) squares_kernel(const __grid_constant__ MuonArgs p) {
   wait_for_earlier_kernels();
   if (skipped(p)) return;
   const float scale = multiplier(p);
@@ -139,9 +144,9 @@ __global__ void __launch_bounds__(kStepThreads) squares_kernel(const __grid_cons
   double sum = 0.0;
   auto pass = [&](int64_t base, auto whole_pass) {
     constexpr bool all = decltype(whole_pass)::value;  // of vectors
-    float u[8][8];
+    float u[kVectors][8];
 #pragma unroll
-    for (int v = 0; v < 8; ++v) {
+    for (int v = 0; v < kVectors; ++v) {
       const int64_t at = base + (v * kStepThreads + threadIdx.x) * 8;
       const int count = all ? 8 : (int)max((int64_t)0, min((int64_t)8, end - at));
       float m[8];
@@ -154,14 +159,14 @@ __global__ void __launch_bounds__(kStepThreads) squares_kernel(const __grid_cons
     }
     float most = 0.0f;
 #pragma unroll
-    for (int v = 0; v < 8; ++v)
+    for (int v = 0; v < kVectors; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(u[v][i]));
     const int e = max(-100, min(126, (int)(__float_as_uint(most) >> 23) - 127));
     const float down = pow2f(-e);
     float s[4] = {};
 #pragma unroll
-    for (int v = 0; v < 8; ++v)
+    for (int v = 0; v < kVectors; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = __fmul_rn(u[v][i], down);
@@ -200,31 +205,33 @@ __global__ void __launch_bounds__(kStepThreads) squares_kernel(const __grid_cons
   }
 }
 
-// A block takes a tile of 64 x 64 of the caller's matrix; a thread 8 neighbours
-// of a row, twice.  A tall matrix's tile is turned in shared memory.
+// A block takes a tile of 64 x 128 of the caller's matrix; a thread 8 neighbours
+// of a row, four times.  A tall matrix's tile is turned in shared memory.
 template <bool STEP, bool G32, bool M32>
 __global__ void __launch_bounds__(kStepThreads) begin_kernel(const __grid_constant__ MuonArgs p) {
-  __shared__ uint32_t turned[kElementTile][kElementTile + 1];
+  __shared__ uint32_t turned[kTileRows][kTileCols + 1];
   wait_for_earlier_kernels();
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < p.counters; i += kStepThreads) p.progress[i] = 0;
   if (skipped(p)) return;
   const float scale = multiplier(p);
   const MuonMatrix& q = p.matrices[p.owner[blockIdx.x]];
   const void* in = pointer_of(p.in, q.index);
-  const int tile = blockIdx.x - q.tile0, i0 = tile / q.tiles_across * kElementTile, j0 = tile % q.tiles_across * kElementTile;
+  const int tile = blockIdx.x - q.tile0, i0 = tile / q.tiles_across * kTileRows, j0 = tile % q.tiles_across * kTileCols;
   const bool vec = q.cols % 8 == 0 && on_16(in) && (!STEP || q.aligned);
   const MuonNorm norm = p.norms[p.owner[blockIdx.x]];
-  const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+  const int r = threadIdx.x / kAcross, c = threadIdx.x % kAcross * 8, rt = threadIdx.x / kAcrossT, ct = threadIdx.x % kAcrossT * 8;
   auto take = [&](auto whole_tile) {
     constexpr bool all = decltype(whole_tile)::value;  // of vectors
-    float m[2][8], u[2][8];
+    float m[kTimes][8], u[kTimes][8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+    for (int h = 0; h < kTimes; ++h) {
+      const int i = i0 + r + kDown * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
       if (all || count) update8<STEP, G32, M32>(p, q, in, (int64_t)i * q.cols + j, count, all || (vec && count == 8), scale, m[h], u[h]);
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+    for (int h = 0; h < kTimes; ++h) {
+      const int i = i0 + r + kDown * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
       uint32_t held[8] = {};
       if (all || count) {
         const int64_t at = (int64_t)i * q.cols + j;
@@ -247,21 +254,21 @@ __global__ void __launch_bounds__(kStepThreads) begin_kernel(const __grid_consta
       }
       if (q.tall) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) turned[r + 32 * h][c + k] = held[k];
+        for (int k = 0; k < 8; ++k) turned[r + kDown * h][c + k] = held[k];
       }
     }
   };
-  if (vec && i0 + kElementTile <= q.rows && j0 + kElementTile <= q.cols) take(std::true_type());
+  if (vec && i0 + kTileRows <= q.rows && j0 + kTileCols <= q.cols) take(std::true_type());
   else take(std::false_type());
   if (!q.tall) return;
   __syncthreads();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int j = j0 + r + 32 * h, i = i0 + c;  // X's row and its first column
+  for (int h = 0; h < kTimesT; ++h) {
+    const int j = j0 + rt + kDownT * h, i = i0 + ct;  // X's row and its first column
     if (j >= q.cols || i >= q.rows) continue;
     uint32_t x[8], hi[4], lo[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = turned[c + k][r + 32 * h];
+    for (int k = 0; k < 8; ++k) x[k] = turned[ct + k][rt + kDownT * h];
 #pragma unroll
     for (int k = 0; k < 4; ++k) hi[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x5410), lo[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x7632);
     const int64_t to = (int64_t)j * q.ld + i;
@@ -296,22 +303,22 @@ __device__ __forceinline__ void random_lanes(const MuonArgs& p, int64_t e, uint3
 
 template <bool STEP, bool W32, bool SR>
 __global__ void __launch_bounds__(kStepThreads) finish_kernel(const __grid_constant__ MuonArgs p) {
-  __shared__ uint16_t turned[kElementTile][kElementTile + 2];
+  __shared__ uint16_t turned[kTileRows][kTileCols + 2];
   wait_for_earlier_kernels();
   if (skipped(p) || *p.err) return;  // (a product that gave up: what there is, is no result)
   const MuonMatrix& q = p.matrices[p.owner[blockIdx.x]];
-  const int tile = blockIdx.x - q.tile0, i0 = tile / q.tiles_across * kElementTile, j0 = tile % q.tiles_across * kElementTile;
-  const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+  const int tile = blockIdx.x - q.tile0, i0 = tile / q.tiles_across * kTileRows, j0 = tile % q.tiles_across * kTileCols;
+  const int r = threadIdx.x / kAcross, c = threadIdx.x % kAcross * 8, rt = threadIdx.x / kAcrossT, ct = threadIdx.x % kAcrossT * 8;
   const uint16_t* x = q.hi[p.last];
   if (q.tall) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int j = j0 + r + 32 * h, i = i0 + c;
+    for (int h = 0; h < kTimesT; ++h) {
+      const int j = j0 + rt + kDownT * h, i = i0 + ct;
       if (j >= q.cols || i >= q.rows) continue;
       const uint4 v = *reinterpret_cast<const uint4*>(x + (int64_t)j * q.ld + i);
       const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) turned[c + k][r + 32 * h] = (uint16_t)(u[k / 2] >> 16 * (k & 1));
+      for (int k = 0; k < 8; ++k) turned[ct + k][rt + kDownT * h] = (uint16_t)(u[k / 2] >> 16 * (k & 1));
     }
     __syncthreads();
   }
@@ -320,24 +327,24 @@ __global__ void __launch_bounds__(kStepThreads) finish_kernel(const __grid_const
   const float ka = __fmul_rn(p.lr, q.factor);
   auto take = [&](auto whole_tile) {
     constexpr bool all = decltype(whole_tile)::value;  // of vectors
-    float weights[2][8];
+    float weights[kTimes][8];
     if (STEP) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+      for (int h = 0; h < kTimes; ++h) {
+        const int i = i0 + r + kDown * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
         if (all || count) load8<W32>(q.w, (int64_t)i * q.cols + j, count, all || (vec && count == 8), weights[h]);
       }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = i0 + r + 32 * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
+    for (int h = 0; h < kTimes; ++h) {
+      const int i = i0 + r + kDown * h, j = j0 + c, count = all ? 8 : i < q.rows ? max(0, min(8, q.cols - j)) : 0;
       if (!all && !count) continue;
       const int64_t at = (int64_t)i * q.cols + j;
       const bool whole = all || (vec && count == 8);
       float o[8];
       if (q.tall) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = of_half(turned[r + 32 * h][c + k]);
+        for (int k = 0; k < 8; ++k) o[k] = of_half(turned[r + kDown * h][c + k]);
       } else {
         const uint4 v = *reinterpret_cast<const uint4*>(x + (int64_t)i * q.ld + j);
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
@@ -367,7 +374,7 @@ __global__ void __launch_bounds__(kStepThreads) finish_kernel(const __grid_const
       if (W32 && q.compute) store8<false>(q.compute, at, count, whole, w);
     }
   };
-  if (vec && i0 + kElementTile <= q.rows && j0 + kElementTile <= q.cols) take(std::true_type());
+  if (vec && i0 + kTileRows <= q.rows && j0 + kTileCols <= q.cols) take(std::true_type());
   else take(std::false_type());
 }
 
