@@ -15,7 +15,8 @@ struct Fp4Args {
   int64_t tokens, rows, cols, ldx, ldy;
   float global_scale;
   int32_t x_f32;
-  int32_t vec_x;          // rows of x start on 16-byte boundaries (set by the launch)
+  int32_t vec_x;          // rows of x start on 16-byte boundaries (set by the launch, as the next)
+  int32_t split;          // blocks of a cluster that share k
 };
 
 cudaError_t launch_fp4_linear(const Fp4Args& a, cudaStream_t stream);

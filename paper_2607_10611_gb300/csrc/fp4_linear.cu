@@ -8,16 +8,17 @@
 #include "fp4.h"
 #include "launch.h"
 #include "step_kernel.cuh"
+#include "tcgen05.cuh"
 
 namespace mpadam {
 
 namespace {
 
+constexpr int kSms = 152;    // GB300
 constexpr int kWarps = 8;
 constexpr int kFp4Threads = 32 * kWarps;
 constexpr int kChunk = 128;  // values of k that a warp takes at once: 32 a lane, 16 bytes of codes, two scales
 
-__device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_later_kernels_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 __device__ __forceinline__ float get(const float* p, int64_t i) { return p[i]; }
@@ -47,6 +48,23 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
+}
+// Two scales times 2^118, twice each: a weight is then q s 2^-8, which BF16 holds exactly.
+struct Scales {
+  uint32_t s[2];
+  __device__ __forceinline__ explicit Scales(uint16_t codes) {
+    const float2 v = scale_values(codes);
+    const float lo = __fmul_rn(v.x, 0x1p118f), hi = __fmul_rn(v.y, 0x1p118f);
+    s[0] = bf16x2_rn(lo, lo), s[1] = bf16x2_rn(hi, hi);
+  }
+};
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+// Eight codes of one row and eight of the row 8 below, as the first operands of two products.
+__device__ __forceinline__ void weights(uint32_t w0, uint32_t w1, uint32_t s0, uint32_t s1, uint32_t (&a0)[4], uint32_t (&a1)[4]) {
+  a0[0] = mul_bf16x2(code_pair<0>(w0), s0), a0[1] = mul_bf16x2(code_pair<0>(w1), s1);
+  a0[2] = mul_bf16x2(code_pair<1>(w0), s0), a0[3] = mul_bf16x2(code_pair<1>(w1), s1);
+  a1[0] = mul_bf16x2(code_pair<2>(w0), s0), a1[1] = mul_bf16x2(code_pair<2>(w1), s1);
+  a1[2] = mul_bf16x2(code_pair<3>(w0), s0), a1[3] = mul_bf16x2(code_pair<3>(w1), s1);
 }
 // d += a b for a 16 x 16 and b 16 x 8 in BF16.
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -112,31 +130,54 @@ struct Staged<float> {
   }
 };
 
-// A block takes 16 ROWS rows of the weight and 8 TILES tokens; its warps are ROWS
-// groups of 16 rows times kWarps / ROWS shares of k, chunks in turn, joined in
-// order through shared memory at the end.  Weights go from memory to registers,
-// a panel of k ahead; x goes through shared memory, where a lane's 32 values of a
-// chunk lie as four times 16 bytes, those of the four lanes of a row next to one
-// another.  Within a chunk the order of k is the lanes': lane l of four takes
-// values 32 l to 32 l + 31, four to each product of 16.
-template <typename X, int TILES, int ROWS>
-__global__ void __launch_bounds__(kFp4Threads) fp4_kernel(const __grid_constant__ Fp4Args p) {
+__device__ __forceinline__ float lds_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// What a block takes at once.
+__host__ __device__ constexpr int fp4_panel(int rows) { return kWarps / rows * 2 * kChunk; }
+template <typename X>
+constexpr int fp4_smem(int tiles, int rows) {
+  return std::max(2 * Staged<X>::kParts * 8 * tiles * (2 * fp4_panel(rows) + 64), (kWarps + rows) * 8 * tiles * 16 * 4);
+}
+
+// A block takes 16 ROWS rows of the weight and 8 TILES tokens, of which up to
+// STAGED are there; its warps are ROWS groups of 16 rows times kWarps / ROWS shares
+// of k, chunks in turn, joined in order through shared memory at the end.  Where
+// that makes too few blocks, a cluster of them takes a run of k's panels each, and
+// their sums are joined in order through the cluster's shared memory.  Weights go
+// from memory to registers, a panel of k ahead; x goes through shared memory, where
+// a lane's 32 values of a chunk lie as four times 16 bytes, those of the four lanes
+// of a row next to one another.  Within a chunk the order of k is the lanes': lane l
+// of four takes values 32 l to 32 l + 31, four to each product of 16.
+template <typename X, int TILES, int ROWS, int STAGED, int BLOCKS>
+__global__ void __launch_bounds__(kFp4Threads, BLOCKS) fp4_kernel(const __grid_constant__ Fp4Args p) {
   constexpr int kShares = kWarps / ROWS, kParts = Staged<X>::kParts;
   constexpr int kOwn = 2;                             // chunks of a warp in a panel
   constexpr int kPanelChunks = kShares * kOwn, kPanel = kPanelChunks * kChunk;
+  static_assert(kPanel == fp4_panel(ROWS), "a panel");
   constexpr int kTokens = 8 * TILES;
   constexpr int kStride = kPanel * 2 + 64;            // bytes of a token in a panel; the 64 keep neighbours off each other's banks
   constexpr int kPartBytes = kTokens * kStride, kBufferBytes = kParts * kPartBytes;
-  constexpr int kPieces = kTokens * kPanel / 8 / kFp4Threads;  // of 8 values, a thread's share of a panel
-  static_assert(kTokens * kPanel % (8 * kFp4Threads) == 0, "whole shares");
+  constexpr int kPieces = STAGED * kPanel / 8 / kFp4Threads;  // of 8 values, a thread's share of a panel
+  static_assert(STAGED <= kTokens && STAGED * kPanel % (8 * kFp4Threads) == 0, "whole shares");
   extern __shared__ uint4 smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, l = lane & 3;
   const int group = warp / kShares, share = warp % kShares;
-  const int64_t row0 = ((int64_t)blockIdx.x * ROWS + group) * 16;
+  const int rank = (int)(blockIdx.x % p.split);
+  const int64_t block_row = (int64_t)(blockIdx.x / p.split) * (16 * ROWS), row0 = block_row + group * 16;
   const int64_t token0 = (int64_t)blockIdx.y * kTokens;
   const int tokens = (int)(p.tokens - token0 < kTokens ? p.tokens - token0 : kTokens);
   const int64_t rows[2] = {min(row0 + g, p.rows - 1), min(row0 + g + 8, p.rows - 1)};
+  if (STAGED < kTokens) {  // the tokens that are never there
+    for (int i = threadIdx.x; i < 2 * kParts * (kTokens - STAGED) * (kStride / 16); i += kFp4Threads) {
+      const int part = i / ((kTokens - STAGED) * (kStride / 16)), in = i % ((kTokens - STAGED) * (kStride / 16));
+      smem_raw[(part * kPartBytes + STAGED * kStride) / 16 + in] = make_uint4(0, 0, 0, 0);
+    }
+  }
   wait_for_earlier_kernels();
   let_later_kernels_begin();
 
@@ -168,15 +209,15 @@ __global__ void __launch_bounds__(kFp4Threads) fp4_kernel(const __grid_constant_
     }
   };
   float acc[TILES][4] = {};
-  const int64_t panels = (p.cols + kPanel - 1) / kPanel;
-  fetch(0);
-  for (int64_t panel = 0; panel < panels; ++panel) {
-    uint8_t* buffer = smem + (panel & 1) * kBufferBytes;
+  const int64_t panels = (p.cols + kPanel - 1) / kPanel, first = panels * rank / p.split, last = panels * (rank + 1) / p.split;
+  fetch(first);
+  for (int64_t panel = first; panel < last; ++panel) {
+    uint8_t* buffer = smem + (panel - first & 1) * kBufferBytes;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int piece = i * kFp4Threads + threadIdx.x, token = piece / (kPanel / 8), in = piece % (kPanel / 8);
       const int chunk = in / 16, owner = in / 4 % 4, quarter = in % 4;  // of 128, 32 and 8 values
-      if (token >= tokens && panel >= 2) continue;  // zeros, which lie there already
+      if (token >= tokens && panel - first >= 2) continue;  // zeros, which lie there already
       uint8_t* to = buffer + token * kStride + chunk * (2 * kChunk) + quarter * 64 + owner * 16;
 #pragma unroll
       for (int part = 0; part < kParts; ++part) *reinterpret_cast<uint4*>(to + part * kPartBytes) = x[i].part(part);
@@ -185,27 +226,15 @@ __global__ void __launch_bounds__(kFp4Threads) fp4_kernel(const __grid_constant_
 #pragma unroll
     for (int c = 0; c < kOwn; ++c) now[c] = next[c];
     __syncthreads();
-    if (panel + 1 < panels) fetch(panel + 1);
+    if (panel + 1 < last) fetch(panel + 1);
 #pragma unroll
     for (int c = 0; c < kOwn; ++c) {
-      // scales times 2^118, twice each: a weight is then q s 2^-8, which BF16 holds exactly
-      uint32_t scale[2][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float2 s = scale_values(now[c].s[h]);
-        const float lo = __fmul_rn(s.x, 0x1p118f), hi = __fmul_rn(s.y, 0x1p118f);
-        scale[h][0] = bf16x2_rn(lo, lo), scale[h][1] = bf16x2_rn(hi, hi);
-      }
+      const Scales scale[2] = {Scales(now[c].s[0]), Scales(now[c].s[1])};
       const uint8_t* from = buffer + g * kStride + (c * kShares + share) * (2 * kChunk) + l * 16;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const uint32_t w0 = q == 0 ? now[c].q[0].x : q == 1 ? now[c].q[0].y : q == 2 ? now[c].q[0].z : now[c].q[0].w;
-        const uint32_t w1 = q == 0 ? now[c].q[1].x : q == 1 ? now[c].q[1].y : q == 2 ? now[c].q[1].z : now[c].q[1].w;
-        const uint32_t s0 = scale[0][q / 2], s1 = scale[1][q / 2];
-        const uint32_t a0[4] = {mul_bf16x2(code_pair<0>(w0), s0), mul_bf16x2(code_pair<0>(w1), s1),
-                                mul_bf16x2(code_pair<1>(w0), s0), mul_bf16x2(code_pair<1>(w1), s1)};
-        const uint32_t a1[4] = {mul_bf16x2(code_pair<2>(w0), s0), mul_bf16x2(code_pair<2>(w1), s1),
-                                mul_bf16x2(code_pair<3>(w0), s0), mul_bf16x2(code_pair<3>(w1), s1)};
+        uint32_t a0[4], a1[4];
+        weights(word_of(now[c].q[0], q), word_of(now[c].q[1], q), scale[0].s[q / 2], scale[1].s[q / 2], a0, a1);
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
 #pragma unroll
@@ -227,15 +256,126 @@ __global__ void __launch_bounds__(kFp4Threads) fp4_kernel(const __grid_constant_
     for (int i = 0; i < 4; ++i)
       sums[(warp * kTokens + t * 8 + 2 * l + (i & 1)) * 16 + g + 8 * (i >> 1)] = acc[t][i];
   __syncthreads();
-  for (int i = threadIdx.x; i < tokens * 16 * ROWS; i += kFp4Threads) {
+  auto shares_of = [&](int i) {
     const int token = i / (16 * ROWS), r = i % (16 * ROWS);
-    const int64_t row = (int64_t)blockIdx.x * ROWS * 16 + r;
-    if (row >= p.rows) continue;
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < kShares; ++k) s = __fadd_rn(s, sums[((r / 16 * kShares + k) * kTokens + token) * 16 + r % 16]);
-    put(static_cast<X*>(p.y), (token0 + token) * p.ldy + row, __fmul_rn(__fmul_rn(s, 256.0f), p.global_scale));
+    return s;
+  };
+  auto finish = [&](int i, float s) {
+    const int64_t row = block_row + i % (16 * ROWS);
+    if (row < p.rows) put(static_cast<X*>(p.y), (token0 + i / (16 * ROWS)) * p.ldy + row, __fmul_rn(__fmul_rn(s, 256.0f), p.global_scale));
+  };
+  const int results = tokens * 16 * ROWS;
+  if (p.split == 1) {
+    for (int i = threadIdx.x; i < results; i += kFp4Threads) finish(i, shares_of(i));
+    return;
   }
+  float* mine = sums + kWarps * kTokens * 16;
+  for (int i = threadIdx.x; i < results; i += kFp4Threads) mine[i] = shares_of(i);
+  cluster_sync();
+  const uint32_t at = smem_addr(mine);
+  for (int i = rank * kFp4Threads + threadIdx.x; i < results; i += p.split * kFp4Threads) {
+    float s = 0.0f;
+    for (int k = 0; k < p.split; ++k) s = __fadd_rn(s, lds_cluster_f32(peer_addr(at + 4 * i, k)));
+    finish(i, s);
+  }
+  cluster_sync();  // nobody leaves while its sums are read
+}
+
+// At most 8 tokens in BF16: nothing is staged and no warp waits for another before
+// the end.  A block takes 16 rows, its warps (and those of its cluster) chunks of k
+// in turn, kFewAhead of them on their way; x comes straight from L1.
+constexpr int kFewWarps = 4, kFewAhead = 4, kFewBlocks = 5;
+__global__ void __launch_bounds__(32 * kFewWarps, kFewBlocks) fp4_few_kernel(const __grid_constant__ Fp4Args p) {
+  constexpr int kTokens = 8;
+  __shared__ float sums[kFewWarps][kTokens * 16], mine[kTokens * 16];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, l = lane & 3;
+  const int rank = (int)(blockIdx.x % p.split);
+  const int64_t block_row = (int64_t)(blockIdx.x / p.split) * 16, token0 = (int64_t)blockIdx.y * kTokens;
+  const int tokens = (int)min(p.tokens - token0, (int64_t)kTokens);
+  const int64_t chunks = (p.cols + kChunk - 1) / kChunk, stride = p.split * kFewWarps;
+  int64_t chunk = rank * kFewWarps + warp;
+  const uint8_t *codes[2], *scales[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t row = min(block_row + g + 8 * h, p.rows - 1);
+    codes[h] = p.codes + row * (p.cols / 2) + chunk * (kChunk / 2) + l * 16;
+    scales[h] = p.scales + row * (p.cols / 16) + chunk * (kChunk / 16) + l * 2;
+  }
+  const uint16_t* x = static_cast<const uint16_t*>(p.x) + (token0 + g) * p.ldx + chunk * kChunk + l * 32;
+  const bool here = g < tokens;
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+
+  uint4 q[kFewAhead][2];
+  uint16_t s[kFewAhead][2];
+  int64_t k = chunk * kChunk + l * 32;  // of the next fetch
+  auto fetch = [&](int d) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      q[d][h] = k < p.cols ? __ldcs(reinterpret_cast<const uint4*>(codes[h])) : make_uint4(0, 0, 0, 0);
+      s[d][h] = k < p.cols ? __ldcs(reinterpret_cast<const uint16_t*>(scales[h])) : (uint16_t)0;
+      codes[h] += stride * (kChunk / 2);
+      scales[h] += stride * (kChunk / 16);
+    }
+    k += stride * kChunk;
+  };
+#pragma unroll
+  for (int d = 0; d < kFewAhead; ++d) fetch(d);
+  float acc[4] = {};
+  while (chunk < chunks) {
+#pragma unroll
+    for (int d = 0; d < kFewAhead; ++d) {
+      if (chunk >= chunks) break;
+      uint4 b[4];
+      if (here && chunk * kChunk + l * 32 < p.cols) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          Staged<uint16_t> v;
+          v.fetch(x + 8 * i, 8, p.vec_x);
+          b[i] = v.part(0);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = make_uint4(0, 0, 0, 0);
+      }
+      const Scales scale[2] = {Scales(s[d][0]), Scales(s[d][1])};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t a0[4], a1[4];
+        weights(word_of(q[d][0], i), word_of(q[d][1], i), scale[0].s[i / 2], scale[1].s[i / 2], a0, a1);
+        mma(acc, a0, b[i].x, b[i].y);
+        mma(acc, a1, b[i].z, b[i].w);
+      }
+      fetch(d);
+      chunk += stride;
+      x += stride * kChunk;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sums[warp][(2 * l + (i & 1)) * 16 + g + 8 * (i >> 1)] = acc[i];
+  __syncthreads();
+  const int i = threadIdx.x;  // a result a thread
+  static_assert(kTokens * 16 == 32 * kFewWarps, "a result a thread");
+  float sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kFewWarps; ++w) sum = __fadd_rn(sum, sums[w][i]);
+  bool out = i < tokens * 16 && block_row + i % 16 < p.rows;
+  if (p.split > 1) {
+    mine[i] = sum;
+    cluster_sync();
+    out = out && i % p.split == rank;
+    if (out) {
+      const uint32_t at = smem_addr(&mine[i]);
+      sum = 0.0f;
+      for (int r = 0; r < p.split; ++r) sum = __fadd_rn(sum, lds_cluster_f32(peer_addr(at, r)));
+    }
+    cluster_sync();  // nobody leaves while its sums are read
+  }
+  if (out)
+    put(static_cast<uint16_t*>(p.y), (token0 + i / 16) * p.ldy + block_row + i % 16, __fmul_rn(__fmul_rn(sum, 256.0f), p.global_scale));
 }
 
 // Any number of columns and any alignment: a warp takes a row and four tokens.
@@ -267,18 +407,28 @@ __global__ void __launch_bounds__(kFp4Threads) fp4_any_kernel(const __grid_const
   }
 }
 
-template <typename X, int TILES, int ROWS>
-cudaError_t launch(const Fp4Args& a, cudaStream_t stream) {
-  constexpr int kPanel = kWarps / ROWS * 2 * kChunk, kTokens = 8 * TILES;
-  constexpr int kSmem = std::max(2 * Staged<X>::kParts * kTokens * (2 * kPanel + 64), kWarps * kTokens * 16 * 4);
+template <typename X, int TILES, int ROWS, int STAGED, int BLOCKS>
+cudaError_t launch(Fp4Args a, cudaStream_t stream) {
+  constexpr int kSmem = fp4_smem<X>(TILES, ROWS), kTokens = 8 * TILES;
+  const void* kernel = (const void*)fp4_kernel<X, TILES, ROWS, STAGED, BLOCKS>;
   if (kSmem > 48 * 1024) {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_smem((const void*)fp4_kernel<X, TILES, ROWS>, kSmem, ready);
+    const cudaError_t e = allow_smem(kernel, kSmem, ready);
     if (e != cudaSuccess) return e;
   }
-  return launch_dependent((const void*)fp4_kernel<X, TILES, ROWS>,
-                          dim3((unsigned)((a.rows + 16 * ROWS - 1) / (16 * ROWS)), (unsigned)((a.tokens + kTokens - 1) / kTokens)),
-                          kFp4Threads, 0, kSmem, &a, stream);
+  const int64_t blocks = (a.rows + 16 * ROWS - 1) / (16 * ROWS), tiles = (a.tokens + kTokens - 1) / kTokens;
+  const int64_t panels = (a.cols + fp4_panel(ROWS) - 1) / fp4_panel(ROWS);
+  a.split = 1;
+  while (a.split < 8 && 2 * a.split <= panels && 2 * blocks * tiles * a.split <= BLOCKS * kSms) a.split *= 2;
+  return launch_dependent(kernel, dim3((unsigned)(blocks * a.split), (unsigned)tiles), kFp4Threads, a.split > 1 ? a.split : 0, kSmem, &a,
+                          stream);
+}
+
+cudaError_t launch_few(Fp4Args a, cudaStream_t stream) {
+  const int64_t blocks = (a.rows + 15) / 16, chunks = (a.cols + kChunk - 1) / kChunk;
+  a.split = 1;
+  while (a.split < 8 && 2 * a.split * kFewWarps <= chunks && 2 * blocks * a.split <= kFewBlocks * kSms) a.split *= 2;
+  return launch_dependent((const void*)fp4_few_kernel, (unsigned)(blocks * a.split), 32 * kFewWarps, a.split > 1 ? a.split : 0, 0, &a, stream);
 }
 
 }  // namespace
@@ -294,11 +444,11 @@ cudaError_t launch_fp4_linear(const Fp4Args& args, cudaStream_t stream) {
     return a.x_f32 ? launch_dependent((const void*)fp4_any_kernel<float>, grid, kFp4Threads, 0, 0, &a, stream)
                    : launch_dependent((const void*)fp4_any_kernel<uint16_t>, grid, kFp4Threads, 0, 0, &a, stream);
   }
-  if (a.x_f32) return launch<float, 1, 2>(a, stream);
-  if (a.tokens <= 2) return launch<uint16_t, 1, 1>(a, stream);
-  if (a.tokens <= 8) return launch<uint16_t, 1, 2>(a, stream);
-  if (a.tokens <= 16) return launch<uint16_t, 2, 4>(a, stream);
-  return launch<uint16_t, 4, 4>(a, stream);
+  if (a.x_f32) return launch<float, 1, 2, 8, 2>(a, stream);
+  if (a.tokens <= 8) return launch_few(a, stream);
+  if (a.tokens <= 16) return launch<uint16_t, 2, 4, 16, 2>(a, stream);
+  if (a.tokens <= 24) return launch<uint16_t, 3, 4, 24, 2>(a, stream);
+  return launch<uint16_t, 4, 4, 32, 2>(a, stream);
 }
 
 }  // namespace mpadam

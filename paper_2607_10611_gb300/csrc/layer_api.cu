@@ -110,6 +110,6 @@ extern "C" int32_t mpadam_nvfp4_linear(const void* x, int32_t x_dtype, int64_t t
   if (!x || !is_aligned(x, size) || ldx < w->cols) return fail(MPADAM_EINVAL, "x NULL or misaligned, or ldx < cols");
   if (!w->codes || !w->scales) return fail(MPADAM_EINVAL, "codes or scales NULL");
   const cudaError_t e = launch_fp4_linear({x, w->codes, w->scales, y, tokens, w->rows, w->cols, ldx, ldy, w->global_scale,
-                                           x_dtype == MPADAM_F32, 0}, stream);
+                                           x_dtype == MPADAM_F32, 0, 1}, stream);
   return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "launch of the product");
 }
