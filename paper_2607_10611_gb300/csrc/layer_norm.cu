@@ -73,6 +73,36 @@ struct Slice {
       }
     }
   }
+  // The same by way of shared memory, where a thread's pieces are its own: it alone waits for them, and reads them.
+  // (A single BF16 is too small for an asynchronous copy.)
+  static constexpr bool kAsync = VEC || sizeof(T) == 4;
+  static constexpr int kPiece = VEC ? 16 : 4;
+  static __host__ __device__ constexpr int bytes(int threads) { return kSlots * threads * kPiece; }
+  static __device__ __forceinline__ void begin(const T* p, int64_t cols, int t, int threads, uint32_t to) {
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const int64_t c = at(s, t, threads);
+      const int size = c < cols ? kPiece : 0;  // nothing read: zeros
+      const T* from = c < cols ? p + c : p;
+      if constexpr (VEC)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (s * threads + t) * kPiece), "l"(from), "r"(size) : "memory");
+      else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + (s * threads + t) * kPiece), "l"(from), "r"(size) : "memory");
+    }
+  }
+  static __device__ __forceinline__ void read(uint32_t from, int t, int threads, float* x) {
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const uint32_t at = from + (s * threads + t) * kPiece;
+      if constexpr (VEC) {
+        uint4 v;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+        Pack<T>::open(v, x + s * kN);
+      } else {
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[s]) : "r"(at) : "memory");
+      }
+    }
+  }
   static __device__ __forceinline__ void open(const uint32_t* raw, float* x) {
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
@@ -115,6 +145,15 @@ struct Slice {
   }
 };
 
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_for_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// Rows on their way at once, of those that a warp or block takes in turn: so many that an SM waits for 64 KB or more, whatever
+// the width; one row ahead in registers left 16384 x 4096 in BF16 at 4 TB/s.
+template <typename X, int E>
+constexpr int kAhead = sizeof(X) == 2 ? (E == 32 ? 3 : 4) : (E == 8 ? 4 : E == 16 ? 3 : 2);
+
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
   for (int d = 16; d; d >>= 1) x = __fadd_rn(x, __shfl_xor_sync(~0u, x, d));
@@ -143,21 +182,9 @@ struct BlockSum {
 // ---------------------------------------------------------------------------
 // Forward: a row in the registers of a warp (ONE) or of a block.
 // ---------------------------------------------------------------------------
-template <typename X, typename W, bool VEC, int E, bool ONE>
-__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads) forward_kernel(const __grid_constant__ NormForwardArgs p) {
+template <typename X, typename W, bool VEC, int E, typename Sum>
+__device__ __forceinline__ void forward_row(const NormForwardArgs& p, int64_t row, int t, int threads, float (&x)[E], Sum sum) {
   using S = Slice<X, VEC, E>;
-  __shared__ float slots[2][32];
-  wait_for_earlier_kernels();
-  let_later_kernels_begin();
-  const int t = ONE ? threadIdx.x & 31 : threadIdx.x, threads = ONE ? 32 : blockDim.x;
-  const int64_t row = ONE ? (int64_t)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5) : blockIdx.x;
-  if (row >= p.rows) return;
-  BlockSum block{slots};
-  auto sum = [&](float x) { return ONE ? warp_sum(x) : block(x); };
-  uint32_t raw[S::kWords];
-  float x[E];
-  S::fetch(static_cast<const X*>(p.x) + row * p.ldx, p.cols, t, threads, raw);
-  S::open(raw, x);
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < E; ++i) s = __fadd_rn(s, x[i]);
@@ -176,6 +203,60 @@ __global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads) forward_ke
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = __fmaf_rn(__fmul_rn(x[i], rstd), w[i], b[i]);
   S::store(static_cast<X*>(p.y) + row * p.ldy, p.cols, t, threads, x);
+}
+
+template <typename X, typename W, bool VEC, int E, bool ONE>
+__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads) forward_kernel(const __grid_constant__ NormForwardArgs p) {
+  using S = Slice<X, VEC, E>;
+  __shared__ float slots[2][32];
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+  const int t = ONE ? threadIdx.x & 31 : threadIdx.x, threads = ONE ? 32 : blockDim.x;
+  const int64_t row = ONE ? (int64_t)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5) : blockIdx.x;
+  if (row >= p.rows) return;
+  BlockSum block{slots};
+  uint32_t raw[S::kWords];
+  float x[E];
+  S::fetch(static_cast<const X*>(p.x) + row * p.ldx, p.cols, t, threads, raw);
+  S::open(raw, x);
+  forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); });
+}
+
+// Blocks an SM, of eight rows each; with more, registers would not do.
+constexpr int forward_blocks(int each) { return each == 32 ? 3 : 4; }
+
+// Many rows: each warp or block takes rows in turn, kAhead of them on their way.
+template <typename X, typename W, bool VEC, int E, bool ONE>
+__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, ONE ? forward_blocks(E) : 2)
+    forward_rows_kernel(const __grid_constant__ NormForwardArgs p) {
+  using S = Slice<X, VEC, E>;
+  constexpr int kDeep = kAhead<X, E>;
+  extern __shared__ uint4 ring[];
+  __shared__ float slots[2][32];
+  wait_for_earlier_kernels();
+  let_later_kernels_begin();
+  const int t = ONE ? threadIdx.x & 31 : threadIdx.x, threads = ONE ? 32 : blockDim.x, warps = blockDim.x / 32;
+  const int64_t stride = ONE ? (int64_t)gridDim.x * warps : gridDim.x;
+  int64_t row = ONE ? (int64_t)blockIdx.x * warps + (threadIdx.x >> 5) : blockIdx.x, next = row;
+  const int stage = S::bytes(threads);
+  const uint32_t mine = smem_addr(ring) + (ONE ? (threadIdx.x >> 5) * kDeep * stage : 0);
+  BlockSum block{slots};
+  auto begin = [&](int at) {
+    if (next < p.rows) S::begin(static_cast<const X*>(p.x) + next * p.ldx, p.cols, t, threads, mine + at * stage);
+    commit_copies();
+    next += stride;
+  };
+#pragma unroll
+  for (int i = 0; i < kDeep - 1; ++i) begin(i);
+  int at = 0;
+  for (; row < p.rows; row += stride) {
+    begin(at ? at - 1 : kDeep - 1);
+    wait_for_copies<kDeep - 1>();
+    float x[E];
+    S::read(mine + at * stage, t, threads, x);
+    forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); });
+    if (++at == kDeep) at = 0;
+  }
 }
 
 // Rows of any width, read three times.
@@ -204,39 +285,59 @@ __global__ void __launch_bounds__(kWideThreads) forward_wide_kernel(const __grid
 
 // ---------------------------------------------------------------------------
 // Backward: a row in the registers of a warp (ONE) or of a block, rows in turn;
-// each thread keeps the sums over its rows of dy n and dy for its columns.  The
-// next row is fetched before the sums over this one are exchanged.
+// each thread keeps the sums over its rows of dy n and dy for its columns.
+// kAhead rows are on their way by asynchronous copies, or one in registers.
 // ---------------------------------------------------------------------------
 template <typename X, typename W, bool VEC, int E, bool ONE>
-__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, 1)
+__global__ void __launch_bounds__(ONE || E == 8 ? 256 : kMaxThreads, ONE ? 2 : E == 8 ? 3 : 1)
     backward_kernel(const __grid_constant__ NormBackwardArgs p) {
   using S = Slice<X, VEC, E>;
-  extern __shared__ float joined[];  // ONE: [2][cols]
+  constexpr int kDeep = S::kAsync ? kAhead<X, E> : 1;
+  extern __shared__ uint4 dynamic[];  // the rows on their way, then, ONE: [2][cols] sums
   __shared__ float2 slots[2][32];
   wait_for_earlier_kernels();
   let_later_kernels_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
   const int t = ONE ? lane : threadIdx.x, threads = ONE ? 32 : blockDim.x;
   const int64_t stride = ONE ? (int64_t)gridDim.x * warps : gridDim.x;
-  int64_t row = ONE ? (int64_t)blockIdx.x * warps + warp : blockIdx.x;
+  int64_t row = ONE ? (int64_t)blockIdx.x * warps + warp : blockIdx.x, next = row;
   const X *x = static_cast<const X*>(p.x), *dy = static_cast<const X*>(p.dy);
+  const int stage = S::kAsync ? 2 * S::bytes(threads) : 0;
+  const uint32_t mine = smem_addr(dynamic) + (ONE ? warp * kDeep * stage : 0);
+  float* joined = reinterpret_cast<float*>(dynamic) + (ONE ? warps : 1) * kDeep * stage / 4;
   float w[E], dw[E], db[E];
   S::vector(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
 #pragma unroll
   for (int i = 0; i < E; ++i) dw[i] = db[i] = 0.0f;
-  uint32_t raw_x[S::kWords], raw_dy[S::kWords];
-  float mean = 0.0f, rstd = 0.0f;
-  auto fetch = [&](int64_t r) {
-    S::fetch(x + r * p.ldx, p.cols, t, threads, raw_x);
-    S::fetch(dy + r * p.lddy, p.cols, t, threads, raw_dy);
-    mean = p.mean[r], rstd = p.rstd[r];
+  uint32_t raw_x[S::kAsync ? 1 : S::kWords], raw_dy[S::kAsync ? 1 : S::kWords];
+  float mean = 0.0f, rstd = 0.0f;  // of the next row
+  auto begin = [&](int at) {
+    if (next < p.rows) {
+      if constexpr (S::kAsync) {
+        S::begin(x + next * p.ldx, p.cols, t, threads, mine + at * stage);
+        S::begin(dy + next * p.lddy, p.cols, t, threads, mine + at * stage + stage / 2);
+      } else {
+        S::fetch(x + next * p.ldx, p.cols, t, threads, raw_x);
+        S::fetch(dy + next * p.lddy, p.cols, t, threads, raw_dy);
+      }
+    }
+    if constexpr (S::kAsync) commit_copies();
+    next += stride;
   };
-  if (row < p.rows) fetch(row);
-  int turn = 0;
+#pragma unroll
+  for (int i = 0; i < kDeep; ++i) begin(i);
+  if (row < p.rows) mean = p.mean[row], rstd = p.rstd[row];
+  int turn = 0, at = 0;
   for (; row < p.rows; row += stride) {
     float n[E], dn[E];
-    S::open(raw_x, n);
-    S::open(raw_dy, dn);
+    if constexpr (S::kAsync) {
+      wait_for_copies<kDeep - 1>();
+      S::read(mine + at * stage, t, threads, n);
+      S::read(mine + at * stage + stage / 2, t, threads, dn);
+    } else {
+      S::open(raw_x, n);
+      S::open(raw_dy, dn);
+    }
     const float scale = rstd;
     float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
@@ -249,7 +350,9 @@ __global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, 1)
       s0 = __fadd_rn(s0, dn[i]);
       s1 = __fmaf_rn(dn[i], n[i], s1);
     }
-    if (row + stride < p.rows) fetch(row + stride);
+    begin(at);
+    if (++at == kDeep) at = 0;
+    if (row + stride < p.rows) mean = p.mean[row + stride], rstd = p.rstd[row + stride];
     if (!p.dx) continue;
     s0 = warp_sum(s0), s1 = warp_sum(s1);
     if (!ONE) {
@@ -365,6 +468,8 @@ __global__ void __launch_bounds__(1024) sums_kernel(const __grid_constant__ Norm
 // Launches
 // ---------------------------------------------------------------------------
 constexpr int64_t kOneCols = 32 * 32;           // widest row of a warp
+constexpr int64_t kWarpCols = 8 * 32;           // and in the backward pass, which has five arrays of a row
+constexpr int64_t kSmallCols = 8 * 256;         // widest row of a block with 8 values a thread there
 constexpr int64_t kBlockCols = 16 * kMaxThreads; // and of a block
 
 bool whole_packs(const void* p, int64_t ld, int64_t rows, int64_t size) {
@@ -372,6 +477,15 @@ bool whole_packs(const void* p, int64_t ld, int64_t rows, int64_t size) {
 }
 
 int threads_for(int64_t cols, int each) { return (int)((cols + 32 * each - 1) / (32 * each)) * 32; }
+
+template <typename Args>
+cudaError_t launch_ring(void (*kernel)(Args), int64_t blocks, int threads, int smem, const Args& a, cudaStream_t stream) {
+  if (smem > 40 * 1024) {  // (what is not asked for is 48 KB, the kernel's own arrays among it)
+    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_dependent((const void*)kernel, (unsigned)blocks, threads, 0, smem, &a, stream);
+}
 
 template <typename X, typename W, bool VEC>
 cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
@@ -383,6 +497,15 @@ cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
   };
   // Few rows: as many threads to a row as there are packs, for its latency.
   if (a.rows <= 2 * kSms && a.cols > 256 && a.cols <= 8 * kMaxThreads) return block(forward_kernel<X, W, VEC, 8, false>, 8);
+  if constexpr (Slice<X, VEC, 8>::kAsync) {  // as many rows in turn as make it worth while
+    const int threads = a.cols <= kOneCols ? 32 * kRowWarps : threads_for(a.cols, 16), blocks = kSms * (a.cols <= kOneCols ? forward_blocks(a.cols <= 768 ? 24 : 32) : 1024 / threads);
+    if (a.cols > 256 && a.cols <= kBlockCols && a.rows >= 4 * (int64_t)blocks * (a.cols <= kOneCols ? kRowWarps : 1)) {
+      if (a.cols <= 512) return launch_ring(forward_rows_kernel<X, W, VEC, 16, true>, blocks, threads, kRowWarps * kAhead<X, 16> * Slice<X, VEC, 16>::bytes(32), a, stream);
+      if (a.cols <= 768) return launch_ring(forward_rows_kernel<X, W, VEC, 24, true>, blocks, threads, kRowWarps * kAhead<X, 24> * Slice<X, VEC, 24>::bytes(32), a, stream);
+      if (a.cols <= kOneCols) return launch_ring(forward_rows_kernel<X, W, VEC, 32, true>, blocks, threads, kRowWarps * kAhead<X, 32> * Slice<X, VEC, 32>::bytes(32), a, stream);
+      return launch_ring(forward_rows_kernel<X, W, VEC, 16, false>, blocks, threads, kAhead<X, 16> * Slice<X, VEC, 16>::bytes(threads), a, stream);
+    }
+  }
   if (a.cols <= 256) return one(forward_kernel<X, W, VEC, 8, true>);
   if (a.cols <= 512) return one(forward_kernel<X, W, VEC, 16, true>);
   if (a.cols <= 768) return one(forward_kernel<X, W, VEC, 24, true>);
@@ -393,16 +516,21 @@ cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
 
 template <typename X, typename W, bool VEC>
 cudaError_t launch_backward(const NormBackwardArgs& a, cudaStream_t stream) {
-  auto one = [&](auto* kernel) {
-    return launch_dependent((const void*)kernel, (unsigned)a.parts, 32 * kRowWarps, 0, (int)(2 * a.cols * sizeof(float)), &a, stream);
-  };
-  if (a.cols <= 256) return one(backward_kernel<X, W, VEC, 8, true>);
-  if (a.cols <= 512) return one(backward_kernel<X, W, VEC, 16, true>);
-  if (a.cols <= 768) return one(backward_kernel<X, W, VEC, 24, true>);
-  if (a.cols <= kOneCols) return one(backward_kernel<X, W, VEC, 32, true>);
-  if (a.cols <= kBlockCols)
-    return launch_dependent((const void*)backward_kernel<X, W, VEC, 16, false>, (unsigned)a.parts, threads_for(a.cols, 16), 0, 0, &a,
-                            stream);
+  if (a.cols <= kWarpCols) {
+    using S = Slice<X, VEC, 8>;
+    const int ring = S::kAsync ? kRowWarps * kAhead<X, 8> * 2 * S::bytes(32) : 0;
+    return launch_ring(backward_kernel<X, W, VEC, 8, true>, a.parts, 32 * kRowWarps, ring + (int)(2 * a.cols * sizeof(float)), a, stream);
+  }
+  if (a.cols <= kSmallCols) {
+    using S = Slice<X, VEC, 8>;
+    const int threads = threads_for(a.cols, 8);
+    return launch_ring(backward_kernel<X, W, VEC, 8, false>, a.parts, threads, S::kAsync ? kAhead<X, 8> * 2 * S::bytes(threads) : 0, a, stream);
+  }
+  if (a.cols <= kBlockCols) {
+    using S = Slice<X, VEC, 16>;
+    const int threads = threads_for(a.cols, 16);
+    return launch_ring(backward_kernel<X, W, VEC, 16, false>, a.parts, threads, S::kAsync ? kAhead<X, 16> * 2 * S::bytes(threads) : 0, a, stream);
+  }
   if (a.dx) {
     const cudaError_t e = launch_dependent((const void*)backward_wide_kernel<X, W>, (unsigned)a.rows, kWideThreads, 0, 0, &a, stream);
     if (e != cudaSuccess) return e;
@@ -414,9 +542,12 @@ cudaError_t launch_backward(const NormBackwardArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
+// Blocks of the backward pass: as many as an SM has room for, of at least 4 rows each (a warp of its own for every row where a
+// row is one warp's), so that what they sum up is little beside what they read.
 int norm_parts(int64_t rows, int64_t cols) {
-  if (cols <= kOneCols) return (int)std::min<int64_t>((rows + kRowWarps - 1) / kRowWarps, 2 * kSms);
-  if (cols <= kBlockCols) return (int)std::min<int64_t>(rows, kSms * std::max<int64_t>(1, std::min<int64_t>(4, 8192 / cols)));
+  if (cols <= kWarpCols) return (int)std::min<int64_t>((rows + kRowWarps - 1) / kRowWarps, 2 * kSms);
+  if (cols <= kSmallCols) return (int)std::min<int64_t>((rows + 3) / 4, kSms * std::min(4, 768 / threads_for(cols, 8)));
+  if (cols <= kBlockCols) return (int)std::min<int64_t>(rows, kSms * std::max(1, 512 / threads_for(cols, 16)));
   return (int)std::min<int64_t>(rows, 32);
 }
 
