@@ -183,7 +183,8 @@ struct BlockSum {
 // Forward: a row in the registers of a warp (ONE) or of a block.
 // ---------------------------------------------------------------------------
 template <typename X, typename W, bool VEC, int E, typename Sum>
-__device__ __forceinline__ void forward_row(const NormForwardArgs& p, int64_t row, int t, int threads, float (&x)[E], Sum sum) {
+__device__ __forceinline__ void forward_row(const NormForwardArgs& p, int64_t row, int t, int threads, float (&x)[E], Sum sum,
+                                            const float* held_w = nullptr, const float* held_b = nullptr) {
   using S = Slice<X, VEC, E>;
   float s = 0.0f;
 #pragma unroll
@@ -198,8 +199,13 @@ __device__ __forceinline__ void forward_row(const NormForwardArgs& p, int64_t ro
   const float rstd = 1.0f / sqrtf(__fmaf_rn(sum(s), p.inv_cols, p.eps));
   if (t == 0 && p.mean) p.mean[row] = mean, p.rstd[row] = rstd;
   float w[E], b[E];
-  S::vector(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
-  S::vector(static_cast<const W*>(p.b), 0.0f, p.cols, t, threads, b);
+  if (held_w) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) w[i] = held_w[i], b[i] = held_b[i];
+  } else {
+    S::vector(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
+    S::vector(static_cast<const W*>(p.b), 0.0f, p.cols, t, threads, b);
+  }
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = __fmaf_rn(__fmul_rn(x[i], rstd), w[i], b[i]);
   S::store(static_cast<X*>(p.y) + row * p.ldy, p.cols, t, threads, x);
@@ -222,12 +228,14 @@ __global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads) forward_ke
   forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); });
 }
 
-// Blocks an SM, of eight rows each; with more, registers would not do.
+// Blocks an SM, of eight rows each; with more, registers would not do.  (A block's own row takes up to 104 registers a thread,
+// without packs 120: weight and bias are held, which made 16384 x 4096 in BF16 take 57 us instead of 68.)
+constexpr int kRegisters = 65536;
 constexpr int forward_blocks(int each) { return each == 32 ? 3 : 4; }
 
 // Many rows: each warp or block takes rows in turn, kAhead of them on their way.
 template <typename X, typename W, bool VEC, int E, bool ONE>
-__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, ONE ? forward_blocks(E) : 2)
+__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, ONE ? forward_blocks(E) : 1)
     forward_rows_kernel(const __grid_constant__ NormForwardArgs p) {
   using S = Slice<X, VEC, E>;
   constexpr int kDeep = kAhead<X, E>;
@@ -248,13 +256,18 @@ __global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, ONE ? forw
   };
 #pragma unroll
   for (int i = 0; i < kDeep - 1; ++i) begin(i);
+  float w[E], b[E];
+  if (!ONE) {
+    S::vector(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
+    S::vector(static_cast<const W*>(p.b), 0.0f, p.cols, t, threads, b);
+  }
   int at = 0;
   for (; row < p.rows; row += stride) {
     begin(at ? at - 1 : kDeep - 1);
     wait_for_copies<kDeep - 1>();
     float x[E];
     S::read(mine + at * stage, t, threads, x);
-    forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); });
+    forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); }, ONE ? nullptr : w, ONE ? nullptr : b);
     if (++at == kDeep) at = 0;
   }
 }
@@ -498,7 +511,7 @@ cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
   // Few rows: as many threads to a row as there are packs, for its latency.
   if (a.rows <= 2 * kSms && a.cols > 256 && a.cols <= 8 * kMaxThreads) return block(forward_kernel<X, W, VEC, 8, false>, 8);
   if constexpr (Slice<X, VEC, 8>::kAsync) {  // as many rows in turn as make it worth while
-    const int threads = a.cols <= kOneCols ? 32 * kRowWarps : threads_for(a.cols, 16), blocks = kSms * (a.cols <= kOneCols ? forward_blocks(a.cols <= 768 ? 24 : 32) : 1024 / threads);
+    const int threads = a.cols <= kOneCols ? 32 * kRowWarps : threads_for(a.cols, 16), blocks = kSms * (a.cols <= kOneCols ? forward_blocks(a.cols <= 768 ? 24 : 32) : std::max(1, kRegisters / ((VEC ? 104 : 120) * threads)));
     if (a.cols > 256 && a.cols <= kBlockCols && a.rows >= 4 * (int64_t)blocks * (a.cols <= kOneCols ? kRowWarps : 1)) {
       if (a.cols <= 512) return launch_ring(forward_rows_kernel<X, W, VEC, 16, true>, blocks, threads, kRowWarps * kAhead<X, 16> * Slice<X, VEC, 16>::bytes(32), a, stream);
       if (a.cols <= 768) return launch_ring(forward_rows_kernel<X, W, VEC, 24, true>, blocks, threads, kRowWarps * kAhead<X, 24> * Slice<X, VEC, 24>::bytes(32), a, stream);
