@@ -100,7 +100,9 @@ struct Newton {
       q.index = k;
       q.factor = factor ? factor(x.rows, x.cols) : 1.0f;
       q.aligned = is_aligned(x.w, 16) && is_aligned(x.m, 16) && is_aligned(x.compute, 16);
-      q.chunk = (int32_t)round_up((count + kMaxChunks - 1) / kMaxChunks, kSquaresPass);
+      // Four passes a block where a matrix has 64 such blocks: its end (a sum, a fence, a count) takes longer than a pass.
+      q.chunk = (int32_t)std::max(round_up((count + kMaxChunks - 1) / kMaxChunks, kSquaresPass),
+                                  std::min<int64_t>(4 * kSquaresPass, round_up(count / 64 + 1, kSquaresPass)));
       q.chunks = (int32_t)((count + q.chunk - 1) / q.chunk);
       q.tiles_across = (int32_t)((x.cols + kTileCols - 1) / kTileCols);
       NewtonMatrix m{};

@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kStepThreads, 4) squares_kernel(const __grid_c
 // A block takes a tile of 64 x 128 of the caller's matrix; a thread 8 neighbours
 // of a row, four times.  A tall matrix's tile is turned in shared memory.
 template <bool STEP, bool G32, bool M32>
-__global__ void __launch_bounds__(kStepThreads) begin_kernel(const __grid_constant__ MuonArgs p) {
+__global__ void __launch_bounds__(kStepThreads, 4) begin_kernel(const __grid_constant__ MuonArgs p) {
   __shared__ uint32_t turned[kTileRows][kTileCols + 1];
   wait_for_earlier_kernels();
   if (blockIdx.x == 0)
@@ -302,7 +302,7 @@ __device__ __forceinline__ void random_lanes(const MuonArgs& p, int64_t e, uint3
 }
 
 template <bool STEP, bool W32, bool SR>
-__global__ void __launch_bounds__(kStepThreads) finish_kernel(const __grid_constant__ MuonArgs p) {
+__global__ void __launch_bounds__(kStepThreads, 5) finish_kernel(const __grid_constant__ MuonArgs p) {
   __shared__ uint16_t turned[kTileRows][kTileCols + 2];
   wait_for_earlier_kernels();
   if (skipped(p) || *p.err) return;  // (a product that gave up: what there is, is no result)

@@ -195,3 +195,26 @@ def test_nothing_and_refusals():
     with torch.autograd.forward_ad.dual_level():
         with pytest.raises(RuntimeError, match="forward-mode"):
             fp4.linear(torch.autograd.forward_ad.make_dual(x, torch.ones_like(x)), w)
+
+
+@pytest.mark.parametrize("n,k", [(16, 11008), (40, 4096), (576, 11008), (1000, 2112), (64, 32768), (4096, 640), (33, 1024)])
+@pytest.mark.parametrize("tokens", [1, 6, 9, 17, 25, 40])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_too_few_for_all_sms(dtype, tokens, n, k):
+    """k is shared out inside a cluster of two, four or eight blocks."""
+    w, x = _weight(n, k), _x(tokens, k, dtype)
+    y = fp4.linear(x, w)
+    _check(y, x, w)
+    assert torch.equal(y, fp4.linear(x, w))
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 8, 11, 24])
+def test_what_lies_behind_the_last_token_and_row_stays(tokens):
+    from paper_2607_10611_gb300 import _native as N
+    n, k, ld = 200, 2080, 208
+    w, x = _weight(n, k), _x(tokens, k, BF16)
+    y = torch.full((tokens + 2, ld), 8.0, dtype=BF16, device="cuda")
+    m = N.mpadam_nvfp4_matrix(w.codes.data_ptr(), w.scales.data_ptr(), n, k, w.global_scale, 0)
+    N.mpadam_nvfp4_linear(x.data_ptr(), N.MPADAM_BF16, tokens, k, m, y.data_ptr(), ld, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(y[:tokens, :n], fp4.linear(x, w))
+    assert bool((y[tokens:] == 8.0).all()) and bool((y[:, n:] == 8.0).all())

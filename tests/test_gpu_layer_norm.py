@@ -316,3 +316,17 @@ def test_captured_and_replayed():
     torch.cuda.synchronize()
     assert all(torch.equal(a, c) for a, c in zip((y.detach(), *grads), want))
     assert all(torch.equal(a, c) for a, c in zip(torch.autograd.grad(eager, (x, w, b), dy), want[1:]))
+
+
+@pytest.mark.parametrize("rows,cols", [(19999, 264), (20003, 511), (20000, 768), (19500, 1000), (14700, 1001), (3100, 2048), (2500, 2056),
+                                       (1217, 4096), (1300, 4097), (1300, 5632), (609, 8192)])
+@pytest.mark.parametrize("dtype,wdtype", TYPES)
+def test_rows_that_a_block_takes_in_turn(dtype, wdtype, rows, cols):
+    """Rows on their way ahead of the one that is worked on, more of them than blocks; the last ones ragged; rows apart."""
+    x, w, b, dy = _inputs(rows, cols, dtype, wdtype, seed=rows + cols)
+    want, bounds = _reference(x, w, b, dy, 1e-5)
+    got = _run(_views(x, "padded"), w, b, dy, 1e-5)
+    for g, v, d, what in zip(got, want, bounds, ("y", "dx", "dw", "db")):
+        _check(g, v, d, what)
+    for first, second in zip(got, _run(_views(x, "padded"), w, b, dy, 1e-5)):
+        assert torch.equal(first, second)

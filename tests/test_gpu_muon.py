@@ -370,3 +370,44 @@ def test_refusals():
         with pytest.raises(ValueError):
             ortho(x, out=out)
     assert Orthogonalizer([])([]) == [] and Muon([], []).step([], 1, 0.1) is None
+
+
+@pytest.mark.parametrize("shape", [(1300, 1500), (1537, 1281), (1290, 2600), (2100, 1800)])
+def test_several_rows_of_tiles_read_from_below_the_diagonal(shape):
+    """Six to eight tiles to a side: most of A and B is read turned."""
+    x = _matrix(*shape, F32, rank=40)
+    ortho = Orthogonalizer([shape], "f32")
+    y, = ortho([x])
+    _near(y, _polar(x))
+    assert torch.equal(ortho([x])[0], y) and ortho.device_status() == 0
+
+
+def test_a_mixed_list_gives_what_its_matrices_give_alone():
+    """The tiles of large and small, wide and tall matrices are taken in turn, and wait for their own matrix's alone: the
+    squares' sums apart, which a matrix's own sizes decide, nothing depends on the list."""
+    shapes = [(1400, 300), (1, 1), (900, 900), (17, 2000), (2000, 17), (513, 1025), (256, 512), (3, 3), (700, 1300), (1024, 64)]
+    x = [_matrix(*s, F32, seed=i) for i, s in enumerate(shapes)]
+    together = Orthogonalizer(shapes, "f32")
+    want = together(x)
+    for s, m, y in zip(shapes, x, want):
+        assert torch.equal(Orthogonalizer([s], "f32")([m])[0], y)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(together(x), want))
+    assert together.device_status() == 0
+
+
+def test_two_lists_at_once_on_two_streams():
+    """Each with a workspace and counters of its own; their pairs of CTAs share the SMs."""
+    lists = [[(1100, 700)] * 6, [(300, 300)] * 40]
+    x = [[_matrix(*s, F32, seed=i) for i, s in enumerate(shapes)] for shapes in lists]
+    ortho = [Orthogonalizer(shapes, "f32") for shapes in lists]
+    want = [o(m) for o, m in zip(ortho, x)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(5):
+        for i in (0, 1):
+            got[i].append(ortho[i](x[i], stream=streams[i]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for call in got[i] for a, b in zip(call, want[i])) and ortho[i].device_status() == 0
