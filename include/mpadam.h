@@ -792,8 +792,11 @@ int32_t mpadam_orthogonal_create(const int64_t* rows, const int64_t* cols, int32
 
 /* out[k] = x[k] orthogonalised, rounded to the nearest; x, out: host arrays of n
  * device pointers; out[k] may be x[k], and must not overlap another x.
- * Asynchronous on `stream`; 3 + 3 steps launches for as many matrices as share
- * the workspace.  A captured call may be replayed.  Errors: EINVAL, ECUDA. */
+ * Asynchronous on `stream`; four launches for as many matrices as share the
+ * workspace.  Calls with one state must not overlap on the device, replayed ones
+ * among them: they share its workspace and counters (a call that finds these
+ * changed ends after a bounded wait, and its status says so).  A captured call may
+ * be replayed.  Errors: EINVAL, ECUDA. */
 int32_t mpadam_orthogonalize(mpadam_orthogonal_state* s, const void* const* x, void* const* out, struct CUstream_st* stream);
 
 /* Device-side status of the calls issued so far: synchronises the device, returns
@@ -851,7 +854,8 @@ typedef struct mpadam_muon_state mpadam_muon_state;
 int32_t mpadam_muon_create(const mpadam_muon_tensor* tensors, int32_t n, const mpadam_muon_config* cfg, mpadam_muon_state** out);
 
 /* Step t (>= 1, for the random lanes) with learning rate lr (finite, >= 0) over
- * every matrix, asynchronously on `stream`; launches as mpadam_orthogonalize's.
+ * every matrix, asynchronously on `stream`; launches, and what must not overlap, as
+ * mpadam_orthogonalize's.
  * grads: host array of n device pointers of grad_dtype.  grad_scale: device
  * binary32 that multiplies every gradient (see mpadam_grad_norm), or NULL; where
  * it is NaN the step changes nothing.  A captured step may be replayed.  Errors:
