@@ -228,14 +228,16 @@ __global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads) forward_ke
   forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); });
 }
 
-// Blocks an SM, of eight rows each; with more, registers would not do.  (A block's own row takes up to 104 registers a thread,
-// without packs 120: weight and bias are held, which made 16384 x 4096 in BF16 take 57 us instead of 68.)
+// Blocks an SM, of eight rows each; with more, registers would not do.  A block of a row of its own holds weight and bias,
+// and has 32 values a thread in BF16 (152 registers), 16 in binary32 (104, without packs 120): as many rows at a time on an
+// SM as have room, since each waits for two sums over its threads.  16384 x 4096 in BF16 takes 48 us so (5.6 TB/s), with 16
+// values 57, without weight and bias held 68.
 constexpr int kRegisters = 65536;
 constexpr int forward_blocks(int each) { return each == 32 ? 3 : 4; }
 
 // Many rows: each warp or block takes rows in turn, kAhead of them on their way.
 template <typename X, typename W, bool VEC, int E, bool ONE>
-__global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads, ONE ? forward_blocks(E) : 1)
+__global__ void __launch_bounds__(ONE || E == 32 ? 256 : kMaxThreads, ONE ? forward_blocks(E) : 1)
     forward_rows_kernel(const __grid_constant__ NormForwardArgs p) {
   using S = Slice<X, VEC, E>;
   constexpr int kDeep = kAhead<X, E>;
@@ -300,9 +302,13 @@ __global__ void __launch_bounds__(kWideThreads) forward_wide_kernel(const __grid
 // Backward: a row in the registers of a warp (ONE) or of a block, rows in turn;
 // each thread keeps the sums over its rows of dy n and dy for its columns.
 // kAhead rows are on their way by asynchronous copies, or one in registers.
+// 16384 x 4096 in BF16 takes 79 us (5.1 TB/s), 8192 x 4096 in binary32 66 (6.1):
+// registers have room for two rows at a time on an SM, which do not cover the
+// exchange of a BF16 row's sums.  32 values a thread took 80, and a third row whose
+// values were read a second time instead of held 100.
 // ---------------------------------------------------------------------------
 template <typename X, typename W, bool VEC, int E, bool ONE>
-__global__ void __launch_bounds__(ONE || E == 8 ? 256 : kMaxThreads, ONE ? 2 : E == 8 ? 3 : 1)
+__global__ void __launch_bounds__(E == 16 ? kMaxThreads : 256, ONE ? 2 : E == 8 ? 3 : 1)
     backward_kernel(const __grid_constant__ NormBackwardArgs p) {
   using S = Slice<X, VEC, E>;
   constexpr int kDeep = S::kAsync ? kAhead<X, E> : 1;
@@ -511,12 +517,20 @@ cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
   // Few rows: as many threads to a row as there are packs, for its latency.
   if (a.rows <= 2 * kSms && a.cols > 256 && a.cols <= 8 * kMaxThreads) return block(forward_kernel<X, W, VEC, 8, false>, 8);
   if constexpr (Slice<X, VEC, 8>::kAsync) {  // as many rows in turn as make it worth while
-    const int threads = a.cols <= kOneCols ? 32 * kRowWarps : threads_for(a.cols, 16), blocks = kSms * (a.cols <= kOneCols ? forward_blocks(a.cols <= 768 ? 24 : 32) : std::max(1, kRegisters / ((VEC ? 104 : 120) * threads)));
-    if (a.cols > 256 && a.cols <= kBlockCols && a.rows >= 4 * (int64_t)blocks * (a.cols <= kOneCols ? kRowWarps : 1)) {
-      if (a.cols <= 512) return launch_ring(forward_rows_kernel<X, W, VEC, 16, true>, blocks, threads, kRowWarps * kAhead<X, 16> * Slice<X, VEC, 16>::bytes(32), a, stream);
-      if (a.cols <= 768) return launch_ring(forward_rows_kernel<X, W, VEC, 24, true>, blocks, threads, kRowWarps * kAhead<X, 24> * Slice<X, VEC, 24>::bytes(32), a, stream);
-      if (a.cols <= kOneCols) return launch_ring(forward_rows_kernel<X, W, VEC, 32, true>, blocks, threads, kRowWarps * kAhead<X, 32> * Slice<X, VEC, 32>::bytes(32), a, stream);
-      return launch_ring(forward_rows_kernel<X, W, VEC, 16, false>, blocks, threads, kAhead<X, 16> * Slice<X, VEC, 16>::bytes(threads), a, stream);
+    if (a.cols > 256 && a.cols <= kOneCols) {
+      const int threads = 32 * kRowWarps, each = a.cols <= 512 ? 16 : a.cols <= 768 ? 24 : 32;
+      const int64_t blocks = kSms * forward_blocks(each);
+      if (a.rows >= 4 * blocks * kRowWarps) {
+        if (each == 16) return launch_ring(forward_rows_kernel<X, W, VEC, 16, true>, blocks, threads, kRowWarps * kAhead<X, 16> * Slice<X, VEC, 16>::bytes(32), a, stream);
+        if (each == 24) return launch_ring(forward_rows_kernel<X, W, VEC, 24, true>, blocks, threads, kRowWarps * kAhead<X, 24> * Slice<X, VEC, 24>::bytes(32), a, stream);
+        return launch_ring(forward_rows_kernel<X, W, VEC, 32, true>, blocks, threads, kRowWarps * kAhead<X, 32> * Slice<X, VEC, 32>::bytes(32), a, stream);
+      }
+    } else if (a.cols > kOneCols && a.cols <= kBlockCols) {
+      constexpr int kEach = sizeof(X) == 2 ? 32 : 16, kRegs = sizeof(X) == 2 ? 152 : VEC ? 104 : 120;
+      const int threads = threads_for(a.cols, kEach);
+      const int64_t blocks = kSms * std::max(1, kRegisters / (kRegs * threads));
+      if (a.rows >= 4 * blocks)
+        return launch_ring(forward_rows_kernel<X, W, VEC, kEach, false>, blocks, threads, kAhead<X, kEach> * Slice<X, VEC, kEach>::bytes(threads), a, stream);
     }
   }
   if (a.cols <= 256) return one(forward_kernel<X, W, VEC, 8, true>);
