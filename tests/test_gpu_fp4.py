@@ -218,3 +218,14 @@ def test_what_lies_behind_the_last_token_and_row_stays(tokens):
     N.mpadam_nvfp4_linear(x.data_ptr(), N.MPADAM_BF16, tokens, k, m, y.data_ptr(), ld, torch.cuda.current_stream().cuda_stream)
     assert torch.equal(y[:tokens, :n], fp4.linear(x, w))
     assert bool((y[tokens:] == 8.0).all()) and bool((y[:, n:] == 8.0).all())
+
+
+@pytest.mark.parametrize("tokens", [2, 12])
+def test_offsets_past_32_bits(tokens):
+    n, k = 1050000, 4128
+    assert n * k > 2 ** 32
+    w, x = _weight(n, k), _x(tokens, k, BF16)
+    y = fp4.linear(x, w)
+    last = 40  # rows, as a matrix of their own: whole bytes and groups, since k is a multiple of 32
+    tail = fp4.NVFP4Matrix(w.codes[-last * k // 2:].clone(), w.scales[-last * k // 16:].clone(), w.global_scale, (last, k))
+    _check(y[:, -last:].contiguous(), x, tail)

@@ -330,3 +330,32 @@ def test_rows_that_a_block_takes_in_turn(dtype, wdtype, rows, cols):
         _check(g, v, d, what)
     for first, second in zip(got, _run(_views(x, "padded"), w, b, dy, 1e-5)):
         assert torch.equal(first, second)
+
+
+def test_offsets_past_32_bits():
+    """The last rows of more than 2^31 values are as they are alone, but for the order of their sums."""
+    rows, cols = 530000, 4096
+    x = torch.zeros(rows, cols, dtype=BF16, device="cuda")
+    dy = torch.zeros(rows, cols, dtype=BF16, device="cuda")
+    assert x.numel() > 2 ** 31
+    tail, w, b, dtail = _inputs(100, cols, BF16, F32)
+    x[-100:], dy[-100:] = tail, dtail
+    want, bounds = _reference(tail, w, b, dtail, 1e-5)
+    y, dx, dw, db = _run(x, w, b, dy, 1e-5)
+    for g, v, d, what in zip((y[-100:], dx[-100:], dw, db), want, bounds, ("y", "dx", "dw", "db")):
+        _check(g, v, d, what)  # (rows of zeros add nothing: dy is 0 there)
+    assert not bool(dx[:-100].any()) and torch.equal(y[0], b.bfloat16())
+
+
+def test_gradients_that_are_broadcast():
+    """y.sum() hands back one value with strides of 0, a mean over rows one row; an expanded x is read as what it shows."""
+    x, w, b, dy = _inputs(40, 768, F32, F32)
+    one_dy = dy[0]
+    for make, dy in ((lambda y: y.sum(), torch.ones_like(x)), (lambda y: (y.sum(0) * one_dy).sum(), one_dy.expand_as(x).clone())):
+        leaves = [t.clone().requires_grad_() for t in (x, w, b)]
+        make(layer_norm(*leaves)).backward()
+        want, bounds = _reference(x, w, b, dy, 1e-5)
+        for leaf, v, d, what in zip(leaves, want[1:], bounds[1:], ("dx", "dw", "db")):
+            _check(leaf.grad, v, d, what)
+    one = x[:1]
+    assert torch.equal(layer_norm(one.expand(40, 768), w, b), layer_norm(one.repeat(40, 1), w, b))

@@ -411,3 +411,42 @@ def test_two_lists_at_once_on_two_streams():
     torch.cuda.synchronize()
     for i in (0, 1):
         assert all(torch.equal(a, b) for call in got[i] for a, b in zip(call, want[i])) and ortho[i].device_status() == 0
+
+
+def test_offsets_past_32_bits():
+    """A block in the last corner of zeros comes out as it does alone, in its place."""
+    rows, cols, block = 70001, 33001, (300, 400)
+    x = torch.zeros(rows, cols, dtype=BF16, device="cuda")
+    assert x.numel() > 2 ** 31
+    corner = _matrix(*block)
+    x[-block[0]:, -block[1]:] = corner
+    ortho = Orthogonalizer([(rows, cols)], "bf16")
+    y, = ortho([x])
+    assert ortho.device_status() == 0
+    _near(y[-block[0]:, -block[1]:].clone(), _polar(corner))
+    assert not bool(y[:-block[0]].any()) and not bool(y[-block[0]:, :-block[1]].any())
+
+
+def test_two_graphs_of_one_state_one_after_another():
+    """They share the workspace and its counters, and leave them as the next one needs them, an eager call too."""
+    shapes = [(600, 900), (300, 100), (1, 5)]
+    x = [_matrix(*s, F32, seed=i) for i, s in enumerate(shapes)]
+    z = [_matrix(*s, F32, seed=7 + i) for i, s in enumerate(shapes)]
+    ortho = Orthogonalizer(shapes, "f32")
+    want_x, want_z = ortho(x), ortho(z)
+    graphs, outs, stream = [], [], torch.cuda.Stream()
+    for v in (x, z):
+        out = [torch.zeros_like(t) for t in v]
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=stream):
+            ortho(v, out=out)
+        graphs.append(g), outs.append(out)
+    for _ in range(3):
+        graphs[0].replay()
+        graphs[1].replay()
+        eager = ortho(x)
+        torch.cuda.synchronize()
+        for got, want in ((outs[0], want_x), (outs[1], want_z), (eager, want_x)):
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert ortho.device_status() == 0
