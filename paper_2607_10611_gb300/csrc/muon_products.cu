@@ -124,7 +124,7 @@ __device__ __forceinline__ void fence_copies_global() { asm volatile("fence.prox
 // power limit lowers the clock, 2.13.
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) newton_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ alignas(8) uint64_t bars[2 * kStages + 5 + 2 * kSlots + kEpiWarps];
+  __shared__ alignas(8) uint64_t bars[2 * kStages + 5 + 3 * kSlots + kEpiWarps];
   __shared__ alignas(16) int4 slots[kSlots];
   __shared__ uint32_t tmem_base_s;
   __shared__ int32_t failed;
@@ -139,7 +139,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   const uint32_t drained = bar0 + 8u * (2 * kStages + 4);
   auto slot_full = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + s); };           // each CTA's own
   auto slot_free = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + kSlots + s); };  // the leader's alone
-  auto addend_full = [&](int w) { return bar0 + 8u * (2 * kStages + 5 + 2 * kSlots + w); };
+  auto slot_ready = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + 2 * kSlots + s); };  // each CTA's own: its tile's rows are there
+  auto addend_full = [&](int w) { return bar0 + 8u * (2 * kStages + 5 + 3 * kSlots + w); };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -154,6 +155,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(slot_full(s), 1);
       mbar_init(slot_free(s), kReaders);
+      mbar_init(slot_ready(s), 1);
     }
     for (int w = 0; w < kEpiWarps; ++w) mbar_init(addend_full(w), 1);
     failed = 0;
@@ -198,14 +200,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     return NewtonTile{v.x, (uint16_t)v.y, (uint16_t)((uint32_t)v.y >> 16), v.z, (uint32_t)v.w};
   };
   // The pair's n-th tile; matrix < 0: there are no more.  By whole warps, or by one lane (whole = false).
-  auto read_slot = [&](int n, NewtonTile& t, bool whole) {
+  // `early` sees the tile before its turn.
+  auto read_slot = [&](int n, NewtonTile& t, bool whole, auto early) {
     const int s = n % kSlots;
-    bool ok = wait_cluster(slot_full(s), (uint32_t)(n / kSlots) & 1);
+    const uint32_t parity = (uint32_t)(n / kSlots) & 1;
+    bool ok = wait_cluster(slot_full(s), parity);
     if (whole) ok = __all_sync(~0u, ok);
     if (!ok) return false;
     const volatile int4& v = slots[s];
     t = tile_of(make_int4(v.x, v.y, v.z, v.w));
-    if (whole) __syncwarp();
+    early();
+    ok = wait_cluster(slot_ready(s), parity);
+    if (whole) ok = __all_sync(~0u, ok);
+    if (!ok) return false;
     if (!whole || lane == 0) mbar_arrive_cluster(peer_addr(slot_free(s), 0));
     return true;
   };
@@ -232,16 +239,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
       bool ok = true;
       for (int n = 0; ok; ++n) {
         NewtonTile t;
-        if (!read_slot(n, t, false)) { give_up(kErrSlot); ok = false; break; }
+        const bool there = read_slot(n, t, false, [&] {  // (a map that this SM has not seen takes half a microsecond)
+          if (t.matrix < 0) return;
+          const NewtonMatrix& q = p.matrices[t.matrix];
+          if (t.which() == 1) {
+            prefetch_map(&q.x[t.from()]);
+          } else {
+            prefetch_map(t.which() == 2 ? &q.a : &q.b);
+            prefetch_map(t.which() == 2 ? &q.a_along : &q.b_along);
+            if (t.which() == 3) prefetch_map(&q.x_along[t.from()]);
+          }
+        });
+        if (!there) { give_up(kErrSlot); ok = false; break; }
         if (t.matrix < 0) break;
         const NewtonMatrix& q = p.matrices[t.matrix];
         const int which = t.which(), from = t.from(), steps = t.steps_k();
         const CUtensorMap* first = which == 1 ? &q.x[from] : which == 2 ? &q.a : &q.b;
         const CUtensorMap* turned = which == 2 ? &q.a_along : &q.b_along;
         const CUtensorMap* second = which == 2 ? turned : &q.x_along[from];
-        prefetch_map(first);
-        if (which != 1) prefetch_map(turned);
-        if (which == 3) prefetch_map(second);
         fence_copies_global();  // what others stored, and the slot's writer waited for, before what is copied here
         const int m0 = t.tm * kNewtonTile + (int)rank * 128, n0 = t.tn * kNewtonTile + (int)rank * 128;
         // (Loops of their own: a choice of maps within one took 130 cycles more a step.)
@@ -289,12 +304,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
         const uint32_t i = atomicAdd(p.taken, 1u);
         const bool more = i < (uint32_t)p.count;
         const int4 v = more ? __ldg(reinterpret_cast<const int4*>(p.tiles) + i) : make_int4(-1, 0, 0, 0);
-        if (more && !wait_turn(tile_of(v))) { give_up(kErrTurn); break; }
         for (uint32_t r = 0; r < 2; ++r) {
           const uint32_t to = peer_addr(smem_addr(&slots[s]), r);
           sts_cluster(to, (uint32_t)v.x), sts_cluster(to + 4, (uint32_t)v.y), sts_cluster(to + 8, (uint32_t)v.z), sts_cluster(to + 12, (uint32_t)v.w);
           mbar_arrive_cluster(peer_addr(slot_full(s), r));
         }
+        if (more && !wait_turn(tile_of(v))) { give_up(kErrTurn); break; }
+        for (uint32_t r = 0; r < 2; ++r) mbar_arrive_cluster(peer_addr(slot_ready(s), r));
         if (!more) break;
       }
     }
@@ -307,7 +323,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     bool ok = true;
     for (int n = 0; ok; ++n) {
       NewtonTile t;
-      if (!read_slot(n, t, true)) { ok = false; break; }
+      if (!read_slot(n, t, true, [] {})) { ok = false; break; }
       if (t.matrix < 0) break;
       const int steps = t.steps_k();
       if (!__all_sync(~0u, wait_cluster(acc_free(acc), acc_phase ^ 1))) { ok = false; break; }
@@ -348,7 +364,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     uint32_t acc_phase = 0, addend_phase = 0;
     for (int at = 0;; ++at) {
       NewtonTile t;
-      if (!read_slot(at, t, true)) { if (lane == 0) give_up(kErrSlot); break; }
+      const bool there = read_slot(at, t, true, [&] {
+        if (t.matrix < 0 || lane) return;
+        const NewtonMatrix& q = p.matrices[t.matrix];
+        prefetch_map(t.which() == 1 ? &q.a_patch : t.which() == 2 ? &q.b_patch : &q.x_patch[t.from() ^ 1]);
+        if (t.adds()) prefetch_map(t.which() == 2 ? &q.a_patch : &q.lo_patch);
+      });
+      if (!there) { if (lane == 0) give_up(kErrSlot); break; }
       if (t.matrix < 0) break;
       const NewtonMatrix& q = p.matrices[t.matrix];
       const int from = t.from();
