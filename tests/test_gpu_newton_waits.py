@@ -1,5 +1,5 @@
-"""What the Newton-Schulz products do when one of their bounded waits gives up: nothing is written out, the status says so, and
-the next call is whole.  In this build the wait has in fact been met and only says that it was not."""
+"""What the Newton-Schulz products do when one of their bounded waits gives up: nothing is written out, the status says so,
+and the next call is whole.  In this build the wait has in fact been met and only says that it was not."""
 import ctypes
 import subprocess
 from pathlib import Path
@@ -31,11 +31,13 @@ def probe(tmp_path_factory):
     return lib
 
 
-# (the pair of the first tile's CTAs are blocks 0 and 1; what an epilogue waits for so is X's second part or A)
+# Which tiles a pair of CTAs (blocks 2 i and 2 i + 1) takes differs from call to call, and so whether it comes to the wait that
+# gives up: a call that does not is whole, and of twenty some do (of 118 tiles a step a pair takes seven or eight in all).
+# What an epilogue waits for with this barrier is X's second part or A.
 @pytest.mark.parametrize("block,warp,lane,parity", [(0, ISSUER, -1, 0), (0, ISSUER, 7, 1), (0, PRODUCER, 0, 0), (1, PRODUCER, 0, 0),
                                                     (3, PRODUCER, 0, 0), (0, EPILOGUE, -1, 0), (1, EPILOGUE, 3, 0), (2, EPILOGUE, 0, 1)])
 def test_nothing_is_written_when_a_wait_gives_up(probe, block, warp, lane, parity):
-    shapes = [(600, 900), (300, 300), (1000, 520)]
+    shapes = [(1500, 1600), (300, 300), (1000, 520)]
     x = [torch.randn(s, device="cuda", generator=torch.Generator(device="cuda").manual_seed(i)) for i, s in enumerate(shapes)]
     n = len(shapes)
     rows, cols = (ctypes.c_int64 * n)(*(r for r, _ in shapes)), (ctypes.c_int64 * n)(*(c for _, c in shapes))
@@ -56,9 +58,13 @@ def test_nothing_is_written_when_a_wait_gives_up(probe, block, warp, lane, parit
         want, code = call()
         assert code == 0 and all(float(t.abs().max()) < 1.5 for t in want)
         assert probe.give_up(block, warp, lane, parity) == 0
-        out, code = call()
+        codes = []
+        while not codes or (not codes[-1] and len(codes) < 20):
+            out, code = call()
+            codes.append(code)
+            assert all(bool((t == 8.0).all()) if code else torch.equal(t, w) for t, w in zip(out, want))
         assert probe.give_up(-1, 0, 0, 0) == 0
-        assert code != 0 and all(bool((t == 8.0).all()) for t in out)
+        assert codes[-1] != 0
         out, code = call()
         assert code == 0 and all(torch.equal(a, b) for a, b in zip(out, want))
     finally:
