@@ -14,6 +14,7 @@
 // steps, without the second part 2.2e-2, with BF16 0.18.
 #pragma once
 
+#include <cstddef>
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -47,6 +48,13 @@ struct alignas(128) NewtonMatrix {
   int32_t row0;        // its first counter: one for every 256 rows
 };
 
+// Its maps, and those of a list of matrices by their number.
+constexpr int kNewtonMaps = 13;
+static_assert(offsetof(NewtonMatrix, hi) == kNewtonMaps * sizeof(CUtensorMap), "nothing but maps before X's pointers");
+__host__ __device__ inline const CUtensorMap* newton_map(const NewtonMatrix* matrices, int64_t i) {
+  return reinterpret_cast<const CUtensorMap*>(matrices + i / kNewtonMaps) + i % kNewtonMaps;
+}
+
 // A tile of a product: rows 256 tm and columns 256 tn of its result.
 struct alignas(16) NewtonTile {
   int32_t matrix;
@@ -70,7 +78,8 @@ struct alignas(16) NewtonTile {
 constexpr uint32_t kSignals = 16;
 
 struct ProductArgs {
-  const NewtonMatrix* matrices;
+  const NewtonMatrix* matrices;  // the list's
+  int32_t first, members;        // those that the tiles belong to
   const NewtonTile* tiles;
   int32_t count;
   uint32_t* progress;  // of every 256 rows; 0 when the launch begins, and so is

@@ -82,6 +82,11 @@ __device__ __forceinline__ void commit_stores() { asm volatile("cp.async.bulk.co
 template <int LEFT>
 __device__ __forceinline__ void wait_for_reads() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
 __device__ __forceinline__ void wait_for_stores() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// A tensor map that the host copied to memory may be used by this block's copies from here on; what the SM kept of
+// another one that lay there before may not.
+__device__ __forceinline__ void acquire_map(const CUtensorMap* map) {
+  asm volatile("fence.proxy.tensormap::generic.acquire.sys [%0], 128;" ::"l"(map) : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
@@ -166,6 +171,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  // The maps' memory may have held another list's (one that was destroyed, whose memory this one got): each block acquires all
+  // that it may use, its threads a share each, before any of them is used.  The host's copy was complete before the launch.
+  for (int64_t i = threadIdx.x; i < (int64_t)kNewtonMaps * p.members; i += kProductThreads) acquire_map(newton_map(p.matrices + p.first, i));
   tc_fence_before();
   __syncthreads();
   cluster_sync();
