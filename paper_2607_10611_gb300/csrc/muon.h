@@ -77,6 +77,20 @@ struct alignas(16) NewtonTile {
 };
 constexpr uint32_t kSignals = 16;
 
+// How a pair of CTAs that share operands in `stages` stages of shared memory ends.  Each CTA copies its half of a step's bytes,
+// both halves to one barrier, on which the leader announces all of them as it asks for its own half.  When nobody asks for any
+// more, CTA `rank` having asked for the first asked[rank] steps, every step before pair_open is whole (its stage was taken again)
+// and the barriers of those from there on, a stage each, become whole once what will not come is made up for:
+enum class PairStep { kWhole, kNoLeader, kNoPeer };  // both asked; the leader did not, so nothing is announced; the other CTA did not
+__host__ __device__ inline int pair_end(int asked0, int asked1) { return asked0 > asked1 ? asked0 : asked1; }
+__host__ __device__ inline int pair_open(int asked0, int asked1, int stages) {
+  const int end = pair_end(asked0, asked1);
+  return end > stages ? end - stages : 0;
+}
+__host__ __device__ inline PairStep pair_step(int step, int asked0, int asked1) {
+  return step >= asked1 ? PairStep::kNoPeer : step >= asked0 ? PairStep::kNoLeader : PairStep::kWhole;
+}
+
 struct ProductArgs {
   const NewtonMatrix* matrices;  // the list's
   int32_t first, members;        // those that the tiles belong to

@@ -63,6 +63,11 @@ __device__ __forceinline__ void pair_mma_f16(uint32_t d, uint64_t a, uint64_t b,
       : "memory");
 }
 
+// Bytes that a barrier waits for as if a copy had brought them.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
 __device__ __forceinline__ void sts_v4(uint32_t addr, const uint32_t (&v)[4]) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
@@ -133,6 +138,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   __shared__ alignas(16) int4 slots[kSlots];
   __shared__ uint32_t tmem_base_s;
   __shared__ int32_t failed;
+  __shared__ int32_t asked[2];  // steps whose copies a CTA has asked for, when it asks for no more; the leader's alone
   const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
@@ -163,7 +169,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
       mbar_init(slot_ready(s), 1);
     }
     for (int w = 0; w < kEpiWarps; ++w) mbar_init(addend_full(w), 1);
-    failed = 0;
+    failed = asked[0] = asked[1] = 0;
     mbar_init_fence();
   }
   if (warp == 1) {
@@ -242,7 +248,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   if (warp == 0) {
     if (lane == 0) {
       const uint32_t full0 = peer_addr(full(0), 0);
-      int s = 0;
+      int s = 0, steps_asked = 0;
       uint32_t phase = 0;
       bool ok = true;
       for (int n = 0; ok; ++n) {
@@ -286,6 +292,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
             } else {
               pair_load_2d(to, first, x, n0, bar);
             }
+            ++steps_asked;
             if (++s == kStages) { s = 0; phase ^= 1; }
           }
         };
@@ -297,12 +304,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
         load(plain, half, no, yes);
         load(half, steps, yes, yes);
       }
-      if (!ok) {
-        // The copies in flight, before the block's memory goes.  Which of a stage's two have begun, neither CTA knows of the
-        // other: half a millisecond, in which they land hundreds of times over.
-        const long long begun = clock64();
-        while (clock64() - begun < 1000000) {}
-      }
+      sts_cluster(peer_addr(smem_addr(&asked[rank]), 0), (uint32_t)steps_asked);
     }
   } else if (warp == 2 && rank == 0) {
     if (lane == 0) {
@@ -358,12 +360,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
       if (issue) pair_commit(acc_full(acc));
       if (++acc == 2) { acc = 0; acc_phase ^= 1; }
     }
-    if (!ok) {  // the products in flight, before their operands' memory goes (the producer waits for the copies)
-      if (issue) {
-        give_up(kErrCopy);
-        pair_commit(drained);
-      }
-      for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(drained, 0); ++i) {}
+    if (issue) {
+      if (!ok) give_up(kErrCopy);
+      pair_commit(drained);
     }
   } else if (warp >= 4) {
     const int quarter = warp & 3, half = (warp - 4) >> 2, who = warp - 4;
@@ -499,9 +498,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     }
     if (lane == 0) wait_for_stores();
   }
+  // The pair's end, the same whoever gave up, or nobody: any of the pair may have left its loop while what others asked for is in
+  // flight.  Past the first barrier nobody asks for copies or products any more; memory goes past the second, when all
+  // products are done (each CTA's own barrier has been arrived at) and all copies of operands have landed.  The epilogue's
+  // warps have seen the ends of their own copies and stores.  (These waits are bounded too, by seconds: copies and products
+  // end by themselves.)
   __syncwarp();
   tc_fence_before();
-  __syncthreads();
+  cluster_sync();
+  if (warp == 1) mbar_wait(drained, 0);
+  if (warp == 0 && rank == 0 && lane == 0) {
+    const volatile int32_t* by = asked;
+    const int first = by[0], second = by[1], end = pair_end(first, second);
+    for (int i = pair_open(first, second, kStages); i < end; ++i) {
+      const PairStep what = pair_step(i, first, second);
+      if (what == PairStep::kNoPeer) mbar_complete_tx(full(i % kStages), kStageTx / 2);
+      if (what == PairStep::kNoLeader) mbar_arrive_tx(full(i % kStages), kStageTx / 2);
+    }
+    for (int i = pair_open(first, second, kStages); i < end; ++i) mbar_wait(full(i % kStages), (uint32_t)(i / kStages) & 1);
+  }
+  __syncwarp();
   cluster_sync();
   tc_fence_after();
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
