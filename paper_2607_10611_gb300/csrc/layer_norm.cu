@@ -495,15 +495,47 @@ bool whole_packs(const void* p, int64_t ld, int64_t rows, int64_t size) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows == 1 || ld * size % 16 == 0);
 }
 
-int threads_for(int64_t cols, int each) { return (int)((cols + 32 * each - 1) / (32 * each)) * 32; }
+constexpr int threads_for(int64_t cols, int each) { return (int)((cols + 32 * each - 1) / (32 * each)) * 32; }
 
-template <typename Args>
-cudaError_t launch_ring(void (*kernel)(Args), int64_t blocks, int threads, int smem, const Args& a, cudaStream_t stream) {
-  if (smem > 40 * 1024) {  // (what is not asked for is 48 KB, the kernel's own arrays among it)
-    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+// A launch of a kernel instance that needs `smem` bytes, and MOST for the widest row that it is taken for.  The limit belongs to
+// the instance, whoever launches it from whatever thread: it is set once, to MOST.  `ready` is the instance's.
+template <int MOST, typename Args>
+cudaError_t launch_ring(void (*kernel)(Args), std::atomic<uint64_t>& ready, int64_t blocks, int threads, int smem, const Args& a,
+                        cudaStream_t stream) {
+  if (MOST > 40 * 1024) {  // (what is not asked for is 48 KB, the kernel's own arrays among it)
+    const cudaError_t e = allow_smem((const void*)kernel, MOST, ready);
     if (e != cudaSuccess) return e;
   }
   return launch_dependent((const void*)kernel, (unsigned)blocks, threads, 0, smem, &a, stream);
+}
+
+// Shared memory of rows on their way, `threads` to a row (ONE: 32, and a block's rows together).
+template <typename X, bool VEC, int E, bool ONE>
+constexpr int forward_ring(int threads) {
+  return (ONE ? kRowWarps : 1) * kAhead<X, E> * Slice<X, VEC, E>::bytes(threads);
+}
+// The same, and the sums of a row's columns where a row is one warp's.
+template <typename X, bool VEC, int E, bool ONE>
+constexpr int backward_ring(int threads, int64_t cols) {
+  using S = Slice<X, VEC, E>;
+  return (S::kAsync ? (ONE ? kRowWarps : 1) * kAhead<X, E> * 2 * S::bytes(threads) : 0) + (ONE ? (int)(2 * cols * sizeof(float)) : 0);
+}
+
+template <typename X, typename W, bool VEC, int E, bool ONE>
+cudaError_t launch_forward_rows(const NormForwardArgs& a, int64_t blocks, int threads, cudaStream_t stream) {
+  static std::atomic<uint64_t> ready{0};
+  constexpr int kMost = forward_ring<X, VEC, E, ONE>(ONE ? 32 : threads_for(kBlockCols, E));
+  return launch_ring<kMost>(forward_rows_kernel<X, W, VEC, E, ONE>, ready, blocks, threads, forward_ring<X, VEC, E, ONE>(ONE ? 32 : threads),
+                            a, stream);
+}
+
+template <typename X, typename W, bool VEC, int E, bool ONE>
+cudaError_t launch_backward_rows(const NormBackwardArgs& a, int threads, cudaStream_t stream) {
+  static std::atomic<uint64_t> ready{0};
+  constexpr int64_t kMostCols = ONE ? kWarpCols : E == 8 ? kSmallCols : kBlockCols;
+  constexpr int kMost = backward_ring<X, VEC, E, ONE>(ONE ? 32 : threads_for(kMostCols, E), kMostCols);
+  return launch_ring<kMost>(backward_kernel<X, W, VEC, E, ONE>, ready, a.parts, threads,
+                            backward_ring<X, VEC, E, ONE>(ONE ? 32 : threads, a.cols), a, stream);
 }
 
 template <typename X, typename W, bool VEC>
@@ -521,16 +553,15 @@ cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
       const int threads = 32 * kRowWarps, each = a.cols <= 512 ? 16 : a.cols <= 768 ? 24 : 32;
       const int64_t blocks = kSms * forward_blocks(each);
       if (a.rows >= 4 * blocks * kRowWarps) {
-        if (each == 16) return launch_ring(forward_rows_kernel<X, W, VEC, 16, true>, blocks, threads, kRowWarps * kAhead<X, 16> * Slice<X, VEC, 16>::bytes(32), a, stream);
-        if (each == 24) return launch_ring(forward_rows_kernel<X, W, VEC, 24, true>, blocks, threads, kRowWarps * kAhead<X, 24> * Slice<X, VEC, 24>::bytes(32), a, stream);
-        return launch_ring(forward_rows_kernel<X, W, VEC, 32, true>, blocks, threads, kRowWarps * kAhead<X, 32> * Slice<X, VEC, 32>::bytes(32), a, stream);
+        if (each == 16) return launch_forward_rows<X, W, VEC, 16, true>(a, blocks, threads, stream);
+        if (each == 24) return launch_forward_rows<X, W, VEC, 24, true>(a, blocks, threads, stream);
+        return launch_forward_rows<X, W, VEC, 32, true>(a, blocks, threads, stream);
       }
     } else if (a.cols > kOneCols && a.cols <= kBlockCols) {
       constexpr int kEach = sizeof(X) == 2 ? 32 : 16, kRegs = sizeof(X) == 2 ? 152 : VEC ? 104 : 120;
       const int threads = threads_for(a.cols, kEach);
       const int64_t blocks = kSms * std::max(1, kRegisters / (kRegs * threads));
-      if (a.rows >= 4 * blocks)
-        return launch_ring(forward_rows_kernel<X, W, VEC, kEach, false>, blocks, threads, kAhead<X, kEach> * Slice<X, VEC, kEach>::bytes(threads), a, stream);
+      if (a.rows >= 4 * blocks) return launch_forward_rows<X, W, VEC, kEach, false>(a, blocks, threads, stream);
     }
   }
   if (a.cols <= 256) return one(forward_kernel<X, W, VEC, 8, true>);
@@ -543,21 +574,9 @@ cudaError_t launch_forward(const NormForwardArgs& a, cudaStream_t stream) {
 
 template <typename X, typename W, bool VEC>
 cudaError_t launch_backward(const NormBackwardArgs& a, cudaStream_t stream) {
-  if (a.cols <= kWarpCols) {
-    using S = Slice<X, VEC, 8>;
-    const int ring = S::kAsync ? kRowWarps * kAhead<X, 8> * 2 * S::bytes(32) : 0;
-    return launch_ring(backward_kernel<X, W, VEC, 8, true>, a.parts, 32 * kRowWarps, ring + (int)(2 * a.cols * sizeof(float)), a, stream);
-  }
-  if (a.cols <= kSmallCols) {
-    using S = Slice<X, VEC, 8>;
-    const int threads = threads_for(a.cols, 8);
-    return launch_ring(backward_kernel<X, W, VEC, 8, false>, a.parts, threads, S::kAsync ? kAhead<X, 8> * 2 * S::bytes(threads) : 0, a, stream);
-  }
-  if (a.cols <= kBlockCols) {
-    using S = Slice<X, VEC, 16>;
-    const int threads = threads_for(a.cols, 16);
-    return launch_ring(backward_kernel<X, W, VEC, 16, false>, a.parts, threads, S::kAsync ? kAhead<X, 16> * 2 * S::bytes(threads) : 0, a, stream);
-  }
+  if (a.cols <= kWarpCols) return launch_backward_rows<X, W, VEC, 8, true>(a, 32 * kRowWarps, stream);
+  if (a.cols <= kSmallCols) return launch_backward_rows<X, W, VEC, 8, false>(a, threads_for(a.cols, 8), stream);
+  if (a.cols <= kBlockCols) return launch_backward_rows<X, W, VEC, 16, false>(a, threads_for(a.cols, 16), stream);
   if (a.dx) {
     const cudaError_t e = launch_dependent((const void*)backward_wide_kernel<X, W>, (unsigned)a.rows, kWideThreads, 0, 0, &a, stream);
     if (e != cudaSuccess) return e;
