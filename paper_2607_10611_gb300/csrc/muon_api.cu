@@ -246,7 +246,11 @@ struct Newton {
     if (rc) return rc;
     cudaError_t e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpy(code, args.err, sizeof(int32_t), cudaMemcpyDeviceToHost);
-    if (e == cudaSuccess && *code) e = cudaMemset(args.err, 0, sizeof(int32_t));
+    if (e == cudaSuccess && *code) {
+      e = cudaMemset(args.err, 0, sizeof(int32_t));
+      // the clear is asynchronous, and the next call may be on a stream that does not wait for it
+      if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);
+    }
     return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "reading the error word");
   }
 };
