@@ -422,6 +422,13 @@ int32_t clear_pool_counters(mpadam_state* s) {
   return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "clearing the tail-pool counters");
 }
 
+// Clears, and copies from pageable memory, run on the legacy stream and may return before they are done; the next step may be on
+// a stream that does not wait for it.
+int32_t finish_tables() {
+  const cudaError_t e = cudaStreamSynchronize(cudaStreamLegacy);
+  return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "waiting for the tables");
+}
+
 int64_t tiles_of(int64_t numel) { return (numel + mpadam::kTile - 1) / mpadam::kTile; }
 
 // Tensor holding each CTA's first tile of the range [tile_base, tile_base +
@@ -811,6 +818,8 @@ int32_t create_state(const std::vector<TensorIn>& t, const mpadam_config* cfg, i
       if (!rc) rc = setup_pool(s, g);
       if (rc) { release(s); return rc; }
     }
+    rc = finish_tables();
+    if (rc) { release(s); return rc; }
   } catch (const std::bad_alloc&) {
     release(s);
     return fail(MPADAM_EALLOC, "host allocation failed");
@@ -1031,7 +1040,7 @@ int32_t mpadam_set_grid(mpadam_state* s, int32_t ctas) {
     if (!rc) rc = setup_pool(s, g);
     if (rc) return rc;
   }
-  return MPADAM_OK;
+  return finish_tables();
 }
 
 int32_t mpadam_set_tail_pool(mpadam_state* s, int32_t static_q, int32_t chunk_tiles) {
@@ -1051,7 +1060,7 @@ int32_t mpadam_set_tail_pool(mpadam_state* s, int32_t static_q, int32_t chunk_ti
     rc = setup_pool(s, g);
     if (rc) return rc;
   }
-  return MPADAM_OK;
+  return finish_tables();
 }
 
 int32_t mpadam_launch_info(const mpadam_state* s, int32_t* ctas, int32_t* threads) {
@@ -1071,7 +1080,8 @@ int32_t mpadam_device_status(mpadam_state* s, int32_t* code) {
   if (e != cudaSuccess) return cuda_fail(e, "reading the error word");
   e = cudaMemset(s->d_err, 0, sizeof(int32_t));
   if (e != cudaSuccess) return cuda_fail(e, "clearing the error word");
-  return clear_pool_counters(s);
+  rc = clear_pool_counters(s);
+  return rc ? rc : finish_tables();
 }
 
 int32_t mpadam_step(mpadam_state* s, const void* const* grads, int64_t step, cudaStream_t stream) {
@@ -1516,6 +1526,7 @@ extern "C" int32_t mpadam_noalloc_status(cudaStream_t stream, int32_t* code) {
   if (*code != 0) {  // a launch that gave up may not have claimed all that it would have
     e = cudaMemset(scratch + kNoAllocPoolOffset, 0, sizeof(uint32_t) * mpadam::kPoolCounters);
     if (e != cudaSuccess) return cuda_fail(e, "clearing the tail-pool counters");
+    return finish_tables();
   }
   return MPADAM_OK;
 }
@@ -1631,7 +1642,7 @@ extern "C" int32_t mpadam_toy_status(mpadam_toy_state* s, int32_t* code) {
   if (e != cudaSuccess) return cuda_fail(e, "reading the error word");
   e = cudaMemset(s->a.err, 0, sizeof(int32_t));
   if (e != cudaSuccess) return cuda_fail(e, "clearing the error word");
-  return MPADAM_OK;
+  return finish_tables();
 }
 
 extern "C" int32_t mpadam_toy_destroy(mpadam_toy_state* s) {

@@ -211,7 +211,11 @@ extern "C" int32_t mpadam_adamw_status(mpadam_adamw_state* s, int32_t* code) {
   if (rc) return rc;
   cudaError_t e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = cudaMemcpy(code, s->args.err, sizeof(int32_t), cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess && *code) e = cudaMemset(s->args.err, 0, sizeof(int32_t));
+  if (e == cudaSuccess && *code) {
+    e = cudaMemset(s->args.err, 0, sizeof(int32_t));
+    // the clear is asynchronous, and the next step may be on a stream that does not wait for it
+    if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);
+  }
   return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "reading the error word");
 }
 
