@@ -43,7 +43,7 @@ extern "C" int32_t mpadam_layer_norm_forward(const mpadam_layer_norm* p, cudaStr
   if (!rc) rc = check_rows("y", p->y, p->ldy, p->cols, size_of(p->x_dtype));
   if (rc) return rc;
   const NormForwardArgs a{p->x, p->w, p->b, p->y, p->mean, p->rstd, p->rows, p->cols, p->ldx, p->ldy, p->eps,
-                          (float)(1.0 / (double)p->cols), p->x_dtype == MPADAM_F32, p->w_dtype == MPADAM_F32};
+                          (float)(1.0 / (double)p->cols), (float)p->cols, p->x_dtype == MPADAM_F32, p->w_dtype == MPADAM_F32};
   const cudaError_t e = launch_norm_forward(a, stream);
   return e == cudaSuccess ? MPADAM_OK : cuda_fail(e, "launch of the layer norm");
 }

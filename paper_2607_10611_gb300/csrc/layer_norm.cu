@@ -2,8 +2,10 @@
 //   n = (x - mean) rstd,  rstd = 1 / sqrt(mean((x - mean)^2) + eps),  y = n w + b
 //   dn = dy w,  dx = (dn - mean(dn) - n mean(dn n)) rstd
 //   dw = sum over rows of dy n,  db = sum over rows of dy
-// Everything is in binary32 from the load to the store; the variance is taken
-// around the mean, so that a mean far from 0 costs no bits.
+// Everything is in binary32 from the load to the store.  The variance is taken
+// around a first mean, whose own roundings are taken off the deviations again
+// (Moments below): a mean far from 0 costs the forward pass no bits, and the
+// backward pass the rounding of the mean that it is given.
 #include <algorithm>
 
 #include "launch.h"
@@ -119,12 +121,12 @@ struct Slice {
       else put(p, c, x[0 + s]);
     }
   }
-  // The same columns of a vector of another type (`absent` where there is none).
-  template <typename W>
+  // The same columns of a vector of another type (`absent` where there is none): those of slots [FIRST, FIRST + SLOTS).
+  template <int FIRST = 0, int SLOTS = kSlots, typename W>
   static __device__ __forceinline__ void vector(const W* p, float absent, int64_t cols, int t, int threads, float* x) {
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      const int64_t c = at(s, t, threads);
+    for (int s = 0; s < SLOTS; ++s) {
+      const int64_t c = at(FIRST + s, t, threads);
       if constexpr (VEC) {
         if (p && c < cols) {
 #pragma unroll
@@ -160,15 +162,18 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-// Sums of `x` over a block's warps, the same in every thread; `slots` (2 x 32
-// values) alternate between calls, so that one barrier a call is enough: a
-// warp that is two calls ahead would have passed the barrier between them.
+// Sums over a block's warps, of one value or two, the same in every thread;
+// `slots` (2 x 32 of each) alternate between calls, so that one barrier a call is
+// enough: a warp that is two calls ahead would have passed the barrier between them.
+struct alignas(16) SumSlots {
+  float x[32], y[32];
+};
 struct BlockSum {
-  float (*slots)[32];
+  SumSlots* slots;  // [2]
   int turn = 0;
   __device__ __forceinline__ float operator()(float x) {
     x = warp_sum(x);
-    float* s = slots[turn];
+    float* s = slots[turn].x;
     turn ^= 1;
     const int warps = blockDim.x / 32;
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = x;
@@ -177,55 +182,130 @@ struct BlockSum {
     for (int i = 0; i < warps; ++i) sum = __fadd_rn(sum, s[i]);
     return sum;
   }
+  __device__ __forceinline__ float2 operator()(float x, float y) {
+    x = warp_sum(x), y = warp_sum(y);
+    SumSlots& s = slots[turn];
+    turn ^= 1;
+    const int warps = blockDim.x / 32;
+    if ((threadIdx.x & 31) == 0) s.x[threadIdx.x >> 5] = x, s.y[threadIdx.x >> 5] = y;
+    __syncthreads();
+    float2 sum = make_float2(0.0f, 0.0f);
+    for (int i = 0; i < warps; i += 4) {
+      const float4 a = *reinterpret_cast<const float4*>(s.x + i), b = *reinterpret_cast<const float4*>(s.y + i);
+      sum.x = __fadd_rn(sum.x, a.x), sum.y = __fadd_rn(sum.y, b.x);
+      if (i + 1 < warps) sum.x = __fadd_rn(sum.x, a.y), sum.y = __fadd_rn(sum.y, b.y);
+      if (i + 2 < warps) sum.x = __fadd_rn(sum.x, a.z), sum.y = __fadd_rn(sum.y, b.z);
+      if (i + 3 < warps) sum.x = __fadd_rn(sum.x, a.w), sum.y = __fadd_rn(sum.y, b.w);
+    }
+    return sum;
+  }
+};
+struct WarpSum {
+  __device__ __forceinline__ float operator()(float x) { return warp_sum(x); }
+  __device__ __forceinline__ float2 operator()(float x, float y) { return make_float2(warp_sum(x), warp_sum(y)); }
+};
+// The sums of a row that is one warp's, or a block's.
+template <bool ONE>
+__device__ __forceinline__ auto row_sum(SumSlots* slots) {
+  if constexpr (ONE) return WarpSum{};
+  else return BlockSum{slots};
+}
+
+// A row's mean and 1 / sigma by its sum, by those of its deviations d from a first mean and of their squares.  The first mean is
+// off by some roundings of its size, and the deviations may be as small: `rest` is what it lacks, shift makes n = d / sigma +
+// shift, and the mean square has the square of the rest too much.  Binary32 values' own sum is off, and the deviations' mean is
+// the rest (4096 x 8192 45 us for 43 without).  A sum of BF16 values of one size is exact up to 2^15 of them, and values of
+// several sizes lie far apart: what the division left is the rest, without another sum over the row (48 us instead of 50 for
+// 16384 x 4096).
+template <typename X>
+struct Moments {
+  static constexpr bool kExactSum = sizeof(X) == 2;
+  float first, rest, mean, rstd, shift;
+  __device__ __forceinline__ Moments(float sum, const NormForwardArgs& p) {
+    first = __fmul_rn(sum, p.inv_cols);
+    rest = kExactSum ? __fmul_rn(__fmaf_rn(-first, p.all_cols, sum), p.inv_cols) : 0.0f;
+  }
+  // One deviation, added to a thread's sums.
+  static __device__ __forceinline__ void add(float d, float& r, float& s) {
+    if (!kExactSum) r = __fadd_rn(r, d);
+    s = __fmaf_rn(d, d, s);
+  }
+  template <typename Sum>
+  __device__ __forceinline__ void finish(float r, float s, Sum& sum, const NormForwardArgs& p) {
+    if (kExactSum) {
+      s = sum(s);
+    } else {
+      const float2 sums = sum(r, s);
+      rest = __fmul_rn(sums.x, p.inv_cols), s = sums.y;
+    }
+    mean = __fadd_rn(first, rest);
+    const float var = __fmaf_rn(-rest, rest, __fmul_rn(s, p.inv_cols));
+    rstd = 1.0f / sqrtf(__fadd_rn(var < 0.0f ? 0.0f : var, p.eps));  // (a NaN stays one)
+    shift = -__fmul_rn(rest, rstd);
+  }
+  __device__ __forceinline__ float normal(float d) const { return __fmaf_rn(d, rstd, shift); }
 };
 
 // ---------------------------------------------------------------------------
 // Forward: a row in the registers of a warp (ONE) or of a block.
 // ---------------------------------------------------------------------------
+// y of what is left of a row from slot FIRST on: weight and bias a pack at a time, which spares the registers of wide rows (32768
+// x 1024 in BF16 30.0 us, 33.1 with all of them at once), but all at once where those have room (32768 x 768 22.7, 24.5) or they
+// come one by one.
+template <typename X, typename W, bool VEC, int E, int FIRST>
+__device__ __forceinline__ void scale_row(const NormForwardArgs& p, int t, int threads, float (&x)[E], const Moments<X>& m) {
+  using S = Slice<X, VEC, E>;
+  constexpr int kSlots = VEC && E != 24 ? 1 : S::kSlots, kPart = kSlots * S::kN;
+  float w[kPart], b[kPart];
+  S::template vector<FIRST, kSlots>(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
+  S::template vector<FIRST, kSlots>(static_cast<const W*>(p.b), 0.0f, p.cols, t, threads, b);
+#pragma unroll
+  for (int i = 0; i < kPart; ++i) x[FIRST * S::kN + i] = __fmaf_rn(m.normal(x[FIRST * S::kN + i]), w[i], b[i]);
+  if constexpr (FIRST + kSlots < S::kSlots) scale_row<X, W, VEC, E, FIRST + kSlots>(p, t, threads, x, m);
+}
+
 template <typename X, typename W, bool VEC, int E, typename Sum>
-__device__ __forceinline__ void forward_row(const NormForwardArgs& p, int64_t row, int t, int threads, float (&x)[E], Sum sum,
+__device__ __forceinline__ void forward_row(const NormForwardArgs& p, int64_t row, int t, int threads, float (&x)[E], Sum& sum,
                                             const float* held_w = nullptr, const float* held_b = nullptr) {
   using S = Slice<X, VEC, E>;
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < E; ++i) s = __fadd_rn(s, x[i]);
-  const float mean = __fmul_rn(sum(s), p.inv_cols);
-  s = 0.0f;
+  Moments<X> m(sum(s), p);
+  float r = s = 0.0f;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    x[i] = __fsub_rn(x[i], mean);
-    if (S::at(i / S::kN, t, threads) < p.cols) s = __fmaf_rn(x[i], x[i], s);
+    x[i] = __fsub_rn(x[i], m.first);
+    if (S::at(i / S::kN, t, threads) < p.cols) m.add(x[i], r, s);
   }
-  const float rstd = 1.0f / sqrtf(__fmaf_rn(sum(s), p.inv_cols, p.eps));
-  if (t == 0 && p.mean) p.mean[row] = mean, p.rstd[row] = rstd;
-  float w[E], b[E];
+  m.finish(r, s, sum, p);
+  if (t == 0 && p.mean) p.mean[row] = m.mean, p.rstd[row] = m.rstd;
   if (held_w) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) w[i] = held_w[i], b[i] = held_b[i];
-  } else {
-    S::vector(static_cast<const W*>(p.w), 1.0f, p.cols, t, threads, w);
-    S::vector(static_cast<const W*>(p.b), 0.0f, p.cols, t, threads, b);
-  }
+    for (int i = 0; i < E; ++i) x[i] = m.normal(x[i]);
 #pragma unroll
-  for (int i = 0; i < E; ++i) x[i] = __fmaf_rn(__fmul_rn(x[i], rstd), w[i], b[i]);
+    for (int i = 0; i < E; ++i) x[i] = __fmaf_rn(x[i], held_w[i], held_b[i]);
+  } else {
+    scale_row<X, W, VEC, E, 0>(p, t, threads, x, m);
+  }
   S::store(static_cast<X*>(p.y) + row * p.ldy, p.cols, t, threads, x);
 }
 
 template <typename X, typename W, bool VEC, int E, bool ONE>
 __global__ void __launch_bounds__(ONE ? 32 * kRowWarps : kMaxThreads) forward_kernel(const __grid_constant__ NormForwardArgs p) {
   using S = Slice<X, VEC, E>;
-  __shared__ float slots[2][32];
+  __shared__ SumSlots slots[2];
   wait_for_earlier_kernels();
   let_later_kernels_begin();
   const int t = ONE ? threadIdx.x & 31 : threadIdx.x, threads = ONE ? 32 : blockDim.x;
   const int64_t row = ONE ? (int64_t)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5) : blockIdx.x;
   if (row >= p.rows) return;
-  BlockSum block{slots};
+  auto sum = row_sum<ONE>(slots);
   uint32_t raw[S::kWords];
   float x[E];
   S::fetch(static_cast<const X*>(p.x) + row * p.ldx, p.cols, t, threads, raw);
   S::open(raw, x);
-  forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); });
+  forward_row<X, W, VEC, E>(p, row, t, threads, x, sum);
 }
 
 // Blocks an SM, of eight rows each; with more, registers would not do.  A block of a row of its own holds weight and bias,
@@ -242,7 +322,7 @@ __global__ void __launch_bounds__(ONE || E == 32 ? 256 : kMaxThreads, ONE ? forw
   using S = Slice<X, VEC, E>;
   constexpr int kDeep = kAhead<X, E>;
   extern __shared__ uint4 ring[];
-  __shared__ float slots[2][32];
+  __shared__ SumSlots slots[2];
   wait_for_earlier_kernels();
   let_later_kernels_begin();
   const int t = ONE ? threadIdx.x & 31 : threadIdx.x, threads = ONE ? 32 : blockDim.x, warps = blockDim.x / 32;
@@ -250,7 +330,7 @@ __global__ void __launch_bounds__(ONE || E == 32 ? 256 : kMaxThreads, ONE ? forw
   int64_t row = ONE ? (int64_t)blockIdx.x * warps + (threadIdx.x >> 5) : blockIdx.x, next = row;
   const int stage = S::bytes(threads);
   const uint32_t mine = smem_addr(ring) + (ONE ? (threadIdx.x >> 5) * kDeep * stage : 0);
-  BlockSum block{slots};
+  auto sum = row_sum<ONE>(slots);
   auto begin = [&](int at) {
     if (next < p.rows) S::begin(static_cast<const X*>(p.x) + next * p.ldx, p.cols, t, threads, mine + at * stage);
     commit_copies();
@@ -269,7 +349,7 @@ __global__ void __launch_bounds__(ONE || E == 32 ? 256 : kMaxThreads, ONE ? forw
     wait_for_copies<kDeep - 1>();
     float x[E];
     S::read(mine + at * stage, t, threads, x);
-    forward_row<X, W, VEC, E>(p, row, t, threads, x, [&](float v) { return ONE ? warp_sum(v) : block(v); }, ONE ? nullptr : w, ONE ? nullptr : b);
+    forward_row<X, W, VEC, E>(p, row, t, threads, x, sum, ONE ? nullptr : w, ONE ? nullptr : b);
     if (++at == kDeep) at = 0;
   }
 }
@@ -277,7 +357,7 @@ __global__ void __launch_bounds__(ONE || E == 32 ? 256 : kMaxThreads, ONE ? forw
 // Rows of any width, read three times.
 template <typename X, typename W>
 __global__ void __launch_bounds__(kWideThreads) forward_wide_kernel(const __grid_constant__ NormForwardArgs p) {
-  __shared__ float slots[2][32];
+  __shared__ SumSlots slots[2];
   wait_for_earlier_kernels();
   let_later_kernels_begin();
   BlockSum sum{slots};
@@ -286,16 +366,13 @@ __global__ void __launch_bounds__(kWideThreads) forward_wide_kernel(const __grid
   const W *w = static_cast<const W*>(p.w), *b = static_cast<const W*>(p.b);
   float s = 0.0f;
   for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) s = __fadd_rn(s, get(x, c));
-  const float mean = __fmul_rn(sum(s), p.inv_cols);
-  s = 0.0f;
-  for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) {
-    const float d = __fsub_rn(get(x, c), mean);
-    s = __fmaf_rn(d, d, s);
-  }
-  const float rstd = 1.0f / sqrtf(__fmaf_rn(sum(s), p.inv_cols, p.eps));
-  if (threadIdx.x == 0 && p.mean) p.mean[blockIdx.x] = mean, p.rstd[blockIdx.x] = rstd;
+  Moments<X> m(sum(s), p);
+  float r = s = 0.0f;
+  for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) m.add(__fsub_rn(get(x, c), m.first), r, s);
+  m.finish(r, s, sum, p);
+  if (threadIdx.x == 0 && p.mean) p.mean[blockIdx.x] = m.mean, p.rstd[blockIdx.x] = m.rstd;
   for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads)
-    put(y, c, __fmaf_rn(__fmul_rn(__fsub_rn(get(x, c), mean), rstd), w ? get(w, c) : 1.0f, b ? get(b, c) : 0.0f));
+    put(y, c, __fmaf_rn(m.normal(__fsub_rn(get(x, c), m.first)), w ? get(w, c) : 1.0f, b ? get(b, c) : 0.0f));
 }
 
 // ---------------------------------------------------------------------------
@@ -414,7 +491,7 @@ __global__ void __launch_bounds__(E == 16 ? kMaxThreads : 256, ONE ? 2 : E == 8 
 // Rows of any width: dx, read twice.
 template <typename X, typename W>
 __global__ void __launch_bounds__(kWideThreads) backward_wide_kernel(const __grid_constant__ NormBackwardArgs p) {
-  __shared__ float slots[2][32];
+  __shared__ SumSlots slots[2];
   wait_for_earlier_kernels();
   let_later_kernels_begin();
   BlockSum sum{slots};
@@ -429,8 +506,9 @@ __global__ void __launch_bounds__(kWideThreads) backward_wide_kernel(const __gri
     s0 = __fadd_rn(s0, dn);
     s1 = __fmaf_rn(dn, n, s1);
   }
-  s0 = __fmul_rn(sum(s0), p.inv_cols);
-  s1 = __fmul_rn(sum(s1), p.inv_cols);
+  const float2 s = sum(s0, s1);
+  s0 = __fmul_rn(s.x, p.inv_cols);
+  s1 = __fmul_rn(s.y, p.inv_cols);
   for (int64_t c = threadIdx.x; c < p.cols; c += kWideThreads) {
     const float n = __fmul_rn(__fsub_rn(get(x, c), mean), rstd), dn = __fmul_rn(get(dy, c), w ? get(w, c) : 1.0f);
     put(dx, c, __fmul_rn(__fsub_rn(__fsub_rn(dn, s0), __fmul_rn(n, s1)), rstd));

@@ -15,7 +15,7 @@ struct NormForwardArgs {
   float* mean;    // rows each, or nullptr
   float* rstd;
   int64_t rows, cols, ldx, ldy;
-  float eps, inv_cols;
+  float eps, inv_cols, all_cols;  // 1 / cols and cols
   int32_t x_f32, w_f32;
 };
 
