@@ -753,7 +753,8 @@ typedef struct {
 /* y[t, i] = G sum over j of x[t, j] q[i, j] s[i, j], rounded once: x and y have
  * x_dtype (MPADAM_F32 or MPADAM_BF16) and row strides ldx >= cols and ldy >=
  * rows.  Products are exact and summed in binary32, in an order that depends on
- * the sizes and alignment alone.  cols a multiple of 32, codes 16-byte and
+ * the sizes and alignment alone; sums are held about as large as their results or
+ * smaller, and leave binary32's range where those do.  cols a multiple of 32, codes 16-byte and
  * scales 2-byte aligned take the tensor cores; else every product is one
  * multiply-add.  0 <= tokens <= 65536; made for few: the weight is read once
  * for every 8 to 32 tokens.  cols = 0 gives 0.  y must not overlap x.

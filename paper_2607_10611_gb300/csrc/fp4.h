@@ -17,6 +17,7 @@ struct Fp4Args {
   int32_t x_f32;
   int32_t vec_x;          // rows of x start on 16-byte boundaries (set by the launch, as the next)
   int32_t split;          // blocks of a cluster that share k
+  float up, out0, out1;   // of the scales, and of the sums
 };
 
 cudaError_t launch_fp4_linear(const Fp4Args& a, cudaStream_t stream);

@@ -1,9 +1,12 @@
 // fp4_linear.cu -- few tokens times a weight in NVFP4, as M+Adam's step leaves it:
 //   y[t, n] = G sum over k of x[t, k] q[n, k] s[n, k / 16]
 // with E2M1 codes q, E4M3 scales s per 16 consecutive weights and a binary32
-// scale G.  Sums are in binary32, one rounding follows.
+// scale G.  Sums are in binary32, one rounding follows.  Weights are q s 2^e, with
+// 2^e the power of two in G (within limits, see launch_fp4_linear): a sum is then
+// about as large as its result, and leaves binary32's range where that does.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "fp4.h"
 #include "launch.h"
@@ -49,12 +52,15 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
-// Two scales times 2^118, twice each: a weight is then q s 2^-8, which BF16 holds exactly.
+// y of a sum: times what G is of 2^e, in two factors of which one is a power of two.
+__device__ __forceinline__ float result_of(const Fp4Args& p, float sum) { return __fmul_rn(__fmul_rn(sum, p.out0), p.out1); }
+
+// Two scales times `up`, 2^(126 + e), twice each: a weight is then q s 2^e, which BF16 holds exactly.
 struct Scales {
   uint32_t s[2];
-  __device__ __forceinline__ explicit Scales(uint16_t codes) {
+  __device__ __forceinline__ Scales(uint16_t codes, float up) {
     const float2 v = scale_values(codes);
-    const float lo = __fmul_rn(v.x, 0x1p118f), hi = __fmul_rn(v.y, 0x1p118f);
+    const float lo = __fmul_rn(v.x, up), hi = __fmul_rn(v.y, up);
     s[0] = bf16x2_rn(lo, lo), s[1] = bf16x2_rn(hi, hi);
   }
 };
@@ -229,7 +235,7 @@ __global__ void __launch_bounds__(kFp4Threads, BLOCKS) fp4_kernel(const __grid_c
     if (panel + 1 < last) fetch(panel + 1);
 #pragma unroll
     for (int c = 0; c < kOwn; ++c) {
-      const Scales scale[2] = {Scales(now[c].s[0]), Scales(now[c].s[1])};
+      const Scales scale[2] = {Scales(now[c].s[0], p.up), Scales(now[c].s[1], p.up)};
       const uint8_t* from = buffer + g * kStride + (c * kShares + share) * (2 * kChunk) + l * 16;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -265,7 +271,7 @@ __global__ void __launch_bounds__(kFp4Threads, BLOCKS) fp4_kernel(const __grid_c
   };
   auto finish = [&](int i, float s) {
     const int64_t row = block_row + i % (16 * ROWS);
-    if (row < p.rows) put(static_cast<X*>(p.y), (token0 + i / (16 * ROWS)) * p.ldy + row, __fmul_rn(__fmul_rn(s, 256.0f), p.global_scale));
+    if (row < p.rows) put(static_cast<X*>(p.y), (token0 + i / (16 * ROWS)) * p.ldy + row, result_of(p, s));
   };
   const int results = tokens * 16 * ROWS;
   if (p.split == 1) {
@@ -341,7 +347,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewBlocks) fp4_few_kernel(con
 #pragma unroll
         for (int i = 0; i < 4; ++i) b[i] = make_uint4(0, 0, 0, 0);
       }
-      const Scales scale[2] = {Scales(s[d][0]), Scales(s[d][1])};
+      const Scales scale[2] = {Scales(s[d][0], p.up), Scales(s[d][1], p.up)};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t a0[4], a1[4];
@@ -375,7 +381,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, kFewBlocks) fp4_few_kernel(con
     cluster_sync();  // nobody leaves while its sums are read
   }
   if (out)
-    put(static_cast<uint16_t*>(p.y), (token0 + i / 16) * p.ldy + block_row + i % 16, __fmul_rn(__fmul_rn(sum, 256.0f), p.global_scale));
+    put(static_cast<uint16_t*>(p.y), (token0 + i / 16) * p.ldy + block_row + i % 16, result_of(p, sum));
 }
 
 // Any number of columns and any alignment: a warp takes a row and four tokens.
@@ -392,8 +398,8 @@ __global__ void __launch_bounds__(kFp4Threads) fp4_any_kernel(const __grid_const
   for (int64_t k = lane; k < p.cols; k += 32) {
     const int64_t at = row * p.cols + k;
     const uint32_t code = p.codes[at >> 1] >> 4 * (at & 1) & 15u;
-    const float q = __fmul_rn(__uint_as_float((code & 8u) << 28 | (code & 7u) << 22), 0x1p126f);
-    const float w = __fmul_rn(q, scale_values(p.scales[at >> 4]).x);
+    const float q = __uint_as_float((code & 8u) << 28 | (code & 7u) << 22);  // times 2^-126
+    const float w = __fmul_rn(q, __fmul_rn(scale_values(p.scales[at >> 4]).x, p.up));
 #pragma unroll
     for (int t = 0; t < kAnyTokens; ++t)
       if (token0 + t < p.tokens) acc[t] = __fmaf_rn(get(x, (token0 + t) * p.ldx + k), w, acc[t]);
@@ -403,7 +409,7 @@ __global__ void __launch_bounds__(kFp4Threads) fp4_any_kernel(const __grid_const
 #pragma unroll
     for (int d = 16; d; d >>= 1) acc[t] = __fadd_rn(acc[t], __shfl_xor_sync(~0u, acc[t], d));
     if (lane == 0 && token0 + t < p.tokens)
-      put(static_cast<X*>(p.y), (token0 + t) * p.ldy + row, __fmul_rn(acc[t], p.global_scale));
+      put(static_cast<X*>(p.y), (token0 + t) * p.ldy + row, result_of(p, acc[t]));
   }
 }
 
@@ -435,6 +441,15 @@ cudaError_t launch_few(Fp4Args a, cudaStream_t stream) {
 
 cudaError_t launch_fp4_linear(const Fp4Args& args, cudaStream_t stream) {
   Fp4Args a = args;
+  // e in [-44, -8]: up times the largest scale, 448, stays in range; with e = -44 no sum leaves it (weights are below 2^12, x
+  // below 2^128, k below 2^31).  G above 2^-8 makes results larger than their sums, so those need no more room.  The factors: 1
+  // and G / 2^e, or, where that might be out of range, 2^-e and G.
+  int e = 0;
+  std::frexp(a.global_scale, &e);
+  e = std::min(std::max(e - 1, -44), -8);
+  a.up = std::ldexp(1.0f, 126 + e);
+  a.out0 = a.global_scale < 1.0f ? 1.0f : std::ldexp(1.0f, -e);
+  a.out1 = a.global_scale < 1.0f ? std::ldexp(a.global_scale, -e) : a.global_scale;
   const int64_t xs = a.x_f32 ? 4 : 2;
   a.vec_x = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.tokens == 1 || a.ldx * xs % 16 == 0);
   // Rows of codes and scales start on 16- and 2-byte boundaries, and whole groups make up a row.
