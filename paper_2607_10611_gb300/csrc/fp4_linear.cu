@@ -149,16 +149,15 @@ constexpr int fp4_smem(int tiles, int rows) {
   return std::max(2 * Staged<X>::kParts * 8 * tiles * (2 * fp4_panel(rows) + 64), (kWarps + rows) * 8 * tiles * 16 * 4);
 }
 
-// A block takes 16 ROWS rows of the weight and 8 TILES tokens, of which up to
-// STAGED are there; its warps are ROWS groups of 16 rows times kWarps / ROWS shares
-// of k, chunks in turn, joined in order through shared memory at the end.  Where
-// that makes too few blocks, a cluster of them takes a run of k's panels each, and
+// A block takes 16 ROWS rows of the weight and 8 TILES tokens; its warps are ROWS
+// groups of 16 rows times kWarps / ROWS shares of k, chunks in turn, joined in
+// order through shared memory at the end.  Where that makes too few blocks, a cluster of them takes a run of k's panels each, and
 // their sums are joined in order through the cluster's shared memory.  Weights go
 // from memory to registers, a panel of k ahead; x goes through shared memory, where
 // a lane's 32 values of a chunk lie as four times 16 bytes, those of the four lanes
 // of a row next to one another.  Within a chunk the order of k is the lanes': lane l
 // of four takes values 32 l to 32 l + 31, four to each product of 16.
-template <typename X, int TILES, int ROWS, int STAGED, int BLOCKS>
+template <typename X, int TILES, int ROWS, int BLOCKS>
 __global__ void __launch_bounds__(kFp4Threads, BLOCKS) fp4_kernel(const __grid_constant__ Fp4Args p) {
   constexpr int kShares = kWarps / ROWS, kParts = Staged<X>::kParts;
   constexpr int kOwn = 2;                             // chunks of a warp in a panel
@@ -167,8 +166,8 @@ __global__ void __launch_bounds__(kFp4Threads, BLOCKS) fp4_kernel(const __grid_c
   constexpr int kTokens = 8 * TILES;
   constexpr int kStride = kPanel * 2 + 64;            // bytes of a token in a panel; the 64 keep neighbours off each other's banks
   constexpr int kPartBytes = kTokens * kStride, kBufferBytes = kParts * kPartBytes;
-  constexpr int kPieces = STAGED * kPanel / 8 / kFp4Threads;  // of 8 values, a thread's share of a panel
-  static_assert(STAGED <= kTokens && STAGED * kPanel % (8 * kFp4Threads) == 0, "whole shares");
+  constexpr int kPieces = kTokens * kPanel / 8 / kFp4Threads;  // of 8 values, a thread's share of a panel
+  static_assert(kTokens * kPanel % (8 * kFp4Threads) == 0, "whole shares");
   extern __shared__ uint4 smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem_raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, l = lane & 3;
@@ -178,12 +177,6 @@ __global__ void __launch_bounds__(kFp4Threads, BLOCKS) fp4_kernel(const __grid_c
   const int64_t token0 = (int64_t)blockIdx.y * kTokens;
   const int tokens = (int)(p.tokens - token0 < kTokens ? p.tokens - token0 : kTokens);
   const int64_t rows[2] = {min(row0 + g, p.rows - 1), min(row0 + g + 8, p.rows - 1)};
-  if (STAGED < kTokens) {  // the tokens that are never there
-    for (int i = threadIdx.x; i < 2 * kParts * (kTokens - STAGED) * (kStride / 16); i += kFp4Threads) {
-      const int part = i / ((kTokens - STAGED) * (kStride / 16)), in = i % ((kTokens - STAGED) * (kStride / 16));
-      smem_raw[(part * kPartBytes + STAGED * kStride) / 16 + in] = make_uint4(0, 0, 0, 0);
-    }
-  }
   wait_for_earlier_kernels();
   let_later_kernels_begin();
 
@@ -413,10 +406,10 @@ __global__ void __launch_bounds__(kFp4Threads) fp4_any_kernel(const __grid_const
   }
 }
 
-template <typename X, int TILES, int ROWS, int STAGED, int BLOCKS>
+template <typename X, int TILES, int ROWS, int BLOCKS>
 cudaError_t launch(Fp4Args a, cudaStream_t stream) {
   constexpr int kSmem = fp4_smem<X>(TILES, ROWS), kTokens = 8 * TILES;
-  const void* kernel = (const void*)fp4_kernel<X, TILES, ROWS, STAGED, BLOCKS>;
+  const void* kernel = (const void*)fp4_kernel<X, TILES, ROWS, BLOCKS>;
   if (kSmem > 48 * 1024) {
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = allow_smem(kernel, kSmem, ready);
@@ -459,11 +452,11 @@ cudaError_t launch_fp4_linear(const Fp4Args& args, cudaStream_t stream) {
     return a.x_f32 ? launch_dependent((const void*)fp4_any_kernel<float>, grid, kFp4Threads, 0, 0, &a, stream)
                    : launch_dependent((const void*)fp4_any_kernel<uint16_t>, grid, kFp4Threads, 0, 0, &a, stream);
   }
-  if (a.x_f32) return launch<float, 1, 2, 8, 2>(a, stream);
+  if (a.x_f32) return launch<float, 1, 2, 2>(a, stream);
   if (a.tokens <= 8) return launch_few(a, stream);
-  if (a.tokens <= 16) return launch<uint16_t, 2, 4, 16, 2>(a, stream);
-  if (a.tokens <= 24) return launch<uint16_t, 3, 4, 24, 2>(a, stream);
-  return launch<uint16_t, 4, 4, 32, 2>(a, stream);
+  if (a.tokens <= 16) return launch<uint16_t, 2, 4, 2>(a, stream);
+  if (a.tokens <= 24) return launch<uint16_t, 3, 4, 2>(a, stream);
+  return launch<uint16_t, 4, 4, 2>(a, stream);
 }
 
 }  // namespace mpadam
