@@ -225,6 +225,7 @@ __global__ void __launch_bounds__(kMatmulThreads, 2) matmul_kernel(const __grid_
     }
     if (at == k1) {
       if (issue) mma_commit(acc_full);
+      warp_wait(acc_full, 0);  // whether or not the epilogue does: the products' memory goes when this warp has left
     } else {
       // The products and copies in flight, before their memory goes (once the products are done, the producer fills every
       // stage again); then the epilogue is woken up to find that it has nothing to store.
@@ -505,13 +506,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
       if (issue) pair_commit(acc_full(acc));
       if (++acc == S::kAccs) { acc = 0; acc_phase ^= 1; }
     }
+    if (issue) {
+      if (at < steps) atomicOr(p.err, kErrCopy);
+      pair_commit(drained);
+    }
+    warp_wait(drained, 0);  // in any case, as in matmul_kernel
     if (at < steps) {
-      // As in matmul_kernel, for both CTAs: their copies arrive here.
-      if (issue) {
-        atomicOr(p.err, kErrCopy);
-        pair_commit(drained);
-      }
-      warp_wait(drained, 0);
+      // As there, for both CTAs: their copies arrive here.
       const int64_t left = (int64_t)((tiles - 1 - t) / pairs) * steps + steps - at;
       for (int i = 0; i < (int)min(left, (int64_t)kPairStages); ++i) {
         warp_wait(full(s), phase);
@@ -584,6 +585,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads, 1)
   tc_fence_before();
   __syncthreads();
   cluster_sync();
+  if (warp == 1 && rank) mbar_wait(drained, 0);  // (the other CTA has; this one's barrier is told of it too)
   tc_fence_after();
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
