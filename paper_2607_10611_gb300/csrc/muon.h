@@ -48,11 +48,21 @@ struct alignas(128) NewtonMatrix {
   int32_t row0;        // its first counter: one for every 256 rows
 };
 
-// Its maps, and those of a list of matrices by their number.
+// Its maps by their number.
 constexpr int kNewtonMaps = 13;
 static_assert(offsetof(NewtonMatrix, hi) == kNewtonMaps * sizeof(CUtensorMap), "nothing but maps before X's pointers");
-__host__ __device__ inline const CUtensorMap* newton_map(const NewtonMatrix* matrices, int64_t i) {
-  return reinterpret_cast<const CUtensorMap*>(matrices + i / kNewtonMaps) + i % kNewtonMaps;
+__host__ __device__ inline const CUtensorMap* newton_map(const NewtonMatrix* q, int i) {
+  return reinterpret_cast<const CUtensorMap*>(q) + i;
+}
+
+// Those that a tile of product `which` (1, 2, 3) copies by, where the step reads X `from`: operands as they lie and turned, the
+// result, X's or A's part that is added to it (X's second part is stored too); fewer than kTileMaps come twice.
+constexpr int kTileMaps = 5;
+__host__ __device__ inline int tile_map(int which, int from, int i) {
+  constexpr int kX = 0, kA = 2, kB = 3, kXAlong = 4, kAAlong = 6, kBAlong = 7, kXPatch = 8, kLoPatch = 10, kAPatch = 11, kBPatch = 12;
+  if (which == 1) return i == 0 ? kX + from : kAPatch;
+  if (which == 2) return i == 0 ? kA : i == 1 ? kAAlong : i == 2 ? kBPatch : kAPatch;
+  return i == 0 ? kB : i == 1 ? kBAlong : i == 2 ? kXAlong + from : i == 3 ? kXPatch + (from ^ 1) : kLoPatch;
 }
 
 // A tile of a product: rows 256 tm and columns 256 tn of its result.
@@ -93,7 +103,7 @@ __host__ __device__ inline PairStep pair_step(int step, int asked0, int asked1) 
 
 struct ProductArgs {
   const NewtonMatrix* matrices;  // the list's
-  int32_t first, members;        // those that the tiles belong to
+  int32_t first;                 // the first one that the tiles belong to
   const NewtonTile* tiles;
   int32_t count;
   uint32_t* progress;  // of every 256 rows; 0 when the launch begins, and so is

@@ -29,7 +29,7 @@ struct Matrix {
 // Matrices whose products run together, and where their entries in the tables begin.
 struct Group {
   int64_t chunk_owner = 0, tile_owner = 0, product = 0;
-  int32_t first = 0, members = 0, chunks = 0, tiles = 0, product_tiles = 0;
+  int32_t first = 0, chunks = 0, tiles = 0, product_tiles = 0;
 };
 
 int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
@@ -131,7 +131,7 @@ struct Newton {
     }
     for (const auto& member : members) {
       Group g;
-      g.first = member.first, g.members = member.second - member.first;
+      g.first = member.first;
       g.chunk_owner = (int64_t)owners.size();
       for (int32_t k = member.first; k < member.second; ++k) {
         matrices[k].chunk0 = (int64_t)owners.size() - g.chunk_owner;
@@ -231,8 +231,7 @@ struct Newton {
       args.owner = d_owners + g.tile_owner;
       args.count = g.tiles;
       if (e == cudaSuccess) e = launch_begin(args, kind, stream);
-      const ProductArgs p{d_newton,      g.first, g.members, d_tiles + g.product, g.product_tiles, args.progress, args.progress + args.counters - 1,
-                          args.err};
+      const ProductArgs p{d_newton, g.first, d_tiles + g.product, g.product_tiles, args.progress, args.progress + args.counters - 1, args.err};
       if (e == cudaSuccess) e = launch_products(p, stream);
       if (e == cudaSuccess) e = launch_finish(args, kind, stream);
       if (e != cudaSuccess) return cuda_fail(e, "launch of the Newton-Schulz steps");

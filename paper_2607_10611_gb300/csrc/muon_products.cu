@@ -43,9 +43,9 @@ constexpr int kPatches = 2;                     // of a warp, in a tile
 constexpr int kEpiBytes = kPatches * kPatchBytes;
 static_assert(64 * kPatches * 2 == kNewtonTile, "two warps side by side");
 constexpr int kDynSmem = kStages * kStageBytes + kEpiWarps * kEpiBytes + 1024;
-constexpr int kProductThreads = 32 * (4 + kEpiWarps);  // producer, issuer, the one who takes tiles, an idle one, then the epilogue
+constexpr int kProductThreads = 32 * (4 + kEpiWarps);  // producer, issuer, the one who takes tiles, their maps', then the epilogue
 constexpr int kSlots = 3;                       // tiles that a pair has taken ahead of its epilogue
-constexpr int kReaders = 2 * kEpiWarps + 3;     // of a slot: epilogue warps and a producer in both CTAs, the issuer
+constexpr int kReaders = 2 * kEpiWarps + 5;     // of a slot: epilogue warps, a producer and the maps' warp in both CTAs, the issuer
 
 enum ProductError : int32_t { kErrCopy = 1, kErrStage = 2, kErrAcc = 4, kErrSlot = 8, kErrTurn = 16 };
 
@@ -150,7 +150,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   const uint32_t drained = bar0 + 8u * (2 * kStages + 4);
   auto slot_full = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + s); };           // each CTA's own
   auto slot_free = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + kSlots + s); };  // the leader's alone
-  auto slot_ready = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + 2 * kSlots + s); };  // each CTA's own: its tile's rows are there
+  auto slot_ready = [&](int s) { return bar0 + 8u * (2 * kStages + 5 + 2 * kSlots + s); };  // each CTA's own: rows and maps are there
   auto addend_full = [&](int w) { return bar0 + 8u * (2 * kStages + 5 + 3 * kSlots + w); };
 
   if (threadIdx.x == 0) {
@@ -166,7 +166,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(slot_full(s), 1);
       mbar_init(slot_free(s), kReaders);
-      mbar_init(slot_ready(s), 1);
+      mbar_init(slot_ready(s), 2);
     }
     for (int w = 0; w < kEpiWarps; ++w) mbar_init(addend_full(w), 1);
     failed = asked[0] = asked[1] = 0;
@@ -177,9 +177,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  // The maps' memory may have held another list's (one that was destroyed, whose memory this one got): each block acquires all
-  // that it may use, its threads a share each, before any of them is used.  The host's copy was complete before the launch.
-  for (int64_t i = threadIdx.x; i < (int64_t)kNewtonMaps * p.members; i += kProductThreads) acquire_map(newton_map(p.matrices + p.first, i));
   tc_fence_before();
   __syncthreads();
   cluster_sync();
@@ -213,20 +210,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
   auto tile_of = [](int4 v) {
     return NewtonTile{v.x, (uint16_t)v.y, (uint16_t)((uint32_t)v.y >> 16), v.z, (uint32_t)v.w};
   };
-  // The pair's n-th tile; matrix < 0: there are no more.  By whole warps, or by one lane (whole = false).
-  // `early` sees the tile before its turn.
-  auto read_slot = [&](int n, NewtonTile& t, bool whole, auto early) {
-    const int s = n % kSlots;
-    const uint32_t parity = (uint32_t)(n / kSlots) & 1;
-    bool ok = wait_cluster(slot_full(s), parity);
-    if (whole) ok = __all_sync(~0u, ok);
-    if (!ok) return false;
+  auto tile_in = [&](int s) {
     const volatile int4& v = slots[s];
-    t = tile_of(make_int4(v.x, v.y, v.z, v.w));
-    early();
-    ok = wait_cluster(slot_ready(s), parity);
+    return tile_of(make_int4(v.x, v.y, v.z, v.w));
+  };
+  // The pair's n-th tile, when its turn has come; matrix < 0: there are no more.  By whole warps, or by one lane (whole = false).
+  auto read_slot = [&](int n, NewtonTile& t, bool whole) {
+    const int s = n % kSlots;
+    bool ok = wait_cluster(slot_ready(s), (uint32_t)(n / kSlots) & 1);
     if (whole) ok = __all_sync(~0u, ok);
     if (!ok) return false;
+    t = tile_in(s);
     if (!whole || lane == 0) mbar_arrive_cluster(peer_addr(slot_free(s), 0));
     return true;
   };
@@ -253,18 +247,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
       bool ok = true;
       for (int n = 0; ok; ++n) {
         NewtonTile t;
-        const bool there = read_slot(n, t, false, [&] {  // (a map that this SM has not seen takes half a microsecond)
-          if (t.matrix < 0) return;
-          const NewtonMatrix& q = p.matrices[t.matrix];
-          if (t.which() == 1) {
-            prefetch_map(&q.x[t.from()]);
-          } else {
-            prefetch_map(t.which() == 2 ? &q.a : &q.b);
-            prefetch_map(t.which() == 2 ? &q.a_along : &q.b_along);
-            if (t.which() == 3) prefetch_map(&q.x_along[t.from()]);
-          }
-        });
-        if (!there) { give_up(kErrSlot); ok = false; break; }
+        if (!read_slot(n, t, false)) { give_up(kErrSlot); ok = false; break; }
         if (t.matrix < 0) break;
         const NewtonMatrix& q = p.matrices[t.matrix];
         const int which = t.which(), from = t.from(), steps = t.steps_k();
@@ -324,6 +307,48 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
         if (!more) break;
       }
     }
+  } else if (warp == 3) {
+    // A tile's tensor maps, before its turn.  They lie in memory that the host filled (its copy was complete before the launch),
+    // where another list's may have lain that this SM still holds: a block acquires those of a matrix's product when it first
+    // comes to a tile of it, then fetches them, since one that the SM does not hold costs half a microsecond.  Acquiring takes
+    // 20 ns a map: 200 matrices of 256 x 256 take 290 us, with all maps of a matrix at once 313, with all of the list's as a
+    // block begins 320 (1000 of 64 x 64 650 and 900).
+    // What was acquired last, a lane's share each: of the products whose numbers are the same modulo kMet the last one.
+    constexpr int kMet = 8 * 32;
+    int32_t met[kMet / 32];
+#pragma unroll
+    for (int i = 0; i < kMet / 32; ++i) met[i] = -1;
+    for (int n = 0;; ++n) {
+      const int s = n % kSlots;
+      if (!__all_sync(~0u, wait_cluster(slot_full(s), (uint32_t)(n / kSlots) & 1))) {
+        if (lane == 0) give_up(kErrSlot);
+        break;
+      }
+      const NewtonTile t = tile_in(s);
+      if (t.matrix >= 0) {
+        const int32_t key = (t.matrix - p.first) * 5 + (t.which() == 2 ? 4 : t.which() - 1 + t.from());  // (B reads no X)
+        const int owner = key % 32, at = key % kMet / 32;
+        int32_t last = -1;
+#pragma unroll
+        for (int i = 0; i < kMet / 32; ++i)
+          if (i == at) last = met[i];
+        const bool known = __shfl_sync(~0u, last, owner) == key;
+        if (lane < kTileMaps) {
+          const CUtensorMap* map = newton_map(p.matrices + t.matrix, tile_map(t.which(), t.from(), lane));
+          if (!known) acquire_map(map);
+          prefetch_map(map);
+        }
+#pragma unroll
+        for (int i = 0; i < kMet / 32; ++i)
+          if (i == at && lane == owner) met[i] = key;
+      }
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive_cluster(peer_addr(slot_ready(s), rank));
+        mbar_arrive_cluster(peer_addr(slot_free(s), 0));
+      }
+      if (t.matrix < 0) break;
+    }
   } else if (warp == 1 && rank == 0) {
     const bool issue = elected();
     // FP16 operands, binary32 sums, 256 x 256
@@ -333,7 +358,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     bool ok = true;
     for (int n = 0; ok; ++n) {
       NewtonTile t;
-      if (!read_slot(n, t, true, [] {})) { ok = false; break; }
+      if (!read_slot(n, t, true)) { ok = false; break; }
       if (t.matrix < 0) break;
       const int steps = t.steps_k();
       if (!__all_sync(~0u, wait_cluster(acc_free(acc), acc_phase ^ 1))) { ok = false; break; }
@@ -371,13 +396,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) 
     uint32_t acc_phase = 0, addend_phase = 0;
     for (int at = 0;; ++at) {
       NewtonTile t;
-      const bool there = read_slot(at, t, true, [&] {
-        if (t.matrix < 0 || lane) return;
-        const NewtonMatrix& q = p.matrices[t.matrix];
-        prefetch_map(t.which() == 1 ? &q.a_patch : t.which() == 2 ? &q.b_patch : &q.x_patch[t.from() ^ 1]);
-        if (t.adds()) prefetch_map(t.which() == 2 ? &q.a_patch : &q.lo_patch);
-      });
-      if (!there) { if (lane == 0) give_up(kErrSlot); break; }
+      if (!read_slot(at, t, true)) { if (lane == 0) give_up(kErrSlot); break; }
       if (t.matrix < 0) break;
       const NewtonMatrix& q = p.matrices[t.matrix];
       const int from = t.from();

@@ -10,7 +10,7 @@ import torch
 
 pytestmark = pytest.mark.gpu
 
-PRODUCER, ISSUER, TAKER, EPILOGUE = 0, 1, 2, 4  # warps; the epilogue's are 4 to 11
+PRODUCER, ISSUER, TAKER, MAPS, EPILOGUE = 0, 1, 2, 3, 4  # warps; the epilogue's are 4 to 11
 SHAPES = [(1500, 1600), (300, 300), (1000, 520)]
 
 
@@ -33,7 +33,7 @@ def probe(tmp_path_factory):
     return lib
 
 
-@pytest.mark.parametrize("block,warp", [(0, TAKER), (2, TAKER), (0, ISSUER), (6, ISSUER), (0, PRODUCER), (1, PRODUCER), (7, PRODUCER),
+@pytest.mark.parametrize("block,warp", [(0, TAKER), (2, TAKER), (0, MAPS), (3, MAPS), (0, ISSUER), (6, ISSUER), (0, PRODUCER), (1, PRODUCER), (7, PRODUCER),
                                         (0, EPILOGUE), (1, EPILOGUE + 5), (4, EPILOGUE + 7)])
 def test_a_wait_that_runs_out_ends_the_launch(probe, block, warp):
     x = [torch.randn(s, device="cuda", generator=torch.Generator(device="cuda").manual_seed(i)) for i, s in enumerate(SHAPES)]
