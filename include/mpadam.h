@@ -684,12 +684,15 @@ int32_t mpadam_e4m3_status(struct CUstream_st* stream, int32_t* code);
  *   dw = sum over rows of dy n,  db = sum over rows of dy
  * The order of every sum depends on the sizes and on 16-byte alignment alone:
  * the same call gives the same bits.  A row whose sums or squared deviations
- * pass binary32's range gives what binary32 makes of it.  Rows of up to 8192 values are read from
- * memory once; wider ones are right, and read two or three times.  Rows of x,
- * y, dy, dx on 16-byte boundaries with whole 16 bytes of values take the
- * vectorised path.  x and y have x_dtype (MPADAM_F32 or MPADAM_BF16), and so
- * have dy and dx; w, b, dw and db have w_dtype, binary32 or x's.  Row strides are in
- * elements, >= cols.  rows, cols < 2^31.  Outputs must not overlap inputs.
+ * pass binary32's range gives what binary32 makes of it.  A mean far from 0 is
+ * taken off to its last bit: y is off by roundings of the deviations' size, and
+ * the gradients by what the mean's own rounding, as it is stored, makes of them.
+ * Rows of up to 8192 values are read from memory once; wider ones are right, and
+ * read two or three times.  Rows of x, y, dy, dx on 16-byte boundaries with whole
+ * 16 bytes of values take the vectorised path.  x and y have x_dtype (MPADAM_F32
+ * or MPADAM_BF16), and so have dy and dx; w, b, dw and db have w_dtype, binary32
+ * or x's.  Row strides are in elements, >= cols.  rows, cols < 2^31.  Outputs must
+ * not overlap inputs.
  * ------------------------------------------------------------------------ */
 typedef struct {
   const void* x;
@@ -776,9 +779,9 @@ int32_t mpadam_nvfp4_linear(const void* x, int32_t x_dtype, int64_t tokens, int6
  * small.  Products are of FP16 values, summed in binary32 on the tensor cores: X
  * is held as the sum of two FP16 values, of which products take the first, A and
  * B as one, all times 2^14.  The error of the result, relative in the 2-norm, is
- * about 1.4e-3 for a random matrix and less for one that a few directions
- * dominate.  A matrix with a value that is not finite gives NaN.  The same call
- * gives the same bits.
+ * about 1.4e-3 for a random matrix (3e-3 for a small one) and less for one that a
+ * few directions dominate; a binary32 result is no nearer.  A matrix with a value
+ * that is not finite gives NaN.  The same call gives the same bits.
  * ------------------------------------------------------------------------ */
 typedef struct mpadam_orthogonal_state mpadam_orthogonal_state;
 
@@ -792,7 +795,7 @@ int32_t mpadam_orthogonal_create(const int64_t* rows, const int64_t* cols, int32
                                  mpadam_orthogonal_state** out);
 
 /* out[k] = x[k] orthogonalised, rounded to the nearest; x, out: host arrays of n
- * device pointers; out[k] may be x[k], and must not overlap another x.
+ * device pointers; out[k] may be x[k], and must not overlap another x or out.
  * Asynchronous on `stream`; four launches for as many matrices as share the
  * workspace.  Calls with one state must not overlap on the device, replayed ones
  * among them: they share its workspace and counters (a call that finds these
@@ -823,8 +826,8 @@ typedef enum { MPADAM_SCALE_RMS = 0, MPADAM_SCALE_SPECTRAL = 1 } mpadam_muon_sca
 
 /* One matrix: w has the config's weight_dtype, m its momentum_dtype; compute:
  * optional BF16 copy of binary32 weights (nearest), overwritten every step, or
- * NULL.  Contiguous, aligned to the element size; where all are 16-byte aligned
- * and cols is a multiple of 8, accesses are vectors. */
+ * NULL.  Contiguous, aligned to the element size, none overlapping another; where
+ * all are 16-byte aligned and cols is a multiple of 8, accesses are vectors. */
 typedef struct {
   void* w;
   void* m;

@@ -285,7 +285,11 @@ __global__ void __launch_bounds__(kFp4Threads, BLOCKS) fp4_kernel(const __grid_c
 
 // At most 8 tokens in BF16: nothing is staged and no warp waits for another before
 // the end.  A block takes 16 rows, its warps (and those of its cluster) chunks of k
-// in turn, kFewAhead of them on their way; x comes straight from L1.
+// in turn, kFewAhead of them on their way; x comes straight from L1.  One token
+// through 11008 x 4096 takes 14.3 us out of memory, 11.0 where the weight lies in L2.
+// For a third of that no block has begun or all have ended; the rest is a wave of
+// blocks whose warps wait for their first codes (31 % of their time), then share the
+// issue slots (used in 58 % of the cycles) for the codes' expansion.
 constexpr int kFewWarps = 4, kFewAhead = 4, kFewBlocks = 5;
 __global__ void __launch_bounds__(32 * kFewWarps, kFewBlocks) fp4_few_kernel(const __grid_constant__ Fp4Args p) {
   constexpr int kTokens = 8;

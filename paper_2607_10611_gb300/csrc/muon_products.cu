@@ -124,14 +124,14 @@ __device__ __forceinline__ void fence_copies_global() { asm volatile("fence.prox
 // memory's bandwidth is what this competes for: the products read 64 bytes a cycle
 // of it and the operands' copies write as many.  A row a lane straight from and to
 // memory (a line of L1 for 16 bytes), and results stored turned as well, took 8 us of
-// a warp's time a tile; this takes 3, and half of GPT-2's hidden matrices 800 us
-// instead of 1080.
+// a warp's time a tile; this takes 3, and a Muon step of half of GPT-2's hidden
+// matrices 770 us, where it took 1087.
 // One lane of the pair takes tiles and waits for their rows, so that nobody else has
 // to look.
 // Within a tile 64 values of k take 526 (A, B) to 565 cycles (X) at 4096 x 11008, of
 // which the products are 512; in half of GPT-2's hidden matrices 590 to 670, with an
-// epilogue every twelve of them.  4096 x 11008 takes 1.85 ms after a pause (1.69 PFLOP/s), in a long run, where the
-// power limit lowers the clock, 2.13.
+// epilogue every twelve of them.  The kernel takes 1.85 ms for 4096 x 11008 after a
+// pause (1.69 PFLOP/s), 2.1 in a long run, where the power limit lowers the clock.
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) newton_kernel(const __grid_constant__ ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ alignas(8) uint64_t bars[2 * kStages + 5 + 3 * kSlots + kEpiWarps];

@@ -29,8 +29,8 @@ inline int64_t newton_tiles(int which, int32_t r, int32_t c) {
 inline void newton_schedule(const std::vector<NewtonMatrix>& matrices, int32_t first, int32_t last, int32_t newton_steps, int pairs,
                             std::vector<NewtonTile>* tiles) {
   // Of a tile, in steps of k: until its pair is free, and until its result can be used.  The second is more than the tile's own
-  // way (about 20 steps): pairs take tiles ahead.  With 20, a 1.5B-width layer takes 1560 us, with 72 1485, with 96 1500; half of
-  // GPT-2's matrices 790, 795, 800.
+  // way (about 20 steps): pairs take tiles ahead.  A Muon step of a 1.5B-width layer takes 1690 us with 20 (in a long run), 1640 to
+  // 1665 with 48, 72 and 96; half of GPT-2's matrices and 4096 x 11008 alone the same with all of them.
   constexpr int64_t kBetween = 1, kLatency = 72;
   struct Tile {
     int64_t way;     // of the matrix from this product on

@@ -16,8 +16,9 @@ _TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 class Orthogonalizer:
     """Matrices of the given shapes, float32 or bfloat16, each by `steps` Newton-Schulz steps nearly its polar factor: its
-    singular values come to lie around 1, its singular vectors stay.  The workspace is the object's, so calls on several
-    streams have to be ordered."""
+    singular values come to lie around 1, its singular vectors stay.  Products are of FP16 values, so that a result, float32 or
+    bfloat16, is good to about 1.4e-3 of itself (2-norm).  The workspace is the object's, so calls on several streams have to be
+    ordered."""
 
     def __init__(self, shapes: Sequence[Tuple[int, int]], dtype: str = "bf16", steps: int = 5,
                  device: Optional[torch.device] = None):
@@ -33,7 +34,7 @@ class Orthogonalizer:
 
     def __call__(self, x: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None,
                  stream: Optional[torch.cuda.Stream] = None) -> List[torch.Tensor]:
-        """The orthogonalised matrices, asynchronously: new ones, or written to `out` (entries may be x's own)."""
+        """The orthogonalised matrices, asynchronously: new ones, or written to `out` (entries may be x's own, but none another's)."""
         if stream is None:
             return self._run(self.state, self._spec, x, out, None)
         with torch.cuda.stream(stream):  # so that new results belong to it
@@ -68,7 +69,8 @@ class Muon:
     (binary32 ones need none).  compute: with binary32 weights, BF16 matrices that
     every step overwrites with the rounded weights (entries may be None).  The
     tensors' memory has to stay where it is; the object keeps references to them,
-    and a workspace, so calls on several streams have to be ordered.  Vectors,
+    and a workspace, so calls on several streams have to be ordered.  An update is
+    good to about 1.4e-3 of itself, as Orthogonalizer's results are.  Vectors,
     embeddings and the head are AdamW's.
     """
 
