@@ -853,8 +853,8 @@ typedef struct {
 
 typedef struct mpadam_muon_state mpadam_muon_state;
 
-/* Copies the list, validates, allocates and uploads as mpadam_orthogonal_create
- * does.  Errors: EINVAL, EALLOC, ECUDA, EUNSUPPORTED.  On error *out is NULL. */
+/* Copies the list, validates (arrays that overlap are refused), allocates and
+ * uploads as mpadam_orthogonal_create does.  Errors: EINVAL, EALLOC, ECUDA, EUNSUPPORTED.  On error *out is NULL. */
 int32_t mpadam_muon_create(const mpadam_muon_tensor* tensors, int32_t n, const mpadam_muon_config* cfg, mpadam_muon_state** out);
 
 /* Step t (>= 1, for the random lanes) with learning rate lr (finite, >= 0) over

@@ -262,6 +262,22 @@ int32_t check_side(int32_t k, int64_t rows, int64_t cols) {
   return MPADAM_OK;
 }
 
+// Whether a step would write two of the list's arrays to the same memory.
+bool any_overlap(const std::vector<Matrix>& list, size_t wsz, size_t msz) {
+  std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+  for (const Matrix& x : list) {
+    const size_t count = (size_t)x.rows * (size_t)x.cols;
+    auto add = [&](const void* p, size_t size) {
+      if (p && count) spans.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + count * size});
+    };
+    add(x.w, wsz), add(x.m, msz), add(x.compute, 2);
+  }
+  std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if (spans[i].first < spans[i - 1].second) return true;
+  return false;
+}
+
 }  // namespace
 
 struct mpadam_orthogonal_state {
@@ -363,6 +379,7 @@ extern "C" int32_t mpadam_muon_create(const mpadam_muon_tensor* tensors, int32_t
       if (!is_aligned(t.w, wsz) || !is_aligned(t.m, msz) || !is_aligned(t.compute, 2))
         return fail(MPADAM_EINVAL, "matrix %d: a pointer is not aligned to its element size", k);
     }
+    if (any_overlap(list, wsz, msz)) return fail(MPADAM_EINVAL, "weights, momentum and compute copies must not overlap");
     std::unique_ptr<mpadam_muon_state> s(new mpadam_muon_state());
     s->cfg = c;
     s->newton.steps = c.steps;
